@@ -451,6 +451,73 @@ commitkv_status commitkv_compact_noalloc(const commitkv_shape *shape, int32_t n_
                                          int32_t *const *pos_out, int32_t *status_out,
                                          cudaStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Attention of new tokens over resident caches: what the agent's own model
+ * computes between two commits, on the caches that this library scores and
+ * compresses (Section 3.1, Eq. 4: the positions p_i stay absolute, so a
+ * compressed cache has gaps in them).  For every trajectory, layer, query
+ * head h and query at position p = q_pos[w], token i of its cache is visible
+ * iff
+ *     pos[i] <= p  and  (window = 0  or  pos[i] > p - window  or
+ *                        (pos[i] < sinks and i < sinks)),
+ * that is, a sliding window of the last `window` positions beside the first
+ * `sinks` tokens of the text, where the cache still holds them; and
+ *     s_i = softmax_scale <q_p, k_i>,   lse = log sum_i exp(s_i),
+ *     out = sum_i exp(s_i - lse) v_i    over the visible tokens.
+ * A query that sees no token gets out = 0 and lse = -inf.  What tokens hold
+ * that a query does not see (infinities, NaN) does not reach its output.  A
+ * visible score that is NaN or +inf makes its row NaN.
+ *
+ *   shape, n_traj, trajs, layer_mask   as for commitkv_page_effects: one
+ *                prompt chunk or, with W = 1, one decoded token per
+ *                trajectory; the pages are not read.  The keys and values of
+ *                the new tokens are in the cache before the call.  q_pos may
+ *                be in any order.
+ *   window >= 0  (0: no window), sinks >= 0 (positions are not negative).
+ *   out          host array [n_traj] of device [M][Hq][W_t][d] dense, dtype of
+ *                the shape (entries with W_t = 0 may be NULL); rows of
+ *                unselected layers are not written.
+ *   lse_out      NULL, or host array [n_traj] of device float [M][Hq][W_t]
+ *                (NULL entries allowed), natural logarithm.  With window = 0
+ *                (m = lse, l = 1, o = out) are row statistics for
+ *                commitkv_page_effects_from_stats.
+ *   workspace    at least commitkv_attention_workspace_size bytes for these
+ *                trajectories or larger ones (S, W, n_traj), 256-byte aligned.
+ * Outputs must not overlap inputs, the workspace or one another.
+ * Weights are fp32; the tensor-core kernels round them to bf16 for the product
+ * with bf16 values.  The same call gives the same bits every time.
+ * -------------------------------------------------------------------- */
+commitkv_status commitkv_window_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                                          const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,
+                                          float *const *lse_out, void *workspace, size_t workspace_bytes,
+                                          cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * commitkv_window_attention for trajectories that share a prefix (the system
+ * prompt and tool descriptions of concurrent agents): the sums run over the
+ * prefix's tokens and the trajectory's own together.  The prefix's K and V are
+ * read once for the queries of all trajectories.
+ *
+ *   prefix       the shared cache: k, v, strides, pos and S are read.  Its
+ *                positions are in the same coordinate as the trajectories'
+ *                (normally below all of theirs).  S = 0: as
+ *                commitkv_window_attention.  "The first sinks tokens" counts
+ *                in each cache: pos[i] < sinks and i < sinks there.
+ *   the rest     as for commitkv_window_attention; the workspace for these
+ *                trajectories and this prefix.
+ * -------------------------------------------------------------------- */
+commitkv_status commitkv_prefix_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                                          const commitkv_traj *prefix, const uint8_t *layer_mask, int32_t window,
+                                          int32_t sinks, void *const *out, float *const *lse_out, void *workspace,
+                                          size_t workspace_bytes, cudaStream_t stream);
+
+/* Size in bytes of the workspace of the two attention calls for these
+ * trajectories (prefix NULL: commitkv_window_attention) and for fewer ones,
+ * smaller caches or fewer queries.  It does not depend on S.  Returns 0 for
+ * invalid arguments. */
+size_t commitkv_attention_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                                         const commitkv_traj *prefix);
+
 #ifdef __cplusplus
 }
 #endif

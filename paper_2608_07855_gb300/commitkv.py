@@ -102,10 +102,15 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.commitkv_test_launches.argtypes = []
     lib.commitkv_test_launches.restype = ctypes.c_uint64
     lib.commitkv_token_scores.argtypes = [P(Shape), i32, P(Traj), vp, vp, vp, vp, sz, vp]
+    lib.commitkv_attention_workspace_size.argtypes = [P(Shape), i32, P(Traj), P(Traj)]
+    lib.commitkv_attention_workspace_size.restype = sz
+    lib.commitkv_window_attention.argtypes = [P(Shape), i32, P(Traj), vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.commitkv_prefix_attention.argtypes = [P(Shape), i32, P(Traj), P(Traj), vp, i32, i32, vp, vp, vp, sz, vp]
     for f in ("commitkv_workspace_init", "commitkv_workspace_status", "commitkv_page_effects",
               "commitkv_page_effects_from_stats", "commitkv_classify", "commitkv_classify_variant",
               "commitkv_joint_test", "commitkv_compact", "commitkv_compact_in_place", "commitkv_compact_noalloc",
-              "commitkv_test_barrier_timeout", "commitkv_test_pruned_pages", "commitkv_token_scores"):
+              "commitkv_test_barrier_timeout", "commitkv_test_pruned_pages", "commitkv_token_scores",
+              "commitkv_window_attention", "commitkv_prefix_attention"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -238,9 +243,11 @@ def commitkv_workspace_size(shape: Shape, trajs: Sequence[TrajTensors]) -> int:
 
 def alloc_workspace(shape: Shape, trajs: Sequence[TrajTensors], device=None):
     """Allocate (with torch) and initialise a workspace for these trajectories."""
-    torch = _torch()
-    n = commitkv_workspace_size(shape, trajs)
-    ws = torch.empty(n + 256, dtype=torch.uint8, device=device or "cuda")
+    return _alloc(commitkv_workspace_size(shape, trajs), device)
+
+
+def _alloc(n: int, device):
+    ws = _torch().empty(n + 256, dtype=_torch().uint8, device=device or "cuda")
     off = (-ws.data_ptr()) % 256
     ws = ws[off: off + n]
     commitkv_workspace_init(ws)
@@ -404,3 +411,110 @@ def commitkv_compact_noalloc(shape: Shape, cache, retired, pending, pending_prio
         _ptr_array(idx_out, n), _ptr(n_idx_out), _ptr_array(k_out, n), _ptr_array(v_out, n),
         _ptr_array(pos_out, n), _ptr(status_out), _stream(stream))
     _check(rc, "commitkv_compact_noalloc")
+
+
+class AttentionBatch:
+    """The arguments of an attention call, checked and marshalled once: the
+    trajectories, their outputs and a shared prefix, for callers that issue
+    many calls on the same buffers.  Caches that grow in place are followed
+    with set_length (the tensors passed in must then be views of buffers that
+    hold the new tokens, and the workspace large enough for them; a
+    workspace does not depend on cache lengths).  The batch keeps the tensors
+    alive."""
+
+    def __init__(self, shape: Shape, trajs: Sequence[TrajTensors], out, lse_out=None, prefix: TrajTensors = None):
+        torch = _torch()
+        n = len(trajs)
+        self.shape, self.trajs, self.descs = shape, trajs, _descs(trajs)
+        self.prefix = None if prefix is None else prefix.desc()
+        self.tensors = (trajs, prefix, out, lse_out)
+        if len(out) != n or (lse_out is not None and len(lse_out) != n):
+            raise ValueError("one output per trajectory")
+        M, H, Hq, d = shape.layers, shape.kv_heads, shape.q_heads, shape.head_dim
+        dt = torch.bfloat16 if shape.dtype == COMMITKV_BF16 else torch.float32
+        devices = set()
+        for i, t in enumerate(list(trajs) + ([prefix] if prefix is not None else [])):
+            if t.k.shape[0] != M or t.k.shape[1] != H or t.k.shape[3] != d or t.k.dtype != dt or t.v.dtype != dt:
+                raise ValueError(f"K and V must be [{M}][{H}][S][{d}] of {dt}")
+            if t.pos.shape != (t.k.shape[2],) or not t.pos.is_contiguous():
+                raise ValueError("pos must be contiguous, one position per cached token")
+            devices |= {x.device for x in (t.k, t.v, t.pos)}
+            if i >= n:
+                continue
+            W = 0 if t.q is None else t.q.shape[2]
+            if W and (tuple(t.q.shape) != (M, Hq, W, d) or t.q_pos is None or t.q_pos.shape != (W,) or
+                      not t.q_pos.is_contiguous()):
+                raise ValueError(f"q must be [{M}][{Hq}][W][{d}] with W contiguous positions")
+            lse = None if lse_out is None else lse_out[i]
+            for x, want, kind, what in ((out[i], (M, Hq, W, d), dt, "out"), (lse, (M, Hq, W), torch.float32, "lse_out")):
+                if x is None and (what == "lse_out" or W == 0):
+                    continue
+                if x is None or tuple(x.shape) != want or x.dtype != kind or not x.is_contiguous():
+                    raise ValueError(f"{what} must be contiguous {want} of {kind}")
+                devices.add(x.device)
+            devices |= {x.device for x in (t.q, t.q_pos) if x is not None}
+        if len(devices) != 1 or next(iter(devices)).type != "cuda":
+            raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
+        self.device = next(iter(devices)).index
+        self._out, self._lse = _ptr_array(out, n), _ptr_array(lse_out, n)
+        # what every call passes, converted once
+        self._args = (ctypes.byref(shape), n, self.descs)
+        self._prefix = None if prefix is None else ctypes.byref(self.prefix)
+
+    def set_length(self, i: int, S: int):
+        """Trajectory i's cache now has S tokens."""
+        if S < 0:
+            raise ValueError("S >= 0")
+        self.descs[i].S = S
+
+
+def attention_batch(shape: Shape, trajs: Sequence[TrajTensors], out, lse_out=None, prefix=None) -> AttentionBatch:
+    return AttentionBatch(shape, trajs, out, lse_out, prefix)
+
+
+def commitkv_attention_workspace_size(shape: Shape, trajs: Sequence[TrajTensors], prefix: TrajTensors = None) -> int:
+    p = None if prefix is None else ctypes.byref(prefix.desc())
+    n = load_library().commitkv_attention_workspace_size(ctypes.byref(shape), len(trajs), _descs(trajs), p)
+    if n == 0:
+        raise CommitKVError(COMMITKV_ERR_INVALID_ARG, "commitkv_attention_workspace_size")
+    return int(n)
+
+
+def alloc_attention_workspace(shape: Shape, trajs: Sequence[TrajTensors], prefix: TrajTensors = None, device=None):
+    """Allocate (with torch) and initialise a workspace for the attention
+    calls on these trajectories."""
+    return _alloc(commitkv_attention_workspace_size(shape, trajs, prefix), device)
+
+
+def _attention(name, shape, trajs, prefix, out, lse_out, window, sinks, layer_mask, workspace, stream):
+    b = trajs
+    if not isinstance(b, AttentionBatch):
+        b = AttentionBatch(shape, trajs, out, lse_out, prefix)
+    elif out is not None or lse_out is not None or prefix is not None or bytes(b.shape) != bytes(shape):
+        raise ValueError("the outputs, the prefix and the shape are those of the batch")
+    if (b.prefix is None) != (name == "commitkv_window_attention"):
+        raise ValueError("commitkv_prefix_attention takes a prefix, commitkv_window_attention none")
+    if workspace is None or workspace.device.index != b.device or _torch().cuda.current_device() != b.device:
+        raise ValueError("the batch and the workspace must be on the current GPU")
+    _mbuf, mptr = _mask(layer_mask, shape.layers)
+    more = () if b.prefix is None else (b._prefix,)
+    rc = getattr(load_library(), name)(*b._args, *more, mptr, window, sinks, b._out, b._lse, workspace.data_ptr(),
+                                       workspace.numel(), _stream(stream))
+    _check(rc, name)
+
+
+def commitkv_window_attention(shape: Shape, trajs, out=None, lse_out=None, window: int = 0, sinks: int = 0,
+                              layer_mask=None, workspace=None, stream=None):
+    """Attention of every trajectory's queries over its resident cache, with a
+    sliding window and sink tokens; trajs may be an AttentionBatch (then
+    without out and lse_out)."""
+    _attention("commitkv_window_attention", shape, trajs, None, out, lse_out, window, sinks, layer_mask, workspace,
+               stream)
+
+
+def commitkv_prefix_attention(shape: Shape, trajs, prefix=None, out=None, lse_out=None, window: int = 0,
+                              sinks: int = 0, layer_mask=None, workspace=None, stream=None):
+    """commitkv_window_attention over a shared prefix and the trajectories'
+    own caches together; trajs may be an AttentionBatch with a prefix."""
+    _attention("commitkv_prefix_attention", shape, trajs, prefix, out, lse_out, window, sinks, layer_mask, workspace,
+               stream)

@@ -1,0 +1,301 @@
+// Attention over resident caches: entry points, work division, and the merge
+// of partial results.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "attend.cuh"
+
+namespace ckv {
+namespace at {
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Items that share rows with others (split tokens), at most: bounds the
+// partial results.  Small row tiles are cheap to merge and come from calls
+// whose time is the reading of the cache, which wants many blocks.
+constexpr int64_t kMaxSplitSmall = 2048;  // up to 16 rows an item
+constexpr int64_t kMaxSplit = 768;
+
+// ------------------------------------------------------------------ merge
+// A warp per row: o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i over the row's
+// partial results.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) combine(const __grid_constant__ Launch L) {
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const int per = L.out_off[L.n_traj];
+  const int li = (int)(w / per);
+  if (li >= L.n_layers) return;
+  int x = (int)(w % per), a = 0, b = L.n_traj;
+  while (b - a > 1) {
+    const int m = (a + b) >> 1;
+    if (x >= L.out_off[m]) a = m;
+    else b = m;
+  }
+  x -= L.out_off[a];
+  const Traj &t = L.t[a];
+  const int R = L.g * t.W, kvh = x / R, r = x % R, l = L.layer_ids[li];
+  float m = -INFINITY, lsum = 0.0f, o[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) o[c] = 0.0f;
+  for (int k = 0; k <= L.prefix; ++k) {
+    const Seg &sg = L.seg[k == L.prefix ? a + L.prefix : 0];
+    const int64_t first = sg.part + (int64_t)(li * L.H + kvh) * sg.nchunk * sg.R + (sg.t < 0 ? t.row0 + r : r);
+    for (int c0 = 0; c0 < sg.nchunk; c0 += 32) {
+      const int n = min(32, sg.nchunk - c0);
+      const float2 ml = lane < n ? L.pml[first + (int64_t)(c0 + lane) * sg.R] : make_float2(-INFINITY, 0.0f);
+      const float mn = fmaxf(m, warp_max(ml.x)), ref = mn == -INFINITY ? 0.0f : mn;
+      const float f = exp2f(m - ref), wt = exp2f(ml.x - ref);
+      m = mn;
+      lsum = fmaf(lsum, f, warp_sum(wt * ml.y));
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[c] *= f;
+#pragma unroll 4
+      for (int c = 0; c < n; ++c) {
+        const float wc = __shfl_sync(0xffffffffu, wt, c);
+        const bool used = __shfl_sync(0xffffffffu, ml.y, c) != 0.0f;
+        const float *p = L.po + (first + (int64_t)(c0 + c) * sg.R) * D;
+#pragma unroll
+        for (int k2 = 0; k2 < D / 32; ++k2) {
+          const float v = p[lane + 32 * k2];
+          o[k2] = used ? fmaf(wc, v, o[k2]) : o[k2];
+        }
+      }
+    }
+  }
+  const int64_t row = row_index(L, t, l, kvh, r);
+  const float inv = norm_of(lsum);
+  T *dst = static_cast<T *>(t.out) + row * D;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) dst[lane + 32 * c] = from_f32<T>(o[c] * inv);
+  if (t.lse && lane == 0) t.lse[row] = lse_of(m, lsum);
+}
+
+}  // namespace
+
+cudaError_t launch_combine(const Launch &L, cudaStream_t s) {
+  const int64_t rows = (int64_t)L.out_off[L.n_traj] * L.n_layers;
+  if (rows == 0) return cudaSuccess;
+  const unsigned n = (unsigned)cdiv(rows, 8);
+  if (L.dtype == COMMITKV_BF16) {
+    if (L.d == 128) combine<__nv_bfloat16, 128><<<n, 256, 0, s>>>(L);
+    else combine<__nv_bfloat16, 64><<<n, 256, 0, s>>>(L);
+  } else {
+    if (L.d == 128) combine<float, 128><<<n, 256, 0, s>>>(L);
+    else combine<float, 64><<<n, 256, 0, s>>>(L);
+  }
+  ++launch_count();
+  return cudaGetLastError();
+}
+
+namespace {
+
+// ------------------------------------------------------------------ host
+int64_t rows_of(const commitkv_shape *s, const commitkv_traj &x) { return (int64_t)(s->q_heads / s->kv_heads) * x.W; }
+
+commitkv_status check_args(const commitkv_shape *s, int n, const commitkv_traj *tr, const commitkv_traj *prefix,
+                           bool need_q) {
+  commitkv_status st = check_shape(s);
+  if (st) return st;
+  if ((st = check_trajs(s, n, tr, need_q))) return st;
+  if (prefix) {
+    commitkv_traj p = *prefix;  // its queries and pages are not read
+    p.W = p.P = 0;
+    if ((st = check_trajs(s, 1, &p, false))) return st;
+  }
+  int64_t rows = 0;  // of one (layer, KV head): indices of a slice are 32-bit
+  for (int t = 0; t < n; ++t) rows += rows_of(s, tr[t]);
+  return rows * s->kv_heads > (1 << 28) ? COMMITKV_ERR_INVALID_ARG : COMMITKV_OK;
+}
+
+// Partial rows that a call can need; monotone in S, W and n_traj.
+int64_t partial_rows(const commitkv_shape *s, int n, const commitkv_traj *tr, const commitkv_traj *prefix) {
+  int64_t all = 0, most = 0;
+  for (int t = 0; t < n; ++t) {
+    all += rows_of(s, tr[t]);
+    most = std::max(most, rows_of(s, tr[t]));
+  }
+  if (prefix) most = all;
+  const int64_t split = std::max(kMaxSplitSmall * std::min<int64_t>(most, 16), kMaxSplit * std::min<int64_t>(most, 256));
+  return split + (prefix ? 2 * all * s->kv_heads * s->layers : 0);
+}
+
+size_t partial_bytes(const commitkv_shape *s, int64_t rows) {
+  return align_up((size_t)rows * s->head_dim * 4) + align_up((size_t)rows * 8);
+}
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  return n;
+}
+
+// Chunk length in tiles: every (slice, row tile) of a segment is cut into
+// ceil(tiles / length) items.  Estimated time in tile periods of `slots`
+// concurrent items: the work and each item's fixed part, spread over the
+// slots, and the tail that the last items leave, or whole waves where all
+// items are alike.
+struct Divide {
+  int64_t base[kMaxSeg];   // slices x row tiles
+  int64_t tiles[kMaxSeg];  // at most, per row tile
+  int n;
+};
+int64_t chunk_tiles(const Divide &v, int64_t slots, double fixed, int64_t most_items) {
+  int64_t longest = 1;
+  for (int s = 0; s < v.n; ++s) longest = std::max(longest, v.tiles[s]);
+  int64_t best = longest;
+  double best_t = INFINITY;
+  for (int64_t k = 1; k <= longest; ++k) {  // chunks of the longest cache
+    const int64_t len = cdiv(longest, k);
+    if (k > 1 && len == cdiv(longest, k - 1)) continue;
+    int64_t items = 0, split = 0, kinds = 0;
+    double work = 0;
+    for (int s = 0; s < v.n; ++s) {
+      const int64_t c = std::max<int64_t>(1, cdiv(v.tiles[s], len));
+      items += v.base[s] * c;
+      if (c > 1) split += v.base[s] * c;
+      work += (double)v.base[s] * (v.tiles[s] + c * fixed);
+      kinds += v.base[s] > 0 && v.tiles[s] > 0;
+    }
+    if (split > most_items) break;
+    const double one = len + fixed;
+    const double t = items <= slots ? one : kinds == 1 ? cdiv(items, slots) * one : work / slots + 0.5 * one;
+    if (t < best_t * 0.98) best_t = t, best = len;  // fewer chunks unless more are clearly better
+  }
+  return best;
+}
+
+commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                       const commitkv_traj *prefix, const uint8_t *layer_mask, int32_t window, int32_t sinks,
+                       void *const *out, float *const *lse_out, void *workspace, size_t workspace_bytes,
+                       cudaStream_t stream) {
+  commitkv_status st = check_args(shape, n_traj, trajs, prefix, true);
+  if (st) return st;
+  if (window < 0 || sinks < 0 || !out) return COMMITKV_ERR_INVALID_ARG;
+  for (int t = 0; t < n_traj; ++t)
+    if (trajs[t].W > 0 && !out[t]) return COMMITKV_ERR_INVALID_ARG;
+  if (!workspace || (uintptr_t)workspace % kAlign ||
+      workspace_bytes < kAlign + partial_bytes(shape, partial_rows(shape, n_traj, trajs, prefix)))
+    return COMMITKV_ERR_WORKSPACE;
+  if (prefix && prefix->S == 0) prefix = nullptr;
+
+  static thread_local Launch L;
+  memset(&L, 0, sizeof L);
+  L.M = shape->layers;
+  L.H = shape->kv_heads;
+  L.Hq = shape->q_heads;
+  L.g = shape->q_heads / shape->kv_heads;
+  L.d = shape->head_dim;
+  L.dtype = shape->dtype;
+  const float scale = shape->softmax_scale > 0.0f ? shape->softmax_scale : 1.0f / sqrtf((float)shape->head_dim);
+  L.scale_log2 = scale * 1.4426950408889634f;
+  L.window = window;
+  L.sinks = sinks;
+  for (int l = 0; l < shape->layers; ++l)
+    if (!layer_mask || layer_mask[l]) L.layer_ids[L.n_layers++] = (uint8_t)l;
+  L.n_traj = n_traj;
+  L.prefix = prefix ? 1 : 0;
+  L.n_seg = n_traj + L.prefix;
+  int64_t all = 0;
+  for (int t = 0; t < n_traj; ++t) {
+    const commitkv_traj &x = trajs[t];
+    L.t[t] = {x.q, x.q_pos, out[t], lse_out ? lse_out[t] : nullptr, x.W, (int32_t)all};
+    all += rows_of(shape, x);
+  }
+  if (all == 0 || L.n_layers == 0) return COMMITKV_OK;
+  int64_t most = prefix ? all : 0;
+  for (int s = 0; s < L.n_seg; ++s) {
+    const bool shared = prefix && s == 0;
+    const commitkv_traj &x = shared ? *prefix : trajs[s - L.prefix];
+    Seg &sg = L.seg[s];
+    sg.k = x.k;
+    sg.v = x.v;
+    sg.sl = x.stride_layer;
+    sg.sh = x.stride_head;
+    sg.st = x.stride_tok;
+    sg.pos = x.pos;
+    sg.S = x.S;
+    sg.t = shared ? -1 : s - L.prefix;
+    sg.R = (int32_t)(shared ? all : rows_of(shape, x));
+    most = std::max<int64_t>(most, sg.R);
+  }
+  const int sms = sm_count();
+  if (sms < 1) return COMMITKV_ERR_CUDA;
+  L.rows_per_item = most <= 16 ? 16 : 64;
+  const int tile = 64, resident = L.rows_per_item == 16 ? 2 : 1;
+  Divide v;
+  v.n = L.n_seg;
+  for (int s = 0; s < L.n_seg; ++s) {
+    Seg &sg = L.seg[s];
+    sg.nrt = (int32_t)cdiv(sg.R, L.rows_per_item);
+    v.base[s] = (int64_t)L.n_layers * L.H * sg.nrt;
+    // a window's rows see at most window + sinks tokens, its tile the rows' span more
+    const int64_t seen = window ? (int64_t)window + sinks + std::min<int64_t>(L.rows_per_item, sg.R) / L.g : sg.S;
+    v.tiles[s] = cdiv(std::min<int64_t>(sg.S, seen), tile);
+  }
+  const int64_t len = chunk_tiles(v, (int64_t)sms * resident, 1.0, L.rows_per_item == 16 ? kMaxSplitSmall : kMaxSplit);
+  int64_t items = 0, parts = 0;
+  bool merge = false;
+  for (int s = 0; s < L.n_seg; ++s) {
+    Seg &sg = L.seg[s];
+    sg.nchunk = (int32_t)std::max<int64_t>(1, cdiv(v.tiles[s], len));
+    if (items > 0x7fffffff) return COMMITKV_ERR_UNSUPPORTED;
+    L.item_off[s] = (int32_t)items;
+    items += v.base[s] * sg.nchunk;
+    const bool split = prefix || sg.nchunk > 1;
+    sg.part = split ? parts : -1;
+    if (split) parts += (int64_t)L.n_layers * L.H * sg.nchunk * sg.R;
+    if (sg.t >= 0) L.out_off[sg.t + 1] = L.out_off[sg.t] + (split ? sg.R * L.H : 0);
+    merge = merge || split;
+  }
+  if (items > 0x7fffffff) return COMMITKV_ERR_UNSUPPORTED;
+  L.item_off[L.n_seg] = (int32_t)items;
+  if (kAlign + partial_bytes(shape, parts) > workspace_bytes) return COMMITKV_ERR_WORKSPACE;  // cannot be: partial_rows bounds it
+  char *base = static_cast<char *>(workspace) + kAlign;
+  L.po = reinterpret_cast<float *>(base);
+  L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
+  cudaError_t e = launch_simt(L, stream);
+  if (e == cudaSuccess && merge) e = launch_combine(L, stream);
+  if (e == cudaSuccess) return COMMITKV_OK;
+  cudaGetLastError();
+  return COMMITKV_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace at
+}  // namespace ckv
+
+using namespace ckv;
+
+extern "C" {
+
+size_t commitkv_attention_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                                         const commitkv_traj *prefix) {
+  if (at::check_args(shape, n_traj, trajs, prefix, false) != COMMITKV_OK) return 0;
+  return at::kAlign + at::partial_bytes(shape, at::partial_rows(shape, n_traj, trajs, prefix));
+}
+
+commitkv_status commitkv_window_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                                          const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,
+                                          float *const *lse_out, void *workspace, size_t workspace_bytes,
+                                          cudaStream_t stream) {
+  return at::attend(shape, n_traj, trajs, nullptr, layer_mask, window, sinks, out, lse_out, workspace, workspace_bytes,
+                    stream);
+}
+
+commitkv_status commitkv_prefix_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                                          const commitkv_traj *prefix, const uint8_t *layer_mask, int32_t window,
+                                          int32_t sinks, void *const *out, float *const *lse_out, void *workspace,
+                                          size_t workspace_bytes, cudaStream_t stream) {
+  if (!prefix) return COMMITKV_ERR_INVALID_ARG;
+  return at::attend(shape, n_traj, trajs, prefix, layer_mask, window, sinks, out, lse_out, workspace, workspace_bytes,
+                    stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,253 @@
+// Attention of new tokens over resident caches (commitkv_window_attention,
+// commitkv_prefix_attention): launch description and what its kernels share.
+//
+// A segment is one cache (a trajectory's own, or the prefix that all of them
+// share) with the query rows that attend to it.  The rows of a (layer, KV
+// head) slice of a segment are numbered position by position, the g query
+// heads of a position side by side: row r of a trajectory is position r / g,
+// head kvh g + r % g, so the rows of a tile see nearly the same tokens; the
+// prefix's rows are those of all trajectories, one after another.  A row sees
+// the tokens [0, se) and [lo, hi) of a cache: positions increase, so both the
+// causal end and the window are found by search.
+//
+// A work item is (segment, layer, KV head, row tile, chunk).  The tokens that
+// a row tile needs, [0, max se) and [min lo, max hi), are only known on the
+// device: its tiles are shared out evenly among the tile's chunks there.
+// Results of a row that has one item go to the outputs, else partial results
+// to the workspace, merged by combine.
+#pragma once
+
+#include "ckv_internal.cuh"
+
+namespace ckv {
+namespace at {
+
+constexpr int kMaxSeg = kMaxTraj + 1;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Seg {
+  const void *k, *v;
+  int64_t sl, sh, st;  // strides in elements
+  const int32_t *pos;
+  int64_t part;  // first partial row; -1: the rows are written to the outputs
+  int32_t S;
+  int32_t R;        // rows of a (layer, KV head) slice
+  int32_t t;        // trajectory, -1: the shared prefix
+  int32_t nrt;      // row tiles
+  int32_t nchunk;
+};
+
+struct Traj {
+  const void *q;
+  const int32_t *qpos;
+  void *out;
+  float *lse;
+  int32_t W;
+  int32_t row0;  // its first row in the prefix segment
+};
+
+struct Launch {
+  Seg seg[kMaxSeg];
+  Traj t[kMaxTraj];
+  int32_t item_off[kMaxSeg + 1];
+  int32_t out_off[kMaxTraj + 1];  // rows of a (selected) layer that combine merges, prefix per trajectory
+  int32_t n_seg, n_traj, prefix;  // prefix: segment 0 is shared
+  int32_t M, H, Hq, g, d, dtype, n_layers;
+  int32_t window, sinks;
+  int32_t rows_per_item;
+  float scale_log2;
+  float *po;      // partial sums [rows][d], not normalised
+  float2 *pml;    // their reference max (base 2) and sum of weights
+  uint8_t layer_ids[kMaxLayers];
+};
+
+// CUDA cores: any layout and type.  Rows per item: 16 or 64.
+cudaError_t launch_simt(const Launch &L, cudaStream_t s);
+cudaError_t launch_combine(const Launch &L, cudaStream_t s);
+
+struct Item {
+  int s, li, l, kvh, rt, c;
+};
+
+__device__ __forceinline__ Item decode_item(const Launch &L, int item) {
+  Item it;
+  int a = 0, b = L.n_seg;  // the last segment that starts at or before the item
+  while (b - a > 1) {
+    const int m = (a + b) >> 1;
+    if (item >= L.item_off[m]) a = m;
+    else b = m;
+  }
+  it.s = a;
+  const Seg &sg = L.seg[a];
+  int x = item - L.item_off[a];
+  it.c = x % sg.nchunk;
+  x /= sg.nchunk;
+  it.kvh = x % L.H;
+  x /= L.H;
+  it.li = x % L.n_layers;
+  // the later rows of a prompt see more: they come first
+  it.rt = sg.nrt - 1 - x / L.n_layers;
+  it.l = L.layer_ids[it.li];
+  return it;
+}
+
+// Trajectory and row within it of row r of a segment.
+__device__ __forceinline__ int traj_of_row(const Launch &L, const Seg &sg, int &r) {
+  if (sg.t >= 0) return sg.t;
+  int a = 0, b = L.n_traj;
+  while (b - a > 1) {
+    const int m = (a + b) >> 1;
+    if (r >= L.t[m].row0) a = m;
+    else b = m;
+  }
+  r -= L.t[a].row0;
+  return a;
+}
+
+// Row (l, h, w) of a [M][Hq][W] array.
+__device__ __forceinline__ int64_t row_index(const Launch &L, const Traj &t, int l, int kvh, int r) {
+  return ((int64_t)l * L.Hq + kvh * L.g + r % L.g) * t.W + r / L.g;
+}
+
+__device__ __forceinline__ int64_t part_index(const Launch &L, const Seg &sg, const Item &it, int r) {
+  return sg.part + ((int64_t)(it.li * L.H + it.kvh) * sg.nchunk + it.c) * sg.R + r;
+}
+
+// First index of [a, b) whose position is above x (b: none).
+__device__ __forceinline__ int first_above(const int32_t *pos, int a, int b, int64_t x) {
+  while (a < b) {
+    const int m = a + ((b - a) >> 1);
+    if ((int64_t)pos[m] > x) b = m;
+    else a = m + 1;
+  }
+  return a;
+}
+
+struct Span {
+  int lo, hi, se;  // a row sees [0, se) and [lo, hi), se <= lo
+};
+
+__device__ __forceinline__ bool sees(const Span &s, int i) { return i < s.se || (i >= s.lo && i < s.hi); }
+
+// What a query at position p sees of a cache.  Positions increase by one or
+// more, so a window holds at most `window` tokens and the sinks are at most
+// the first `sinks`: without gaps (the latest tokens, or a cache before its
+// first checkpoint) the first guess is right and costs a round trip or two
+// instead of a search.
+__device__ __forceinline__ Span row_span(const int32_t *pos, int S, int p, int window, int sinks) {
+  Span r = {0, 0, 0};
+  if (S == 0) return r;
+  const int64_t back = (int64_t)pos[S - 1] - p;  // >= the number of tokens after p
+  if (back <= 0) r.hi = S;
+  else {
+    const int64_t gss = (int64_t)S - back;  // the end if they have no gaps, else before it
+    if (gss >= 1 && pos[gss - 1] == p) r.hi = (int)gss;
+    else r.hi = first_above(pos, gss > 0 ? (int)gss : 0, S, p);
+  }
+  if (window == 0) return r;
+  const int64_t edge = (int64_t)p - window;  // positions above it are inside
+  const int least = r.hi > window ? r.hi - window : 0;
+  r.lo = least;
+  if (least < r.hi && (int64_t)pos[least] <= edge) r.lo = first_above(pos, least + 1, r.hi, edge);
+  const int most = sinks < r.lo ? sinks : r.lo;
+  r.se = most;
+  if (most > 0 && pos[most - 1] >= sinks) r.se = first_above(pos, 0, most, (int64_t)sinks - 1);
+  return r;
+}
+
+// The tokens of a row tile, cut into tiles of `tile`: [0, se), then [lo, hi).
+struct Tiles {
+  int lo, hi, se, nA, n;  // nA tiles of sinks, n in all
+};
+
+__device__ __forceinline__ Tiles make_tiles(int lo, int hi, int se, int tile) {
+  Tiles t;
+  if (hi <= lo) lo = 0, hi = se, se = 0;  // sinks alone
+  else if (se >= lo) lo = se = 0;         // one piece
+  t.lo = lo, t.hi = hi, t.se = se;
+  t.nA = (se + tile - 1) / tile;
+  t.n = t.nA + (hi - lo + tile - 1) / tile;
+  return t;
+}
+__device__ __forceinline__ int tile_start(const Tiles &t, int j, int tile) {
+  return j < t.nA ? j * tile : t.lo + (j - t.nA) * tile;
+}
+__device__ __forceinline__ int tile_end(const Tiles &t, int j, int tile) {
+  const int e = tile_start(t, j, tile) + tile, lim = j < t.nA ? t.se : t.hi;
+  return e < lim ? e : lim;
+}
+// Tiles [first, last) of chunk c of n.
+__device__ __forceinline__ int chunk_tile(const Tiles &t, int c, int n) { return (int)((int64_t)t.n * c / n); }
+
+// sum of exp2(s - m) v over the visible tokens of tiles [j0, j1) for one row,
+// by the 32 lanes of a warp: o[k] is channel lane + 32 k.  Only visible tokens
+// are read.  The tile kernels multiply masked tokens by weights of zero, which
+// is wrong where a masked value is infinite or NaN, so they redo a row whose
+// sums are not finite this way (its m and l never see masked tokens).
+template <typename T, int D>
+__device__ __noinline__ void redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
+                                      Tiles tl, int tile, int j0, int j1, float m, float *o) {
+  const int lane = threadIdx.x & 31;
+  const T *q = static_cast<const T *>(qrow);
+  const T *k = static_cast<const T *>(sg.k) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
+  const T *v = static_cast<const T *>(sg.v) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
+  float qv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    qv[i] = to_f32(q[lane + 32 * i]);
+    o[i] = 0.0f;
+  }
+  for (int j = j0; j < j1; ++j) {
+    const int e = tile_end(tl, j, tile);
+    for (int i = tile_start(tl, j, tile); i < e; ++i) {
+      if (!sees(sp, i)) continue;
+      float dot = 0.0f;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) dot = fmaf(qv[c], to_f32(k[(int64_t)i * sg.st + lane + 32 * c]), dot);
+      const float p = exp2f(fmaf(warp_sum(dot), L.scale_log2, -m));
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[c] = fmaf(p, to_f32(v[(int64_t)i * sg.st + lane + 32 * c]), o[c]);
+    }
+    bool done = true;  // NaN in every channel stays
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) done = done && isnan(o[c]);
+    if (__all_sync(0xffffffffu, done)) break;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
+
+// Log-sum-exp of a row from its reference max (base 2) and sum; -inf where it saw nothing.
+__device__ __forceinline__ float lse_of(float m, float l) { return fmaf(m, kLn2, logf(l)); }
+// What its sums are multiplied by: 0 for a row that saw nothing.
+__device__ __forceinline__ float norm_of(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+// Writes one row's sums (relative to m, base 2; channel lane + 32 k in o[k])
+// as a warp: a partial result, or the outputs.
+template <typename T, int D>
+__device__ __forceinline__ void write_row_warp(const Launch &L, const Seg &sg, const Item &it, int r, const float *o,
+                                               float m, float l) {
+  const int lane = threadIdx.x & 31;
+  if (sg.part >= 0) {
+    const int64_t pr = part_index(L, sg, it, r);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) L.po[pr * D + lane + 32 * c] = o[c];
+    if (lane == 0) L.pml[pr] = make_float2(m, l);
+  } else {
+    const Traj &t = L.t[traj_of_row(L, sg, r)];
+    const int64_t row = row_index(L, t, it.l, it.kvh, r);
+    const float inv = norm_of(l);
+    T *dst = static_cast<T *>(t.out) + row * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) dst[lane + 32 * c] = from_f32<T>(o[c] * inv);
+    if (t.lse && lane == 0) t.lse[row] = lse_of(m, l);
+  }
+}
+
+}  // namespace at
+}  // namespace ckv

@@ -1,0 +1,225 @@
+// Attention on the CUDA cores: fp32 caches, and bf16 ones that the tensor-core
+// kernels cannot read (unaligned pointers or strides).
+//
+// One block of 256 threads per item; tiles of 64 tokens.  Thread (ty, tx) of a
+// 16 x 16 grid owns TM rows: their scores against four tokens (tx + 16 j) of a
+// tile, then D / 16 channels of their sums, so a row's running max and sum
+// live in registers of the 16 lanes that share it.  Q, K, V and the weights go
+// through shared memory as fp32.
+#include <string.h>
+
+#include "attend.cuh"
+#include "sm103.cuh"
+
+namespace ckv {
+namespace at {
+namespace {
+
+using sm103::ffma2;
+
+constexpr int TT = 64;   // tokens per tile
+constexpr int NT = 256;  // threads
+
+template <int D, int TM>
+struct Smem {
+  static constexpr int BM = 16 * TM;
+  static constexpr int KP = D + 4;  // rows 16 bytes apart in the banks
+  float q[BM][KP];
+  float k[TT][KP];
+  float v[TT][D];
+  float p[BM][TT + 4];
+  int lo[BM], hi[BM], se[BM];
+  int u_lo, u_hi, u_se;
+};
+
+template <typename T, int D, int TM>
+__global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch L) {
+  constexpr int BM = 16 * TM, CH = D / 16;
+  extern __shared__ __align__(16) uint8_t raw[];
+  Smem<D, TM> &sm = *reinterpret_cast<Smem<D, TM> *>(raw);
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  const Item it = decode_item(L, blockIdx.x);
+  const Seg &sg = L.seg[it.s];
+  const int r0 = it.rt * BM;
+  if (tid == 0) sm.u_lo = 0x7fffffff, sm.u_hi = 0, sm.u_se = 0;
+  __syncthreads();
+  for (int r = tid; r < BM; r += NT) {
+    Span sp = {0, 0, 0};
+    int rr = r0 + r;
+    if (rr < sg.R) {
+      const Traj &t = L.t[traj_of_row(L, sg, rr)];
+      sp = row_span(sg.pos, sg.S, t.qpos[rr / L.g], L.window, L.sinks);
+      if (sp.lo < sp.hi) {
+        atomicMin(&sm.u_lo, sp.lo);
+        atomicMax(&sm.u_hi, sp.hi);
+      }
+      atomicMax(&sm.u_se, sp.se);
+    }
+    sm.lo[r] = sp.lo, sm.hi[r] = sp.hi, sm.se[r] = sp.se;
+  }
+  for (int e = tid; e < BM * D; e += NT) {
+    const int r = e / D, c = e % D;
+    int rr = r0 + r;
+    float x = 0.0f;
+    if (rr < sg.R) {
+      const Traj &t = L.t[traj_of_row(L, sg, rr)];
+      x = to_f32(static_cast<const T *>(t.q)[row_index(L, t, it.l, it.kvh, rr) * D + c]);
+    }
+    sm.q[r][c] = x;
+  }
+  __syncthreads();
+  const Tiles tl = make_tiles(sm.u_lo, sm.u_hi, sm.u_se, TT);
+  const int j0 = chunk_tile(tl, it.c, sg.nchunk), j1 = chunk_tile(tl, it.c + 1, sg.nchunk);
+  const T *kb = static_cast<const T *>(sg.k) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
+  const T *vb = static_cast<const T *>(sg.v) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
+  Span sp[TM];
+  float m[TM], lsum[TM];
+  float2 o[TM][CH / 2];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int r = ty * TM + i;
+    sp[i] = {sm.lo[r], sm.hi[r], sm.se[r]};
+    m[i] = -INFINITY;
+    lsum[i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH / 2; ++c) o[i][c] = make_float2(0.0f, 0.0f);
+  }
+  for (int j = j0; j < j1; ++j) {
+    const int a = tile_start(tl, j, TT), n = tile_end(tl, j, TT) - a;
+    __syncthreads();
+    for (int e = tid; e < TT * D; e += NT) {
+      const int i = e / D, c = e % D;
+      const bool in = i < n;
+      sm.k[i][c] = in ? to_f32(kb[(int64_t)(a + i) * sg.st + c]) : 0.0f;
+      sm.v[i][c] = in ? to_f32(vb[(int64_t)(a + i) * sg.st + c]) : 0.0f;
+    }
+    __syncthreads();
+    float2 s2[TM][4];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s2[i][c] = make_float2(0.0f, 0.0f);
+#pragma unroll 4
+    for (int c = 0; c < D; c += 4) {
+      float4 q4[TM], k4[4];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) q4[i] = *reinterpret_cast<const float4 *>(&sm.q[ty * TM + i][c]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) k4[t] = *reinterpret_cast<const float4 *>(&sm.k[tx + 16 * t][c]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          s2[i][t] = ffma2(make_float2(q4[i].x, q4[i].y), make_float2(k4[t].x, k4[t].y), s2[i][t]);
+          s2[i][t] = ffma2(make_float2(q4[i].z, q4[i].w), make_float2(k4[t].z, k4[t].w), s2[i][t]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      float s[4], mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int tok = tx + 16 * t;
+        s[t] = tok < n && sees(sp[i], a + tok) ? (s2[i][t].x + s2[i][t].y) * L.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, s[t]);
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+      const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.0f : mn;
+      const float f = exp2f(m[i] - ref);
+      float ps = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float p = exp2f(s[t] - ref);
+        ps += p;
+        sm.p[ty * TM + i][tx + 16 * t] = p;
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, w);
+      lsum[i] = fmaf(lsum[i], f, ps);
+      m[i] = mn;
+#pragma unroll
+      for (int c = 0; c < CH / 2; ++c) o[i][c].x *= f, o[i][c].y *= f;
+    }
+    __syncwarp();  // a row's weights are written and read by the same half warp
+#pragma unroll 2
+    for (int t = 0; t < TT; t += 4) {
+      float4 p4[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) p4[i] = *reinterpret_cast<const float4 *>(&sm.p[ty * TM + i][t]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float2 v2[CH / 2];
+#pragma unroll
+        for (int c = 0; c < CH / 4; ++c) {
+          const float4 x = *reinterpret_cast<const float4 *>(&sm.v[t + u][64 * c + 4 * tx]);
+          v2[2 * c] = make_float2(x.x, x.y);
+          v2[2 * c + 1] = make_float2(x.z, x.w);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const float p = u == 0 ? p4[i].x : u == 1 ? p4[i].y : u == 2 ? p4[i].z : p4[i].w;
+#pragma unroll
+          for (int c = 0; c < CH / 2; ++c) o[i][c] = ffma2(make_float2(p, p), v2[c], o[i][c]);
+        }
+      }
+    }
+  }
+  // the rows' sums through shared memory, then a warp per row
+  __syncthreads();
+  float(*so)[Smem<D, TM>::KP] = sm.q;
+  float *sml = &sm.p[0][0];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int r = ty * TM + i;
+#pragma unroll
+    for (int c = 0; c < CH / 4; ++c)
+      *reinterpret_cast<float4 *>(&so[r][64 * c + 4 * tx]) =
+          make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y);
+    if (tx == 0) sml[2 * r] = m[i], sml[2 * r + 1] = lsum[i];
+  }
+  __syncthreads();
+  for (int r = tid / 32; r < BM && r0 + r < sg.R; r += NT / 32) {
+    float x[D / 32];
+    bool fine = true;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      x[c] = so[r][tid % 32 + 32 * c];
+      fine = fine && isfinite(x[c]);
+    }
+    const float mr = sml[2 * r], lr = sml[2 * r + 1];
+    if (!__all_sync(0xffffffffu, fine) && isfinite(lr)) {
+      int rr = r0 + r;
+      const Traj &t = L.t[traj_of_row(L, sg, rr)];
+      const Span one = {sm.lo[r], sm.hi[r], sm.se[r]};
+      redo_row<T, D>(L, sg, it.l, it.kvh, static_cast<const T *>(t.q) + row_index(L, t, it.l, it.kvh, rr) * D, one, tl,
+                     TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x);
+    }
+    write_row_warp<T, D>(L, sg, it, r0 + r, x, mr, lr);
+  }
+}
+
+template <typename T, int D, int TM>
+cudaError_t launch(const Launch &L, cudaStream_t s) {
+  const int smem = (int)sizeof(Smem<D, TM>);
+  cudaError_t e = cudaFuncSetAttribute(attend_simt<T, D, TM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  attend_simt<T, D, TM><<<L.item_off[L.n_seg], NT, smem, s>>>(L);
+  ++launch_count();
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_t(const Launch &L, cudaStream_t s) {
+  if (L.rows_per_item == 16) return L.d == 128 ? launch<T, 128, 1>(L, s) : launch<T, 64, 1>(L, s);
+  return L.d == 128 ? launch<T, 128, 4>(L, s) : launch<T, 64, 4>(L, s);
+}
+
+}  // namespace
+
+cudaError_t launch_simt(const Launch &L, cudaStream_t s) {
+  return L.dtype == COMMITKV_BF16 ? launch_t<__nv_bfloat16>(L, s) : launch_t<float>(L, s);
+}
+
+}  // namespace at
+}  // namespace ckv
