@@ -1,6 +1,7 @@
 // Attention over resident caches: entry points, work division, and the merge
 // of partial results.
 #include <math.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -171,6 +172,33 @@ int64_t chunk_tiles(const Divide &v, int64_t slots, double fixed, int64_t most_i
   return best;
 }
 
+enum { kSimt16, kSimt64, kTc, kPaths };
+struct PathInfo {
+  int rows, tile;    // of an item, tokens of a tile
+  int resident;      // items at a time on an SM
+  double fixed;      // an item's fixed part, in tiles
+};
+constexpr PathInfo kPath[kPaths] = {{16, 64, 2, 1.0}, {64, 64, 1, 1.0}, {256, 128, 1, 2.0}};
+
+bool force_cuda_cores() {
+  const char *e = getenv("COMMITKV_SCORING");
+  return e && (e[0] == 's' || e[0] == 'S');
+}
+
+// Tensor cores for bf16 where TMA can read the cache (16-byte aligned
+// pointers and strides, distinct heads and layers) and the rows' queries and
+// outputs are 16-byte aligned.
+int path_of(const Launch &L, const Seg &sg) {
+  const int cuda_cores = sg.R <= 16 ? kSimt16 : kSimt64;
+  if (L.dtype != COMMITKV_BF16 || force_cuda_cores()) return cuda_cores;
+  uintptr_t bits = (uintptr_t)sg.k | (uintptr_t)sg.v | (uintptr_t)((sg.sl | sg.sh | sg.st) * 2);
+  for (int t = sg.t < 0 ? 0 : sg.t; t < (sg.t < 0 ? L.n_traj : sg.t + 1); ++t)
+    bits |= L.t[t].W ? (uintptr_t)L.t[t].q | (uintptr_t)L.t[t].out : 0;
+  if (bits % 16) return cuda_cores;
+  if (sg.S > 0 && (sg.sh == 0 || sg.sl == 0 || std::max(sg.sl, std::max(sg.sh, sg.st)) >= (1ll << 39))) return cuda_cores;
+  return kTc;
+}
+
 commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
                        const commitkv_traj *prefix, const uint8_t *layer_mask, int32_t window, int32_t sinks,
                        void *const *out, float *const *lse_out, void *workspace, size_t workspace_bytes,
@@ -227,40 +255,61 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   }
   const int sms = sm_count();
   if (sms < 1) return COMMITKV_ERR_CUDA;
-  L.rows_per_item = most <= 16 ? 16 : 64;
-  const int tile = 64, resident = L.rows_per_item == 16 ? 2 : 1;
-  Divide v;
-  v.n = L.n_seg;
-  for (int s = 0; s < L.n_seg; ++s) {
-    Seg &sg = L.seg[s];
-    sg.nrt = (int32_t)cdiv(sg.R, L.rows_per_item);
-    v.base[s] = (int64_t)L.n_layers * L.H * sg.nrt;
-    // a window's rows see at most window + sinks tokens, its tile the rows' span more
-    const int64_t seen = window ? (int64_t)window + sinks + std::min<int64_t>(L.rows_per_item, sg.R) / L.g : sg.S;
-    v.tiles[s] = cdiv(std::min<int64_t>(sg.S, seen), tile);
-  }
-  const int64_t len = chunk_tiles(v, (int64_t)sms * resident, 1.0, L.rows_per_item == 16 ? kMaxSplitSmall : kMaxSplit);
-  int64_t items = 0, parts = 0;
+  // which kernel takes each segment's rows, and how its tokens are divided
+  int path[kMaxSeg];
+  int64_t parts = 0;
   bool merge = false;
+  for (int p = 0; p < kPaths; ++p) {
+    const PathInfo &pi = kPath[p];
+    Divide v;
+    int ids[kMaxSeg];
+    v.n = 0;
+    for (int s = 0; s < L.n_seg; ++s) {
+      Seg &sg = L.seg[s];
+      if (p == 0) path[s] = path_of(L, sg);
+      if (path[s] != p) continue;
+      sg.nrt = (int32_t)cdiv(sg.R, pi.rows);
+      // a window's rows see at most window + sinks tokens, its tile the rows' span more
+      const int64_t seen = window ? (int64_t)window + sinks + std::min(pi.rows, sg.R) / L.g : sg.S;
+      v.base[v.n] = (int64_t)L.n_layers * L.H * sg.nrt;
+      v.tiles[v.n] = cdiv(std::min<int64_t>(sg.S, seen), pi.tile);
+      ids[v.n++] = s;
+    }
+    if (v.n == 0) continue;
+    const int64_t len = chunk_tiles(v, (int64_t)sms * pi.resident, pi.fixed, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit);
+    int64_t items = 0;
+    for (int i = 0; i < v.n; ++i) {
+      Seg &sg = L.seg[ids[i]];
+      sg.nchunk = (int32_t)std::max<int64_t>(1, cdiv(v.tiles[i], len));
+      items += v.base[i] * sg.nchunk;
+      if (items > (1 << 30)) return COMMITKV_ERR_UNSUPPORTED;
+    }
+  }
   for (int s = 0; s < L.n_seg; ++s) {
     Seg &sg = L.seg[s];
-    sg.nchunk = (int32_t)std::max<int64_t>(1, cdiv(v.tiles[s], len));
-    if (items > 0x7fffffff) return COMMITKV_ERR_UNSUPPORTED;
-    L.item_off[s] = (int32_t)items;
-    items += v.base[s] * sg.nchunk;
     const bool split = prefix || sg.nchunk > 1;
     sg.part = split ? parts : -1;
     if (split) parts += (int64_t)L.n_layers * L.H * sg.nchunk * sg.R;
     if (sg.t >= 0) L.out_off[sg.t + 1] = L.out_off[sg.t] + (split ? sg.R * L.H : 0);
     merge = merge || split;
   }
-  if (items > 0x7fffffff) return COMMITKV_ERR_UNSUPPORTED;
-  L.item_off[L.n_seg] = (int32_t)items;
-  if (kAlign + partial_bytes(shape, parts) > workspace_bytes) return COMMITKV_ERR_WORKSPACE;  // cannot be: partial_rows bounds it
+  if (kAlign + partial_bytes(shape, parts) > workspace_bytes) return COMMITKV_ERR_WORKSPACE;  // partial_rows bounds it
   char *base = static_cast<char *>(workspace) + kAlign;
   L.po = reinterpret_cast<float *>(base);
   L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
-  cudaError_t e = launch_simt(L, stream);
+  cudaError_t e = cudaSuccess;
+  for (int p = 0; p < kPaths && e == cudaSuccess; ++p) {
+    int32_t items = 0;
+    for (int s = 0; s < L.n_seg; ++s) {
+      const Seg &sg = L.seg[s];
+      L.item_off[s] = items;
+      if (path[s] == p) items += L.n_layers * L.H * sg.nrt * sg.nchunk;
+    }
+    L.item_off[L.n_seg] = items;
+    if (items == 0) continue;
+    L.rows_per_item = kPath[p].rows;
+    e = p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream, sms) : launch_simt(L, stream);
+  }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);
   if (e == cudaSuccess) return COMMITKV_OK;
   cudaGetLastError();

@@ -63,6 +63,8 @@ struct Launch {
 
 // CUDA cores: any layout and type.  Rows per item: 16 or 64.
 cudaError_t launch_simt(const Launch &L, cudaStream_t s);
+// Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
+cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, int sms);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);
 
 struct Item {
@@ -180,10 +182,11 @@ __device__ __forceinline__ int tile_end(const Tiles &t, int j, int tile) {
 __device__ __forceinline__ int chunk_tile(const Tiles &t, int c, int n) { return (int)((int64_t)t.n * c / n); }
 
 // sum of exp2(s - m) v over the visible tokens of tiles [j0, j1) for one row,
-// by the 32 lanes of a warp: o[k] is channel lane + 32 k.  Only visible tokens
-// are read.  The tile kernels multiply masked tokens by weights of zero, which
-// is wrong where a masked value is infinite or NaN, so they redo a row whose
-// sums are not finite this way (its m and l never see masked tokens).
+// by the 32 lanes of a warp: o[k] is channel lane + 32 k.  A masked token's
+// values have no part in it.  The tile kernels multiply masked tokens by
+// weights of zero, which is wrong where a masked value is infinite or NaN, so
+// they redo a row whose sums are not finite this way (its m and l never see
+// masked tokens).  32 tokens at a time, a lane each for the scores.
 template <typename T, int D>
 __device__ __noinline__ void redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
                                       Tiles tl, int tile, int j0, int j1, float m, float *o) {
@@ -191,22 +194,29 @@ __device__ __noinline__ void redo_row(const Launch &L, const Seg &sg, int l, int
   const T *q = static_cast<const T *>(qrow);
   const T *k = static_cast<const T *>(sg.k) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
   const T *v = static_cast<const T *>(sg.v) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
-  float qv[D / 32];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    qv[i] = to_f32(q[lane + 32 * i]);
-    o[i] = 0.0f;
-  }
+  for (int c = 0; c < D / 32; ++c) o[c] = 0.0f;
   for (int j = j0; j < j1; ++j) {
-    const int e = tile_end(tl, j, tile);
-    for (int i = tile_start(tl, j, tile); i < e; ++i) {
-      if (!sees(sp, i)) continue;
-      float dot = 0.0f;
+    const int a = tile_start(tl, j, tile), e = tile_end(tl, j, tile);
+    for (int i0 = a; i0 < e; i0 += 32) {
+      const int i = i0 + lane;
+      const bool in = i < e && sees(sp, i);
+      float p = 0.0f;
+      if (in) {
+        const T *ki = k + (int64_t)i * sg.st;
+        float dot = 0.0f;
+#pragma unroll 16
+        for (int c = 0; c < D; ++c) dot = fmaf(to_f32(q[c]), to_f32(ki[c]), dot);
+        p = exp2f(fmaf(dot, L.scale_log2, -m));
+      }
+      const unsigned seen = __ballot_sync(0xffffffffu, in);
+#pragma unroll 8
+      for (int u = 0; u < 32; ++u) {
+        const float pu = __shfl_sync(0xffffffffu, p, u);
+        if (!(seen >> u & 1)) continue;
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) dot = fmaf(qv[c], to_f32(k[(int64_t)i * sg.st + lane + 32 * c]), dot);
-      const float p = exp2f(fmaf(warp_sum(dot), L.scale_log2, -m));
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) o[c] = fmaf(p, to_f32(v[(int64_t)i * sg.st + lane + 32 * c]), o[c]);
+        for (int c = 0; c < D / 32; ++c) o[c] = fmaf(pu, to_f32(v[(int64_t)(i0 + u) * sg.st + lane + 32 * c]), o[c]);
+      }
     }
     bool done = true;  // NaN in every channel stays
 #pragma unroll

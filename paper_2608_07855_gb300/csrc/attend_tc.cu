@@ -1,0 +1,581 @@
+// Attention on the tensor cores (bf16, 16-byte aligned caches).
+//
+// A persistent CTA of 384 threads per SM takes items of up to 256 query rows,
+// two tiles of 128, over 128-token tiles of K and V:
+//   warp 0      TMA: K and V tiles through one ring of stages
+//   warp 1      the MMAs: S_b = Q_b K^T and O_b += P_b V (tcgen05, fp32 in TMEM)
+//   warp 3      the plan of the next item (what its rows see) and its Q rows,
+//               which lie apart in memory (heads of one position side by side)
+//   warps 4-11  two softmax groups of 128 threads, a thread per row
+// With two row tiles a group has one each and both take every K and V tile:
+// while one group works on its scores the tensor cores run the other's
+// products.  With one row tile the groups take alternate token tiles of it and
+// join their sums at the end of the item.
+// Per tile a thread reads its 128 scores from TMEM once, keeps a running
+// maximum that is only raised when it falls behind by 2^8 (O is rescaled
+// then), and puts the weights back over the scores as bf16 for P V.  Weights
+// are rounded to bf16 because the product with bf16 values takes one type: an
+// error of 2^-9 of each weight on average, that of the output's own rounding.
+// Sums of weights are fp32 and not rounded.
+// TMEM: S/P of group b at column 128 b, O of group b at 256 + D b.
+#include <cudaTypedefs.h>
+#include <string.h>
+
+#include "attend.cuh"
+#include "sm103.cuh"
+
+namespace ckv {
+namespace at {
+namespace {
+
+using namespace ckv::sm103;
+
+constexpr int BM = 128;  // rows of a tile
+constexpr int BT = 128;  // tokens of a tile
+// Long enough for the rows that redo_row takes (32 rows of a million tokens: under a second).
+constexpr uint64_t kWait = 4000000000ull;
+constexpr float kLazy = 8.0f;
+
+struct TcParams {
+  Launch L;
+  CUtensorMap k[kMaxSeg], v[kMaxSeg];  // [M][H][S][d], box 64 x 128 x 1 x 1
+};
+
+static_assert(sizeof(TcParams) <= 32764, "kernel parameters");
+
+struct Plan {
+  Tiles tl;
+  int j0, j1, rows;
+};
+
+template <int D>
+struct Smem {
+  static constexpr int kTile = BT * D * 2;
+  static constexpr int NST = D == 128 ? 4 : 8;
+  alignas(1024) uint8_t q[2][kTile];
+  alignas(1024) uint8_t kv[NST][kTile];
+  Span span[2][2 * BM];
+  Plan plan[2];
+  float2 pub[BM];  // one row tile: group 1's (m, l)
+  uint64_t plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
+      o_empty[2], pub_full, pub_empty, drain;
+  uint32_t tmem;
+  int abort_flag;
+};
+
+__device__ __forceinline__ void tma4(void *dst, const CUtensorMap *m, int x, int tok, int h, int l, uint64_t *bar,
+                                     uint64_t pol) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(tok), "r"(h), "r"(l), "r"(smem_addr(bar)), "l"(pol)
+      : "memory");
+}
+
+constexpr uint32_t kHalf = BT * 128;  // one 64-channel half of a tile
+
+__device__ __forceinline__ uint64_t desc_kmajor(const uint8_t *tile, int ks) {
+  return smem_desc(smem_addr(tile) + (ks >> 2) * kHalf + (ks & 3) * 32, 16, 1024, kSwizzle128B);
+}
+__device__ __forceinline__ uint64_t desc_v(const uint8_t *tile, int ks) {
+  return smem_desc(smem_addr(tile) + ks * 2048, kHalf, 1024, kSwizzle128B);
+}
+
+// The n-th item of this CTA: rounds run forwards and backwards in turn, which
+// evens out item lengths that fall from the first to the last.
+__device__ __forceinline__ int nth_item(int n) {
+  const int G = gridDim.x, b = blockIdx.x;
+  return n * G + ((n & 1) ? G - 1 - b : b);
+}
+
+// Columns of tile j that are worked on: a multiple of 32.
+__device__ __forceinline__ int tile_cols(const Tiles &t, int j) {
+  return (tile_end(t, j, BT) - tile_start(t, j, BT) + 31) & ~31;
+}
+
+__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, kWait, abort_flag));
+}
+
+template <int D>
+__global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcParams P, WsHeader *hdr) {
+  using S = Smem<D>;
+  constexpr int NST = S::NST;
+  extern __shared__ uint8_t smem_raw[];
+  S &sm = *reinterpret_cast<S *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const Launch &L = P.L;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int n_items = L.item_off[L.n_seg];
+  volatile int *abort_flag = &sm.abort_flag;
+
+  if (threadIdx.x == 0) {
+    sm.abort_flag = 0;
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&sm.plan_full[b], 1);
+      mbar_init(&sm.plan_empty[b], 10);  // TMA, MMA, eight softmax warps
+      mbar_init(&sm.s_full[b], 1);
+      mbar_init(&sm.p_full[b], 4);
+      mbar_init(&sm.o_full[b], 1);
+      mbar_init(&sm.o_empty[b], 4);
+    }
+    mbar_init(&sm.q_full, 1);
+    mbar_init(&sm.q_empty, 1);
+    for (int s = 0; s < NST; ++s) {
+      mbar_init(&sm.kv_full[s], 1);
+      mbar_init(&sm.kv_empty[s], 1);
+    }
+    mbar_init(&sm.pub_full, 4);
+    mbar_init(&sm.pub_empty, 4);
+    mbar_init(&sm.drain, 1);
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&sm.tmem, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = sm.tmem;
+
+  // registers: 104 + 2 x 200 a thread of each group of four warps = 3 x 168
+  if (warp < 4) {
+    regs_dec<104>();
+    if (warp == 0 && lane == 0) {
+      // ------------------------------------------------------------ TMA
+      const uint64_t pol = policy_evict_normal();
+      uint32_t g = 0;  // tiles copied
+      bool ok = true;
+      auto load = [&](const CUtensorMap *m, int tok, const Item &it) {
+        const int s = g % NST;
+        if (g >= NST && !mbar_wait(&sm.kv_empty[s], (g / NST - 1) & 1, kWait, abort_flag)) return false;
+        mbar_expect_tx(&sm.kv_full[s], S::kTile);
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) tma4(sm.kv[s] + x * kHalf, m, 64 * x, tok, it.kvh, it.l, &sm.kv_full[s], pol);
+        ++g;
+        return true;
+      };
+      for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
+        if (!mbar_wait(&sm.plan_full[n & 1], (n >> 1) & 1, kWait, abort_flag)) break;
+        const Plan pl = sm.plan[n & 1];
+        mbar_arrive(&sm.plan_empty[n & 1]);
+        const Item it = decode_item(L, item);
+        for (int j = pl.j0; j < pl.j1 && ok; ++j) {
+          const int tok = tile_start(pl.tl, j, BT);
+          ok = load(&P.k[it.s], tok, it) && load(&P.v[it.s], tok, it);
+        }
+      }
+      if (*abort_flag)  // let the copies already issued land before the CTA leaves
+        for (uint32_t u = g > NST ? g - NST : 0; u < g; ++u) mbar_wait_drain(&sm.kv_full[u % NST], (u / NST) & 1, kWait);
+    } else if (warp == 1 && lane == 0) {
+      // ------------------------------------------------------------ MMA
+      uint32_t g = 0, np[2] = {0, 0};  // tile pairs (K at 2 g, V at 2 g + 1) of earlier items; tiles of each buffer
+      uint32_t uses[2] = {0, 0};       // items in which O_b was filled
+      bool ok = true;
+      auto kv_wait = [&](uint32_t u) { return mbar_wait(&sm.kv_full[u % NST], (u / NST) & 1, kWait, abort_flag); };
+      auto qk = [&](int qt, int b, uint32_t u, int cols) {
+        const uint32_t idesc = idesc_bf16_f32(BM, 0, 0, 0) | ((uint32_t)(cols >> 3) << 17);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          mma_bf16(tm + BT * b, desc_kmajor(sm.q[qt], ks), desc_kmajor(sm.kv[u % NST], ks), idesc, ks > 0);
+        mma_commit(&sm.s_full[b]);
+      };
+      auto pv = [&](int b, uint32_t u, int cols, bool first) {
+        const uint32_t idesc = idesc_bf16_f32(BM, D, 0, 1);
+#pragma unroll
+        for (int ks = 0; ks < BT / 16; ++ks)
+          if (16 * ks < cols)
+            mma_bf16_ts(tm + 256 + D * b, tm + BT * b + 8 * ks, desc_v(sm.kv[u % NST], ks), idesc, !(first && ks == 0));
+      };
+      for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
+        if (!mbar_wait(&sm.plan_full[n & 1], (n >> 1) & 1, kWait, abort_flag)) break;
+        const Plan pl = sm.plan[n & 1];
+        mbar_arrive(&sm.plan_empty[n & 1]);
+        if (!mbar_wait(&sm.q_full, n & 1, kWait, abort_flag)) break;
+        tc_fence_after();
+        const int nt = pl.j1 - pl.j0;
+        if (nt == 0) mbar_arrive(&sm.q_empty);
+        if (pl.rows > BM) {
+          // two row tiles, every token tile for both
+          for (int j = 0; j <= nt && ok && nt > 0; ++j) {
+            // P V of tile j - 1, Q K^T of tile j
+            for (int b = 0; b < 2 && ok; ++b) {
+              if (j > 0) {
+                const uint32_t u = 2 * (g + j - 1) + 1;
+                ok = (b || kv_wait(u)) && (j > 1 || uses[b] == 0 || mbar_wait(&sm.o_empty[b], (uses[b] - 1) & 1, kWait, abort_flag)) &&
+                     mbar_wait(&sm.p_full[b], np[b] & 1, kWait, abort_flag);
+                if (!ok) break;
+                ++np[b];
+                tc_fence_after();
+                pv(b, u, tile_cols(pl.tl, pl.j0 + j - 1), j == 1);
+                if (b) mma_commit(&sm.kv_empty[u % NST]);
+                if (j == nt) mma_commit(&sm.o_full[b]), ++uses[b];
+              }
+              if (j < nt) {
+                const uint32_t u = 2 * (g + j);
+                if (!(ok = b || kv_wait(u))) break;
+                tc_fence_after();
+                qk(b, b, u, tile_cols(pl.tl, pl.j0 + j));
+                if (b) mma_commit(&sm.kv_empty[u % NST]);
+                if (b && j + 1 == nt) mma_commit(&sm.q_empty);
+              }
+            }
+          }
+        } else {
+          // one row tile, the groups take alternate token tiles
+          for (int j = 0; j < nt + 2 && ok && nt > 0; ++j) {
+            const int b = j & 1;
+            if (j >= 2) {  // P V of tile j - 2
+              const int i = j - 2;
+              const uint32_t u = 2 * (g + i) + 1;
+              ok = kv_wait(u) && (i > 1 || uses[b] == 0 || mbar_wait(&sm.o_empty[b], (uses[b] - 1) & 1, kWait, abort_flag)) &&
+                   mbar_wait(&sm.p_full[b], np[b] & 1, kWait, abort_flag);
+              if (!ok) break;
+              ++np[b];
+              tc_fence_after();
+              pv(b, u, tile_cols(pl.tl, pl.j0 + i), i < 2);
+              mma_commit(&sm.kv_empty[u % NST]);
+              if (j >= nt) mma_commit(&sm.o_full[b]), ++uses[b];
+            }
+            if (j < nt) {
+              const uint32_t u = 2 * (g + j);
+              if (!(ok = kv_wait(u))) break;
+              tc_fence_after();
+              qk(0, b, u, tile_cols(pl.tl, pl.j0 + j));
+              mma_commit(&sm.kv_empty[u % NST]);
+              if (j + 1 == nt) mma_commit(&sm.q_empty);
+            }
+          }
+        }
+        g += nt;
+      }
+      if (*abort_flag) {
+        mma_commit(&sm.drain);  // every MMA issued by this thread has completed
+        mbar_wait_drain(&sm.drain, 0, kWait);
+      }
+    } else if (warp == 3) {
+      // ------------------------------------------------------------ plans and Q rows
+      for (int n = 0, item; (item = nth_item(n)) < n_items; ++n) {
+        const int buf = n & 1;
+        if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, abort_flag)) break;
+        const Item it = decode_item(L, item);
+        const Seg &sg = L.seg[it.s];
+        const int r0 = it.rt * 2 * BM, rows = min(2 * BM, sg.R - r0);
+        const __nv_bfloat16 *src[2 * BM / 32];
+        int lo = 0x7fffffff, hi = 0, se = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * BM / 32; ++i) {
+          Span sp = {0, 0, 0};
+          int rr = r0 + lane + 32 * i;
+          src[i] = nullptr;
+          if (rr < sg.R) {
+            const Traj &t = L.t[traj_of_row(L, sg, rr)];
+            src[i] = static_cast<const __nv_bfloat16 *>(t.q) + row_index(L, t, it.l, it.kvh, rr) * D;
+            sp = row_span(sg.pos, sg.S, t.qpos[rr / L.g], L.window, L.sinks);
+            if (sp.lo < sp.hi) lo = min(lo, sp.lo), hi = max(hi, sp.hi);
+            se = max(se, sp.se);
+          }
+          sm.span[buf][lane + 32 * i] = sp;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+          hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+          se = max(se, __shfl_xor_sync(0xffffffffu, se, o));
+        }
+        if (lane == 0) {
+          const Tiles tl = make_tiles(lo, hi, se, BT);
+          sm.plan[buf] = {tl, chunk_tile(tl, it.c, sg.nchunk), chunk_tile(tl, it.c + 1, sg.nchunk), rows};
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
+        if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
+        // rows of D x 2 bytes, each by D / 8 lanes
+        constexpr int LR = D / 8, RW = 32 / LR;  // lanes a row, rows a step
+        const int part = lane % LR;
+#pragma unroll
+        for (int i = 0; i < 2 * BM / 32; ++i) {
+          if (32 * i >= rows) break;
+#pragma unroll
+          for (int k = 0; k < 32 / RW; ++k) {
+            const int r = k * RW + lane / LR;  // within the 32 rows
+            const uint64_t p = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src[i]), r);
+            if (!p) continue;
+            const int row = (32 * i + r) % BM;
+            uint8_t *dst = sm.q[32 * i / BM] + (part >> 3) * kHalf + sw128_offset(row, part & 7);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(p + 16 * part) : "memory");
+          }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.q_full);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ softmax
+    regs_inc<200>();
+    const int hb = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane;
+    const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+    const uint32_t s_col = tm + lanes + BT * hb, o_col = tm + lanes + 256 + D * hb;
+    const float2 scale2 = make_float2(L.scale_log2, L.scale_log2);
+    uint32_t ns = 0, uses = 0, npub = 0;  // score tiles, items that filled O_hb, joined items
+    bool ok = true;
+    for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
+      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+      const Plan pl = sm.plan[n & 1];
+      const bool two = pl.rows > BM;
+      const int lrow = two ? hb * BM + row : row;  // row of the item
+      const Span sp = sm.span[n & 1][lrow];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
+      const Item it = decode_item(L, item);
+      const Seg &sg = L.seg[it.s];
+      const bool warp_rows = lrow - lane < pl.rows;  // the warp has a row of the item
+      float m_used = -INFINITY, lsum = 0.0f;
+      const int step = two ? 1 : 2, first = pl.j0 + (two ? 0 : hb);
+      for (int j = first; j < pl.j1; j += step) {
+        if (!wait_warp(&sm.s_full[hb], ns & 1, abort_flag)) {
+          ok = false;
+          break;
+        }
+        ++ns;
+        tc_fence_after();
+        if (!warp_rows) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.p_full[hb]);
+          continue;
+        }
+        const int t0 = tile_start(pl.tl, j, BT), t1 = tile_end(pl.tl, j, BT), nc = (t1 - t0 + 31) >> 5;
+        float x[BT];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c < nc) tmem_ld32f(s_col + 32 * c, &x[32 * c]);
+        tmem_wait_ld();
+        // every row of the warp sees every column: nothing to mask
+        const bool all = (sp.lo <= t0 && t0 + 32 * nc <= sp.hi) && t0 + 32 * nc <= t1;
+        if (!__all_sync(0xffffffffu, all)) {
+          const int a = t0 - sp.lo, end = min(sp.hi, t1) - sp.lo, se = min(sp.se, t1) - t0;
+          const unsigned len = end > 0 ? (unsigned)end : 0u;
+#pragma unroll
+          for (int c = 0; c < BT; ++c) x[c] = (unsigned)(a + c) < len || c < se ? x[c] : -INFINITY;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c < nc) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mx[k] = fmax3(mx[k], x[32 * c + i + 2 * k], x[32 * c + i + 2 * k + 1]);
+          }
+        const float mt = fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]) * L.scale_log2;
+        const bool raise = mt > m_used + kLazy;  // false while both are -inf
+        const bool fix = raise && m_used != -INFINITY;  // -inf: the row's sums are still zero
+        const float f = fix ? exp2f(m_used - mt) : 1.0f;
+        if (raise) m_used = mt;
+        // the scores of this tile came after the products of the last one, so O is stable
+        if (__any_sync(0xffffffffu, fix)) {
+#pragma unroll
+          for (int c0 = 0; c0 < D; c0 += 32) {
+            uint32_t r[32];
+            tmem_ld32(o_col + c0, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+            tmem_st32(o_col + c0, r);
+          }
+          lsum *= f;
+        }
+        const float neg = m_used == -INFINITY ? 0.0f : -m_used;
+        const float2 neg2 = make_float2(neg, neg);
+        float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c < nc) {
+            uint32_t p[16];
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const float2 t = ffma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), scale2, neg2);
+              const float2 e = make_float2(fast_exp2(t.x), fast_exp2(t.y));
+              ps[(i >> 1) & 1] = fadd2(ps[(i >> 1) & 1], e);
+              const __nv_bfloat162 h = __floats2bfloat162_rn(e.x, e.y);
+              p[i >> 1] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+            tmem_st16(s_col + 16 * c, p);
+          }
+        tmem_wait_st();
+        const float2 pa = fadd2(ps[0], ps[1]);
+        lsum += pa.x + pa.y;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.p_full[hb]);
+      }
+      if (!ok) break;
+      // ---------------------------------------------------------- results
+      const bool mine = first < pl.j1, other = !two && pl.j0 + 1 < pl.j1;  // O_hb / O_1 of a joined item was filled
+      if (mine && !wait_warp(&sm.o_full[hb], uses & 1, abort_flag)) break;
+      if (mine) ++uses;
+      tc_fence_after();
+      float f0 = 1.0f, f1 = 0.0f, m = m_used;
+      if (!two) {
+        if (hb == 1) {
+          if (npub > 0 && !wait_warp(&sm.pub_empty, (npub - 1) & 1, abort_flag)) break;
+          ++npub;
+          sm.pub[row] = make_float2(m_used, lsum);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.pub_full);
+          continue;  // group 0 reads O_1
+        }
+        if (!wait_warp(&sm.pub_full, npub & 1, abort_flag)) break;
+        ++npub;
+        tc_fence_after();
+        const float2 o1 = sm.pub[row];
+        m = fmaxf(m_used, o1.x);
+        const float ref = m == -INFINITY ? 0.0f : m;
+        f0 = exp2f(m_used - ref), f1 = exp2f(o1.x - ref);
+        lsum = fmaf(lsum, f0, o1.y * f1);
+      }
+      const int r = it.rt * 2 * BM + lrow;
+      const bool valid = lrow < pl.rows;
+      const Traj *t = nullptr;
+      int64_t orow = 0;
+      __nv_bfloat16 *dst = nullptr;
+      float *pdst = nullptr;
+      const void *qrow = nullptr;
+      if (valid) {
+        int rr = r;
+        t = &L.t[traj_of_row(L, sg, rr)];
+        orow = row_index(L, *t, it.l, it.kvh, rr);
+        qrow = static_cast<const __nv_bfloat16 *>(t->q) + orow * D;
+        if (sg.part >= 0) pdst = L.po + part_index(L, sg, it, r) * D;
+        else dst = static_cast<__nv_bfloat16 *>(t->out) + orow * D;
+      }
+      const float inv = norm_of(lsum);
+      const float g0 = dst ? f0 * inv : f0, g1 = dst ? f1 * inv : f1;
+      float chk = 0.0f;
+      if (warp_rows) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          float y[32];
+          if (mine) {
+            tmem_ld32f(o_col + c0, y);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] *= g0;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = 0.0f;
+          }
+          if (other) {
+            float z[32];
+            tmem_ld32f(o_col + D + c0, z);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = fmaf(z[i], g1, y[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) chk = fmaf(y[i], 0.0f, chk);  // NaN if any is not finite
+          if (pdst) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              *reinterpret_cast<float4 *>(pdst + c0 + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+          } else if (dst) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint4 w;
+              uint32_t *wp = &w.x;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(y[i + 2 * k], y[i + 2 * k + 1]);
+                wp[k] = *reinterpret_cast<const uint32_t *>(&h);
+              }
+              *reinterpret_cast<uint4 *>(dst + c0 + i) = w;
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (mine) mbar_arrive(&sm.o_empty[hb]);
+        if (other) mbar_arrive(&sm.o_empty[1]);
+        if (!two) mbar_arrive(&sm.pub_empty);
+      }
+      if (valid) {
+        if (pdst) L.pml[part_index(L, sg, it, r)] = make_float2(m, lsum);
+        else if (t->lse) t->lse[orow] = lse_of(m, lsum);
+      }
+      unsigned bad = __ballot_sync(0xffffffffu, valid && chk != 0.0f && isfinite(lsum));
+      while (bad) {  // a masked value that is not finite met a weight of zero
+        const int b = __ffs(bad) - 1;
+        bad &= bad - 1;
+        const Span one = {__shfl_sync(0xffffffffu, sp.lo, b), __shfl_sync(0xffffffffu, sp.hi, b),
+                          __shfl_sync(0xffffffffu, sp.se, b)};
+        const float mb = __shfl_sync(0xffffffffu, m, b), lb = __shfl_sync(0xffffffffu, lsum, b);
+        const void *qb = reinterpret_cast<const void *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(qrow), b));
+        float o[D / 32];
+        redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1, mb == -INFINITY ? 0.0f : mb,
+                                   o);
+        __syncwarp();
+        write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, lb);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tm, 512);
+  if (threadIdx.x == 0 && sm.abort_flag) record_error(hdr, COMMITKV_ERR_TIMEOUT, 30);
+}
+
+// ------------------------------------------------------------------ host
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+  static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
+                        cudaSuccess &&
+                    q == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p) : nullptr;
+  }();
+  return fn;
+}
+
+bool map_kv(CUtensorMap *m, const void *base, const Launch &L, const Seg &sg) {
+  auto enc = encode_fn();
+  if (!enc) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)L.d, (cuuint64_t)sg.S, (cuuint64_t)L.H, (cuuint64_t)L.M};
+  const cuuint64_t strides[3] = {(cuuint64_t)sg.st * 2, (cuuint64_t)sg.sh * 2, (cuuint64_t)sg.sl * 2};
+  const cuuint32_t box[4] = {64, BT, 1, 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s, int sms) {
+  const int smem = (int)sizeof(Smem<D>) + 1024, items = P.L.item_off[P.L.n_seg];
+  const cudaError_t e = cudaFuncSetAttribute(attend_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  attend_tc<D><<<items < sms ? items : sms, 384, smem, s>>>(P, hdr);
+  ++launch_count();
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, int sms) {
+  static thread_local TcParams P;
+  P.L = L;
+  for (int i = 0; i < L.n_seg; ++i) {
+    const Seg &sg = L.seg[i];
+    if (sg.S == 0 || L.item_off[i] == L.item_off[i + 1]) continue;
+    if (!map_kv(&P.k[i], sg.k, L, sg) || !map_kv(&P.v[i], sg.v, L, sg)) return cudaErrorInvalidValue;
+  }
+  return L.d == 128 ? launch<128>(P, hdr, s, sms) : launch<64>(P, hdr, s, sms);
+}
+
+}  // namespace at
+}  // namespace ckv

@@ -1,0 +1,416 @@
+"""Attention over resident caches against its definition in 64 bits: types,
+layouts, lengths, masks, positions with gaps, values that are not finite,
+graphs, streams, and the calls around it."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_07855_gb300 import commitkv as ck  # noqa: E402
+
+import attention_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+SENT = 12352.0  # representable in bf16
+
+
+class Problem:
+    """Trajectories (S, W) with their data on the host, and the call on the device."""
+
+    def __init__(self, dtype, d, M, H, Hq, trajs, gaps=1.0, prefix=0, layout="dense", seed=0, qpos=None, spread=1.0,
+                 scale=0.0, edit=None):
+        self.shape = ck.make_shape(M, H, Hq, d, dtype, scale)
+        self.dtype, self.scale = dtype, scale
+        self.pre, self.host = None, []
+        g = torch.Generator().manual_seed(seed + 99)
+        if prefix:
+            k, v = ref.cache(M, H, prefix, d, dtype, seed + 7)
+            self.pre = [k, v, ref.positions(prefix, 0, gaps, 0, seed + 5)]
+        first = int(self.pre[2][-1]) + 1 if prefix else 0
+        for i, (S, W) in enumerate(trajs):
+            k, v = ref.cache(M, H, S, d, dtype, seed + 10 * i)
+            pos = ref.positions(S, first, gaps, 16, seed + i)
+            Q = (spread * torch.randn(M, Hq, W, d, generator=g)).to(dtype)
+            last = int(pos[-1]) if S else first
+            p = np.arange(last - W + 1, last + 1) if qpos is None else np.asarray(qpos(pos, W))
+            self.host.append([k, v, pos, Q, p])
+        if edit:
+            edit(self)
+        self.layout = layout
+
+    def upload(self):
+        i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.int32)).cuda()  # noqa: E731
+        put = lambda x: ref.place(x, self.layout)  # noqa: E731
+        self.trajs = [ck.TrajTensors(put(k), put(v), i32(pos), q.cuda().contiguous(), i32(p))
+                      for k, v, pos, q, p in self.host]
+        self.prefix = None if self.pre is None else ck.TrajTensors(put(self.pre[0]), put(self.pre[1]), i32(self.pre[2]))
+        n = sum(t.q.numel() for t in self.trajs)
+        # outputs side by side with values between them that must stay
+        self.flat = torch.full((n + 64 * (len(self.trajs) + 1),), SENT, dtype=self.dtype, device="cuda")
+        self.flat_l = torch.full((n // self.shape.head_dim + 64 * (len(self.trajs) + 1),), SENT, device="cuda")
+        self.out, self.lse, a, b = [], [], 64, 64
+        for t in self.trajs:
+            m = t.q.numel()
+            self.out.append(self.flat[a:a + m].view(t.q.shape))
+            self.lse.append(self.flat_l[b:b + m // self.shape.head_dim].view(t.q.shape[:3]))
+            a, b = a + m + 64, b + m // self.shape.head_dim + 64
+        self.ws = ck.alloc_attention_workspace(self.shape, self.trajs, self.prefix)
+        return self
+
+    def call(self, window=0, sinks=0, lse=True, layer_mask=None, stream=None):
+        f = ck.commitkv_window_attention if self.pre is None else ck.commitkv_prefix_attention
+        kw = {} if self.pre is None else dict(prefix=self.prefix)
+        f(self.shape, self.trajs, out=self.out, lse_out=self.lse if lse else None, window=window, sinks=sinks,
+          layer_mask=layer_mask, workspace=self.ws, stream=stream, **kw)
+
+    def check(self, window=0, sinks=0, layers=None, lse=True):
+        torch.cuda.synchronize()
+        assert ck.commitkv_workspace_status(self.ws) == ck.COMMITKV_OK
+        for i, (k, v, pos, q, p) in enumerate(self.host):
+            parts = ([tuple(self.pre)] if self.pre else []) + [(k, v, pos)]
+            if layers is not None:
+                parts, q = [(x[layers], y[layers], z) for x, y, z in parts], q[layers]
+            if q.numel() == 0:
+                continue
+            o, l, to, tl = ref.attention(parts, q, p, window, sinks, self.scale, self.dtype == BF)
+            pick = (lambda x: x) if layers is None else (lambda x: x[layers])
+            ref.check(pick(self.out[i]), o, to, "out %d" % i)
+            if lse:
+                ref.check(pick(self.lse[i]), l, tl, "lse %d" % i)
+        self.guards()
+
+    def guards(self):
+        for flat, step in ((self.flat, 1), (self.flat_l, self.shape.head_dim)):
+            a = 0
+            for t in self.trajs:
+                assert (flat[a:a + 64] == SENT).all(), "written outside the outputs"
+                a += 64 + t.q.numel() // step
+            assert (flat[a:] == SENT).all(), "written outside the outputs"
+
+
+def run(window=0, sinks=0, **kw):
+    p = Problem(**kw).upload()
+    p.call(window, sinks)
+    p.check(window, sinks)
+    return p
+
+
+TYPES = [(F32, 64), (F32, 128), (BF, 64), (BF, 128)]
+IDS = ["f32-64", "f32-128", "bf16-64", "bf16-128"]
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("S", [1, 2, 31, 33, 127, 128, 129, 640, 1025])
+def test_single_token_lengths(dtype, d, S):
+    run(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(S, 1)], gaps=0.5)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [2, 5, 17, 64, 65, 130])
+def test_prompt_lengths(dtype, d, W):
+    run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(W + 150, W)], gaps=0.6)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("H,Hq", [(1, 1), (2, 2), (1, 3), (2, 10), (1, 16), (1, 40)])
+@pytest.mark.parametrize("W", [1, 9])
+def test_heads(dtype, d, H, Hq, W):
+    run(dtype=dtype, d=d, M=2, H=H, Hq=Hq, trajs=[(201, W)], window=150, sinks=3)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (7, 4), (64, 0), (100, 5), (128, 4), (300, 200), (1000, 64),
+                                          (2**31 - 1, 2**31 - 1)])
+@pytest.mark.parametrize("W,gaps", [(1, 0.4), (40, 0.4), (300, 1.0)])
+def test_windows(dtype, d, window, sinks, W, gaps):
+    run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(700, W), (333, W)], gaps=gaps, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+def test_ragged_batch(dtype, d):
+    """Lengths from none to long ones, trajectories without queries or tokens."""
+    run(dtype=dtype, d=d, M=1, H=2, Hq=4, gaps=0.7, window=200, sinks=4,
+        trajs=[(0, 3), (1, 1), (500, 1), (64, 64), (300, 0), (1400, 33), (0, 0), (257, 2), (129, 129)])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n", [1, 17, 64])
+def test_many_trajectories(dtype, d, n):
+    run(dtype=dtype, d=d, M=1, H=1, Hq=2, trajs=[(5 + 13 * i, 1) for i in range(n)])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 48])
+def test_rows_that_see_nothing(dtype, d, W):
+    """Queries before the first token, behind the last window, in any order."""
+    def qpos(pos, W):
+        return np.array([1000, 3, 99, 100, 101, 5000, 100 + len(pos), 350] * 6, np.int64)[:W] if W > 1 else [3]
+
+    def late(p):
+        for t in p.host:
+            t[2] += 100
+
+    p = run(dtype=dtype, d=d, M=1, H=2, Hq=4, trajs=[(400, W)], qpos=qpos, window=120, edit=late)
+    assert torch.isinf(p.lse[0][:, :, 1 if W > 1 else 0]).all() and (p.out[0][:, :, 1 if W > 1 else 0] == 0).all()
+    run(dtype=dtype, d=d, M=1, H=2, Hq=4, trajs=[(400, W)], qpos=qpos, window=120, sinks=130, edit=late)
+    run(dtype=dtype, d=d, M=1, H=2, Hq=4, trajs=[(400, W)], qpos=qpos, edit=late)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 24])
+def test_far_positions(dtype, d, W):
+    """Positions up to the largest int32."""
+    def far(p):
+        for t in p.host:
+            move = 2**31 - 1 - int(t[2][-1])
+            t[2] = t[2] + move
+            t[4] = t[4] + move
+
+    run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(500, W)], gaps=0.5, edit=far)
+    run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(500, W)], gaps=0.5, edit=far, window=77)
+
+
+@pytest.mark.parametrize("layout", ["tokens", "padded", "odd"])
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 70])
+def test_layouts(dtype, d, layout, W):
+    """Tokens outermost, rows with padding (NaN behind the last token and
+    channel), caches that only the CUDA cores can read."""
+    run(dtype=dtype, d=d, M=2, H=2, Hq=6, trajs=[(300, W), (77, W)], layout=layout, gaps=0.5, window=111, sinks=2)
+
+
+def test_offsets_beyond_32_bits():
+    """Tokens more than 2^31 elements apart."""
+    for dtype, d in ((BF, 128), (BF, 64), (F32, 64)):
+        for W in (1, 70):
+            p = Problem(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(2200, W)])
+            p.upload()
+            t, stride = p.trajs[0], (1 << 20) + 16
+            for name in ("k", "v"):
+                base = torch.empty(2200 * stride, dtype=dtype, device="cuda")
+                x = base.as_strided((1, 1, 2200, d), (2200 * stride, 2200 * stride, stride, 1))
+                x.copy_(getattr(t, name))
+                setattr(t, name, x)
+            p.call()
+            p.check()
+            del p, t, x, base
+            torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 40, 150])
+@pytest.mark.parametrize("prefix", [0, 90])
+def test_masked_values_that_are_not_finite(dtype, d, W, prefix):
+    """Infinities and NaN in tokens that no query, or only some, see."""
+    def edit(p):
+        k, v, pos, q, qp = p.host[0]
+        qp -= 30  # the last 30 tokens are seen by none
+        k[:, :, -30::2] = float("nan")
+        v[:, :, -29::2] = float("nan")
+        v[:, :, -20] = float("inf")
+        if W > 10:  # a token that only the later queries see
+            v[:, :, -30 - W // 2, 5] = float("inf")
+            k[:, 0, -33] = float("nan")
+        v[:, :, 3] = float("-inf")  # before every window
+        k[:, :, 4] = float("inf")
+        if prefix:
+            p.pre[1][:, :, 10:20] = float("nan")
+
+    p = run(dtype=dtype, d=d, M=1, H=2, Hq=4, trajs=[(400, W), (300, W)], window=120, sinks=2, edit=edit, prefix=prefix)
+    assert torch.isfinite(p.out[0][:, :, 0]).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+def test_visible_values_that_are_not_finite(dtype, d):
+    """A visible NaN or infinity reaches exactly the rows that see it."""
+    def edit(p):
+        p.host[0][1][:, :, 150, 7] = float("inf")
+        p.host[0][0][:, :, 260] = float("nan")
+
+    p = Problem(dtype=dtype, d=d, M=1, H=1, Hq=2, trajs=[(300, 100)], edit=edit).upload()
+    p.call()
+    torch.cuda.synchronize()
+    o = p.out[0].float()
+    seen = torch.tensor(p.host[0][4] >= 260, device="cuda")
+    assert torch.isnan(o[:, :, seen]).all() and torch.isnan(p.lse[0][:, :, seen]).all()
+    rest = o[:, :, ~seen]
+    assert torch.isinf(rest[..., 7]).all()
+    rest[..., 7] = 0
+    assert torch.isfinite(rest).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 33])
+def test_large_scores(dtype, d, W):
+    """Scores of several hundred: the running maximum moves often and far."""
+    run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(900, W)], spread=30.0)
+    run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(900, W)], scale=0.7)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("prefix", [1, 17, 128, 700])
+@pytest.mark.parametrize("n,W", [(1, 1), (3, 1), (9, 1), (2, 40), (40, 3)])
+def test_prefix(dtype, d, prefix, n, W):
+    run(dtype=dtype, d=d, M=1, H=2, Hq=8, prefix=prefix, trajs=[(W + (37 * i) % 150, W) for i in range(n)], gaps=0.6)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("window,sinks", [(50, 4), (200, 0), (400, 300), (3, 1)])
+def test_prefix_with_window(dtype, d, window, sinks):
+    """Windows that end inside the prefix, or before it is reached."""
+    run(dtype=dtype, d=d, M=2, H=1, Hq=4, prefix=260, window=window, sinks=sinks,
+        trajs=[(100, 1), (9, 3), (0, 2), (150, 0), (301, 80), (1, 1)])
+
+
+def test_prefix_equals_one_cache():
+    """A shared prefix and the same tokens in every cache agree within both tolerances."""
+    for dtype, d in TYPES:
+        p = run(dtype=dtype, d=d, M=1, H=2, Hq=4, prefix=333, trajs=[(70, 2), (20, 2)], window=90, sinks=4)
+        joined = [ck.TrajTensors(torch.cat([p.prefix.k, t.k], 2), torch.cat([p.prefix.v, t.v], 2),
+                                 torch.cat([p.prefix.pos, t.pos]), t.q, t.q_pos) for t in p.trajs]
+        out = [torch.empty_like(t.q) for t in joined]
+        ws = ck.alloc_attention_workspace(p.shape, joined)
+        ck.commitkv_window_attention(p.shape, joined, out=out, window=90, sinks=4, workspace=ws)
+        torch.cuda.synchronize()
+        for a, b in zip(out, p.out):
+            tol = 0.02 if dtype == BF else 1e-5
+            assert (a.float() - b.float()).abs().max() <= tol
+
+
+def test_empty_prefix():
+    p = run(dtype=BF, d=128, M=1, H=2, Hq=4, trajs=[(200, 5)])
+    want = p.out[0].clone()
+    z = torch.empty(1, 2, 0, 128, dtype=BF, device="cuda")
+    pre = ck.TrajTensors(z, z, torch.empty(0, dtype=torch.int32, device="cuda"))
+    p.flat.fill_(SENT)
+    ck.commitkv_prefix_attention(p.shape, p.trajs, prefix=pre, out=p.out, workspace=ck.alloc_attention_workspace(
+        p.shape, p.trajs, pre))
+    torch.cuda.synchronize()
+    assert torch.equal(want, p.out[0])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("prefix", [0, 200])
+@pytest.mark.parametrize("W", [1, 70])
+def test_layer_mask(dtype, d, prefix, W):
+    """Only the selected layers' rows are written; none selected: nothing."""
+    p = Problem(dtype=dtype, d=d, M=4, H=1, Hq=4, trajs=[(800, W)], prefix=prefix).upload()
+    p.call(layer_mask=[0, 0, 0, 0])
+    torch.cuda.synchronize()
+    assert (p.flat == SENT).all()
+    p.call(layer_mask=[1, 0, 1, 0])
+    p.check(layers=[0, 2])
+    assert (p.out[0][[1, 3]] == SENT).all() and (p.lse[0][[1, 3]] == SENT).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("prefix,W", [(0, 1), (0, 90), (300, 1), (300, 30)])
+def test_same_bits_every_time(dtype, d, prefix, W):
+    p = Problem(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(900, W), (55, W)], prefix=prefix).upload()
+    p.call()
+    torch.cuda.synchronize()
+    first = p.flat.clone(), p.flat_l.clone()
+    for _ in range(3):
+        p.ws[256:].fill_(0xFF)  # what an earlier call left in the workspace does not matter
+        p.call(lse=True)
+        torch.cuda.synchronize()
+        assert torch.equal(first[0], p.flat) and torch.equal(first[1], p.flat_l)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("prefix,W", [(0, 1), (0, 90), (300, 1)])
+def test_graph_and_stream(dtype, d, prefix, W):
+    """Captured on another stream and replayed on new data; two graphs share a workspace."""
+    p = Problem(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(600, W), (155, W)], prefix=prefix).upload()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    p.call(stream=s)
+    s.synchronize()
+    graphs = []
+    for window in (0, 100):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            p.call(window=window, sinks=4)
+        graphs.append(g)
+    new = Problem(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(600, W), (155, W)], prefix=prefix, seed=1000)
+    for t, h in zip(p.trajs, new.host):
+        t.k.copy_(h[0])
+        t.v.copy_(h[1])
+        t.q.copy_(h[3])
+    p.host = [n[:2] + o[2:3] + n[3:4] + o[4:] for n, o in zip(new.host, p.host)]
+    if prefix:
+        p.prefix.k.copy_(new.pre[0])
+        p.prefix.v.copy_(new.pre[1])
+        p.pre = new.pre[:2] + p.pre[2:]
+    for g, window in ((graphs[1], 100), (graphs[0], 0), (graphs[1], 100)):
+        p.flat.fill_(SENT)
+        p.flat_l.fill_(SENT)
+        g.replay()
+        p.check(window, 4)
+
+
+def test_calls_at_once():
+    """Two streams with a workspace each."""
+    ps = [Problem(dtype=BF, d=128, M=1, H=2, Hq=8, trajs=[(900, W)], prefix=pre, seed=W).upload()
+          for W, pre in ((1, 0), (90, 0), (1, 400), (64, 400))]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ps]
+    for _ in range(20):
+        for p, s in zip(ps, streams):
+            p.call(stream=s)
+    for p in ps:
+        p.check()
+
+
+def test_batch_kept_while_caches_grow():
+    """An AttentionBatch over buffers with room: lengths move, tokens are added in place."""
+    cap, d = 700, 128
+    p = Problem(dtype=BF, d=d, M=1, H=2, Hq=8, trajs=[(cap, 1), (cap, 1)], gaps=0.5).upload()
+    b = ck.attention_batch(p.shape, p.trajs, p.out, p.lse)
+    full = [list(h) for h in p.host]
+    for S in ((1, 3), (128, 200), (129, 640), (700, 699)):
+        for i, n in enumerate(S):
+            b.set_length(i, n)
+            p.trajs[i].q_pos.fill_(int(full[i][2][n - 1]))
+            k, v, pos, q, _ = full[i]
+            p.host[i] = [k[:, :, :n], v[:, :, :n], pos[:n], q, np.array([pos[n - 1]])]
+        ck.commitkv_window_attention(p.shape, b, window=300, sinks=2, workspace=p.ws)
+        p.check(300, 2)
+
+
+def test_cuda_cores_and_tensor_cores_agree(monkeypatch):
+    for d in (64, 128):
+        for W, prefix in ((1, 0), (60, 0), (1, 200)):
+            p = Problem(dtype=BF, d=d, M=1, H=2, Hq=8, trajs=[(500, W)], prefix=prefix).upload()
+            monkeypatch.setenv("COMMITKV_SCORING", "simt")
+            p.call(100, 4)
+            p.check(100, 4)
+            monkeypatch.delenv("COMMITKV_SCORING")
+            p.call(100, 4)
+            p.check(100, 4)
+
+
+def test_effects_from_attention():
+    """The attention of the probe window is a valid source of row statistics:
+    fp32 effects from (lse, 1, out) as from the library's own statistics."""
+    from paper_2608_07855_gb300 import synth
+    from paper_2608_07855_gb300.workload import DeviceTrajectory, shape_of
+
+    cfg = synth.CONFIGS["tiny"]
+    dev = DeviceTrajectory.upload(synth.make_trajectory(cfg, 0))
+    shape, tr = shape_of(cfg), dev.post()
+    out = torch.empty_like(tr.q)
+    lse = torch.empty(tr.q.shape[:3], device="cuda")
+    ck.commitkv_window_attention(shape, [tr], out=[out], lse_out=[lse], workspace=ck.alloc_attention_workspace(shape, [tr]))
+    stats = torch.cat([torch.stack([lse, torch.ones_like(lse), torch.zeros_like(lse), torch.zeros_like(lse)], -1), out], -1)
+    R, want = (torch.zeros(dev.P_post, device="cuda") for _ in range(2))
+    ws = ck.alloc_workspace(shape, [tr])
+    ck.commitkv_page_effects_from_stats(shape, [tr], [stats.contiguous()], [R], workspace=ws)
+    ck.commitkv_page_effects(shape, [tr], [want], workspace=ws)
+    torch.cuda.synchronize()
+    assert ck.commitkv_workspace_status(ws) == ck.COMMITKV_OK
+    assert ((R - want).abs() <= 1e-4 * want.abs()).all()
