@@ -36,6 +36,14 @@ constexpr int BT = 128;  // tokens of a tile
 constexpr uint64_t kWait = 4000000000ull;
 constexpr float kLazy = 8.0f;
 
+// mbar_wait that parks the thread before it first reads the clock.
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i)
+    if (mbar_try_wait_sleep(bar, parity, 20000)) return true;
+  return mbar_wait(bar, parity, kWait, abort_flag);
+}
+
 struct TcParams {
   Launch L;
   CUtensorMap k[kMaxSeg], v[kMaxSeg];  // [M][H][S][d], box 64 x 128 x 1 x 1
@@ -94,7 +102,114 @@ __device__ __forceinline__ int tile_cols(const Tiles &t, int j) {
 }
 
 __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, kWait, abort_flag));
+  return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
+}
+
+// The scores of a tile become weights relative to the row's reference maximum
+// m (base 2), which is raised where a score is above it by more than kLazy;
+// the row's sums are rescaled then.  The scores of this tile came after the
+// products of the last one, so O is stable.
+template <int D>
+__device__ __forceinline__ void raise_max(uint32_t o_col, float top, float &m, float &lsum) {
+  const bool raise = top > m + kLazy;           // false while both are -inf
+  const bool fix = raise && m != -INFINITY;     // -inf: the row's sums are still zero
+  if (__any_sync(0xffffffffu, fix)) {
+    const float f = fix ? exp2f(m - top) : 1.0f;
+    lsum *= f;
+#pragma unroll 1
+    for (int c0 = 0; c0 < D; c0 += 32) {
+      uint32_t r[32];
+      tmem_ld32(o_col + c0, r);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+      tmem_st32(o_col + c0, r);
+    }
+  }
+  if (raise) m = top;
+}
+
+// Weights of 32 columns, as bf16 pairs, and their sum.
+__device__ __forceinline__ void weigh32(const float *x, float2 scale2, float2 neg2, float2 (&ps)[2], uint32_t (&p)[16]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    const float2 t = ffma2(make_float2(x[i], x[i + 1]), scale2, neg2);
+    const float2 e = make_float2(fast_exp2(t.x), fast_exp2(t.y));
+    ps[(i >> 1) & 1] = fadd2(ps[(i >> 1) & 1], e);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(e.x, e.y);
+    p[i >> 1] = *reinterpret_cast<const uint32_t *>(&h);
+  }
+}
+
+__device__ __forceinline__ float max32(const float *x, float m) {
+  float mx[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mx[k] = fmax3(mx[k], x[i + 2 * k], x[i + 2 * k + 1]);
+  return fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]);
+}
+
+// A tile that every row of the warp sees whole.
+template <int D>
+__device__ __forceinline__ void soft_full(uint32_t s_col, uint32_t o_col, float scale, float &m, float &lsum) {
+  float x[BT];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) tmem_ld32f(s_col + 32 * c, &x[32 * c]);
+  tmem_wait_ld();
+  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < BT; i += 8)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mx[k] = fmax3(mx[k], x[i + 2 * k], x[i + 2 * k + 1]);
+  raise_max<D>(o_col, fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]) * scale, m, lsum);
+  const float neg = m == -INFINITY ? 0.0f : -m;
+  const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(neg, neg);
+  float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint32_t p[16];
+    weigh32(&x[32 * c], scale2, neg2, ps, p);
+    tmem_st16(s_col + 16 * c, p);
+  }
+  tmem_wait_st();
+  const float2 a = fadd2(ps[0], ps[1]);
+  lsum += a.x + a.y;
+}
+
+// A tile that ends early or that some rows see in part: 32 columns at a time,
+// read twice.
+template <int D>
+__device__ __forceinline__ void soft_masked(uint32_t s_col, uint32_t o_col, float scale, const Span &sp, int t0, int t1,
+                                            float &m, float &lsum) {
+  const int nc = (t1 - t0 + 31) >> 5, a = t0 - sp.lo, end = min(sp.hi, t1) - sp.lo, se = min(sp.se, t1) - t0;
+  const unsigned len = end > 0 ? (unsigned)end : 0u;
+  float x[32], top = -INFINITY;
+  auto load = [&](int c) {
+    tmem_ld32f(s_col + 32 * c, x);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = (unsigned)(a + 32 * c + i) < len || 32 * c + i < se ? x[i] : -INFINITY;
+  };
+#pragma unroll 1
+  for (int c = 0; c < nc; ++c) {
+    load(c);
+    top = max32(x, top);
+  }
+  raise_max<D>(o_col, top * scale, m, lsum);
+  const float neg = m == -INFINITY ? 0.0f : -m;
+  const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(neg, neg);
+  float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll 1
+  for (int c = 0; c < nc; ++c) {
+    uint32_t p[16];
+    load(c);
+    weigh32(x, scale2, neg2, ps, p);
+    tmem_st16(s_col + 16 * c, p);
+  }
+  tmem_wait_st();
+  const float2 b = fadd2(ps[0], ps[1]);
+  lsum += b.x + b.y;
 }
 
 template <int D>
@@ -148,7 +263,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       bool ok = true;
       auto load = [&](const CUtensorMap *m, int tok, const Item &it) {
         const int s = g % NST;
-        if (g >= NST && !mbar_wait(&sm.kv_empty[s], (g / NST - 1) & 1, kWait, abort_flag)) return false;
+        if (g >= NST && !wait(&sm.kv_empty[s], (g / NST - 1) & 1, abort_flag)) return false;
         mbar_expect_tx(&sm.kv_full[s], S::kTile);
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) tma4(sm.kv[s] + x * kHalf, m, 64 * x, tok, it.kvh, it.l, &sm.kv_full[s], pol);
@@ -156,7 +271,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         return true;
       };
       for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
-        if (!mbar_wait(&sm.plan_full[n & 1], (n >> 1) & 1, kWait, abort_flag)) break;
+        if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
         mbar_arrive(&sm.plan_empty[n & 1]);
         const Item it = decode_item(L, item);
@@ -172,7 +287,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       uint32_t g = 0, np[2] = {0, 0};  // tile pairs (K at 2 g, V at 2 g + 1) of earlier items; tiles of each buffer
       uint32_t uses[2] = {0, 0};       // items in which O_b was filled
       bool ok = true;
-      auto kv_wait = [&](uint32_t u) { return mbar_wait(&sm.kv_full[u % NST], (u / NST) & 1, kWait, abort_flag); };
+      auto kv_wait = [&](uint32_t u) { return wait(&sm.kv_full[u % NST], (u / NST) & 1, abort_flag); };
       auto qk = [&](int qt, int b, uint32_t u, int cols) {
         const uint32_t idesc = idesc_bf16_f32(BM, 0, 0, 0) | ((uint32_t)(cols >> 3) << 17);
 #pragma unroll
@@ -188,10 +303,10 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
             mma_bf16_ts(tm + 256 + D * b, tm + BT * b + 8 * ks, desc_v(sm.kv[u % NST], ks), idesc, !(first && ks == 0));
       };
       for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
-        if (!mbar_wait(&sm.plan_full[n & 1], (n >> 1) & 1, kWait, abort_flag)) break;
+        if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
         mbar_arrive(&sm.plan_empty[n & 1]);
-        if (!mbar_wait(&sm.q_full, n & 1, kWait, abort_flag)) break;
+        if (!wait(&sm.q_full, n & 1, abort_flag)) break;
         tc_fence_after();
         const int nt = pl.j1 - pl.j0;
         if (nt == 0) mbar_arrive(&sm.q_empty);
@@ -202,8 +317,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
             for (int b = 0; b < 2 && ok; ++b) {
               if (j > 0) {
                 const uint32_t u = 2 * (g + j - 1) + 1;
-                ok = (b || kv_wait(u)) && (j > 1 || uses[b] == 0 || mbar_wait(&sm.o_empty[b], (uses[b] - 1) & 1, kWait, abort_flag)) &&
-                     mbar_wait(&sm.p_full[b], np[b] & 1, kWait, abort_flag);
+                ok = (b || kv_wait(u)) && (j > 1 || uses[b] == 0 || wait(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag)) &&
+                     wait(&sm.p_full[b], np[b] & 1, abort_flag);
                 if (!ok) break;
                 ++np[b];
                 tc_fence_after();
@@ -228,8 +343,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
             if (j >= 2) {  // P V of tile j - 2
               const int i = j - 2;
               const uint32_t u = 2 * (g + i) + 1;
-              ok = kv_wait(u) && (i > 1 || uses[b] == 0 || mbar_wait(&sm.o_empty[b], (uses[b] - 1) & 1, kWait, abort_flag)) &&
-                   mbar_wait(&sm.p_full[b], np[b] & 1, kWait, abort_flag);
+              ok = kv_wait(u) && (i > 1 || uses[b] == 0 || wait(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag)) &&
+                   wait(&sm.p_full[b], np[b] & 1, abort_flag);
               if (!ok) break;
               ++np[b];
               tc_fence_after();
@@ -318,12 +433,12 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     const int hb = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane;
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     const uint32_t s_col = tm + lanes + BT * hb, o_col = tm + lanes + 256 + D * hb;
-    const float2 scale2 = make_float2(L.scale_log2, L.scale_log2);
     uint32_t ns = 0, uses = 0, npub = 0;  // score tiles, items that filled O_hb, joined items
     bool ok = true;
     for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
       if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
       const Plan pl = sm.plan[n & 1];
+      const Tiles tl = pl.tl;
       const bool two = pl.rows > BM;
       const int lrow = two ? hb * BM + row : row;  // row of the item
       const Span sp = sm.span[n & 1][lrow];
@@ -347,67 +462,11 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           if (lane == 0) mbar_arrive(&sm.p_full[hb]);
           continue;
         }
-        const int t0 = tile_start(pl.tl, j, BT), t1 = tile_end(pl.tl, j, BT), nc = (t1 - t0 + 31) >> 5;
-        float x[BT];
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c < nc) tmem_ld32f(s_col + 32 * c, &x[32 * c]);
-        tmem_wait_ld();
-        // every row of the warp sees every column: nothing to mask
-        const bool all = (sp.lo <= t0 && t0 + 32 * nc <= sp.hi) && t0 + 32 * nc <= t1;
-        if (!__all_sync(0xffffffffu, all)) {
-          const int a = t0 - sp.lo, end = min(sp.hi, t1) - sp.lo, se = min(sp.se, t1) - t0;
-          const unsigned len = end > 0 ? (unsigned)end : 0u;
-#pragma unroll
-          for (int c = 0; c < BT; ++c) x[c] = (unsigned)(a + c) < len || c < se ? x[c] : -INFINITY;
-        }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c < nc) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) mx[k] = fmax3(mx[k], x[32 * c + i + 2 * k], x[32 * c + i + 2 * k + 1]);
-          }
-        const float mt = fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]) * L.scale_log2;
-        const bool raise = mt > m_used + kLazy;  // false while both are -inf
-        const bool fix = raise && m_used != -INFINITY;  // -inf: the row's sums are still zero
-        const float f = fix ? exp2f(m_used - mt) : 1.0f;
-        if (raise) m_used = mt;
-        // the scores of this tile came after the products of the last one, so O is stable
-        if (__any_sync(0xffffffffu, fix)) {
-#pragma unroll
-          for (int c0 = 0; c0 < D; c0 += 32) {
-            uint32_t r[32];
-            tmem_ld32(o_col + c0, r);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-            tmem_st32(o_col + c0, r);
-          }
-          lsum *= f;
-        }
-        const float neg = m_used == -INFINITY ? 0.0f : -m_used;
-        const float2 neg2 = make_float2(neg, neg);
-        float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c < nc) {
-            uint32_t p[16];
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float2 t = ffma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), scale2, neg2);
-              const float2 e = make_float2(fast_exp2(t.x), fast_exp2(t.y));
-              ps[(i >> 1) & 1] = fadd2(ps[(i >> 1) & 1], e);
-              const __nv_bfloat162 h = __floats2bfloat162_rn(e.x, e.y);
-              p[i >> 1] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-            tmem_st16(s_col + 16 * c, p);
-          }
-        tmem_wait_st();
-        const float2 pa = fadd2(ps[0], ps[1]);
-        lsum += pa.x + pa.y;
+        const int t0 = tile_start(tl, j, BT), t1 = tile_end(tl, j, BT);
+        if (__all_sync(0xffffffffu, sp.lo <= t0 && t0 + BT <= min(sp.hi, t1)))
+          soft_full<D>(s_col, o_col, L.scale_log2, m_used, lsum);
+        else
+          soft_masked<D>(s_col, o_col, L.scale_log2, sp, t0, t1, m_used, lsum);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.p_full[hb]);
