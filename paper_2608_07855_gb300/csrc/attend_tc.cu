@@ -101,6 +101,17 @@ __device__ __forceinline__ int tile_cols(const Tiles &t, int j) {
   return (tile_end(t, j, BT) - tile_start(t, j, BT) + 31) & ~31;
 }
 
+// One lane of a converged warp, always the same.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(e));
+  return e != 0;
+}
+
 __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
   return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
 }
@@ -219,7 +230,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   extern __shared__ uint8_t smem_raw[];
   S &sm = *reinterpret_cast<S *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const Launch &L = P.L;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int n_items = L.item_off[L.n_seg];
   volatile int *abort_flag = &sm.abort_flag;
 
@@ -239,9 +250,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       mbar_init(&sm.kv_full[s], 1);
       mbar_init(&sm.kv_empty[s], 1);
     }
+    mbar_init(&sm.drain, 1);
     mbar_init(&sm.pub_full, 4);
     mbar_init(&sm.pub_empty, 4);
-    mbar_init(&sm.drain, 1);
     fence_mbar_init();
   }
   if (warp == 1) {
@@ -282,91 +293,83 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       }
       if (*abort_flag)  // let the copies already issued land before the CTA leaves
         for (uint32_t u = g > NST ? g - NST : 0; u < g; ++u) mbar_wait_drain(&sm.kv_full[u % NST], (u / NST) & 1, kWait);
-    } else if (warp == 1 && lane == 0) {
-      // ------------------------------------------------------------ MMA
-      uint32_t g = 0, np[2] = {0, 0};  // tile pairs (K at 2 g, V at 2 g + 1) of earlier items; tiles of each buffer
-      uint32_t uses[2] = {0, 0};       // items in which O_b was filled
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ MMAs
+      // The whole warp keeps step and one elected lane issues: in code that a
+      // single lane runs, an MMA took 100 cycles to issue.  (A warp for each
+      // group: 2,330 against 2,050 us on a 4K prompt over 36K tokens.)
+      uint32_t g = 0, np[2] = {0, 0}, uses[2] = {0, 0};  // earlier items: tiles, tiles of each group, items that filled O_b
       bool ok = true;
-      auto kv_wait = [&](uint32_t u) { return wait(&sm.kv_full[u % NST], (u / NST) & 1, abort_flag); };
-      auto qk = [&](int qt, int b, uint32_t u, int cols) {
+      auto kv_wait = [&](uint32_t u) { return wait_warp(&sm.kv_full[u % NST], (u / NST) & 1, abort_flag); };
+      auto qk = [&](int qt, int b, uint32_t u, int cols, bool last, bool end) {
         const uint32_t idesc = idesc_bf16_f32(BM, 0, 0, 0) | ((uint32_t)(cols >> 3) << 17);
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          mma_bf16(tm + BT * b, desc_kmajor(sm.q[qt], ks), desc_kmajor(sm.kv[u % NST], ks), idesc, ks > 0);
-        mma_commit(&sm.s_full[b]);
+          for (int ks = 0; ks < D / 16; ++ks)
+            mma_bf16(tm + BT * b, desc_kmajor(sm.q[qt], ks), desc_kmajor(sm.kv[u % NST], ks), idesc, ks > 0);
+          mma_commit(&sm.s_full[b]);
+          if (last) mma_commit(&sm.kv_empty[u % NST]);
+          if (end) mma_commit(&sm.q_empty);
+        }
+        __syncwarp();
       };
-      auto pv = [&](int b, uint32_t u, int cols, bool first) {
+      // P V of the i-th tile of group b in this item (last: nothing else needs the V tile, end: of the item)
+      auto pv = [&](int b, int i, uint32_t u, int cols, bool last, bool end) {
+        if (!(i > 0 || uses[b] == 0 || wait_warp(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag))) return false;
+        if (!wait_warp(&sm.p_full[b], (np[b] + i) & 1, abort_flag)) return false;
         const uint32_t idesc = idesc_bf16_f32(BM, D, 0, 1);
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
-        for (int ks = 0; ks < BT / 16; ++ks)
-          if (16 * ks < cols)
-            mma_bf16_ts(tm + 256 + D * b, tm + BT * b + 8 * ks, desc_v(sm.kv[u % NST], ks), idesc, !(first && ks == 0));
+          for (int ks = 0; ks < BT / 16; ++ks)
+            if (16 * ks < cols)
+              mma_bf16_ts(tm + 256 + D * b, tm + BT * b + 8 * ks, desc_v(sm.kv[u % NST], ks), idesc, i > 0 || ks > 0);
+          if (last) mma_commit(&sm.kv_empty[u % NST]);
+          if (end) mma_commit(&sm.o_full[b]);
+        }
+        __syncwarp();
+        return true;
       };
       for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
-        if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+        if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
-        mbar_arrive(&sm.plan_empty[n & 1]);
-        if (!wait(&sm.q_full, n & 1, abort_flag)) break;
-        tc_fence_after();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
+        if (!wait_warp(&sm.q_full, n & 1, abort_flag)) break;
         const int nt = pl.j1 - pl.j0;
-        if (nt == 0) mbar_arrive(&sm.q_empty);
+        if (nt == 0 && lane == 0) mbar_arrive(&sm.q_empty);  // else behind the last Q K^T
         if (pl.rows > BM) {
-          // two row tiles, every token tile for both
+          // two row tiles: tile j's Q K^T behind tile j - 1's P V, group by group
           for (int j = 0; j <= nt && ok && nt > 0; ++j) {
-            // P V of tile j - 1, Q K^T of tile j
+            const uint32_t uk = 2 * (g + j), uv = uk - 1;
+            const int ck = j < nt ? tile_cols(pl.tl, pl.j0 + j) : 0, cv = j > 0 ? tile_cols(pl.tl, pl.j0 + j - 1) : 0;
             for (int b = 0; b < 2 && ok; ++b) {
-              if (j > 0) {
-                const uint32_t u = 2 * (g + j - 1) + 1;
-                ok = (b || kv_wait(u)) && (j > 1 || uses[b] == 0 || wait(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag)) &&
-                     wait(&sm.p_full[b], np[b] & 1, abort_flag);
-                if (!ok) break;
-                ++np[b];
-                tc_fence_after();
-                pv(b, u, tile_cols(pl.tl, pl.j0 + j - 1), j == 1);
-                if (b) mma_commit(&sm.kv_empty[u % NST]);
-                if (j == nt) mma_commit(&sm.o_full[b]), ++uses[b];
-              }
-              if (j < nt) {
-                const uint32_t u = 2 * (g + j);
-                if (!(ok = b || kv_wait(u))) break;
-                tc_fence_after();
-                qk(b, b, u, tile_cols(pl.tl, pl.j0 + j));
-                if (b) mma_commit(&sm.kv_empty[u % NST]);
-                if (b && j + 1 == nt) mma_commit(&sm.q_empty);
-              }
+              if (j > 0) ok = (b || kv_wait(uv)) && pv(b, j - 1, uv, cv, b == 1, j == nt);
+              if (ok && j < nt && (ok = b || kv_wait(uk))) qk(b, b, uk, ck, b == 1, b == 1 && j + 1 == nt);
             }
           }
+          np[0] += nt, np[1] += nt;
+          uses[0] += nt > 0, uses[1] += nt > 0;
         } else {
           // one row tile, the groups take alternate token tiles
           for (int j = 0; j < nt + 2 && ok && nt > 0; ++j) {
+            const uint32_t uk = 2 * (g + j), uv = uk - 3;
             const int b = j & 1;
-            if (j >= 2) {  // P V of tile j - 2
-              const int i = j - 2;
-              const uint32_t u = 2 * (g + i) + 1;
-              ok = kv_wait(u) && (i > 1 || uses[b] == 0 || wait(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag)) &&
-                   wait(&sm.p_full[b], np[b] & 1, abort_flag);
-              if (!ok) break;
-              ++np[b];
-              tc_fence_after();
-              pv(b, u, tile_cols(pl.tl, pl.j0 + i), i < 2);
-              mma_commit(&sm.kv_empty[u % NST]);
-              if (j >= nt) mma_commit(&sm.o_full[b]), ++uses[b];
-            }
-            if (j < nt) {
-              const uint32_t u = 2 * (g + j);
-              if (!(ok = kv_wait(u))) break;
-              tc_fence_after();
-              qk(0, b, u, tile_cols(pl.tl, pl.j0 + j));
-              mma_commit(&sm.kv_empty[u % NST]);
-              if (j + 1 == nt) mma_commit(&sm.q_empty);
-            }
+            if (j >= 2) ok = kv_wait(uv) && pv(b, (j - 2) >> 1, uv, tile_cols(pl.tl, pl.j0 + j - 2), true, j >= nt);
+            if (ok && j < nt && (ok = kv_wait(uk))) qk(0, b, uk, tile_cols(pl.tl, pl.j0 + j), true, j + 1 == nt);
           }
+          np[0] += (nt + 1) / 2, np[1] += nt / 2;
+          uses[0] += nt > 0, uses[1] += nt > 1;
         }
         g += nt;
       }
-      if (*abort_flag) {
-        mma_commit(&sm.drain);  // every MMA issued by this thread has completed
-        mbar_wait_drain(&sm.drain, 0, kWait);
+      if (__any_sync(0xffffffffu, *abort_flag != 0)) {
+        if (elect_one()) {
+          mma_commit(&sm.drain);  // every MMA issued by this thread has completed
+          mbar_wait_drain(&sm.drain, 0, kWait);
+        }
+        __syncwarp();
       }
     } else if (warp == 3) {
       // ------------------------------------------------------------ plans and Q rows
