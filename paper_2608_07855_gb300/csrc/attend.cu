@@ -40,16 +40,16 @@ __global__ void __launch_bounds__(256) combine(const __grid_constant__ Launch L)
   }
   x -= L.out_off[a];
   const Traj &t = L.t[a];
-  const int R = L.g * t.W, kvh = x / R, r = x % R, l = L.layer_ids[li];
+  const int R = L.seg[a + L.prefix].Rs, kvh = x / R, r = x % R, l = L.layer_ids[li];
   float m = -INFINITY, lsum = 0.0f, o[D / 32];
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) o[c] = 0.0f;
   for (int k = 0; k <= L.prefix; ++k) {
     const Seg &sg = L.seg[k == L.prefix ? a + L.prefix : 0];
-    const int64_t first = sg.part + (int64_t)(li * L.H + kvh) * sg.nchunk * sg.R + (sg.t < 0 ? t.row0 + r : r);
+    const int64_t first = sg.part + (int64_t)(li * L.H + kvh) * sg.nchunk * sg.Rs + (sg.t < 0 ? t.row0 + r : r);
     for (int c0 = 0; c0 < sg.nchunk; c0 += 32) {
       const int n = min(32, sg.nchunk - c0);
-      const float2 ml = lane < n ? L.pml[first + (int64_t)(c0 + lane) * sg.R] : make_float2(-INFINITY, 0.0f);
+      const float2 ml = lane < n ? L.pml[first + (int64_t)(c0 + lane) * sg.Rs] : make_float2(-INFINITY, 0.0f);
       const float mn = fmaxf(m, warp_max(ml.x)), ref = mn == -INFINITY ? 0.0f : mn;
       const float f = exp2f(m - ref), wt = exp2f(ml.x - ref);
       m = mn;
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(256) combine(const __grid_constant__ Launch L)
       for (int c = 0; c < n; ++c) {
         const float wc = __shfl_sync(0xffffffffu, wt, c);
         const bool used = __shfl_sync(0xffffffffu, ml.y, c) != 0.0f;
-        const float *p = L.po + (first + (int64_t)(c0 + c) * sg.R) * D;
+        const float *p = L.po + (first + (int64_t)(c0 + c) * sg.Rs) * D;
 #pragma unroll
         for (int k2 = 0; k2 < D / 32; ++k2) {
           const float v = p[lane + 32 * k2];
@@ -137,37 +137,52 @@ int sm_count() {
   return n;
 }
 
-// Chunk length in tiles: every (slice, row tile) of a segment is cut into
-// ceil(tiles / length) items.  Estimated time in tile periods of `slots`
-// concurrent items: the work and each item's fixed part, spread over the
-// slots, and the tail that the last items leave, or whole waves where all
-// items are alike.
+// How the row tiles of a path's segments are divided: estimated time, in tile
+// periods of `slots` concurrent items, each of which costs `fixed` tiles
+// besides its own.
 struct Divide {
   int64_t base[kMaxSeg];   // slices x row tiles
-  int64_t tiles[kMaxSeg];  // at most, per row tile
+  int64_t tiles[kMaxSeg];  // of a row tile, at most
   int n;
 };
-int64_t chunk_tiles(const Divide &v, int64_t slots, double fixed, int64_t most_items) {
-  int64_t longest = 1;
-  for (int s = 0; s < v.n; ++s) longest = std::max(longest, v.tiles[s]);
-  int64_t best = longest;
+struct Division {
+  int64_t len;  // every row tile in chunks of `len` tiles,
+  int64_t rest, chunks;  // or, where rest >= 0, the last `rest` row tiles alone, in `chunks`
+};
+Division divide(const Divide &v, int64_t slots, double fixed, int64_t most_items, int64_t slices, bool tail) {
+  int64_t longest = 1, kinds = 0, kind = 0;
+  for (int s = 0; s < v.n; ++s) {
+    longest = std::max(longest, v.tiles[s]);
+    if (v.base[s] > 0 && v.tiles[s] > 0) ++kinds, kind = s;
+  }
+  Division best = {longest, -1, 0};
   double best_t = INFINITY;
-  for (int64_t k = 1; k <= longest; ++k) {  // chunks of the longest cache
-    const int64_t len = cdiv(longest, k);
-    if (k > 1 && len == cdiv(longest, k - 1)) continue;
-    int64_t items = 0, split = 0, kinds = 0;
+  for (int64_t k = 1, len = 0; k <= longest; ++k) {  // chunks of the longest cache
+    if (len == cdiv(longest, k)) continue;
+    len = cdiv(longest, k);
+    int64_t items = 0, split = 0;
     double work = 0;
     for (int s = 0; s < v.n; ++s) {
       const int64_t c = std::max<int64_t>(1, cdiv(v.tiles[s], len));
       items += v.base[s] * c;
       if (c > 1) split += v.base[s] * c;
       work += (double)v.base[s] * (v.tiles[s] + c * fixed);
-      kinds += v.base[s] > 0 && v.tiles[s] > 0;
     }
     if (split > most_items) break;
+    // whole waves where all items are alike, else the work and the tail that the last items leave
     const double one = len + fixed;
     const double t = items <= slots ? one : kinds == 1 ? cdiv(items, slots) * one : work / slots + 0.5 * one;
-    if (t < best_t * 0.98) best_t = t, best = len;  // fewer chunks unless more are clearly better
+    if (t < best_t * 0.98) best_t = t, best.len = len;  // fewer chunks unless more are clearly better
+  }
+  // one segment that fills some waves: only what is left of the last one is cut
+  const int64_t total = kinds == 1 && tail ? v.base[kind] : 0, waves = total / slots;
+  if (waves > 0) {
+    const int64_t rest = total / slices - waves * slots / slices;
+    for (int64_t n = 2; rest > 0 && rest * slices * n <= most_items && n <= v.tiles[kind]; ++n) {
+      const double t = waves * (v.tiles[kind] + fixed) +
+                       cdiv(rest * slices * n, slots) * ((double)v.tiles[kind] / n + fixed);
+      if (t < best_t * 0.98) best_t = t, best.rest = rest, best.chunks = n;
+    }
   }
   return best;
 }
@@ -276,22 +291,26 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
       ids[v.n++] = s;
     }
     if (v.n == 0) continue;
-    const int64_t len = chunk_tiles(v, (int64_t)sms * pi.resident, pi.fixed, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit);
+    const int64_t slices = (int64_t)L.n_layers * L.H;
+    const Division dv = divide(v, (int64_t)sms * pi.resident, pi.fixed, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit, slices, !prefix);
     int64_t items = 0;
     for (int i = 0; i < v.n; ++i) {
       Seg &sg = L.seg[ids[i]];
-      sg.nchunk = (int32_t)std::max<int64_t>(1, cdiv(v.tiles[i], len));
-      items += v.base[i] * sg.nchunk;
+      const bool rest = dv.rest >= 0 && v.base[i] > 0 && v.tiles[i] > 0;
+      sg.nchunk = (int32_t)(rest ? dv.chunks : std::max<int64_t>(1, cdiv(v.tiles[i], dv.len)));
+      sg.nsplit = (int32_t)(rest ? dv.rest : sg.nchunk > 1 ? sg.nrt : 0);
+      if (prefix) sg.nsplit = sg.nrt;  // two caches: all results are partial
+      sg.Rs = std::min(sg.R, sg.nsplit * pi.rows);
+      items += slices * ((sg.nrt - sg.nsplit) + (int64_t)sg.nsplit * sg.nchunk);
       if (items > (1 << 30)) return COMMITKV_ERR_UNSUPPORTED;
     }
   }
   for (int s = 0; s < L.n_seg; ++s) {
     Seg &sg = L.seg[s];
-    const bool split = prefix || sg.nchunk > 1;
-    sg.part = split ? parts : -1;
-    if (split) parts += (int64_t)L.n_layers * L.H * sg.nchunk * sg.R;
-    if (sg.t >= 0) L.out_off[sg.t + 1] = L.out_off[sg.t] + (split ? sg.R * L.H : 0);
-    merge = merge || split;
+    sg.part = parts;
+    parts += (int64_t)L.n_layers * L.H * sg.nchunk * sg.Rs;
+    if (sg.t >= 0) L.out_off[sg.t + 1] = L.out_off[sg.t] + sg.Rs * L.H;
+    merge = merge || sg.Rs > 0;
   }
   if (kAlign + partial_bytes(shape, parts) > workspace_bytes) return COMMITKV_ERR_WORKSPACE;  // partial_rows bounds it
   char *base = static_cast<char *>(workspace) + kAlign;
@@ -303,12 +322,12 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     for (int s = 0; s < L.n_seg; ++s) {
       const Seg &sg = L.seg[s];
       L.item_off[s] = items;
-      if (path[s] == p) items += L.n_layers * L.H * sg.nrt * sg.nchunk;
+      if (path[s] == p) items += L.n_layers * L.H * (sg.nrt - sg.nsplit + sg.nsplit * sg.nchunk);
     }
     L.item_off[L.n_seg] = items;
     if (items == 0) continue;
     L.rows_per_item = kPath[p].rows;
-    e = p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream, sms) : launch_simt(L, stream);
+    e = p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream) : launch_simt(L, stream);
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);
   if (e == cudaSuccess) return COMMITKV_OK;

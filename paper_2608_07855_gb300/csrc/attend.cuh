@@ -29,12 +29,14 @@ struct Seg {
   const void *k, *v;
   int64_t sl, sh, st;  // strides in elements
   const int32_t *pos;
-  int64_t part;  // first partial row; -1: the rows are written to the outputs
+  int64_t part;  // first partial row
   int32_t S;
   int32_t R;        // rows of a (layer, KV head) slice
   int32_t t;        // trajectory, -1: the shared prefix
   int32_t nrt;      // row tiles
+  int32_t nsplit;   // the first nsplit of them have partial results, of nchunk items each; the others one item
   int32_t nchunk;
+  int32_t Rs;       // rows of the first nsplit tiles
 };
 
 struct Traj {
@@ -64,11 +66,13 @@ struct Launch {
 // CUDA cores: any layout and type.  Rows per item: 16 or 64.
 cudaError_t launch_simt(const Launch &L, cudaStream_t s);
 // Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
-cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, int sms);
+cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);
 
 struct Item {
   int s, li, l, kvh, rt, c;
+  int n;       // chunks of its row tile
+  bool split;  // results are partial
 };
 
 __device__ __forceinline__ Item decode_item(const Launch &L, int item) {
@@ -81,14 +85,23 @@ __device__ __forceinline__ Item decode_item(const Launch &L, int item) {
   }
   it.s = a;
   const Seg &sg = L.seg[a];
-  int x = item - L.item_off[a];
-  it.c = x % sg.nchunk;
-  x /= sg.nchunk;
-  it.kvh = x % L.H;
-  x /= L.H;
-  it.li = x % L.n_layers;
   // the later rows of a prompt see more: they come first
-  it.rt = sg.nrt - 1 - x / L.n_layers;
+  int x = item - L.item_off[a], rt = sg.nrt - 1;
+  const int slices = L.H * L.n_layers, whole = slices * (sg.nrt - sg.nsplit);
+  it.split = x >= whole;
+  it.c = 0;
+  it.n = 1;
+  if (it.split) {
+    x -= whole;
+    it.n = sg.nchunk;
+    it.c = x % sg.nchunk;
+    x /= sg.nchunk;
+    rt = sg.nsplit - 1;
+  }
+  it.rt = rt - x / slices;
+  x %= slices;
+  it.kvh = x % L.H;
+  it.li = x / L.H;
   it.l = L.layer_ids[it.li];
   return it;
 }
@@ -112,7 +125,7 @@ __device__ __forceinline__ int64_t row_index(const Launch &L, const Traj &t, int
 }
 
 __device__ __forceinline__ int64_t part_index(const Launch &L, const Seg &sg, const Item &it, int r) {
-  return sg.part + ((int64_t)(it.li * L.H + it.kvh) * sg.nchunk + it.c) * sg.R + r;
+  return sg.part + ((int64_t)(it.li * L.H + it.kvh) * sg.nchunk + it.c) * sg.Rs + r;
 }
 
 // First index of [a, b) whose position is above x (b: none).
@@ -243,7 +256,7 @@ template <typename T, int D>
 __device__ __forceinline__ void write_row_warp(const Launch &L, const Seg &sg, const Item &it, int r, const float *o,
                                                float m, float l) {
   const int lane = threadIdx.x & 31;
-  if (sg.part >= 0) {
+  if (it.split) {
     const int64_t pr = part_index(L, sg, it, r);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) L.po[pr * D + lane + 32 * c] = o[c];

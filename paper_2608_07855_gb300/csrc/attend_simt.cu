@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch
   }
   __syncthreads();
   const Tiles tl = make_tiles(sm.u_lo, sm.u_hi, sm.u_se, TT);
-  const int j0 = chunk_tile(tl, it.c, sg.nchunk), j1 = chunk_tile(tl, it.c + 1, sg.nchunk);
+  const int j0 = chunk_tile(tl, it.c, it.n), j1 = chunk_tile(tl, it.c + 1, it.n);
   const T *kb = static_cast<const T *>(sg.k) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
   const T *vb = static_cast<const T *>(sg.v) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
   Span sp[TM];

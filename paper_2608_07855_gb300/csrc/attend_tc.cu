@@ -1,7 +1,7 @@
 // Attention on the tensor cores (bf16, 16-byte aligned caches).
 //
-// A persistent CTA of 384 threads per SM takes items of up to 256 query rows,
-// two tiles of 128, over 128-token tiles of K and V:
+// A CTA of 384 threads per SM takes items of up to 256 query rows, two tiles of
+// 128, over 128-token tiles of K and V:
 //   warp 0      TMA: K and V tiles through one ring of stages
 //   warp 1      the MMAs: S_b = Q_b K^T and O_b += P_b V (tcgen05, fp32 in TMEM)
 //   warp 3      the plan of the next item (what its rows see) and its Q rows,
@@ -54,6 +54,7 @@ static_assert(sizeof(TcParams) <= 32764, "kernel parameters");
 struct Plan {
   Tiles tl;
   int j0, j1, rows;
+  int item;  // -1: no more
 };
 
 template <int D>
@@ -65,7 +66,8 @@ struct Smem {
   Span span[2][2 * BM];
   Plan plan[2];
   float2 pub[BM];  // one row tile: group 1's (m, l)
-  uint64_t plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
+  alignas(16) uint4 next;  // answer to the request for another item
+  uint64_t next_full, plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
       o_empty[2], pub_full, pub_empty, drain;
   uint32_t tmem;
   int abort_flag;
@@ -89,11 +91,30 @@ __device__ __forceinline__ uint64_t desc_v(const uint8_t *tile, int ks) {
   return smem_desc(smem_addr(tile) + ks * 2048, kHalf, 1024, kSwizzle128B);
 }
 
-// The n-th item of this CTA: rounds run forwards and backwards in turn, which
-// evens out item lengths that fall from the first to the last.
-__device__ __forceinline__ int nth_item(int n) {
-  const int G = gridDim.x, b = blockIdx.x;
-  return n * G + ((n & 1) ? G - 1 - b : b);
+// One block is launched per item, and one that is done with its own takes the
+// next block's that has not started (PTX clusterlaunchcontrol), so items are
+// handed out as SMs get free while a block keeps its tensor memory, its
+// barriers and the pipeline across items.
+__device__ __forceinline__ void ask_next(uint4 *answer, uint64_t *bar) {
+  fence_proxy_async();  // the last answer has been read
+  mbar_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   smem_addr(answer)),
+               "r"(smem_addr(bar))
+               : "memory");
+}
+__device__ __forceinline__ int read_next(const uint4 *answer) {
+  int x;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t"
+      "ld.shared.b128 a, [%1];\n\t"
+      "mov.s32 %0, -1;\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
+      : "=r"(x)
+      : "r"(smem_addr(answer))
+      : "memory");
+  return x;
 }
 
 // Columns of tile j that are worked on: a multiple of 32.
@@ -231,7 +252,6 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   S &sm = *reinterpret_cast<S *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const Launch &L = P.L;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-  const int n_items = L.item_off[L.n_seg];
   volatile int *abort_flag = &sm.abort_flag;
 
   if (threadIdx.x == 0) {
@@ -244,6 +264,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       mbar_init(&sm.o_full[b], 1);
       mbar_init(&sm.o_empty[b], 4);
     }
+    mbar_init(&sm.next_full, 1);
     mbar_init(&sm.q_full, 1);
     mbar_init(&sm.q_empty, 1);
     for (int s = 0; s < NST; ++s) {
@@ -281,11 +302,12 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         ++g;
         return true;
       };
-      for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
+      for (int n = 0; ok; ++n) {
         if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
+        if (pl.item < 0) break;
         mbar_arrive(&sm.plan_empty[n & 1]);
-        const Item it = decode_item(L, item);
+        const Item it = decode_item(L, pl.item);
         for (int j = pl.j0; j < pl.j1 && ok; ++j) {
           const int tok = tile_start(pl.tl, j, BT);
           ok = load(&P.k[it.s], tok, it) && load(&P.v[it.s], tok, it);
@@ -331,9 +353,10 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         __syncwarp();
         return true;
       };
-      for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
+      for (int n = 0; ok; ++n) {
         if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
+        if (pl.item < 0) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
         if (!wait_warp(&sm.q_full, n & 1, abort_flag)) break;
@@ -373,9 +396,26 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       }
     } else if (warp == 3) {
       // ------------------------------------------------------------ plans and Q rows
-      for (int n = 0, item; (item = nth_item(n)) < n_items; ++n) {
+      int item = blockIdx.x;
+      bool asked = false;
+      for (int n = 0;; ++n) {
         const int buf = n & 1;
         if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, abort_flag)) break;
+        if (asked) {
+          if (!wait_warp(&sm.next_full, (n - 1) & 1, abort_flag)) break;
+          asked = false;
+          item = read_next(&sm.next);
+          __syncwarp();
+        }
+        if (item < 0) {
+          if (lane == 0) {
+            sm.plan[buf].item = -1;
+            mbar_arrive(&sm.plan_full[buf]);
+          }
+          break;
+        }
+        if (lane == 0) ask_next(&sm.next, &sm.next_full);
+        asked = true;
         const Item it = decode_item(L, item);
         const Seg &sg = L.seg[it.s];
         const int r0 = it.rt * 2 * BM, rows = min(2 * BM, sg.R - r0);
@@ -403,7 +443,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         }
         if (lane == 0) {
           const Tiles tl = make_tiles(lo, hi, se, BT);
-          sm.plan[buf] = {tl, chunk_tile(tl, it.c, sg.nchunk), chunk_tile(tl, it.c + 1, sg.nchunk), rows};
+          sm.plan[buf] = {tl, chunk_tile(tl, it.c, it.n), chunk_tile(tl, it.c + 1, it.n), rows, item};
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
@@ -429,6 +469,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.q_full);
       }
+      if (asked && lane == 0) {  // left early: the answer lands before the block's memory goes
+        for (int k = 0; k < 2; ++k) mbar_wait_drain(&sm.next_full, k, kWait / 4);
+      }
     }
   } else {
     // ------------------------------------------------------------ softmax
@@ -438,16 +481,17 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     const uint32_t s_col = tm + lanes + BT * hb, o_col = tm + lanes + 256 + D * hb;
     uint32_t ns = 0, uses = 0, npub = 0;  // score tiles, items that filled O_hb, joined items
     bool ok = true;
-    for (int n = 0, item; ok && (item = nth_item(n)) < n_items; ++n) {
+    for (int n = 0; ok; ++n) {
       if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
       const Plan pl = sm.plan[n & 1];
+      if (pl.item < 0) break;
       const Tiles tl = pl.tl;
       const bool two = pl.rows > BM;
       const int lrow = two ? hb * BM + row : row;  // row of the item
       const Span sp = sm.span[n & 1][lrow];
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
-      const Item it = decode_item(L, item);
+      const Item it = decode_item(L, pl.item);
       const Seg &sg = L.seg[it.s];
       const bool warp_rows = lrow - lane < pl.rows;  // the warp has a row of the item
       float m_used = -INFINITY, lsum = 0.0f;
@@ -512,7 +556,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         t = &L.t[traj_of_row(L, sg, rr)];
         orow = row_index(L, *t, it.l, it.kvh, rr);
         qrow = static_cast<const __nv_bfloat16 *>(t->q) + orow * D;
-        if (sg.part >= 0) pdst = L.po + part_index(L, sg, it, r) * D;
+        if (it.split) pdst = L.po + part_index(L, sg, it, r) * D;
         else dst = static_cast<__nv_bfloat16 *>(t->out) + orow * D;
       }
       const float inv = norm_of(lsum);
@@ -617,18 +661,18 @@ bool map_kv(CUtensorMap *m, const void *base, const Launch &L, const Seg &sg) {
 }
 
 template <int D>
-cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s, int sms) {
-  const int smem = (int)sizeof(Smem<D>) + 1024, items = P.L.item_off[P.L.n_seg];
+cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s) {
+  const int smem = (int)sizeof(Smem<D>) + 1024;
   const cudaError_t e = cudaFuncSetAttribute(attend_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  attend_tc<D><<<items < sms ? items : sms, 384, smem, s>>>(P, hdr);
+  attend_tc<D><<<P.L.item_off[P.L.n_seg], 384, smem, s>>>(P, hdr);
   ++launch_count();
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, int sms) {
+cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s) {
   static thread_local TcParams P;
   P.L = L;
   for (int i = 0; i < L.n_seg; ++i) {
@@ -636,7 +680,7 @@ cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, int sms) {
     if (sg.S == 0 || L.item_off[i] == L.item_off[i + 1]) continue;
     if (!map_kv(&P.k[i], sg.k, L, sg) || !map_kv(&P.v[i], sg.v, L, sg)) return cudaErrorInvalidValue;
   }
-  return L.d == 128 ? launch<128>(P, hdr, s, sms) : launch<64>(P, hdr, s, sms);
+  return L.d == 128 ? launch<128>(P, hdr, s) : launch<64>(P, hdr, s);
 }
 
 }  // namespace at
