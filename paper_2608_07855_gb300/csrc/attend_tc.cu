@@ -423,7 +423,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         int lo = 0x7fffffff, hi = 0, se = 0;
 #pragma unroll
         for (int i = 0; i < 2 * BM / 32; ++i) {
-          Span sp = {0, 0, 0};
+          // rows behind the last one: zeros as queries, nothing to mask
+          Span sp = {0, 0x7fffffff, 0};
           int rr = r0 + lane + 32 * i;
           src[i] = nullptr;
           if (rr < sg.R) {
@@ -458,10 +459,10 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           for (int k = 0; k < 32 / RW; ++k) {
             const int r = k * RW + lane / LR;  // within the 32 rows
             const uint64_t p = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src[i]), r);
-            if (!p) continue;
             const int row = (32 * i + r) % BM;
             uint8_t *dst = sm.q[32 * i / BM] + (part >> 3) * kHalf + sw128_offset(row, part & 7);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(p + 16 * part) : "memory");
+            if (!p) *reinterpret_cast<uint4 *>(dst) = make_uint4(0, 0, 0, 0);
+            else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(p + 16 * part) : "memory");
           }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
