@@ -187,13 +187,13 @@ Division divide(const Divide &v, int64_t slots, double fixed, int64_t most_items
   return best;
 }
 
-enum { kSimt16, kSimt64, kTc, kPaths };
+enum { kSimt16, kSimt64, kRows, kTc, kPaths };
 struct PathInfo {
   int rows, tile;    // of an item, tokens of a tile
   int resident;      // items at a time on an SM
   double fixed;      // an item's fixed part, in tiles
 };
-constexpr PathInfo kPath[kPaths] = {{16, 64, 2, 1.0}, {64, 64, 1, 1.0}, {256, 128, 1, 2.0}};
+constexpr PathInfo kPath[kPaths] = {{16, 64, 2, 1.0}, {64, 64, 1, 1.0}, {16, 64, 2, 2.0}, {256, 128, 1, 2.0}};
 
 bool force_cuda_cores() {
   const char *e = getenv("COMMITKV_SCORING");
@@ -211,7 +211,7 @@ int path_of(const Launch &L, const Seg &sg) {
     bits |= L.t[t].W ? (uintptr_t)L.t[t].q | (uintptr_t)L.t[t].out : 0;
   if (bits % 16) return cuda_cores;
   if (sg.S > 0 && (sg.sh == 0 || sg.sl == 0 || std::max(sg.sl, std::max(sg.sh, sg.st)) >= (1ll << 39))) return cuda_cores;
-  return kTc;
+  return sg.R <= 16 ? kRows : kTc;
 }
 
 commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
@@ -327,7 +327,7 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     L.item_off[L.n_seg] = items;
     if (items == 0) continue;
     L.rows_per_item = kPath[p].rows;
-    e = p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream) : launch_simt(L, stream);
+    e = p == kRows ? launch_rows(L, stream) : p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream) : launch_simt(L, stream);
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);
   if (e == cudaSuccess) return COMMITKV_OK;

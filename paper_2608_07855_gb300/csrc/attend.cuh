@@ -65,6 +65,8 @@ struct Launch {
 
 // CUDA cores: any layout and type.  Rows per item: 16 or 64.
 cudaError_t launch_simt(const Launch &L, cudaStream_t s);
+// Up to 16 rows of a slice, bf16, caches and queries 16-byte aligned.
+cudaError_t launch_rows(const Launch &L, cudaStream_t s);
 // Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
 cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);
