@@ -23,12 +23,19 @@ constexpr int64_t kMaxSplitSmall = 2048;  // up to 16 rows an item
 constexpr int64_t kMaxSplit = 768;
 
 // ------------------------------------------------------------------ merge
-// A warp per row: o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i over the row's
-// partial results.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) combine(const __grid_constant__ Launch L) {
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+// o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i over a row's partial results,
+// those of the prefix first.  NW warps to a row take kBatch parts each at a
+// time, all loads of a batch in flight together: the call's time here is
+// latency (16 parts of 32 rows: 13 us a part after the other, @COMBINE@ so).
+constexpr int kBatch = 8;
+
+template <typename T, int D, int NW>
+__global__ void __launch_bounds__(128) combine(const __grid_constant__ Launch L) {
+  constexpr int C = D / 32;  // channels of a lane: C lane ..
+  __shared__ float so[NW > 1 ? NW : 1][D];
+  __shared__ float2 sml[NW];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int64_t w = NW == 1 ? (int64_t)blockIdx.x * 4 + warp : blockIdx.x;
   const int per = L.out_off[L.n_traj];
   const int li = (int)(w / per);
   if (li >= L.n_layers) return;
@@ -40,58 +47,99 @@ __global__ void __launch_bounds__(256) combine(const __grid_constant__ Launch L)
   }
   x -= L.out_off[a];
   const Traj &t = L.t[a];
-  const int R = L.seg[a + L.prefix].Rs, kvh = x / R, r = x % R, l = L.layer_ids[li];
-  float m = -INFINITY, lsum = 0.0f, o[D / 32];
+  const Seg &own = L.seg[a + L.prefix], &pre = L.seg[0];
+  const int R = own.Rs, kvh = x / R, r = x % R, l = L.layer_ids[li], slice = li * L.H + kvh;
+  const int64_t first = own.part + (int64_t)slice * own.nchunk * own.Rs + r;
+  const int64_t pfirst = pre.part + (int64_t)slice * pre.nchunk * pre.Rs + t.row0 + r;
+  const int np = L.prefix ? pre.nchunk : 0, n = np + own.nchunk;
+  pdl_wait();  // the parts are written
+  float m = -INFINITY, lsum = 0.0f, o[C];
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) o[c] = 0.0f;
-  for (int k = 0; k <= L.prefix; ++k) {
-    const Seg &sg = L.seg[k == L.prefix ? a + L.prefix : 0];
-    const int64_t first = sg.part + (int64_t)(li * L.H + kvh) * sg.nchunk * sg.Rs + (sg.t < 0 ? t.row0 + r : r);
-    for (int c0 = 0; c0 < sg.nchunk; c0 += 32) {
-      const int n = min(32, sg.nchunk - c0);
-      const float2 ml = lane < n ? L.pml[first + (int64_t)(c0 + lane) * sg.Rs] : make_float2(-INFINITY, 0.0f);
-      const float mn = fmaxf(m, warp_max(ml.x)), ref = mn == -INFINITY ? 0.0f : mn;
-      const float f = exp2f(m - ref), wt = exp2f(ml.x - ref);
-      m = mn;
-      lsum = fmaf(lsum, f, warp_sum(wt * ml.y));
+  for (int c = 0; c < C; ++c) o[c] = 0.0f;
+  for (int p0 = NW == 1 ? 0 : warp; p0 < n; p0 += kBatch * NW) {
+    float2 ml[kBatch];
+    float y[kBatch][C];
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) o[c] *= f;
-#pragma unroll 4
-      for (int c = 0; c < n; ++c) {
-        const float wc = __shfl_sync(0xffffffffu, wt, c);
-        const bool used = __shfl_sync(0xffffffffu, ml.y, c) != 0.0f;
-        const float *p = L.po + (first + (int64_t)(c0 + c) * sg.Rs) * D;
+    for (int i = 0; i < kBatch; ++i) {
+      const int p = p0 + i * NW;
+      ml[i] = make_float2(-INFINITY, 0.0f);
 #pragma unroll
-        for (int k2 = 0; k2 < D / 32; ++k2) {
-          const float v = p[lane + 32 * k2];
-          o[k2] = used ? fmaf(wc, v, o[k2]) : o[k2];
+      for (int c = 0; c < C; ++c) y[i][c] = 0.0f;
+      if (p < n) {
+        const int64_t row = p < np ? pfirst + (int64_t)p * pre.Rs : first + (int64_t)(p - np) * own.Rs;
+        ml[i] = L.pml[row];
+        const float *src = L.po + row * D + C * lane;
+        if constexpr (C == 4) {
+          const float4 v = *reinterpret_cast<const float4 *>(src);
+          y[i][0] = v.x, y[i][1] = v.y, y[i][2] = v.z, y[i][3] = v.w;
+        } else {
+          const float2 v = *reinterpret_cast<const float2 *>(src);
+          y[i][0] = v.x, y[i][1] = v.y;
         }
       }
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) mn = fmaxf(mn, ml[i].x);
+    const float ref = mn == -INFINITY ? 0.0f : mn, f = exp2f(m - ref);
+    m = mn;
+    lsum *= f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] *= f;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float wt = exp2f(ml[i].x - ref);
+      lsum = fmaf(ml[i].y, wt, lsum);
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = ml[i].y != 0.0f ? fmaf(y[i][c], wt, o[c]) : o[c];
+    }
+  }
+  if constexpr (NW > 1) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) so[warp][C * lane + c] = o[c];
+    if (lane == 0) sml[warp] = make_float2(m, lsum);
+    __syncthreads();
+    if (warp) return;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) m = fmaxf(m, sml[i].x);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    lsum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const float wt = exp2f(sml[i].x - ref);
+      lsum = fmaf(sml[i].y, wt, lsum);
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = sml[i].y != 0.0f ? fmaf(so[i][C * lane + c], wt, o[c]) : o[c];
     }
   }
   const int64_t row = row_index(L, t, l, kvh, r);
   const float inv = norm_of(lsum);
-  T *dst = static_cast<T *>(t.out) + row * D;
+  T *dst = static_cast<T *>(t.out) + row * D + C * lane;
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) dst[lane + 32 * c] = from_f32<T>(o[c] * inv);
+  for (int c = 0; c < C; ++c) dst[c] = from_f32<T>(o[c] * inv);
   if (t.lse && lane == 0) t.lse[row] = lse_of(m, lsum);
+}
+
+template <typename T, int D>
+cudaError_t launch_combine_td(const Launch &L, cudaStream_t s) {
+  const int64_t rows = (int64_t)L.out_off[L.n_traj] * L.n_layers;
+  int parts = 1;
+  for (int t = 0; t < L.n_traj; ++t)
+    parts = std::max(parts, L.seg[t + L.prefix].nchunk + (L.prefix ? L.seg[0].nchunk : 0));
+  // up to a batch of parts: a warp to a row
+  if (parts <= kBatch) return launch_after(combine<T, D, 1>, (unsigned)cdiv(rows, 4), 128, 0, s, true, L);
+  return launch_after(combine<T, D, 4>, (unsigned)rows, 128, 0, s, true, L);
 }
 
 }  // namespace
 
 cudaError_t launch_combine(const Launch &L, cudaStream_t s) {
-  const int64_t rows = (int64_t)L.out_off[L.n_traj] * L.n_layers;
-  if (rows == 0) return cudaSuccess;
-  const unsigned n = (unsigned)cdiv(rows, 8);
-  if (L.dtype == COMMITKV_BF16) {
-    if (L.d == 128) combine<__nv_bfloat16, 128><<<n, 256, 0, s>>>(L);
-    else combine<__nv_bfloat16, 64><<<n, 256, 0, s>>>(L);
-  } else {
-    if (L.d == 128) combine<float, 128><<<n, 256, 0, s>>>(L);
-    else combine<float, 64><<<n, 256, 0, s>>>(L);
-  }
-  ++launch_count();
-  return cudaGetLastError();
+  if (L.out_off[L.n_traj] == 0 || L.n_layers == 0) return cudaSuccess;
+  if (L.dtype == COMMITKV_BF16)
+    return L.d == 128 ? launch_combine_td<__nv_bfloat16, 128>(L, s) : launch_combine_td<__nv_bfloat16, 64>(L, s);
+  return L.d == 128 ? launch_combine_td<float, 128>(L, s) : launch_combine_td<float, 64>(L, s);
 }
 
 namespace {
@@ -317,6 +365,7 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   L.po = reinterpret_cast<float *>(base);
   L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
   cudaError_t e = cudaSuccess;
+  bool launched = false;
   for (int p = 0; p < kPaths && e == cudaSuccess; ++p) {
     int32_t items = 0;
     for (int s = 0; s < L.n_seg; ++s) {
@@ -327,7 +376,8 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     L.item_off[L.n_seg] = items;
     if (items == 0) continue;
     L.rows_per_item = kPath[p].rows;
-    e = p == kRows ? launch_rows(L, stream) : p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream) : launch_simt(L, stream);
+    e = p == kRows ? launch_rows(L, stream, launched) : p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream, launched) : launch_simt(L, stream, launched);
+    launched = true;
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);
   if (e == cudaSuccess) return COMMITKV_OK;

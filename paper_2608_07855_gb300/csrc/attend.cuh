@@ -63,12 +63,38 @@ struct Launch {
   uint8_t layer_ids[kMaxLayers];
 };
 
+// The kernels of a call overlap where they can (programmatic launches): each
+// lets the next one start once all of its own blocks have, the kernels of the
+// segments do not depend on one another, and the merge waits for all of them:
+// a kernel that started early does not end before the one ahead of it.
+__device__ __forceinline__ void pdl_start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Launches a kernel; `early`: it may start before the call's last kernel ends.
+template <typename... A>
+cudaError_t launch_after(void (*kernel)(A...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t s, bool early,
+                         const A &...args) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(blocks);
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = s;
+  cudaLaunchAttribute a = {};
+  a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  a.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &a;
+  c.numAttrs = early ? 1 : 0;
+  void *p[] = {const_cast<void *>(static_cast<const void *>(&args))...};
+  ++launch_count();
+  return cudaLaunchKernelExC(&c, reinterpret_cast<const void *>(kernel), p);
+}
+
 // CUDA cores: any layout and type.  Rows per item: 16 or 64.
-cudaError_t launch_simt(const Launch &L, cudaStream_t s);
+cudaError_t launch_simt(const Launch &L, cudaStream_t s, bool early);
 // Up to 16 rows of a slice, bf16, caches and queries 16-byte aligned.
-cudaError_t launch_rows(const Launch &L, cudaStream_t s);
+cudaError_t launch_rows(const Launch &L, cudaStream_t s, bool early);
 // Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
-cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s);
+cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);
 
 struct Item {

@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
   extern __shared__ __align__(128) uint8_t raw[];
   S &sm = *reinterpret_cast<S *>(raw);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  pdl_start_next();
   const Item it = decode_item(L, blockIdx.x);
   const Seg &sg = L.seg[it.s];
 
@@ -253,21 +254,22 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
     }
     write_row_warp<__nv_bfloat16, D>(L, sg, it, r, x, mr, lr);
   }
+  pdl_wait();
 }
 
 template <int D>
-cudaError_t launch(const Launch &L, cudaStream_t s) {
+cudaError_t launch(const Launch &L, cudaStream_t s, bool early) {
   const cudaError_t e =
       cudaFuncSetAttribute(attend_rows<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>));
   if (e != cudaSuccess) return e;
-  attend_rows<D><<<L.item_off[L.n_seg], NW * 32, sizeof(Smem<D>), s>>>(L);
-  ++launch_count();
-  return cudaGetLastError();
+  return launch_after(attend_rows<D>, L.item_off[L.n_seg], NW * 32, sizeof(Smem<D>), s, early, L);
 }
 
 }  // namespace
 
-cudaError_t launch_rows(const Launch &L, cudaStream_t s) { return L.d == 128 ? launch<128>(L, s) : launch<64>(L, s); }
+cudaError_t launch_rows(const Launch &L, cudaStream_t s, bool early) {
+  return L.d == 128 ? launch<128>(L, s, early) : launch<64>(L, s, early);
+}
 
 }  // namespace at
 }  // namespace ckv

@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch
   extern __shared__ __align__(16) uint8_t raw[];
   Smem<D, TM> &sm = *reinterpret_cast<Smem<D, TM> *>(raw);
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  pdl_start_next();
   const Item it = decode_item(L, blockIdx.x);
   const Seg &sg = L.seg[it.s];
   const int r0 = it.rt * BM;
@@ -197,28 +198,27 @@ __global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch
     }
     write_row_warp<T, D>(L, sg, it, r0 + r, x, mr, lr);
   }
+  pdl_wait();
 }
 
 template <typename T, int D, int TM>
-cudaError_t launch(const Launch &L, cudaStream_t s) {
+cudaError_t launch(const Launch &L, cudaStream_t s, bool early) {
   const int smem = (int)sizeof(Smem<D, TM>);
-  cudaError_t e = cudaFuncSetAttribute(attend_simt<T, D, TM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const cudaError_t e = cudaFuncSetAttribute(attend_simt<T, D, TM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  attend_simt<T, D, TM><<<L.item_off[L.n_seg], NT, smem, s>>>(L);
-  ++launch_count();
-  return cudaGetLastError();
+  return launch_after(attend_simt<T, D, TM>, L.item_off[L.n_seg], NT, smem, s, early, L);
 }
 
 template <typename T>
-cudaError_t launch_t(const Launch &L, cudaStream_t s) {
-  if (L.rows_per_item == 16) return L.d == 128 ? launch<T, 128, 1>(L, s) : launch<T, 64, 1>(L, s);
-  return L.d == 128 ? launch<T, 128, 4>(L, s) : launch<T, 64, 4>(L, s);
+cudaError_t launch_t(const Launch &L, cudaStream_t s, bool early) {
+  if (L.rows_per_item == 16) return L.d == 128 ? launch<T, 128, 1>(L, s, early) : launch<T, 64, 1>(L, s, early);
+  return L.d == 128 ? launch<T, 128, 4>(L, s, early) : launch<T, 64, 4>(L, s, early);
 }
 
 }  // namespace
 
-cudaError_t launch_simt(const Launch &L, cudaStream_t s) {
-  return L.dtype == COMMITKV_BF16 ? launch_t<__nv_bfloat16>(L, s) : launch_t<float>(L, s);
+cudaError_t launch_simt(const Launch &L, cudaStream_t s, bool early) {
+  return L.dtype == COMMITKV_BF16 ? launch_t<__nv_bfloat16>(L, s, early) : launch_t<float>(L, s, early);
 }
 
 }  // namespace at

@@ -65,6 +65,7 @@ struct Smem {
   alignas(1024) uint8_t kv[NST][kTile];
   Span span[2][2 * BM];
   Plan plan[2];
+  int3 first[8];  // what the rows of a softmax warp see of the first item
   float2 pub[BM];  // one row tile: group 1's (m, l)
   alignas(16) uint4 next;  // answer to the request for another item
   uint64_t next_full, plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
@@ -135,6 +136,54 @@ __device__ __forceinline__ bool elect_one() {
 
 __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
   return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
+}
+
+// Row r of an item: its query, and what it sees.  Behind the last row: zeros
+// as queries, nothing to mask.
+__device__ __forceinline__ const __nv_bfloat16 *row_query(const Launch &L, const Seg &sg, const Item &it, int r, int d) {
+  if (r >= sg.R) return nullptr;
+  const Traj &t = L.t[traj_of_row(L, sg, r)];
+  return static_cast<const __nv_bfloat16 *>(t.q) + row_index(L, t, it.l, it.kvh, r) * d;
+}
+__device__ __forceinline__ Span row_sees(const Launch &L, const Seg &sg, int r, int3 &u) {
+  Span sp = {0, 0x7fffffff, 0};
+  if (r < sg.R) {
+    const Traj &t = L.t[traj_of_row(L, sg, r)];
+    sp = row_span(sg.pos, sg.S, t.qpos[r / L.g], L.window, L.sinks);
+    if (sp.lo < sp.hi) u.x = min(u.x, sp.lo), u.y = max(u.y, sp.hi);
+    u.z = max(u.z, sp.se);
+  }
+  return sp;
+}
+// The union of what the rows of a warp see: (least lo, largest hi, largest se).
+__device__ __forceinline__ int3 join_warp(int3 u) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    u.x = min(u.x, __shfl_xor_sync(0xffffffffu, u.x, o));
+    u.y = max(u.y, __shfl_xor_sync(0xffffffffu, u.y, o));
+    u.z = max(u.z, __shfl_xor_sync(0xffffffffu, u.z, o));
+  }
+  return u;
+}
+
+// A warp copies 32 rows (lane r has row r's address; none: zeros) into rows
+// row0 .. of a Q tile, D / 8 lanes to a row.
+template <int D>
+__device__ __forceinline__ void copy_q(uint8_t *tile, int row0, const __nv_bfloat16 *src, int lane) {
+  constexpr int LR = D / 8, RW = 32 / LR;  // lanes a row, rows a step
+  const int part = lane % LR;
+#pragma unroll
+  for (int k = 0; k < 32 / RW; ++k) {
+    const int r = k * RW + lane / LR;
+    const uint64_t p = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), r);
+    uint8_t *dst = tile + (part >> 3) * kHalf + sw128_offset(row0 + r, part & 7);
+    if (!p) *reinterpret_cast<uint4 *>(dst) = make_uint4(0, 0, 0, 0);
+    else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(p + 16 * part) : "memory");
+  }
+}
+__device__ __forceinline__ void copy_q_done() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  fence_proxy_async();
 }
 
 // The scores of a tile become weights relative to the row's reference maximum
@@ -254,6 +303,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   volatile int *abort_flag = &sm.abort_flag;
 
+  pdl_start_next();
   if (threadIdx.x == 0) {
     sm.abort_flag = 0;
     for (int b = 0; b < 2; ++b) {
@@ -279,6 +329,17 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   if (warp == 1) {
     tmem_alloc(&sm.tmem, 512);
     tmem_relinquish();
+  }
+  if (warp >= 4) {  // the first item's rows, a thread each (later ones are planned ahead by one warp)
+    const Item it = decode_item(L, blockIdx.x);
+    const Seg &sg = L.seg[it.s];
+    const int i = threadIdx.x - 128, r = it.rt * 2 * BM + i;
+    int3 u = make_int3(0x7fffffff, 0, 0);
+    copy_q<D>(sm.q[i / BM], (i % BM) & ~31, row_query(L, sg, it, r, D), lane);
+    sm.span[0][i] = row_sees(L, sg, r, u);
+    u = join_warp(u);
+    if (lane == 0) sm.first[warp - 4] = u;
+    copy_q_done();
   }
   tc_fence_before();
   __syncthreads();
@@ -419,55 +480,28 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         const Item it = decode_item(L, item);
         const Seg &sg = L.seg[it.s];
         const int r0 = it.rt * 2 * BM, rows = min(2 * BM, sg.R - r0);
-        const __nv_bfloat16 *src[2 * BM / 32];
-        int lo = 0x7fffffff, hi = 0, se = 0;
-#pragma unroll
-        for (int i = 0; i < 2 * BM / 32; ++i) {
-          // rows behind the last one: zeros as queries, nothing to mask
-          Span sp = {0, 0x7fffffff, 0};
-          int rr = r0 + lane + 32 * i;
-          src[i] = nullptr;
-          if (rr < sg.R) {
-            const Traj &t = L.t[traj_of_row(L, sg, rr)];
-            src[i] = static_cast<const __nv_bfloat16 *>(t.q) + row_index(L, t, it.l, it.kvh, rr) * D;
-            sp = row_span(sg.pos, sg.S, t.qpos[rr / L.g], L.window, L.sinks);
-            if (sp.lo < sp.hi) lo = min(lo, sp.lo), hi = max(hi, sp.hi);
-            se = max(se, sp.se);
-          }
-          sm.span[buf][lane + 32 * i] = sp;
+        int3 u = make_int3(0x7fffffff, 0, 0);
+        if (n == 0) {
+          if (lane < 8) u = sm.first[lane];
+        } else {
+#pragma unroll 1
+          for (int i = lane; i < 2 * BM; i += 32) sm.span[buf][i] = row_sees(L, sg, r0 + i, u);
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-          hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-          se = max(se, __shfl_xor_sync(0xffffffffu, se, o));
-        }
+        u = join_warp(u);
         if (lane == 0) {
-          const Tiles tl = make_tiles(lo, hi, se, BT);
+          const Tiles tl = make_tiles(u.x, u.y, u.z, BT);
           sm.plan[buf] = {tl, chunk_tile(tl, it.c, it.n), chunk_tile(tl, it.c + 1, it.n), rows, item};
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
-        if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
-        // rows of D x 2 bytes, each by D / 8 lanes
-        constexpr int LR = D / 8, RW = 32 / LR;  // lanes a row, rows a step
-        const int part = lane % LR;
-#pragma unroll
-        for (int i = 0; i < 2 * BM / 32; ++i) {
-          if (32 * i >= rows) break;
-#pragma unroll
-          for (int k = 0; k < 32 / RW; ++k) {
-            const int r = k * RW + lane / LR;  // within the 32 rows
-            const uint64_t p = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src[i]), r);
-            const int row = (32 * i + r) % BM;
-            uint8_t *dst = sm.q[32 * i / BM] + (part >> 3) * kHalf + sw128_offset(row, part & 7);
-            if (!p) *reinterpret_cast<uint4 *>(dst) = make_uint4(0, 0, 0, 0);
-            else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(p + 16 * part) : "memory");
-          }
+        if (n > 0) {
+          if (!wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
+#pragma unroll 1
+          for (int i = 0; i < rows; i += 32)
+            copy_q<D>(sm.q[i / BM], i % BM, row_query(L, sg, it, r0 + i + lane, D), lane);
+          copy_q_done();
+          __syncwarp();
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_proxy_async();
-        __syncwarp();
         if (lane == 0) mbar_arrive(&sm.q_full);
       }
       if (asked && lane == 0) {  // left early: the answer lands before the block's memory goes
@@ -635,6 +669,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   __syncthreads();
   if (warp == 1) tmem_dealloc(tm, 512);
   if (threadIdx.x == 0 && sm.abort_flag) record_error(hdr, COMMITKV_ERR_TIMEOUT, 30);
+  pdl_wait();
 }
 
 // ------------------------------------------------------------------ host
@@ -662,18 +697,16 @@ bool map_kv(CUtensorMap *m, const void *base, const Launch &L, const Seg &sg) {
 }
 
 template <int D>
-cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s) {
+cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s, bool early) {
   const int smem = (int)sizeof(Smem<D>) + 1024;
   const cudaError_t e = cudaFuncSetAttribute(attend_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  attend_tc<D><<<P.L.item_off[P.L.n_seg], 384, smem, s>>>(P, hdr);
-  ++launch_count();
-  return cudaGetLastError();
+  return launch_after(attend_tc<D>, P.L.item_off[P.L.n_seg], 384, smem, s, early, P, hdr);
 }
 
 }  // namespace
 
-cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s) {
+cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early) {
   static thread_local TcParams P;
   P.L = L;
   for (int i = 0; i < L.n_seg; ++i) {
@@ -681,7 +714,7 @@ cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s) {
     if (sg.S == 0 || L.item_off[i] == L.item_off[i + 1]) continue;
     if (!map_kv(&P.k[i], sg.k, L, sg) || !map_kv(&P.v[i], sg.v, L, sg)) return cudaErrorInvalidValue;
   }
-  return L.d == 128 ? launch<128>(P, hdr, s) : launch<64>(P, hdr, s);
+  return L.d == 128 ? launch<128>(P, hdr, s, early) : launch<64>(P, hdr, s, early);
 }
 
 }  // namespace at
