@@ -235,13 +235,13 @@ Division divide(const Divide &v, int64_t slots, double fixed, int64_t most_items
   return best;
 }
 
-enum { kSimt16, kSimt64, kRows, kTc, kPaths };
+enum { kSimt16, kSimt64, kTc, kRows, kPaths };
 struct PathInfo {
   int rows, tile;    // of an item, tokens of a tile
   int resident;      // items at a time on an SM
   double fixed;      // an item's fixed part, in tiles
 };
-constexpr PathInfo kPath[kPaths] = {{16, 64, 2, 1.0}, {64, 64, 1, 1.0}, {16, 64, 2, 2.0}, {256, 128, 1, 2.0}};
+constexpr PathInfo kPath[kPaths] = {{16, 64, 2, 1.0}, {64, 64, 1, 1.0}, {256, 128, 1, 2.0}, {16, 64, 2, 2.0}};
 
 bool force_cuda_cores() {
   const char *e = getenv("COMMITKV_SCORING");

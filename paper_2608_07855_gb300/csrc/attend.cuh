@@ -134,10 +134,14 @@ __device__ __forceinline__ Item decode_item(const Launch &L, int item) {
   return it;
 }
 
-// Trajectory and row within it of row r of a segment.
+// Trajectory and row within it of row r of a segment.  The launch description
+// is read by the constant cache, one address at a time, so the lanes' searches
+// are kept short: with as many queries everywhere the first guess is right.
 __device__ __forceinline__ int traj_of_row(const Launch &L, const Seg &sg, int &r) {
   if (sg.t >= 0) return sg.t;
-  int a = 0, b = L.n_traj;
+  int a = (int)((int64_t)r * L.n_traj / sg.R), b = a + 1;
+  if (r < L.t[a].row0) b = a, a = 0;
+  else if (b < L.n_traj && r >= L.t[b].row0) a = b, b = L.n_traj;
   while (b - a > 1) {
     const int m = (a + b) >> 1;
     if (r >= L.t[m].row0) a = m;
@@ -219,8 +223,10 @@ __device__ __forceinline__ int tile_end(const Tiles &t, int j, int tile) {
   const int e = tile_start(t, j, tile) + tile, lim = j < t.nA ? t.se : t.hi;
   return e < lim ? e : lim;
 }
-// Tiles [first, last) of chunk c of n.
-__device__ __forceinline__ int chunk_tile(const Tiles &t, int c, int n) { return (int)((int64_t)t.n * c / n); }
+// Tiles [chunk_tile(c), chunk_tile(c + 1)) are chunk c's of n (n^2 fits 32 bits).
+__device__ __forceinline__ int chunk_tile(const Tiles &t, int c, int n) {
+  return t.n / n * c + t.n % n * c / n;
+}
 
 // sum of exp2(s - m) v over the visible tokens of tiles [j0, j1) for one row,
 // by the 32 lanes of a warp: o[k] is channel lane + 32 k.  A masked token's

@@ -53,8 +53,9 @@ static_assert(sizeof(TcParams) <= 32764, "kernel parameters");
 
 struct Plan {
   Tiles tl;
-  int j0, j1, rows;
-  int item;  // -1: no more
+  int j0, j1;
+  int rows;  // of the item; 0: no more items
+  Item it;
 };
 
 template <int D>
@@ -65,6 +66,7 @@ struct Smem {
   alignas(1024) uint8_t kv[NST][kTile];
   Span span[2][2 * BM];
   Plan plan[2];
+  float4 stage[8][32 * 5];  // results of a softmax warp on their way out: 64 bytes of each row, 16 apart
   int3 first[8];  // what the rows of a softmax warp see of the first item
   float2 pub[BM];  // one row tile: group 1's (m, l)
   alignas(16) uint4 next;  // answer to the request for another item
@@ -140,16 +142,17 @@ __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volati
 
 // Row r of an item: its query, and what it sees.  Behind the last row: zeros
 // as queries, nothing to mask.
-__device__ __forceinline__ const __nv_bfloat16 *row_query(const Launch &L, const Seg &sg, const Item &it, int r, int d) {
+__device__ __forceinline__ const __nv_bfloat16 *row_query(const Launch &L, const Seg &sg, const Item &it, int r, int d,
+                                                          const int32_t *&qpos) {
   if (r >= sg.R) return nullptr;
   const Traj &t = L.t[traj_of_row(L, sg, r)];
+  qpos = t.qpos + r / L.g;
   return static_cast<const __nv_bfloat16 *>(t.q) + row_index(L, t, it.l, it.kvh, r) * d;
 }
-__device__ __forceinline__ Span row_sees(const Launch &L, const Seg &sg, int r, int3 &u) {
+__device__ __forceinline__ Span row_sees(const Launch &L, const Seg &sg, const int32_t *qpos, int3 &u) {
   Span sp = {0, 0x7fffffff, 0};
-  if (r < sg.R) {
-    const Traj &t = L.t[traj_of_row(L, sg, r)];
-    sp = row_span(sg.pos, sg.S, t.qpos[r / L.g], L.window, L.sinks);
+  if (qpos) {
+    sp = row_span(sg.pos, sg.S, *qpos, L.window, L.sinks);
     if (sp.lo < sp.hi) u.x = min(u.x, sp.lo), u.y = max(u.y, sp.hi);
     u.z = max(u.z, sp.se);
   }
@@ -333,10 +336,11 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   if (warp >= 4) {  // the first item's rows, a thread each (later ones are planned ahead by one warp)
     const Item it = decode_item(L, blockIdx.x);
     const Seg &sg = L.seg[it.s];
-    const int i = threadIdx.x - 128, r = it.rt * 2 * BM + i;
+    const int i = threadIdx.x - 128, r = it.rt * L.rows_per_item + i;
     int3 u = make_int3(0x7fffffff, 0, 0);
-    copy_q<D>(sm.q[i / BM], (i % BM) & ~31, row_query(L, sg, it, r, D), lane);
-    sm.span[0][i] = row_sees(L, sg, r, u);
+    const int32_t *qpos = nullptr;
+    copy_q<D>(sm.q[i / BM], (i % BM) & ~31, i < L.rows_per_item ? row_query(L, sg, it, r, D, qpos) : nullptr, lane);
+    sm.span[0][i] = row_sees(L, sg, qpos, u);
     u = join_warp(u);
     if (lane == 0) sm.first[warp - 4] = u;
     copy_q_done();
@@ -366,9 +370,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       for (int n = 0; ok; ++n) {
         if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
-        if (pl.item < 0) break;
+        if (pl.rows == 0) break;
         mbar_arrive(&sm.plan_empty[n & 1]);
-        const Item it = decode_item(L, pl.item);
+        const Item it = pl.it;
         for (int j = pl.j0; j < pl.j1 && ok; ++j) {
           const int tok = tile_start(pl.tl, j, BT);
           ok = load(&P.k[it.s], tok, it) && load(&P.v[it.s], tok, it);
@@ -417,7 +421,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       for (int n = 0; ok; ++n) {
         if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
         const Plan pl = sm.plan[n & 1];
-        if (pl.item < 0) break;
+        if (pl.rows == 0) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
         if (!wait_warp(&sm.q_full, n & 1, abort_flag)) break;
@@ -470,7 +474,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         }
         if (item < 0) {
           if (lane == 0) {
-            sm.plan[buf].item = -1;
+            sm.plan[buf].rows = 0;
             mbar_arrive(&sm.plan_full[buf]);
           }
           break;
@@ -479,26 +483,32 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         asked = true;
         const Item it = decode_item(L, item);
         const Seg &sg = L.seg[it.s];
-        const int r0 = it.rt * 2 * BM, rows = min(2 * BM, sg.R - r0);
+        const int r0 = it.rt * L.rows_per_item, rows = min(L.rows_per_item, sg.R - r0);
         int3 u = make_int3(0x7fffffff, 0, 0);
         if (n == 0) {
           if (lane < 8) u = sm.first[lane];
         } else {
 #pragma unroll 1
-          for (int i = lane; i < 2 * BM; i += 32) sm.span[buf][i] = row_sees(L, sg, r0 + i, u);
+          for (int i = lane; i < 2 * BM; i += 32) {
+            const int32_t *qpos = nullptr;
+            if (i < rows) row_query(L, sg, it, r0 + i, D, qpos);
+            sm.span[buf][i] = row_sees(L, sg, qpos, u);
+          }
         }
         u = join_warp(u);
         if (lane == 0) {
           const Tiles tl = make_tiles(u.x, u.y, u.z, BT);
-          sm.plan[buf] = {tl, chunk_tile(tl, it.c, it.n), chunk_tile(tl, it.c + 1, it.n), rows, item};
+          sm.plan[buf] = {tl, chunk_tile(tl, it.c, it.n), chunk_tile(tl, it.c + 1, it.n), rows, it};
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
         if (n > 0) {
           if (!wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
 #pragma unroll 1
-          for (int i = 0; i < rows; i += 32)
-            copy_q<D>(sm.q[i / BM], i % BM, row_query(L, sg, it, r0 + i + lane, D), lane);
+          for (int i = 0; i < rows; i += 32) {
+            const int32_t *qpos;
+            copy_q<D>(sm.q[i / BM], i % BM, i + lane < rows ? row_query(L, sg, it, r0 + i + lane, D, qpos) : nullptr, lane);
+          }
           copy_q_done();
           __syncwarp();
         }
@@ -519,14 +529,14 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     for (int n = 0; ok; ++n) {
       if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
       const Plan pl = sm.plan[n & 1];
-      if (pl.item < 0) break;
+      if (pl.rows == 0) break;
       const Tiles tl = pl.tl;
       const bool two = pl.rows > BM;
       const int lrow = two ? hb * BM + row : row;  // row of the item
       const Span sp = sm.span[n & 1][lrow];
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
-      const Item it = decode_item(L, pl.item);
+      const Item it = pl.it;
       const Seg &sg = L.seg[it.s];
       const bool warp_rows = lrow - lane < pl.rows;  // the warp has a row of the item
       float m_used = -INFINITY, lsum = 0.0f;
@@ -579,61 +589,62 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         f0 = exp2f(m_used - ref), f1 = exp2f(o1.x - ref);
         lsum = fmaf(lsum, f0, o1.y * f1);
       }
-      const int r = it.rt * 2 * BM + lrow;
+      const int r = it.rt * L.rows_per_item + lrow;
       const bool valid = lrow < pl.rows;
-      const Traj *t = nullptr;
-      int64_t orow = 0;
+      float *pdst = nullptr, *ldst = nullptr;
       __nv_bfloat16 *dst = nullptr;
-      float *pdst = nullptr;
-      const void *qrow = nullptr;
-      if (valid) {
+      if (valid && it.split) {
+        pdst = L.po + part_index(L, sg, it, r) * D;
+        L.pml[part_index(L, sg, it, r)] = make_float2(m, lsum);
+      } else if (valid) {
         int rr = r;
-        t = &L.t[traj_of_row(L, sg, rr)];
-        orow = row_index(L, *t, it.l, it.kvh, rr);
-        qrow = static_cast<const __nv_bfloat16 *>(t->q) + orow * D;
-        if (it.split) pdst = L.po + part_index(L, sg, it, r) * D;
-        else dst = static_cast<__nv_bfloat16 *>(t->out) + orow * D;
+        const Traj &t = L.t[traj_of_row(L, sg, rr)];
+        const int64_t orow = row_index(L, t, it.l, it.kvh, rr);
+        dst = static_cast<__nv_bfloat16 *>(t.out) + orow * D;
+        if (t.lse) ldst = t.lse + orow;
       }
+      if (ldst) *ldst = lse_of(m, lsum);
       const float inv = norm_of(lsum);
       const float g0 = dst ? f0 * inv : f0, g1 = dst ? f1 * inv : f1;
       float chk = 0.0f;
       if (warp_rows) {
+        // 16 channels of every row at a time through shared memory, so that
+        // four lanes store them side by side; a short loop, because an item's
+        // end runs on cold instructions
+        float4 *stage = sm.stage[warp - 4];
+        const uint64_t row_out = pdst ? reinterpret_cast<uint64_t>(pdst) : reinterpret_cast<uint64_t>(dst);
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-          float y[32];
-          if (mine) {
-            tmem_ld32f(o_col + c0, y);
+        for (int c0 = 0; c0 < D; c0 += 16) {
+          float y[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[i] = 0.0f;
+#pragma unroll 1
+          for (int k = 0; k < 1 + other; ++k) {
+            if (!mine) break;
+            uint32_t z[16];
+            const float gk = k ? g1 : g0;
+            tmem_ld16(o_col + D * k + c0, z);
             tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] *= g0;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = 0.0f;
-          }
-          if (other) {
-            float z[32];
-            tmem_ld32f(o_col + D + c0, z);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = fmaf(z[i], g1, y[i]);
+            for (int i = 0; i < 16; ++i) y[i] = fmaf(__uint_as_float(z[i]), gk, y[i]);
           }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) chk = fmaf(y[i], 0.0f, chk);  // NaN if any is not finite
-          if (pdst) {
+          for (int i = 0; i < 16; ++i) chk = fmaf(y[i], 0.0f, chk);  // NaN if any is not finite
+          __syncwarp();  // the last piece has been read
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              *reinterpret_cast<float4 *>(pdst + c0 + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-          } else if (dst) {
+          for (int k = 0; k < 4; ++k) stage[lane * 5 + k] = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+          __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint4 w;
-              uint32_t *wp = &w.x;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(y[i + 2 * k], y[i + 2 * k + 1]);
-                wp[k] = *reinterpret_cast<const uint32_t *>(&h);
-              }
-              *reinterpret_cast<uint4 *>(dst + c0 + i) = w;
+          for (int k = 0; k < 4; ++k) {
+            const int rr = 8 * k + lane / 4, q = c0 / 4 + lane % 4;
+            const uint64_t p = __shfl_sync(0xffffffffu, row_out, rr);
+            const float4 v = stage[rr * 5 + lane % 4];
+            if (!p) continue;
+            if (it.split) {
+              reinterpret_cast<float4 *>(p)[q] = v;
+            } else {
+              const __nv_bfloat162 h[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+              reinterpret_cast<uint2 *>(p)[q] = *reinterpret_cast<const uint2 *>(h);
             }
           }
         }
@@ -645,10 +656,6 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (other) mbar_arrive(&sm.o_empty[1]);
         if (!two) mbar_arrive(&sm.pub_empty);
       }
-      if (valid) {
-        if (pdst) L.pml[part_index(L, sg, it, r)] = make_float2(m, lsum);
-        else if (t->lse) t->lse[orow] = lse_of(m, lsum);
-      }
       unsigned bad = __ballot_sync(0xffffffffu, valid && chk != 0.0f && isfinite(lsum));
       while (bad) {  // a masked value that is not finite met a weight of zero
         const int b = __ffs(bad) - 1;
@@ -656,7 +663,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         const Span one = {__shfl_sync(0xffffffffu, sp.lo, b), __shfl_sync(0xffffffffu, sp.hi, b),
                           __shfl_sync(0xffffffffu, sp.se, b)};
         const float mb = __shfl_sync(0xffffffffu, m, b), lb = __shfl_sync(0xffffffffu, lsum, b);
-        const void *qb = reinterpret_cast<const void *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(qrow), b));
+        const int32_t *qpos;
+        const void *qb = row_query(L, sg, it, r - lane + b, D, qpos);
         float o[D / 32];
         redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1, mb == -INFINITY ? 0.0f : mb,
                                    o);
