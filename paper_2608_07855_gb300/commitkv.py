@@ -490,17 +490,20 @@ def _attention(name, shape, trajs, prefix, out, lse_out, window, sinks, layer_ma
     b = trajs
     if not isinstance(b, AttentionBatch):
         b = AttentionBatch(shape, trajs, out, lse_out, prefix)
-    elif out is not None or lse_out is not None or prefix is not None or bytes(b.shape) != bytes(shape):
+    elif out is not None or lse_out is not None or prefix is not None or \
+            (b.shape is not shape and bytes(b.shape) != bytes(shape)):
         raise ValueError("the outputs, the prefix and the shape are those of the batch")
-    if (b.prefix is None) != (name == "commitkv_window_attention"):
+    if (b._prefix is None) != (name == "commitkv_window_attention"):
         raise ValueError("commitkv_prefix_attention takes a prefix, commitkv_window_attention none")
-    if workspace is None or workspace.device.index != b.device or _torch().cuda.current_device() != b.device:
+    torch = _torch()
+    if workspace is None or workspace.get_device() != b.device or torch.cuda.current_device() != b.device:
         raise ValueError("the batch and the workspace must be on the current GPU")
     _mbuf, mptr = _mask(layer_mask, shape.layers)
-    more = () if b.prefix is None else (b._prefix,)
-    rc = getattr(load_library(), name)(*b._args, *more, mptr, window, sinks, b._out, b._lse, workspace.data_ptr(),
-                                       workspace.numel(), _stream(stream))
-    _check(rc, name)
+    more = () if b._prefix is None else (b._prefix,)
+    rc = getattr(_lib or load_library(), name)(
+        *b._args, *more, mptr, window, sinks, b._out, b._lse, workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if rc != COMMITKV_OK:
+        raise CommitKVError(rc, name)
 
 
 def commitkv_window_attention(shape: Shape, trajs, out=None, lse_out=None, window: int = 0, sinks: int = 0,

@@ -185,19 +185,29 @@ int sm_count() {
   return n;
 }
 
-// How the row tiles of a path's segments are divided: estimated time, in tile
-// periods of `slots` concurrent items, each of which costs `fixed` tiles
-// besides its own.
+// How the row tiles of a path's segments are divided: estimated time in us of
+// `slots` concurrent items.  An item costs `fixed` tiles besides its own, a
+// call with partial results another kernel (kMergeUs) and their rows'
+// writing and reading back.  Measured: a three-prompt batch of 84 row tiles of
+// 9 token tiles, 64 channels, 49 us in two chunks each, @D64@ whole; one token
+// over 16 caches of a 4K window 50 us in chunks, @WHOLE@ whole.
+constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3;
+struct PathInfo {
+  int rows, tile;        // of an item, tokens of a tile
+  int resident;          // items at a time on an SM
+  double fixed, tile_us;
+};
 struct Divide {
   int64_t base[kMaxSeg];   // slices x row tiles
   int64_t tiles[kMaxSeg];  // of a row tile, at most
+  int64_t rows[kMaxSeg];   // of all slices
   int n;
 };
 struct Division {
   int64_t len;  // every row tile in chunks of `len` tiles,
   int64_t rest, chunks;  // or, where rest >= 0, the last `rest` row tiles alone, in `chunks`
 };
-Division divide(const Divide &v, int64_t slots, double fixed, int64_t most_items, int64_t slices, bool tail) {
+Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most_items, int64_t slices, bool prefix) {
   int64_t longest = 1, kinds = 0, kind = 0;
   for (int s = 0; s < v.n; ++s) {
     longest = std::max(longest, v.tiles[s]);
@@ -208,27 +218,30 @@ Division divide(const Divide &v, int64_t slots, double fixed, int64_t most_items
   for (int64_t k = 1, len = 0; k <= longest; ++k) {  // chunks of the longest cache
     if (len == cdiv(longest, k)) continue;
     len = cdiv(longest, k);
-    int64_t items = 0, split = 0;
+    int64_t items = 0, split = 0, parts = 0;
     double work = 0;
     for (int s = 0; s < v.n; ++s) {
       const int64_t c = std::max<int64_t>(1, cdiv(v.tiles[s], len));
       items += v.base[s] * c;
       if (c > 1) split += v.base[s] * c;
-      work += (double)v.base[s] * (v.tiles[s] + c * fixed);
+      if (c > 1 || prefix) parts += v.rows[s] * c;
+      work += (double)v.base[s] * (v.tiles[s] + c * pi.fixed);
     }
     if (split > most_items) break;
     // whole waves where all items are alike, else the work and the tail that the last items leave
-    const double one = len + fixed;
-    const double t = items <= slots ? one : kinds == 1 ? cdiv(items, slots) * one : work / slots + 0.5 * one;
+    const double one = len + pi.fixed;
+    double t = items <= slots ? one : kinds == 1 ? cdiv(items, slots) * one : work / slots + 0.5 * one;
+    t = t * pi.tile_us + parts * kMergeRowUs + (split > 0 && !prefix ? kMergeUs : 0.0);
     if (t < best_t * 0.98) best_t = t, best.len = len;  // fewer chunks unless more are clearly better
   }
   // one segment that fills some waves: only what is left of the last one is cut
-  const int64_t total = kinds == 1 && tail ? v.base[kind] : 0, waves = total / slots;
+  const int64_t total = kinds == 1 && !prefix ? v.base[kind] : 0, waves = total / slots;
   if (waves > 0) {
     const int64_t rest = total / slices - waves * slots / slices;
     for (int64_t n = 2; rest > 0 && rest * slices * n <= most_items && n <= v.tiles[kind]; ++n) {
-      const double t = waves * (v.tiles[kind] + fixed) +
-                       cdiv(rest * slices * n, slots) * ((double)v.tiles[kind] / n + fixed);
+      const double t = (waves * (v.tiles[kind] + pi.fixed) +
+                        cdiv(rest * slices * n, slots) * ((double)v.tiles[kind] / n + pi.fixed)) * pi.tile_us +
+                       kMergeUs + rest * slices * pi.rows * n * kMergeRowUs;
       if (t < best_t * 0.98) best_t = t, best.rest = rest, best.chunks = n;
     }
   }
@@ -236,12 +249,8 @@ Division divide(const Divide &v, int64_t slots, double fixed, int64_t most_items
 }
 
 enum { kSimt16, kSimt64, kTc, kRows, kPaths };
-struct PathInfo {
-  int rows, tile;    // of an item, tokens of a tile
-  int resident;      // items at a time on an SM
-  double fixed;      // an item's fixed part, in tiles
-};
-constexpr PathInfo kPath[kPaths] = {{16, 64, 2, 1.0}, {64, 64, 1, 1.0}, {256, 128, 1, 2.0}, {16, 64, 2, 2.0}};
+constexpr PathInfo kPath[kPaths] = {
+    {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {16, 64, 2, 2.0, 1.4}};
 
 bool force_cuda_cores() {
   const char *e = getenv("COMMITKV_SCORING");
@@ -335,12 +344,14 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
       // a window's rows see at most window + sinks tokens, its tile the rows' span more
       const int64_t seen = window ? (int64_t)window + sinks + std::min(pi.rows, sg.R) / L.g : sg.S;
       v.base[v.n] = (int64_t)L.n_layers * L.H * sg.nrt;
+      v.rows[v.n] = (int64_t)L.n_layers * L.H * sg.R;
       v.tiles[v.n] = cdiv(std::min<int64_t>(sg.S, seen), pi.tile);
       ids[v.n++] = s;
     }
     if (v.n == 0) continue;
     const int64_t slices = (int64_t)L.n_layers * L.H;
-    const Division dv = divide(v, (int64_t)sms * pi.resident, pi.fixed, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit, slices, !prefix);
+    const Division dv =
+        divide(v, pi, (int64_t)sms * pi.resident, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit, slices, prefix != nullptr);
     int64_t items = 0;
     for (int i = 0; i < v.n; ++i) {
       Seg &sg = L.seg[ids[i]];

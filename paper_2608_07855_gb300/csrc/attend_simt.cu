@@ -5,7 +5,8 @@
 // 16 x 16 grid owns TM rows: their scores against four tokens (tx + 16 j) of a
 // tile, then D / 16 channels of their sums, so a row's running max and sum
 // live in registers of the 16 lanes that share it.  Q, K, V and the weights go
-// through shared memory as fp32.
+// through shared memory as fp32.  Bound by fp32 FMAs (taken in packed pairs)
+// and the shared-memory reads that feed them.
 #include <string.h>
 
 #include "attend.cuh"
@@ -25,15 +26,33 @@ struct Smem {
   static constexpr int BM = 16 * TM;
   static constexpr int KP = D + 4;  // rows 16 bytes apart in the banks
   float q[BM][KP];
-  float k[TT][KP];
+  union {  // the weights take the place of the keys: two blocks of 64 rows fit an SM
+    float k[TT][KP];
+    float p[BM][TT + 4];
+  };
   float v[TT][D];
-  float p[BM][TT + 4];
   int lo[BM], hi[BM], se[BM];
   int u_lo, u_hi, u_se;
 };
 
+// Row i of a tile of K and V, channels 4 c .. 4 c + 3, as fp32.
+template <typename T>
+__device__ __forceinline__ void copy4(float *dst, const T *src, bool in, bool wide) {
+  if constexpr (sizeof(T) == 4) {
+    if (wide) {
+      const int n = in ? 16 : 0;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sm103::smem_addr(dst)), "l"(src), "r"(n)
+                   : "memory");
+      return;
+    }
+  }
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (in) x = make_float4(to_f32(src[0]), to_f32(src[1]), to_f32(src[2]), to_f32(src[3]));
+  *reinterpret_cast<float4 *>(dst) = x;
+}
+
 template <typename T, int D, int TM>
-__global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch L) {
+__global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Launch L) {
   constexpr int BM = 16 * TM, CH = D / 16;
   extern __shared__ __align__(16) uint8_t raw[];
   Smem<D, TM> &sm = *reinterpret_cast<Smem<D, TM> *>(raw);
@@ -73,6 +92,7 @@ __global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch
   const int j0 = chunk_tile(tl, it.c, it.n), j1 = chunk_tile(tl, it.c + 1, it.n);
   const T *kb = static_cast<const T *>(sg.k) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
   const T *vb = static_cast<const T *>(sg.v) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
+  const bool wide = (((uintptr_t)kb | (uintptr_t)vb | (uintptr_t)(sg.st * 4)) & 15) == 0;
   Span sp[TM];
   float m[TM], lsum[TM];
   float2 o[TM][CH / 2];
@@ -88,12 +108,14 @@ __global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch
   for (int j = j0; j < j1; ++j) {
     const int a = tile_start(tl, j, TT), n = tile_end(tl, j, TT) - a;
     __syncthreads();
-    for (int e = tid; e < TT * D; e += NT) {
-      const int i = e / D, c = e % D;
-      const bool in = i < n;
-      sm.k[i][c] = in ? to_f32(kb[(int64_t)(a + i) * sg.st + c]) : 0.0f;
-      sm.v[i][c] = in ? to_f32(vb[(int64_t)(a + i) * sg.st + c]) : 0.0f;
+#pragma unroll 4
+    for (int e = tid; e < TT * D / 4; e += NT) {
+      const int i = e / (D / 4), c = 4 * (e % (D / 4));
+      const int64_t at = (int64_t)(i < n ? a + i : 0) * sg.st + c;
+      copy4(&sm.k[i][c], kb + at, i < n, wide);
+      copy4(&sm.v[i][c], vb + at, i < n, wide);
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     float2 s2[TM][4];
 #pragma unroll
@@ -115,6 +137,7 @@ __global__ void __launch_bounds__(NT) attend_simt(const __grid_constant__ Launch
           s2[i][t] = ffma2(make_float2(q4[i].z, q4[i].w), make_float2(k4[t].z, k4[t].w), s2[i][t]);
         }
     }
+    __syncthreads();  // the keys have been read
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       float s[4], mx = -INFINITY;
