@@ -388,35 +388,33 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       uint32_t g = 0, np[2] = {0, 0}, uses[2] = {0, 0};  // earlier items: tiles, tiles of each group, items that filled O_b
       bool ok = true;
       auto kv_wait = [&](uint32_t u) { return wait_warp(&sm.kv_full[u % NST], (u / NST) & 1, abort_flag); };
-      auto qk = [&](int qt, int b, uint32_t u, int cols, bool last, bool end) {
+      // descriptors of stage 0 and of Q: a stage, k-step or row tile further adds to the address field
+      const uint64_t k0 = desc_kmajor(sm.kv[0], 0), v0 = desc_v(sm.kv[0], 0), q0 = desc_kmajor(sm.q[0], 0);
+      constexpr uint64_t kStep = S::kTile >> 4;
+      // by one lane: S_b = Q K^T with K tile u
+      auto qk = [&](int qt, int b, uint32_t u, int cols) {
         const uint32_t idesc = idesc_bf16_f32(BM, 0, 0, 0) | ((uint32_t)(cols >> 3) << 17);
-        tc_fence_after();
-        if (elect_one()) {
+        const uint64_t ka = k0 + (u % NST) * kStep, qa = q0 + qt * kStep;
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            mma_bf16(tm + BT * b, desc_kmajor(sm.q[qt], ks), desc_kmajor(sm.kv[u % NST], ks), idesc, ks > 0);
-          mma_commit(&sm.s_full[b]);
-          if (last) mma_commit(&sm.kv_empty[u % NST]);
-          if (end) mma_commit(&sm.q_empty);
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint64_t at = ((ks >> 2) * kHalf + (ks & 3) * 32) >> 4;
+          mma_bf16(tm + BT * b, qa + at, ka + at, idesc, ks > 0);
         }
-        __syncwarp();
+        mma_commit(&sm.s_full[b]);
       };
-      // P V of the i-th tile of group b in this item (last: nothing else needs the V tile, end: of the item)
-      auto pv = [&](int b, int i, uint32_t u, int cols, bool last, bool end) {
-        if (!(i > 0 || uses[b] == 0 || wait_warp(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag))) return false;
-        if (!wait_warp(&sm.p_full[b], (np[b] + i) & 1, abort_flag)) return false;
-        const uint32_t idesc = idesc_bf16_f32(BM, D, 0, 1);
-        tc_fence_after();
-        if (elect_one()) {
+      // by one lane: O_b (+)= P_b V with V tile u
+      auto pv = [&](int b, uint32_t u, int cols, bool first) {
+        constexpr uint32_t idesc = idesc_bf16_f32(BM, D, 0, 1);
+        const uint64_t va = v0 + (u % NST) * kStep;
 #pragma unroll
-          for (int ks = 0; ks < BT / 16; ++ks)
-            if (16 * ks < cols)
-              mma_bf16_ts(tm + 256 + D * b, tm + BT * b + 8 * ks, desc_v(sm.kv[u % NST], ks), idesc, i > 0 || ks > 0);
-          if (last) mma_commit(&sm.kv_empty[u % NST]);
-          if (end) mma_commit(&sm.o_full[b]);
-        }
-        __syncwarp();
-        return true;
+        for (int ks = 0; ks < BT / 16; ++ks)
+          if (16 * ks < cols)
+            mma_bf16_ts(tm + 256 + D * b, tm + BT * b + 8 * ks, va + ks * (2048 >> 4), idesc, !first || ks > 0);
+      };
+      // weights of group b's i-th tile of this item are there, and O_b may be written
+      auto p_wait = [&](int b, int i) {
+        return (i > 0 || uses[b] == 0 || wait_warp(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag)) &&
+               wait_warp(&sm.p_full[b], (np[b] + i) & 1, abort_flag);
       };
       for (int n = 0; ok; ++n) {
         if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
@@ -428,13 +426,41 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         const int nt = pl.j1 - pl.j0;
         if (nt == 0 && lane == 0) mbar_arrive(&sm.q_empty);  // else behind the last Q K^T
         if (pl.rows > BM) {
-          // two row tiles: tile j's Q K^T behind tile j - 1's P V, group by group
-          for (int j = 0; j <= nt && ok && nt > 0; ++j) {
+          // two row tiles: tile j's Q K^T right behind tile j - 1's P V, group by group
+          if (nt > 0 && (ok = kv_wait(2 * g))) {
+            tc_fence_after();
+            if (elect_one()) {
+              const int cols = tile_cols(pl.tl, pl.j0);
+              qk(0, 0, 2 * g, cols);
+              qk(1, 1, 2 * g, cols);
+              mma_commit(&sm.kv_empty[2 * g % NST]);
+              if (nt == 1) mma_commit(&sm.q_empty);
+            }
+            __syncwarp();
+          }
+          for (int j = 1; j <= nt && ok; ++j) {
             const uint32_t uk = 2 * (g + j), uv = uk - 1;
-            const int ck = j < nt ? tile_cols(pl.tl, pl.j0 + j) : 0, cv = j > 0 ? tile_cols(pl.tl, pl.j0 + j - 1) : 0;
-            for (int b = 0; b < 2 && ok; ++b) {
-              if (j > 0) ok = (b || kv_wait(uv)) && pv(b, j - 1, uv, cv, b == 1, j == nt);
-              if (ok && j < nt && (ok = b || kv_wait(uk))) qk(b, b, uk, ck, b == 1, b == 1 && j + 1 == nt);
+            const int cv = tile_cols(pl.tl, pl.j0 + j - 1), ck = j < nt ? tile_cols(pl.tl, pl.j0 + j) : 0;
+            if (!(ok = kv_wait(uv) && (j == nt || kv_wait(uk)))) break;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              if (!p_wait(b, j - 1)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              if (elect_one()) {
+                pv(b, uv, cv, j == 1);
+                if (b) mma_commit(&sm.kv_empty[uv % NST]);
+                if (j < nt) {
+                  qk(b, b, uk, ck);
+                  if (b) mma_commit(&sm.kv_empty[uk % NST]);
+                  if (b && j + 1 == nt) mma_commit(&sm.q_empty);
+                } else {
+                  mma_commit(&sm.o_full[b]);
+                }
+              }
+              __syncwarp();
             }
           }
           np[0] += nt, np[1] += nt;
@@ -443,9 +469,28 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           // one row tile, the groups take alternate token tiles
           for (int j = 0; j < nt + 2 && ok && nt > 0; ++j) {
             const uint32_t uk = 2 * (g + j), uv = uk - 3;
-            const int b = j & 1;
-            if (j >= 2) ok = kv_wait(uv) && pv(b, (j - 2) >> 1, uv, tile_cols(pl.tl, pl.j0 + j - 2), true, j >= nt);
-            if (ok && j < nt && (ok = kv_wait(uk))) qk(0, b, uk, tile_cols(pl.tl, pl.j0 + j), true, j + 1 == nt);
+            const int b = j & 1, i = (j - 2) >> 1;
+            if (j >= 2) {
+              ok = (uint32_t)(j - 2) >= (uint32_t)nt || (kv_wait(uv) && p_wait(b, i));
+              if (!ok) break;
+              tc_fence_after();
+              if (j - 2 < nt && elect_one()) {
+                pv(b, uv, tile_cols(pl.tl, pl.j0 + j - 2), i == 0);
+                mma_commit(&sm.kv_empty[uv % NST]);
+                if (j >= nt) mma_commit(&sm.o_full[b]);
+              }
+              __syncwarp();
+            }
+            if (j < nt) {
+              if (!(ok = kv_wait(uk))) break;
+              tc_fence_after();
+              if (elect_one()) {
+                qk(0, b, uk, tile_cols(pl.tl, pl.j0 + j));
+                mma_commit(&sm.kv_empty[uk % NST]);
+                if (j + 1 == nt) mma_commit(&sm.q_empty);
+              }
+              __syncwarp();
+            }
           }
           np[0] += (nt + 1) / 2, np[1] += nt / 2;
           uses[0] += nt > 0, uses[1] += nt > 1;
