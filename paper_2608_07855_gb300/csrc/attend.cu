@@ -191,7 +191,7 @@ int sm_count() {
 // writing and reading back.  Measured: a three-prompt batch of 84 row tiles of
 // 9 token tiles, 64 channels, 49 us in two chunks each, @D64@ whole; one token
 // over 16 caches of a 4K window 50 us in chunks, @WHOLE@ whole.
-constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3;
+constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3, kBytesPerUs = 6.5e6;
 struct PathInfo {
   int rows, tile;        // of an item, tokens of a tile
   int resident;          // items at a time on an SM
@@ -271,6 +271,12 @@ int path_of(const Launch &L, const Seg &sg) {
   return sg.R <= 16 ? kRows : kTc;
 }
 
+// Tokens of a cache that a row tile needs, at most: with a window its rows see
+// `window` + `sinks` tokens each, their positions' span more.
+int64_t most_seen(const Launch &L, const Seg &sg, int rows) {
+  return L.window ? (int64_t)L.window + L.sinks + std::min(rows, sg.R) / L.g : sg.S;
+}
+
 commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
                        const commitkv_traj *prefix, const uint8_t *layer_mask, int32_t window, int32_t sinks,
                        void *const *out, float *const *lse_out, void *workspace, size_t workspace_bytes,
@@ -331,6 +337,14 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   int path[kMaxSeg];
   int64_t parts = 0;
   bool merge = false;
+  const int64_t slices = (int64_t)L.n_layers * L.H;
+  double rows_us = 0.0;  // time of the decode kernel, which reads its caches at the memory's rate
+  for (int s = 0; s < L.n_seg; ++s) {
+    const Seg &sg = L.seg[s];
+    path[s] = path_of(L, sg);
+    if (path[s] == kRows && sg.R > 0)
+      rows_us += (double)slices * std::min<int64_t>(sg.S, most_seen(L, sg, 16)) * L.d * 4 / kBytesPerUs;
+  }
   for (int p = 0; p < kPaths; ++p) {
     const PathInfo &pi = kPath[p];
     Divide v;
@@ -338,20 +352,24 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     v.n = 0;
     for (int s = 0; s < L.n_seg; ++s) {
       Seg &sg = L.seg[s];
-      if (p == 0) path[s] = path_of(L, sg);
       if (path[s] != p) continue;
       sg.nrt = (int32_t)cdiv(sg.R, pi.rows);
-      // a window's rows see at most window + sinks tokens, its tile the rows' span more
-      const int64_t seen = window ? (int64_t)window + sinks + std::min(pi.rows, sg.R) / L.g : sg.S;
-      v.base[v.n] = (int64_t)L.n_layers * L.H * sg.nrt;
-      v.rows[v.n] = (int64_t)L.n_layers * L.H * sg.R;
-      v.tiles[v.n] = cdiv(std::min<int64_t>(sg.S, seen), pi.tile);
+      v.base[v.n] = slices * sg.nrt;
+      v.rows[v.n] = slices * sg.R;
+      v.tiles[v.n] = cdiv(std::min<int64_t>(sg.S, most_seen(L, sg, pi.rows)), pi.tile);
       ids[v.n++] = s;
     }
     if (v.n == 0) continue;
-    const int64_t slices = (int64_t)L.n_layers * L.H;
+    int64_t slots = (int64_t)sms * pi.resident;
+    // A prefix on the tensor cores beside decoded caches, which run at the same
+    // time: as few blocks as finish with them, the others' SMs read the caches
+    // (64 agents behind a 16K prefix, 2,048 tokens each at most: 99 us with the
+    // prefix on all SMs first, @OVER@ so).
+    if (p == kTc && v.n == 1 && rows_us > 0.0)
+      slots = std::min(slots, std::max<int64_t>(
+                                  1, (int64_t)(v.base[0] * v.tiles[0] / std::max(1.0, rows_us / pi.tile_us - 2 * pi.fixed))));
     const Division dv =
-        divide(v, pi, (int64_t)sms * pi.resident, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit, slices, prefix != nullptr);
+        divide(v, pi, slots, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit, slices, prefix != nullptr);
     int64_t items = 0;
     for (int i = 0; i < v.n; ++i) {
       Seg &sg = L.seg[ids[i]];

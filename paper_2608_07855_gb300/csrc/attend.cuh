@@ -66,9 +66,14 @@ struct Launch {
 // The kernels of a call overlap where they can (programmatic launches): each
 // lets the next one start once all of its own blocks have, the kernels of the
 // segments do not depend on one another, and the merge waits for all of them:
-// a kernel that started early does not end before the one ahead of it.
+// the last block of a kernel that started early ends after the kernel ahead of
+// it (every block: those that are done would keep their places from the rest).
 __device__ __forceinline__ void pdl_start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+__device__ __forceinline__ void pdl_chain() {
+  if (blockIdx.x == gridDim.x - 1) pdl_wait();
+}
 
 // Launches a kernel; `early`: it may start before the call's last kernel ends.
 template <typename... A>

@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
     }
     write_row_warp<__nv_bfloat16, D>(L, sg, it, r, x, mr, lr);
   }
-  pdl_wait();
+  pdl_chain();
 }
 
 template <int D>

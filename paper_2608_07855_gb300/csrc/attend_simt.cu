@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Lau
     }
     write_row_warp<T, D>(L, sg, it, r0 + r, x, mr, lr);
   }
-  pdl_wait();
+  pdl_chain();
 }
 
 template <typename T, int D, int TM>
