@@ -24,6 +24,11 @@ library's entry points in the order of Algorithm 1:
                says when, and decode_checkpoint() fills the budget by each
                resident token's largest attention weight from the latest
                window (commitkv_token_scores on the window's row stats).
+  attend       between commits, the attention of the agent's own model:
+               new tokens (a prompt chunk, or one decoded token) over the
+               resident cache, whose positions have gaps after a checkpoint
+               (commitkv_window_attention), or over a prefix that agents
+               share and the resident cache (commitkv_prefix_attention).
   post_commit  R+ over the post-commit window with the row stats;
                classification (Eq. 9-10, or an ablation variant of Section
                4.4); at most scan_cap candidates in order (the paper scans at
@@ -77,6 +82,7 @@ class Session:
         self.checkpoint_every = checkpoint_every  # decoded tokens between checkpoints (0: caller-driven only)
         self.decoded_since = 0  # decoded tokens appended since the last checkpoint
         self.ws = None
+        self.attention_ws = None
 
     # ---------------------------------------------------------------- helpers
     def _traj(self, Q=None, qpos=None) -> ck.TrajTensors:
@@ -168,6 +174,26 @@ class Session:
             for s in range(b, b + m, self.G):
                 self.pages.append([self.next_id, S0 + (s - p0), min(self.G, b + m - s)])
                 self.next_id += 1
+
+    def attend(self, Q, qpos, window: int = 0, sinks: int = 0, prefix: ck.TrajTensors = None):
+        """Attention of the queries Q [M][Hq][W][d] at positions qpos [W]
+        (device tensors) over the resident cache, the new tokens appended
+        before: (out like Q, lse [M][Hq][W]).  window and sinks as in
+        commitkv_window_attention; prefix: a cache shared by agents, whose
+        positions come before this session's."""
+        torch = _torch()
+        s, S = self.shape, self.S
+        tr = ck.TrajTensors(self.K[:, :, :S], self.V[:, :, :S], self.pos[:S], Q, qpos)
+        out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], device=self.dev)
+        need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
+        if self.attention_ws is None or self.attention_ws.numel() < need:
+            self.attention_ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+        ws = self.attention_ws
+        if prefix is None:
+            ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
+        else:
+            ck.commitkv_prefix_attention(s, [tr], prefix, [out], [lse], window, sinks, workspace=ws)
+        return out, lse
 
     # ---------------------------------------------------------------- commit
     def pre_commit(self, Q, qpos):

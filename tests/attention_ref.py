@@ -73,7 +73,8 @@ def check(got, want, tol, what=""):
     inf = np.isinf(want)
     assert np.array_equal(got[inf], want[inf]) and not np.isinf(got[~inf]).any(), what + ": infinities"
     f = np.isfinite(want)
-    off = np.abs(got - want)
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got - want)
     bad = f & ~(off <= tol)
     if bad.any():
         at = tuple(x[0] for x in np.nonzero(bad))

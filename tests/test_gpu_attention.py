@@ -276,9 +276,9 @@ def test_prefix_equals_one_cache():
         ws = ck.alloc_attention_workspace(p.shape, joined)
         ck.commitkv_window_attention(p.shape, joined, out=out, window=90, sinks=4, workspace=ws)
         torch.cuda.synchronize()
-        for a, b in zip(out, p.out):
-            tol = 0.02 if dtype == BF else 1e-5
-            assert (a.float() - b.float()).abs().max() <= tol
+        for o, (k, v, pos, q, at) in zip(out, p.host):
+            want, _, tol, _ = ref.attention([tuple(p.pre), (k, v, pos)], q, at, 90, 4, rounded_weights=dtype == BF)
+            ref.check(o, want, tol, "one cache")
 
 
 def test_empty_prefix():
@@ -414,3 +414,73 @@ def test_effects_from_attention():
     torch.cuda.synchronize()
     assert ck.commitkv_workspace_status(ws) == ck.COMMITKV_OK
     assert ((R - want).abs() <= 1e-4 * want.abs()).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("prefix", [0, 900])
+def test_many_items(d, prefix):
+    """More work items than SMs, of one and of two row tiles: blocks go from item to item."""
+    p = Problem(dtype=BF, d=d, M=24, H=4, Hq=8, prefix=prefix, gaps=0.8,
+                trajs=[(300, 40), (420, 150), (700, 9), (64, 64), (0, 20), (333, 33)]).upload()
+    for window, sinks in ((0, 0), (130, 3)):
+        p.flat.fill_(SENT)
+        p.flat_l.fill_(SENT)
+        p.call(window, sinks)
+        p.check(window, sinks, layers=[0, 13, 23])
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64)], ids=["bf16-128", "bf16-64", "f32-64"])
+def test_long_prompt_is_cut_at_its_end(dtype, d):
+    """Whole waves of row tiles and a cut remainder: written and merged rows side by side."""
+    W = 2600 if dtype == BF else 700
+    p = Problem(dtype=dtype, d=d, M=4, H=4, Hq=16, trajs=[(W + 300, W)]).upload()
+    p.call()
+    torch.cuda.synchronize()
+    t = p.trajs[0]
+    for l, h in ((0, 0), (3, 15), (2, 6)):
+        s = (t.q[l, h].double() @ t.k[l, h // 4].double().T) * d ** -0.5
+        s.masked_fill_(t.pos[None, :] > t.q_pos[:, None], -math.inf)
+        want = torch.softmax(s, 1) @ t.v[l, h // 4].double()
+        spread = torch.softmax(s, 1) @ t.v[l, h // 4].double().abs()
+        # half a step of the output and of every weight, and fp32 sums (attention_ref.attention)
+        eps = 2.0 ** -8 if dtype == BF else 2.0 ** -24
+        tol = eps * want.abs() + (eps if dtype == BF else 0.0) * spread + 2.0 ** -14 * spread
+        assert ((p.out[0][l, h].double() - want).abs() <= tol).all()
+        assert ((p.lse[0][l, h].double() - torch.logsumexp(s, 1)).abs() <= 2.0 ** -14).all()
+    p.guards()
+
+
+def test_session_attends_before_and_after_a_checkpoint():
+    """A session's own attention over its cache, compressed in between, and behind a shared prefix."""
+    from paper_2608_07855_gb300.lifecycle import Session
+
+    M, H, Hq, d, n = 2, 2, 8, 128, 500
+    g = torch.Generator().manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=g).to(BF)  # noqa: E731
+    shape = ck.make_shape(M, H, Hq, d, BF)
+    s = Session(shape, 32, 200, 0.5, 1000)
+    k, v = rand(M, H, n, d), rand(M, H, n, d)
+    first = 100  # behind a prefix of 100 tokens
+    s.append(k.cuda(), v.cuda(), torch.arange(first, first + n, dtype=torch.int32, device="cuda"), [("obs", first, 300)])
+    pk, pv = rand(M, H, first, d), rand(M, H, first, d)
+    pre = ck.TrajTensors(pk.cuda(), pv.cuda(), torch.arange(first, dtype=torch.int32, device="cuda"))
+
+    def look(W, window=0, sinks=0, prefix=False):
+        Q = rand(M, Hq, W, d)
+        p = np.arange(first + n - W, first + n)
+        o, l = s.attend(Q.cuda(), torch.from_numpy(p.astype(np.int32)).cuda(), window, sinks, pre if prefix else None)
+        S = s.S
+        own = (s.K[:, :, :S].cpu(), s.V[:, :, :S].cpu(), s.pos[:S].cpu().numpy())
+        parts = ([(pk, pv, np.arange(first))] if prefix else []) + [own]
+        wo, wl, to, tl = ref.attention(parts, Q, p, window, sinks, rounded_weights=True)
+        ref.check(o, wo, to, "out")
+        ref.check(l, wl, tl, "lse")
+
+    for W in (1, 40):
+        look(W)
+        look(W, 150, 4, True)
+    s.checkpoint(torch.rand(n, generator=g).cuda())
+    assert s.S == 200
+    for W in (1, 40):
+        look(W)
+        look(W, 150, 4, True)
