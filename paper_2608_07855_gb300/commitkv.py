@@ -499,6 +499,8 @@ def _attention(name, shape, trajs, prefix, out, lse_out, window, sinks, layer_ma
     if workspace is None or workspace.get_device() != b.device or torch.cuda.current_device() != b.device:
         raise ValueError("the batch and the workspace must be on the current GPU")
     _mbuf, mptr = _mask(layer_mask, shape.layers)
+    if stream is None:  # of this device: asking for the device's index as well takes twice as long
+        stream = torch.cuda.current_stream(b.device)
     more = () if b._prefix is None else (b._prefix,)
     rc = getattr(_lib or load_library(), name)(
         *b._args, *more, mptr, window, sinks, b._out, b._lse, workspace.data_ptr(), workspace.numel(), _stream(stream))

@@ -25,11 +25,10 @@ constexpr int64_t kMaxSplit = 768;
 // ------------------------------------------------------------------ merge
 // o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i over a row's partial results,
 // those of the prefix first.  NW warps to a row take kBatch parts each at a
-// time, all loads of a batch in flight together: the call's time here is
+// time (no more registers than the call has parts, so that rows are in flight
+// together too), all loads of a batch in flight together: the call's time here is
 // latency (16 parts of 32 rows: 13 us a part after the other, @COMBINE@ so).
-constexpr int kBatch = 8;
-
-template <typename T, int D, int NW>
+template <typename T, int D, int NW, int kBatch>
 __global__ void __launch_bounds__(128) combine(const __grid_constant__ Launch L) {
   constexpr int C = D / 32;  // channels of a lane: C lane ..
   __shared__ float so[NW > 1 ? NW : 1][D];
@@ -128,9 +127,9 @@ cudaError_t launch_combine_td(const Launch &L, cudaStream_t s) {
   int parts = 1;
   for (int t = 0; t < L.n_traj; ++t)
     parts = std::max(parts, L.seg[t + L.prefix].nchunk + (L.prefix ? L.seg[0].nchunk : 0));
-  // up to a batch of parts: a warp to a row
-  if (parts <= kBatch) return launch_after(combine<T, D, 1>, (unsigned)cdiv(rows, 4), 128, 0, s, true, L);
-  return launch_after(combine<T, D, 4>, (unsigned)rows, 128, 0, s, true, L);
+  if (parts <= 2) return launch_after(combine<T, D, 1, 2>, (unsigned)cdiv(rows, 4), 128, 0, s, true, L);
+  if (parts <= 8) return launch_after(combine<T, D, 1, 8>, (unsigned)cdiv(rows, 4), 128, 0, s, true, L);
+  return launch_after(combine<T, D, 4, 8>, (unsigned)rows, 128, 0, s, true, L);
 }
 
 }  // namespace

@@ -44,9 +44,13 @@ __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, volatile in
   return mbar_wait(bar, parity, kWait, abort_flag);
 }
 
+constexpr int kMaxQ = 32;  // trajectories whose Q tiles TMA copies: what the launch parameters have room for
+
 struct TcParams {
   Launch L;
   CUtensorMap k[kMaxSeg], v[kMaxSeg];  // [M][H][S][d], box 64 x 128 x 1 x 1
+  CUtensorMap q[kMaxQ];                // [M H][W][g][d], box 64 x g x 128 / g x 1: a row tile
+  int32_t has_q;                       // the q maps are there: at most kMaxQ trajectories, g divides 128
 };
 
 static_assert(sizeof(TcParams) <= 32764, "kernel parameters");
@@ -82,6 +86,15 @@ __device__ __forceinline__ void tma4(void *dst, const CUtensorMap *m, int x, int
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
       " [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(smem_addr(dst)),
       "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(tok), "r"(h), "r"(l), "r"(smem_addr(bar)), "l"(pol)
+      : "memory");
+}
+
+// A Q row tile's 64 channels from x: all heads of the positions from w.
+__device__ __forceinline__ void tma_q(void *dst, const CUtensorMap *m, int x, int w, int slice, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(0), "r"(w), "r"(slice), "r"(smem_addr(bar))
       : "memory");
 }
 
@@ -507,6 +520,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     } else if (warp == 3) {
       // ------------------------------------------------------------ plans and Q rows
       int item = blockIdx.x;
+      int q_last = -1;  // the last item whose Q TMA copied
       bool asked = false;
       for (int n = 0;; ++n) {
         const int buf = n & 1;
@@ -547,8 +561,22 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
+        if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
+        if (n > 0 && P.has_q && sg.t >= 0) {
+          // between two items nothing else hides this copy: TMA, which a warp's
+          // own copies take twice as long as (window of 4K: @QCOPY@)
+          if (lane == 0) {
+            const int nq = rows > BM ? 2 : 1;
+            mbar_expect_tx(&sm.q_full, nq * S::kTile);
+            for (int i = 0; i < nq; ++i)
+              for (int x = 0; x < D / 64; ++x)
+                tma_q(sm.q[i] + x * kHalf, &P.q[sg.t], 64 * x, (r0 + i * BM) / L.g, it.l * L.H + it.kvh, &sm.q_full);
+          }
+          q_last = n;
+          __syncwarp();
+          continue;
+        }
         if (n > 0) {
-          if (!wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
 #pragma unroll 1
           for (int i = 0; i < rows; i += 32) {
             const int32_t *qpos;
@@ -559,9 +587,10 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         }
         if (lane == 0) mbar_arrive(&sm.q_full);
       }
-      if (asked && lane == 0) {  // left early: the answer lands before the block's memory goes
+      // left early: what is under way lands before the block's memory goes
+      if (asked && lane == 0)
         for (int k = 0; k < 2; ++k) mbar_wait_drain(&sm.next_full, k, kWait / 4);
-      }
+      if (*abort_flag && q_last >= 0 && lane == 0) mbar_wait_drain(&sm.q_full, q_last & 1, kWait);
     }
   } else {
     // ------------------------------------------------------------ softmax
@@ -749,6 +778,18 @@ bool map_kv(CUtensorMap *m, const void *base, const Launch &L, const Seg &sg) {
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool map_q(CUtensorMap *m, const Launch &L, const Traj &t) {
+  auto enc = encode_fn();
+  if (!enc) return false;
+  const cuuint64_t d2 = (cuuint64_t)L.d * 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)L.d, (cuuint64_t)L.g, (cuuint64_t)t.W, (cuuint64_t)L.M * L.H};
+  const cuuint64_t strides[3] = {t.W * d2, d2, (cuuint64_t)L.g * t.W * d2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)L.g, (cuuint32_t)(BM / L.g), 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(t.q), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s, bool early) {
   const int smem = (int)sizeof(Smem<D>) + 1024;
@@ -762,9 +803,12 @@ cudaError_t launch(const TcParams &P, WsHeader *hdr, cudaStream_t s, bool early)
 cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early) {
   static thread_local TcParams P;
   P.L = L;
+  P.has_q = L.n_traj <= kMaxQ && L.g <= BM && BM % L.g == 0;
   for (int i = 0; i < L.n_seg; ++i) {
     const Seg &sg = L.seg[i];
-    if (sg.S == 0 || L.item_off[i] == L.item_off[i + 1]) continue;
+    if (L.item_off[i] == L.item_off[i + 1]) continue;
+    if (P.has_q && sg.t >= 0 && !map_q(&P.q[sg.t], L, L.t[sg.t])) return cudaErrorInvalidValue;
+    if (sg.S == 0) continue;
     if (!map_kv(&P.k[i], sg.k, L, sg) || !map_kv(&P.v[i], sg.v, L, sg)) return cudaErrorInvalidValue;
   }
   return L.d == 128 ? launch<128>(P, hdr, s, early) : launch<64>(P, hdr, s, early);
