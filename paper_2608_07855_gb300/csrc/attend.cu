@@ -27,7 +27,7 @@ constexpr int64_t kMaxSplit = 768;
 // those of the prefix first.  NW warps to a row take kBatch parts each at a
 // time (no more registers than the call has parts, so that rows are in flight
 // together too), all loads of a batch in flight together: the call's time here is
-// latency (16 parts of 32 rows: 13 us a part after the other, @COMBINE@ so).
+// latency (16 parts of 32 rows: 13 us a part after the other, 3.5 so).
 template <typename T, int D, int NW, int kBatch>
 __global__ void __launch_bounds__(128) combine(const __grid_constant__ Launch L) {
   constexpr int C = D / 32;  // channels of a lane: C lane ..
@@ -188,8 +188,8 @@ int sm_count() {
 // `slots` concurrent items.  An item costs `fixed` tiles besides its own, a
 // call with partial results another kernel (kMergeUs) and their rows'
 // writing and reading back.  Measured: a three-prompt batch of 84 row tiles of
-// 9 token tiles, 64 channels, 49 us in two chunks each, @D64@ whole; one token
-// over 16 caches of a 4K window 50 us in chunks, @WHOLE@ whole.
+// 9 token tiles, 64 channels, 49 us in two chunks each, 28 whole; one token over
+// 4 caches of 4,096 tokens 15 us in chunks, 46 whole.
 constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3, kBytesPerUs = 6.5e6;
 struct PathInfo {
   int rows, tile;        // of an item, tokens of a tile
@@ -256,24 +256,48 @@ bool force_cuda_cores() {
   return e && (e[0] == 's' || e[0] == 'S');
 }
 
-// Tensor cores for bf16 where TMA can read the cache (16-byte aligned
-// pointers and strides, distinct heads and layers) and the rows' queries and
-// outputs are 16-byte aligned.
+// Tensor cores where 16-byte copies can read the cache and the rows' queries
+// and outputs: fp32 and up to 16 rows the kernel of 16-row items, other bf16
+// rows the one of 256 (but see few_rows), whose TMA also wants distinct heads
+// and layers.
 int path_of(const Launch &L, const Seg &sg) {
   const int cuda_cores = sg.R <= 16 ? kSimt16 : kSimt64;
-  if (L.dtype != COMMITKV_BF16 || force_cuda_cores()) return cuda_cores;
-  uintptr_t bits = (uintptr_t)sg.k | (uintptr_t)sg.v | (uintptr_t)((sg.sl | sg.sh | sg.st) * 2);
+  if (force_cuda_cores()) return cuda_cores;
+  const int eb = L.dtype == COMMITKV_BF16 ? 2 : 4;
+  uintptr_t bits = (uintptr_t)sg.k | (uintptr_t)sg.v | (uintptr_t)((sg.sl | sg.sh | sg.st) * eb);
   for (int t = sg.t < 0 ? 0 : sg.t; t < (sg.t < 0 ? L.n_traj : sg.t + 1); ++t)
     bits |= L.t[t].W ? (uintptr_t)L.t[t].q | (uintptr_t)L.t[t].out : 0;
   if (bits % 16) return cuda_cores;
-  if (sg.S > 0 && (sg.sh == 0 || sg.sl == 0 || std::max(sg.sl, std::max(sg.sh, sg.st)) >= (1ll << 39))) return cuda_cores;
-  return sg.R <= 16 ? kRows : kTc;
+  if (eb == 4 || sg.R <= 16) return kRows;
+  if (sg.S > 0 && (sg.sh == 0 || sg.sl == 0 || std::max(sg.sl, std::max(sg.sh, sg.st)) >= (1ll << 39))) return kRows;
+  return kTc;
 }
 
 // Tokens of a cache that a row tile needs, at most: with a window its rows see
 // `window` + `sinks` tokens each, their positions' span more.
 int64_t most_seen(const Launch &L, const Seg &sg, int rows) {
   return L.window ? (int64_t)L.window + L.sinks + std::min(rows, sg.R) / L.g : sg.S;
+}
+
+// Whether the bf16 segments of more than 16 rows go to the kernel of 16-row
+// items as well: it reads K and V again for every 16 rows, but has half the
+// other's start and end.  Estimates in us; measured there and here, 32 query
+// on 8 KV heads of 128 channels: 8 queries over 1,000 tokens 17.4 and 11.4, over
+// 16,000 26.0 and 23.4, 16 over 4,000 18.5 and 17.1, 100 over 500 21.2 and
+// 15.3, 8 agents behind 16,000 31.8 and 27.2; 5 over 16 caches to 16,000 127
+// and 161, 12 over 16 to 1,000 23 and 31, 32 over 32,768 44 and 120.
+bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
+  double few = 0.0, many = 15.0, tiles = 0.0, bytes = 0.0, start = 7.0;
+  for (int s = 0; s < L.n_seg; ++s) {
+    const Seg &sg = L.seg[s];
+    if (path[s] == kRows) start = 0.0;  // launched anyway
+    if (path[s] != kTc) continue;
+    const int64_t seen = std::min<int64_t>(sg.S, most_seen(L, sg, 256));
+    few += 1.25 * slices * cdiv(sg.R, 16) * (cdiv(seen, 64) + 1) / (2.0 * sms);
+    tiles += (double)slices * cdiv(sg.R, 256) * cdiv(seen, 128);
+    bytes += (double)slices * seen * L.d * 4;
+  }
+  return start + few < many + std::max(bytes / kBytesPerUs, kPath[kTc].tile_us * tiles / sms);
 }
 
 commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
@@ -337,15 +361,19 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   int64_t parts = 0;
   bool merge = false;
   const int64_t slices = (int64_t)L.n_layers * L.H;
+  for (int s = 0; s < L.n_seg; ++s) path[s] = path_of(L, L.seg[s]);
+  if (few_rows(L, path, slices, sms))
+    for (int s = 0; s < L.n_seg; ++s) path[s] = path[s] == kTc ? kRows : path[s];
   double rows_us = 0.0;  // time of the decode kernel, which reads its caches at the memory's rate
   for (int s = 0; s < L.n_seg; ++s) {
     const Seg &sg = L.seg[s];
-    path[s] = path_of(L, sg);
     if (path[s] == kRows && sg.R > 0)
-      rows_us += (double)slices * std::min<int64_t>(sg.S, most_seen(L, sg, 16)) * L.d * 4 / kBytesPerUs;
+      rows_us += (double)slices * std::min<int64_t>(sg.S, most_seen(L, sg, 16)) * L.d *
+                 (L.dtype == COMMITKV_BF16 ? 4 : 8) / kBytesPerUs;
   }
   for (int p = 0; p < kPaths; ++p) {
-    const PathInfo &pi = kPath[p];
+    PathInfo pi = kPath[p];
+    if (p == kRows) pi.tile = rows_tile(L);
     Divide v;
     int ids[kMaxSeg];
     v.n = 0;
@@ -363,7 +391,7 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     // A prefix on the tensor cores beside decoded caches, which run at the same
     // time: as few blocks as finish with them, the others' SMs read the caches
     // (64 agents behind a 16K prefix, 2,048 tokens each at most: 99 us with the
-    // prefix on all SMs first, @OVER@ so).
+    // prefix on all SMs first, 78 so).
     if (p == kTc && v.n == 1 && rows_us > 0.0)
       slots = std::min(slots, std::max<int64_t>(
                                   1, (int64_t)(v.base[0] * v.tiles[0] / std::max(1.0, rows_us / pi.tile_us - 2 * pi.fixed))));

@@ -96,8 +96,9 @@ cudaError_t launch_after(void (*kernel)(A...), unsigned blocks, unsigned threads
 
 // CUDA cores: any layout and type.  Rows per item: 16 or 64.
 cudaError_t launch_simt(const Launch &L, cudaStream_t s, bool early);
-// Up to 16 rows of a slice, bf16, caches and queries 16-byte aligned.
+// 16 rows per item, caches and queries 16-byte aligned; tiles of rows_tile tokens.
 cudaError_t launch_rows(const Launch &L, cudaStream_t s, bool early);
+inline int rows_tile(const Launch &L) { return L.dtype != COMMITKV_BF16 && L.d == 128 ? 32 : 64; }
 // Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
 cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);
@@ -233,19 +234,29 @@ __device__ __forceinline__ int chunk_tile(const Tiles &t, int c, int n) {
   return t.n / n * c + t.n % n * c / n;
 }
 
-// sum of exp2(s - m) v over the visible tokens of tiles [j0, j1) for one row,
-// by the 32 lanes of a warp: o[k] is channel lane + 32 k.  A masked token's
-// values have no part in it.  The tile kernels multiply masked tokens by
-// weights of zero, which is wrong where a masked value is infinite or NaN, so
-// they redo a row whose sums are not finite this way (its m and l never see
-// masked tokens).  32 tokens at a time, a lane each for the scores.
+// Score of token i against a query, both read by one thread.
 template <typename T, int D>
-__device__ __noinline__ void redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
-                                      Tiles tl, int tile, int j0, int j1, float m, float *o) {
+__device__ __forceinline__ float score_of(const T *q, const T *ki) {
+  float dot = 0.0f;
+#pragma unroll 16
+  for (int c = 0; c < D; ++c) dot = fmaf(to_f32(q[c]), to_f32(ki[c]), dot);
+  return dot;
+}
+
+// sum of exp2(s - m) v and of exp2(s - m) over the visible tokens of tiles
+// [j0, j1) for one row, by the 32 lanes of a warp: o[k] is channel lane + 32 k.
+// A masked token's values have no part in it.  The tile kernels multiply masked
+// tokens by weights of zero, which is wrong where a masked value is infinite or
+// NaN, so they redo a row whose sums are not finite this way (its m and l never
+// see masked tokens).  32 tokens at a time, a lane each for the scores.
+template <typename T, int D>
+__device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
+                                       Tiles tl, int tile, int j0, int j1, float m, float *o) {
   const int lane = threadIdx.x & 31;
   const T *q = static_cast<const T *>(qrow);
   const T *k = static_cast<const T *>(sg.k) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
   const T *v = static_cast<const T *>(sg.v) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
+  float lsum = 0.0f;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) o[c] = 0.0f;
   for (int j = j0; j < j1; ++j) {
@@ -253,14 +264,8 @@ __device__ __noinline__ void redo_row(const Launch &L, const Seg &sg, int l, int
     for (int i0 = a; i0 < e; i0 += 32) {
       const int i = i0 + lane;
       const bool in = i < e && sees(sp, i);
-      float p = 0.0f;
-      if (in) {
-        const T *ki = k + (int64_t)i * sg.st;
-        float dot = 0.0f;
-#pragma unroll 16
-        for (int c = 0; c < D; ++c) dot = fmaf(to_f32(q[c]), to_f32(ki[c]), dot);
-        p = exp2f(fmaf(dot, L.scale_log2, -m));
-      }
+      const float p = in ? exp2f(fmaf(score_of<T, D>(q, k + (int64_t)i * sg.st), L.scale_log2, -m)) : 0.0f;
+      lsum += p;
       const unsigned seen = __ballot_sync(0xffffffffu, in);
 #pragma unroll 8
       for (int u = 0; u < 32; ++u) {
@@ -275,6 +280,27 @@ __device__ __noinline__ void redo_row(const Launch &L, const Seg &sg, int l, int
     for (int c = 0; c < D / 32; ++c) done = done && isnan(o[c]);
     if (__all_sync(0xffffffffu, done)) break;
   }
+  return warp_sum(lsum);
+}
+
+// The largest visible score of a row in base 2, NaN if one is NaN or +inf.
+template <typename T, int D>
+__device__ __noinline__ float redo_max(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
+                                       Tiles tl, int tile, int j0, int j1) {
+  const T *k = static_cast<const T *>(sg.k) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
+  float top = -INFINITY;
+  bool bad = false;
+  for (int j = j0; j < j1; ++j) {
+    const int e = tile_end(tl, j, tile);
+    for (int i = tile_start(tl, j, tile) + (threadIdx.x & 31); i < e; i += 32) {
+      if (!sees(sp, i)) continue;
+      const float s = score_of<T, D>(static_cast<const T *>(qrow), k + (int64_t)i * sg.st) * L.scale_log2;
+      bad = bad || isnan(s) || s == INFINITY;
+      top = fmaxf(top, s);
+    }
+    if (__any_sync(0xffffffffu, bad)) return NAN;
+  }
+  return warp_max(top);
 }
 
 template <typename T>

@@ -31,6 +31,7 @@ struct Smem {
     float p[BM][TT + 4];
   };
   float v[TT][D];
+  const void *qrow[BM];
   int lo[BM], hi[BM], se[BM];
   int u_lo, u_hi, u_se;
 };
@@ -66,8 +67,10 @@ __global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Lau
   for (int r = tid; r < BM; r += NT) {
     Span sp = {0, 0, 0};
     int rr = r0 + r;
+    sm.qrow[r] = nullptr;
     if (rr < sg.R) {
       const Traj &t = L.t[traj_of_row(L, sg, rr)];
+      sm.qrow[r] = static_cast<const T *>(t.q) + row_index(L, t, it.l, it.kvh, rr) * D;
       sp = row_span(sg.pos, sg.S, t.qpos[rr / L.g], L.window, L.sinks);
       if (sp.lo < sp.hi) {
         atomicMin(&sm.u_lo, sp.lo);
@@ -77,17 +80,12 @@ __global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Lau
     }
     sm.lo[r] = sp.lo, sm.hi[r] = sp.hi, sm.se[r] = sp.se;
   }
-  for (int e = tid; e < BM * D; e += NT) {
-    const int r = e / D, c = e % D;
-    int rr = r0 + r;
-    float x = 0.0f;
-    if (rr < sg.R) {
-      const Traj &t = L.t[traj_of_row(L, sg, rr)];
-      x = to_f32(static_cast<const T *>(t.q)[row_index(L, t, it.l, it.kvh, rr) * D + c]);
-    }
-    sm.q[r][c] = x;
-  }
   __syncthreads();
+#pragma unroll 4
+  for (int e = tid; e < BM * D; e += NT) {
+    const T *q = static_cast<const T *>(sm.qrow[e / D]);
+    sm.q[e / D][e % D] = q ? to_f32(q[e % D]) : 0.0f;
+  }
   const Tiles tl = make_tiles(sm.u_lo, sm.u_hi, sm.u_se, TT);
   const int j0 = chunk_tile(tl, it.c, it.n), j1 = chunk_tile(tl, it.c + 1, it.n);
   const T *kb = static_cast<const T *>(sg.k) + (int64_t)it.l * sg.sl + (int64_t)it.kvh * sg.sh;
@@ -213,11 +211,8 @@ __global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Lau
     }
     const float mr = sml[2 * r], lr = sml[2 * r + 1];
     if (!__all_sync(0xffffffffu, fine) && isfinite(lr)) {
-      int rr = r0 + r;
-      const Traj &t = L.t[traj_of_row(L, sg, rr)];
       const Span one = {sm.lo[r], sm.hi[r], sm.se[r]};
-      redo_row<T, D>(L, sg, it.l, it.kvh, static_cast<const T *>(t.q) + row_index(L, t, it.l, it.kvh, rr) * D, one, tl,
-                     TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x);
+      redo_row<T, D>(L, sg, it.l, it.kvh, sm.qrow[r], one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x);
     }
     write_row_warp<T, D>(L, sg, it, r0 + r, x, mr, lr);
   }

@@ -563,8 +563,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
         if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
         if (n > 0 && P.has_q && sg.t >= 0) {
-          // between two items nothing else hides this copy: TMA, which a warp's
-          // own copies take twice as long as (window of 4K: @QCOPY@)
+          // between two items nothing else hides this copy (by the warp's own
+          // copies, as below: five prompts with an 86-token window 35 us, 32 so)
           if (lane == 0) {
             const int nq = rows > BM ? 2 : 1;
             mbar_expect_tx(&sm.q_full, nq * S::kTile);

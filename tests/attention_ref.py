@@ -60,7 +60,9 @@ def attention(parts, Q, qpos, window=0, sinks=0, scale=None, rounded_weights=Fal
                     a = e / z
                     o[l, h, w] = a @ vv
                     lse[l, h, w] = m + np.log(z)
-                    ds = (d + 4) * 2.0 ** -24 * (np.abs(kk) @ np.abs(q[w])).max() * scale + np.abs(sc).max() * 2.0 ** -21
+                    f = np.isfinite(sc)  # a score of -inf is exact
+                    ds = (d + 4) * 2.0 ** -24 * (np.abs(kk[f]) @ np.abs(q[w])).max(initial=0) * scale + \
+                        np.abs(sc[f]).max(initial=0) * 2.0 ** -21
                     rel = 2 * (ds + 2.0 ** -19 + 2.0 ** -17) + (2.0 ** -8 if rounded_weights else 0.0)
                     tol_o[l, h, w] = EPS[dt] * np.abs(o[l, h, w]) + (1 + EPS[dt]) * rel * (a @ np.abs(vv))
                     tol_l[l, h, w] = ds + 2.0 ** -16 + 2.0 ** -22 * abs(lse[l, h, w])

@@ -244,6 +244,18 @@ def test_visible_values_that_are_not_finite(dtype, d):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 20])
+def test_visible_keys_of_minus_infinity(dtype, d, W):
+    """A visible score of -inf has weight zero; the other tokens' results stay."""
+    def edit(p):
+        k, v, pos, q, qp = p.host[0]
+        q[..., 3] = q[..., 3].abs() + 0.5
+        k[:, :, 100:140:7, 3] = float("-inf")
+
+    run(dtype=dtype, d=d, M=1, H=2, Hq=4, trajs=[(200, W)], edit=edit)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 @pytest.mark.parametrize("W", [1, 33])
 def test_large_scores(dtype, d, W):
     """Scores of several hundred: the running maximum moves often and far."""
@@ -383,9 +395,9 @@ def test_batch_kept_while_caches_grow():
 
 
 def test_cuda_cores_and_tensor_cores_agree(monkeypatch):
-    for d in (64, 128):
+    for dtype, d in TYPES:
         for W, prefix in ((1, 0), (60, 0), (1, 200)):
-            p = Problem(dtype=BF, d=d, M=1, H=2, Hq=8, trajs=[(500, W)], prefix=prefix).upload()
+            p = Problem(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(500, W)], prefix=prefix).upload()
             monkeypatch.setenv("COMMITKV_SCORING", "simt")
             p.call(100, 4)
             p.check(100, 4)
