@@ -420,13 +420,16 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   char *base = static_cast<char *>(workspace) + kAlign;
   L.po = reinterpret_cast<float *>(base);
   L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
+  for (int s = 0; s < L.n_seg; ++s) L.order[s] = (uint8_t)s;
+  std::stable_sort(L.order, L.order + L.n_seg, [&](int a, int b) { return L.seg[a].S > L.seg[b].S; });
   cudaError_t e = cudaSuccess;
   bool launched = false;
   for (int p = 0; p < kPaths && e == cudaSuccess; ++p) {
     int32_t items = 0;
-    for (int s = 0; s < L.n_seg; ++s) {
+    for (int k = 0; k < L.n_seg; ++k) {
+      const int s = L.order[k];
       const Seg &sg = L.seg[s];
-      L.item_off[s] = items;
+      L.item_off[k] = items;
       if (path[s] == p) items += L.n_layers * L.H * (sg.nrt - sg.nsplit + sg.nsplit * sg.nchunk);
     }
     L.item_off[L.n_seg] = items;

@@ -51,7 +51,8 @@ struct Traj {
 struct Launch {
   Seg seg[kMaxSeg];
   Traj t[kMaxTraj];
-  int32_t item_off[kMaxSeg + 1];
+  int32_t item_off[kMaxSeg + 1];  // first item of the segment at each place of the order
+  uint8_t order[kMaxSeg];         // segments, the longest first: what starts last ends soon
   int32_t out_off[kMaxTraj + 1];  // rows of a (selected) layer that combine merges, prefix per trajectory
   int32_t n_seg, n_traj, prefix;  // prefix: segment 0 is shared
   int32_t M, H, Hq, g, d, dtype, n_layers;
@@ -111,14 +112,14 @@ struct Item {
 
 __device__ __forceinline__ Item decode_item(const Launch &L, int item) {
   Item it;
-  int a = 0, b = L.n_seg;  // the last segment that starts at or before the item
+  int a = 0, b = L.n_seg;  // the last place that starts at or before the item
   while (b - a > 1) {
     const int m = (a + b) >> 1;
     if (item >= L.item_off[m]) a = m;
     else b = m;
   }
-  it.s = a;
-  const Seg &sg = L.seg[a];
+  it.s = L.order[a];
+  const Seg &sg = L.seg[it.s];
   // the later rows of a prompt see more: they come first
   int x = item - L.item_off[a], rt = sg.nrt - 1;
   const int slices = L.H * L.n_layers, whole = slices * (sg.nrt - sg.nsplit);

@@ -804,9 +804,11 @@ cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early
   static thread_local TcParams P;
   P.L = L;
   P.has_q = L.n_traj <= kMaxQ && L.g <= BM && BM % L.g == 0;
+  bool used[kMaxSeg] = {};
+  for (int k = 0; k < L.n_seg; ++k) used[L.order[k]] = L.item_off[k] < L.item_off[k + 1];
   for (int i = 0; i < L.n_seg; ++i) {
     const Seg &sg = L.seg[i];
-    if (L.item_off[i] == L.item_off[i + 1]) continue;
+    if (!used[i]) continue;
     if (P.has_q && sg.t >= 0 && !map_q(&P.q[sg.t], L, L.t[sg.t])) return cudaErrorInvalidValue;
     if (sg.S == 0) continue;
     if (!map_kv(&P.k[i], sg.k, L, sg) || !map_kv(&P.v[i], sg.v, L, sg)) return cudaErrorInvalidValue;
