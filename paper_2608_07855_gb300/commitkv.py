@@ -416,11 +416,9 @@ def commitkv_compact_noalloc(shape: Shape, cache, retired, pending, pending_prio
 class AttentionBatch:
     """The arguments of an attention call, checked and marshalled once: the
     trajectories, their outputs and a shared prefix, for callers that issue
-    many calls on the same buffers.  Caches that grow in place are followed
-    with set_length (the tensors passed in must then be views of buffers that
-    hold the new tokens, and the workspace large enough for them; a
-    workspace does not depend on cache lengths).  The batch keeps the tensors
-    alive."""
+    many calls on the same buffers.  Caches that grow in place are passed as
+    the whole buffers, and set_length says how many tokens they hold (the
+    workspace does not depend on it).  The batch keeps the tensors alive."""
 
     def __init__(self, shape: Shape, trajs: Sequence[TrajTensors], out, lse_out=None, prefix: TrajTensors = None):
         torch = _torch()
@@ -462,9 +460,9 @@ class AttentionBatch:
         self._prefix = None if prefix is None else ctypes.byref(self.prefix)
 
     def set_length(self, i: int, S: int):
-        """Trajectory i's cache now has S tokens."""
-        if S < 0:
-            raise ValueError("S >= 0")
+        """Trajectory i's cache has S tokens, the first ones of its tensors."""
+        if not 0 <= S <= self.trajs[i].k.shape[2]:
+            raise ValueError(f"0 <= S <= {self.trajs[i].k.shape[2]}, the tokens of the tensors")
         self.descs[i].S = S
 
 

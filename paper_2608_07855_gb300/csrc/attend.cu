@@ -421,7 +421,8 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   L.po = reinterpret_cast<float *>(base);
   L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
   for (int s = 0; s < L.n_seg; ++s) L.order[s] = (uint8_t)s;
-  std::stable_sort(L.order, L.order + L.n_seg, [&](int a, int b) { return L.seg[a].S > L.seg[b].S; });
+  std::sort(L.order, L.order + L.n_seg,
+            [&](int a, int b) { return L.seg[a].S != L.seg[b].S ? L.seg[a].S > L.seg[b].S : a < b; });
   cudaError_t e = cudaSuccess;
   bool launched = false;
   for (int p = 0; p < kPaths && e == cudaSuccess; ++p) {

@@ -384,6 +384,9 @@ def test_batch_kept_while_caches_grow():
     p = Problem(dtype=BF, d=d, M=1, H=2, Hq=8, trajs=[(cap, 1), (cap, 1)], gaps=0.5).upload()
     b = ck.attention_batch(p.shape, p.trajs, p.out, p.lse)
     full = [list(h) for h in p.host]
+    for bad in (-1, cap + 1):
+        with pytest.raises(ValueError):
+            b.set_length(0, bad)
     for S in ((1, 3), (128, 200), (129, 640), (700, 699)):
         for i, n in enumerate(S):
             b.set_length(i, n)
@@ -496,3 +499,46 @@ def test_session_attends_before_and_after_a_checkpoint():
     for W in (1, 40):
         look(W)
         look(W, 150, 4, True)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prefix_beside_decoded_caches(d):
+    """Many agents behind a long prefix: its kernel and that of their own
+    caches overlap, eager and in a graph, and the merge waits for both."""
+    n, H, Hq, pre = 64, 8, 32, 7000
+    p = Problem(dtype=BF, d=d, M=1, H=H, Hq=Hq, prefix=pre, trajs=[(40 + 31 * i, 1) for i in range(n)]).upload()
+    K, V, pos = p.prefix.k[0].double(), p.prefix.v[0].double(), p.prefix.pos
+
+    def check():
+        torch.cuda.synchronize()
+        assert ck.commitkv_workspace_status(p.ws) == ck.COMMITKV_OK
+        for i, t in enumerate(p.trajs):
+            k, v = torch.cat([K, t.k[0].double()], 1), torch.cat([V, t.v[0].double()], 1)
+            q = t.q[0, :, 0].double().view(H, Hq // H, d)
+            s = (q @ k.transpose(1, 2)) * d ** -0.5
+            a = torch.softmax(s, -1)
+            want, spread = a @ v, a @ v.abs()
+            # half a step of the output and of every weight, and fp32 sums (attention_ref.attention)
+            tol = 2.0 ** -8 * want.abs() + 2.0 ** -8 * spread + 2.0 ** -14 * spread
+            assert ((p.out[i][0, :, 0].double().view(want.shape) - want).abs() <= tol).all(), i
+            assert ((p.lse[i][0, :, 0].double().view(H, -1) - torch.logsumexp(s, -1)).abs() <= 2.0 ** -14).all(), i
+        p.guards()
+
+    for _ in range(3):
+        p.flat.fill_(SENT)
+        p.flat_l.fill_(SENT)
+        p.call()
+        check()
+    first = p.flat.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        p.call()
+        p.call()
+    for _ in range(3):
+        p.flat.fill_(SENT)
+        p.ws[256:].fill_(0xFF)
+        g.replay()
+        check()
+        assert torch.equal(first, p.flat)
