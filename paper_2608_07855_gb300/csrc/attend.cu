@@ -293,7 +293,7 @@ bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
     if (path[s] == kRows) start = 0.0;  // launched anyway
     if (path[s] != kTc) continue;
     const int64_t seen = std::min<int64_t>(sg.S, most_seen(L, sg, 256));
-    few += 1.25 * slices * cdiv(sg.R, 16) * (cdiv(seen, 64) + 1) / (2.0 * sms);
+    few += 1.25 * slices * cdiv(sg.R, 16) * (cdiv(seen, rows_tile(L)) + 1) / (2.0 * sms);
     tiles += (double)slices * cdiv(sg.R, 256) * cdiv(seen, 128);
     bytes += (double)slices * seen * L.d * 4;
   }

@@ -100,7 +100,7 @@ cudaError_t launch_after(void (*kernel)(A...), unsigned blocks, unsigned threads
 cudaError_t launch_simt(const Launch &L, cudaStream_t s, bool early);
 // 16 rows per item, caches and queries 16-byte aligned; tiles of rows_tile tokens.
 cudaError_t launch_rows(const Launch &L, cudaStream_t s, bool early);
-inline int rows_tile(const Launch &L) { return L.dtype != COMMITKV_BF16 && L.d == 128 ? 32 : 64; }
+inline int rows_tile(const Launch &L) { return 16384 / (L.d * (L.dtype == COMMITKV_BF16 ? 2 : 4)); }
 // Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
 cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);

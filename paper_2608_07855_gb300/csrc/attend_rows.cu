@@ -36,7 +36,7 @@ constexpr float kLazy = 8.0f;
 template <typename T, int D>
 struct Smem {
   static constexpr int kRow = D * (int)sizeof(T);
-  static constexpr int WT = kRow == 512 ? 8 : 16;  // tokens of a warp
+  static constexpr int WT = 4096 / kRow;  // tokens of a warp: 4 KB of K and of V
   static constexpr int TT = NW * WT;               // of a tile
   union {
     alignas(128) uint8_t ring[NW][NST][2][WT * kRow];
@@ -224,15 +224,17 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
           for (int i = 0; i < 4; ++i) s[t][i] += d[t][i];
       }
     } else {
-      // K rows lane % 8 (+ 8: the second eight tokens), 16-byte pieces 2 k and 2 k + 1
+      // of 16 tokens K rows lane % 8 (+ 8: the second eight), 16-byte pieces 2 k and 2 k + 1
       const int kr = lane % 8 + (lane / 16) * 8, kc = (lane / 8) % 2;
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        uint32_t b[4];
-        ldsm4(b, ks + kr * S::kRow + (((2 * k + kc) ^ (kr & 7)) << 4));
-        mma16816(s[0], q[k], b[0], b[1]);
-        mma16816(s[NT - 1], q[k], b[2], b[3]);
-      }
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int u = 0; u < NT / 2; ++u) {
+          uint32_t b[4];
+          ldsm4(b, ks + (16 * u + kr) * S::kRow + (((2 * k + kc) ^ (kr & 7)) << 4));
+          mma16816(s[2 * u], q[k], b[0], b[1]);
+          mma16816(s[2 * u + 1], q[k], b[2], b[3]);
+        }
     }
     const int a = tile_start(tl, j, TT) + WT * warp, e = tile_end(tl, j, TT);
 #pragma unroll
@@ -296,21 +298,24 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
       }
     } else {
       // V: tokens as the k dimension, two groups of eight channels at a time
-      uint32_t hi4[4], lo4[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        split2(s[0][2 * h], s[0][2 * h + 1], hi4[h], lo4[h]);
-        split2(s[NT - 1][2 * h], s[NT - 1][2 * h + 1], hi4[2 + h], lo4[2 + h]);
-      }
       const int vr = lane % 16, vc = lane / 16;
 #pragma unroll
-      for (int n = 0; n < D / 16; ++n) {
-        uint32_t b[4];
-        ldsm4t(b, vs + vr * S::kRow + (((2 * n + vc) ^ (vr & 7)) << 4));
-        mma16816(o[2 * n], hi4, b[0], b[1]);
-        mma16816(o[2 * n + 1], hi4, b[2], b[3]);
-        mma16816(o[2 * n], lo4, b[0], b[1]);
-        mma16816(o[2 * n + 1], lo4, b[2], b[3]);
+      for (int u = 0; u < NT / 2; ++u) {
+        uint32_t hi4[4], lo4[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          split2(s[2 * u][2 * h], s[2 * u][2 * h + 1], hi4[h], lo4[h]);
+          split2(s[2 * u + 1][2 * h], s[2 * u + 1][2 * h + 1], hi4[2 + h], lo4[2 + h]);
+        }
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) {
+          uint32_t b[4];
+          ldsm4t(b, vs + (16 * u + vr) * S::kRow + (((2 * n + vc) ^ (vr & 7)) << 4));
+          mma16816(o[2 * n], hi4, b[0], b[1]);
+          mma16816(o[2 * n + 1], hi4, b[2], b[3]);
+          mma16816(o[2 * n], lo4, b[0], b[1]);
+          mma16816(o[2 * n + 1], lo4, b[2], b[3]);
+        }
       }
     }
   }
