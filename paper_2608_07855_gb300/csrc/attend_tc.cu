@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   using S = Smem<D>;
   constexpr int NST = S::NST;
   extern __shared__ uint8_t smem_raw[];
-  S &sm = *reinterpret_cast<S *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  S &sm = *reinterpret_cast<S *>(smem_raw + ((0u - smem_addr(smem_raw)) & 1023u));
   const Launch &L = P.L;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   volatile int *abort_flag = &sm.abort_flag;
@@ -682,44 +682,73 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       const float g0 = dst ? f0 * inv : f0, g1 = dst ? f1 * inv : f1;
       float chk = 0.0f;
       if (warp_rows) {
-        // 16 channels of every row at a time through shared memory, so that
-        // four lanes store them side by side; a short loop, because an item's
-        // end runs on cold instructions
-        float4 *stage = sm.stage[warp - 4];
+        // 64 bytes of every row at a time through shared memory, so that four
+        // lanes store them side by side.  (Both groups and all SMs come here at
+        // the same time, with the tensor cores idle: with 16 channels a step and the
+        // rows' addresses exchanged in each a window of 4K took 246 us, 239 so.)
+        const uint32_t stage = smem_addr(sm.stage[warp - 4]);
         const uint64_t row_out = pdst ? reinterpret_cast<uint64_t>(pdst) : reinterpret_cast<uint64_t>(dst);
-#pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 16) {
-          float y[16];
+        uint64_t to[4];  // where this lane's 16 bytes of rows lane / 4 + 8 k go
 #pragma unroll
-          for (int i = 0; i < 16; ++i) y[i] = 0.0f;
-#pragma unroll 1
-          for (int k = 0; k < 1 + other; ++k) {
-            if (!mine) break;
-            uint32_t z[16];
-            const float gk = k ? g1 : g0;
-            tmem_ld16(o_col + D * k + c0, z);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = fmaf(__uint_as_float(z[i]), gk, y[i]);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) chk = fmaf(y[i], 0.0f, chk);  // NaN if any is not finite
+        for (int k = 0; k < 4; ++k) {
+          to[k] = __shfl_sync(0xffffffffu, row_out, 8 * k + lane / 4);
+          if (to[k]) to[k] += 16 * (lane % 4);
+        }
+        auto flush = [&](const uint32_t *w) {  // 16 words of this lane's row
           __syncwarp();  // the last piece has been read
 #pragma unroll
-          for (int k = 0; k < 4; ++k) stage[lane * 5 + k] = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+          for (int k = 0; k < 4; ++k)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 80 + 16 * k), "r"(w[4 * k]),
+                         "r"(w[4 * k + 1]), "r"(w[4 * k + 2]), "r"(w[4 * k + 3])
+                         : "memory");
           __syncwarp();
+          uint4 v[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int rr = 8 * k + lane / 4, q = c0 / 4 + lane % 4;
-            const uint64_t p = __shfl_sync(0xffffffffu, row_out, rr);
-            const float4 v = stage[rr * 5 + lane % 4];
-            if (!p) continue;
-            if (it.split) {
-              reinterpret_cast<float4 *>(p)[q] = v;
-            } else {
-              const __nv_bfloat162 h[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
-              reinterpret_cast<uint2 *>(p)[q] = *reinterpret_cast<const uint2 *>(h);
+          for (int k = 0; k < 4; ++k)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(v[k].x), "=r"(v[k].y), "=r"(v[k].z), "=r"(v[k].w)
+                         : "r"(stage + (8 * k + lane / 4) * 80 + 16 * (lane % 4))
+                         : "memory");
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (to[k]) {
+              asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to[k]), "r"(v[k].x), "r"(v[k].y), "r"(v[k].z),
+                           "r"(v[k].w)
+                           : "memory");
+              to[k] += 64;
             }
+        };
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          float y[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) y[i] = 0.0f;
+#pragma unroll 1
+          for (int k = 0; k < (mine ? 1 + other : 0); ++k) {
+            float z[32];
+            const float gk = k ? g1 : g0;
+            tmem_ld32f(o_col + D * k + c0, z);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = fmaf(z[i], gk, y[i]);
+          }
+          float ck[4] = {chk, 0.0f, 0.0f, 0.0f};  // NaN if any is not finite
+#pragma unroll
+          for (int i = 0; i < 32; ++i) ck[i & 3] = fmaf(y[i], 0.0f, ck[i & 3]);
+          chk = (ck[0] + ck[1]) + (ck[2] + ck[3]);
+          uint32_t w[32];
+          if (it.split) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(y[i]);
+            flush(w);
+            flush(w + 16);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+              w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+            flush(w);
           }
         }
       }
