@@ -247,28 +247,32 @@ Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most
   return best;
 }
 
-enum { kSimt16, kSimt64, kTc, kRows, kPaths };
+enum { kSimt16, kSimt64, kTc, kTcF32, kRows, kPaths };
 constexpr PathInfo kPath[kPaths] = {
-    {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {16, 64, 2, 2.0, 1.4}};
+    {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {128, 64, 1, 3.0, 3.3}, {16, 64, 2, 2.0, 1.4}};
 
-bool force_cuda_cores() {
-  const char *e = getenv("COMMITKV_SCORING");
-  return e && (e[0] == 's' || e[0] == 'S');
+// For tests and diagnosis: COMMITKV_SCORING=simt takes the CUDA cores where a
+// call could have the tensor cores, COMMITKV_ATTENTION=tiles the kernels of row
+// tiles however few rows there are.
+bool env_starts(const char *name, char c) {
+  const char *e = getenv(name);
+  return e && e[0] == c;
 }
 
 // Tensor cores where 16-byte copies can read the cache and the rows' queries
-// and outputs: fp32 and up to 16 rows the kernel of 16-row items, other bf16
-// rows the one of 256 (but see few_rows), whose TMA also wants distinct heads
-// and layers.
+// and outputs: up to 16 rows the kernel of 16-row items, others those of row
+// tiles (but see few_rows); TMA, which bf16 tiles take, also wants distinct
+// heads and layers.
 int path_of(const Launch &L, const Seg &sg) {
   const int cuda_cores = sg.R <= 16 ? kSimt16 : kSimt64;
-  if (force_cuda_cores()) return cuda_cores;
+  if (env_starts("COMMITKV_SCORING", 's')) return cuda_cores;
   const int eb = L.dtype == COMMITKV_BF16 ? 2 : 4;
   uintptr_t bits = (uintptr_t)sg.k | (uintptr_t)sg.v | (uintptr_t)((sg.sl | sg.sh | sg.st) * eb);
   for (int t = sg.t < 0 ? 0 : sg.t; t < (sg.t < 0 ? L.n_traj : sg.t + 1); ++t)
     bits |= L.t[t].W ? (uintptr_t)L.t[t].q | (uintptr_t)L.t[t].out : 0;
   if (bits % 16) return cuda_cores;
-  if (eb == 4 || sg.R <= 16) return kRows;
+  if (sg.R <= 16 && !env_starts("COMMITKV_ATTENTION", 't')) return kRows;
+  if (eb == 4) return kTcF32;
   if (sg.S > 0 && (sg.sh == 0 || sg.sl == 0 || std::max(sg.sl, std::max(sg.sh, sg.st)) >= (1ll << 39))) return kRows;
   return kTc;
 }
@@ -279,25 +283,42 @@ int64_t most_seen(const Launch &L, const Seg &sg, int rows) {
   return L.window ? (int64_t)L.window + L.sinks + std::min(rows, sg.R) / L.g : sg.S;
 }
 
-// Whether the bf16 segments of more than 16 rows go to the kernel of 16-row
-// items as well: it reads K and V again for every 16 rows, but has half the
-// other's start and end.  Estimates in us; measured there and here, 32 query
-// on 8 KV heads of 128 channels: 8 queries over 1,000 tokens 17.4 and 11.4, over
+// What of a path's costs goes by the type.
+PathInfo path_info(const Launch &L, int p) {
+  PathInfo pi = kPath[p];
+  if (p == kRows) {
+    pi.tile = rows_tile(L);
+    if (L.dtype == COMMITKV_F32) pi.tile_us = 2.3;
+  }
+  if (p == kTcF32 && L.d == 64) pi.tile_us = 1.8;
+  return pi;
+}
+
+// Whether the segments of more than 16 rows go to the kernel of 16-row items as
+// well: it reads K and V again for every 16 rows, but has half the others'
+// start and end.  Estimates in us; measured there and here, bf16, 32 query on 8
+// KV heads of 128 channels: 8 queries over 1,000 tokens 17.4 and 11.4, over
 // 16,000 26.0 and 23.4, 16 over 4,000 18.5 and 17.1, 100 over 500 21.2 and
 // 15.3, 8 agents behind 16,000 31.8 and 27.2; 5 over 16 caches to 16,000 127
-// and 161, 12 over 16 to 1,000 23 and 31, 32 over 32,768 44 and 120.
+// and 161, 12 over 16 to 1,000 23 and 31, 32 over 32,768 44 and 120.  fp32, 16
+// on 4: 16 over 6,000 27 and 31, 32 over 2,000 24 and 25, 64 over 3,000 27 and
+// 56, 8 over 8 caches to 4,000 48 and 46, 16 agents behind 4,000 43 and 36; 4 on
+// 2: 40 over 1,000 19 and 15.
 bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
-  double few = 0.0, many = 15.0, tiles = 0.0, bytes = 0.0, start = 7.0;
+  const bool bf16 = L.dtype == COMMITKV_BF16;
+  const PathInfo few_pi = path_info(L, kRows), many_pi = path_info(L, bf16 ? kTc : kTcF32);
+  const double few_us = bf16 ? 1.25 : 2.3;
+  double few = 0.0, many = bf16 ? 15.0 : 18.0, tiles = 0.0, bytes = 0.0, start = bf16 ? 7.0 : 9.0;
   for (int s = 0; s < L.n_seg; ++s) {
     const Seg &sg = L.seg[s];
     if (path[s] == kRows) start = 0.0;  // launched anyway
-    if (path[s] != kTc) continue;
-    const int64_t seen = std::min<int64_t>(sg.S, most_seen(L, sg, 256));
-    few += 1.25 * slices * cdiv(sg.R, 16) * (cdiv(seen, rows_tile(L)) + 1) / (2.0 * sms);
-    tiles += (double)slices * cdiv(sg.R, 256) * cdiv(seen, 128);
-    bytes += (double)slices * seen * L.d * 4;
+    if (path[s] != kTc && path[s] != kTcF32) continue;
+    const int64_t seen = std::min<int64_t>(sg.S, most_seen(L, sg, many_pi.rows));
+    few += few_us * slices * cdiv(sg.R, 16) * (cdiv(seen, few_pi.tile) + 1) / (2.0 * sms);
+    tiles += (double)slices * cdiv(sg.R, many_pi.rows) * (cdiv(seen, many_pi.tile) + (bf16 ? 0 : 3));
+    bytes += (double)slices * seen * L.d * (bf16 ? 4 : 8);
   }
-  return start + few < many + std::max(bytes / kBytesPerUs, kPath[kTc].tile_us * tiles / sms);
+  return start + few < many + std::max(bytes / kBytesPerUs, many_pi.tile_us * tiles / sms);
 }
 
 commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
@@ -362,8 +383,8 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   bool merge = false;
   const int64_t slices = (int64_t)L.n_layers * L.H;
   for (int s = 0; s < L.n_seg; ++s) path[s] = path_of(L, L.seg[s]);
-  if (few_rows(L, path, slices, sms))
-    for (int s = 0; s < L.n_seg; ++s) path[s] = path[s] == kTc ? kRows : path[s];
+  if (!env_starts("COMMITKV_ATTENTION", 't') && few_rows(L, path, slices, sms))
+    for (int s = 0; s < L.n_seg; ++s) path[s] = path[s] == kTc || path[s] == kTcF32 ? kRows : path[s];
   double rows_us = 0.0;  // time of the decode kernel, which reads its caches at the memory's rate
   for (int s = 0; s < L.n_seg; ++s) {
     const Seg &sg = L.seg[s];
@@ -372,8 +393,7 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
                  (L.dtype == COMMITKV_BF16 ? 4 : 8) / kBytesPerUs;
   }
   for (int p = 0; p < kPaths; ++p) {
-    PathInfo pi = kPath[p];
-    if (p == kRows) pi.tile = rows_tile(L);
+    const PathInfo pi = path_info(L, p);
     Divide v;
     int ids[kMaxSeg];
     v.n = 0;
@@ -392,7 +412,7 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     // time: as few blocks as finish with them, the others' SMs read the caches
     // (64 agents behind a 16K prefix, 2,048 tokens each at most: 99 us with the
     // prefix on all SMs first, 78 so).
-    if (p == kTc && v.n == 1 && rows_us > 0.0)
+    if ((p == kTc || p == kTcF32) && v.n == 1 && rows_us > 0.0)
       slots = std::min(slots, std::max<int64_t>(
                                   1, (int64_t)(v.base[0] * v.tiles[0] / std::max(1.0, rows_us / pi.tile_us - 2 * pi.fixed))));
     const Division dv =
@@ -436,7 +456,11 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     L.item_off[L.n_seg] = items;
     if (items == 0) continue;
     L.rows_per_item = kPath[p].rows;
-    e = p == kRows ? launch_rows(L, stream, launched) : p == kTc ? launch_tc(L, static_cast<WsHeader *>(workspace), stream, launched) : launch_simt(L, stream, launched);
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    e = p == kRows    ? launch_rows(L, stream, launched)
+        : p == kTc    ? launch_tc(L, hdr, stream, launched)
+        : p == kTcF32 ? launch_tc_f32(L, hdr, stream, launched)
+                      : launch_simt(L, stream, launched);
     launched = true;
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);

@@ -103,6 +103,8 @@ cudaError_t launch_rows(const Launch &L, cudaStream_t s, bool early);
 inline int rows_tile(const Launch &L) { return 16384 / (L.d * (L.dtype == COMMITKV_BF16 ? 2 : 4)); }
 // Tensor cores: bf16, caches and queries 16-byte aligned.  256 rows per item.
 cudaError_t launch_tc(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early);
+// Tensor cores: fp32, caches, queries and outputs 16-byte aligned.  128 rows per item.
+cudaError_t launch_tc_f32(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early);
 cudaError_t launch_combine(const Launch &L, cudaStream_t s);
 
 struct Item {

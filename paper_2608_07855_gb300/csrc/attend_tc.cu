@@ -21,29 +21,13 @@
 #include <cudaTypedefs.h>
 #include <string.h>
 
-#include "attend.cuh"
-#include "sm103.cuh"
+#include "attend_tc.cuh"
 
 namespace ckv {
 namespace at {
 namespace {
 
-using namespace ckv::sm103;
-
-constexpr int BM = 128;  // rows of a tile
 constexpr int BT = 128;  // tokens of a tile
-// Long enough for the rows that redo_row takes (32 rows of a million tokens: under a second).
-constexpr uint64_t kWait = 4000000000ull;
-constexpr float kLazy = 8.0f;
-
-// mbar_wait that parks the thread before it first reads the clock.
-__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i)
-    if (mbar_try_wait_sleep(bar, parity, 20000)) return true;
-  return mbar_wait(bar, parity, kWait, abort_flag);
-}
-
 constexpr int kMaxQ = 32;  // trajectories whose Q tiles TMA copies: what the launch parameters have room for
 
 struct TcParams {
@@ -55,13 +39,6 @@ struct TcParams {
 
 static_assert(sizeof(TcParams) <= 32764, "kernel parameters");
 
-struct Plan {
-  Tiles tl;
-  int j0, j1;
-  int rows;  // of the item; 0: no more items
-  Item it;
-};
-
 template <int D>
 struct Smem {
   static constexpr int kTile = BT * D * 2;
@@ -70,7 +47,7 @@ struct Smem {
   alignas(1024) uint8_t kv[NST][kTile];
   Span span[2][2 * BM];
   Plan plan[2];
-  float4 stage[8][32 * 5];  // results of a softmax warp on their way out: 64 bytes of each row, 16 apart
+  float4 stage[8][RowsOut::kStage];
   int3 first[8];  // what the rows of a softmax warp see of the first item
   float2 pub[BM];  // one row tile: group 1's (m, l)
   alignas(16) uint4 next;  // answer to the request for another item
@@ -107,79 +84,9 @@ __device__ __forceinline__ uint64_t desc_v(const uint8_t *tile, int ks) {
   return smem_desc(smem_addr(tile) + ks * 2048, kHalf, 1024, kSwizzle128B);
 }
 
-// One block is launched per item, and one that is done with its own takes the
-// next block's that has not started (PTX clusterlaunchcontrol), so items are
-// handed out as SMs get free while a block keeps its tensor memory, its
-// barriers and the pipeline across items.
-__device__ __forceinline__ void ask_next(uint4 *answer, uint64_t *bar) {
-  fence_proxy_async();  // the last answer has been read
-  mbar_expect_tx(bar, 16);
-  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
-                   smem_addr(answer)),
-               "r"(smem_addr(bar))
-               : "memory");
-}
-__device__ __forceinline__ int read_next(const uint4 *answer) {
-  int x;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t"
-      "ld.shared.b128 a, [%1];\n\t"
-      "mov.s32 %0, -1;\n\t"
-      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
-      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
-      : "=r"(x)
-      : "r"(smem_addr(answer))
-      : "memory");
-  return x;
-}
-
 // Columns of tile j that are worked on: a multiple of 32.
 __device__ __forceinline__ int tile_cols(const Tiles &t, int j) {
   return (tile_end(t, j, BT) - tile_start(t, j, BT) + 31) & ~31;
-}
-
-// One lane of a converged warp, always the same.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t e;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(e));
-  return e != 0;
-}
-
-__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
-  return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
-}
-
-// Row r of an item: its query, and what it sees.  Behind the last row: zeros
-// as queries, nothing to mask.
-__device__ __forceinline__ const __nv_bfloat16 *row_query(const Launch &L, const Seg &sg, const Item &it, int r, int d,
-                                                          const int32_t *&qpos) {
-  if (r >= sg.R) return nullptr;
-  const Traj &t = L.t[traj_of_row(L, sg, r)];
-  qpos = t.qpos + r / L.g;
-  return static_cast<const __nv_bfloat16 *>(t.q) + row_index(L, t, it.l, it.kvh, r) * d;
-}
-__device__ __forceinline__ Span row_sees(const Launch &L, const Seg &sg, const int32_t *qpos, int3 &u) {
-  Span sp = {0, 0x7fffffff, 0};
-  if (qpos) {
-    sp = row_span(sg.pos, sg.S, *qpos, L.window, L.sinks);
-    if (sp.lo < sp.hi) u.x = min(u.x, sp.lo), u.y = max(u.y, sp.hi);
-    u.z = max(u.z, sp.se);
-  }
-  return sp;
-}
-// The union of what the rows of a warp see: (least lo, largest hi, largest se).
-__device__ __forceinline__ int3 join_warp(int3 u) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    u.x = min(u.x, __shfl_xor_sync(0xffffffffu, u.x, o));
-    u.y = max(u.y, __shfl_xor_sync(0xffffffffu, u.y, o));
-    u.z = max(u.z, __shfl_xor_sync(0xffffffffu, u.z, o));
-  }
-  return u;
 }
 
 // A warp copies 32 rows (lane r has row r's address; none: zeros) into rows
@@ -352,7 +259,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     const int i = threadIdx.x - 128, r = it.rt * L.rows_per_item + i;
     int3 u = make_int3(0x7fffffff, 0, 0);
     const int32_t *qpos = nullptr;
-    copy_q<D>(sm.q[i / BM], (i % BM) & ~31, i < L.rows_per_item ? row_query(L, sg, it, r, D, qpos) : nullptr, lane);
+    copy_q<D>(sm.q[i / BM], (i % BM) & ~31, i < L.rows_per_item ? row_query<__nv_bfloat16>(L, sg, it, r, D, qpos) : nullptr, lane);
     sm.span[0][i] = row_sees(L, sg, qpos, u);
     u = join_warp(u);
     if (lane == 0) sm.first[warp - 4] = u;
@@ -550,7 +457,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
 #pragma unroll 1
           for (int i = lane; i < 2 * BM; i += 32) {
             const int32_t *qpos = nullptr;
-            if (i < rows) row_query(L, sg, it, r0 + i, D, qpos);
+            if (i < rows) row_query<__nv_bfloat16>(L, sg, it, r0 + i, D, qpos);
             sm.span[buf][i] = row_sees(L, sg, qpos, u);
           }
         }
@@ -580,7 +487,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
 #pragma unroll 1
           for (int i = 0; i < rows; i += 32) {
             const int32_t *qpos;
-            copy_q<D>(sm.q[i / BM], i % BM, i + lane < rows ? row_query(L, sg, it, r0 + i + lane, D, qpos) : nullptr, lane);
+            copy_q<D>(sm.q[i / BM], i % BM, i + lane < rows ? row_query<__nv_bfloat16>(L, sg, it, r0 + i + lane, D, qpos) : nullptr, lane);
           }
           copy_q_done();
           __syncwarp();
@@ -686,38 +593,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         // lanes store them side by side.  (Both groups and all SMs come here at
         // the same time, with the tensor cores idle: with 16 channels a step and the
         // rows' addresses exchanged in each a window of 4K took 246 us, 239 so.)
-        const uint32_t stage = smem_addr(sm.stage[warp - 4]);
-        const uint64_t row_out = pdst ? reinterpret_cast<uint64_t>(pdst) : reinterpret_cast<uint64_t>(dst);
-        uint64_t to[4];  // where this lane's 16 bytes of rows lane / 4 + 8 k go
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          to[k] = __shfl_sync(0xffffffffu, row_out, 8 * k + lane / 4);
-          if (to[k]) to[k] += 16 * (lane % 4);
-        }
-        auto flush = [&](const uint32_t *w) {  // 16 words of this lane's row
-          __syncwarp();  // the last piece has been read
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 80 + 16 * k), "r"(w[4 * k]),
-                         "r"(w[4 * k + 1]), "r"(w[4 * k + 2]), "r"(w[4 * k + 3])
-                         : "memory");
-          __syncwarp();
-          uint4 v[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(v[k].x), "=r"(v[k].y), "=r"(v[k].z), "=r"(v[k].w)
-                         : "r"(stage + (8 * k + lane / 4) * 80 + 16 * (lane % 4))
-                         : "memory");
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (to[k]) {
-              asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to[k]), "r"(v[k].x), "r"(v[k].y), "r"(v[k].z),
-                           "r"(v[k].w)
-                           : "memory");
-              to[k] += 64;
-            }
-        };
+        RowsOut rows_out(smem_addr(sm.stage[warp - 4]),
+                         pdst ? reinterpret_cast<uint64_t>(pdst) : reinterpret_cast<uint64_t>(dst), lane);
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += 32) {
           float y[32];
@@ -740,15 +617,15 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           if (it.split) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(y[i]);
-            flush(w);
-            flush(w + 16);
+            rows_out.put(w);
+            rows_out.put(w + 16);
           } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
               w[i] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            flush(w);
+            rows_out.put(w);
           }
         }
       }
@@ -767,7 +644,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
                           __shfl_sync(0xffffffffu, sp.se, b)};
         const float mb = __shfl_sync(0xffffffffu, m, b), lb = __shfl_sync(0xffffffffu, lsum, b);
         const int32_t *qpos;
-        const void *qb = row_query(L, sg, it, r - lane + b, D, qpos);
+        const void *qb = row_query<__nv_bfloat16>(L, sg, it, r - lane + b, D, qpos);
         float o[D / 32];
         redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1, mb == -INFINITY ? 0.0f : mb,
                                    o);

@@ -18,6 +18,17 @@ BF, F32 = torch.bfloat16, torch.float32
 SENT = 12352.0  # representable in bf16
 
 
+@pytest.fixture(autouse=True, params=["", "tiles", "cuda_cores"])
+def kernels(request, monkeypatch):
+    """Every test on the kernels that the library picks, on those of row tiles
+    (which small calls would not reach), and on the CUDA cores."""
+    if request.param == "tiles":
+        monkeypatch.setenv("COMMITKV_ATTENTION", "tiles")
+    elif request.param:
+        monkeypatch.setenv("COMMITKV_SCORING", "simt")
+    return request.param
+
+
 class Problem:
     """Trajectories (S, W) with their data on the host, and the call on the device."""
 
@@ -397,18 +408,6 @@ def test_batch_kept_while_caches_grow():
         p.check(300, 2)
 
 
-def test_cuda_cores_and_tensor_cores_agree(monkeypatch):
-    for dtype, d in TYPES:
-        for W, prefix in ((1, 0), (60, 0), (1, 200)):
-            p = Problem(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(500, W)], prefix=prefix).upload()
-            monkeypatch.setenv("COMMITKV_SCORING", "simt")
-            p.call(100, 4)
-            p.check(100, 4)
-            monkeypatch.delenv("COMMITKV_SCORING")
-            p.call(100, 4)
-            p.check(100, 4)
-
-
 def test_effects_from_attention():
     """The attention of the probe window is a valid source of row statistics:
     fp32 effects from (lse, 1, out) as from the library's own statistics."""
@@ -445,9 +444,9 @@ def test_many_items(d, prefix):
 
 
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64)], ids=["bf16-128", "bf16-64", "f32-64"])
-def test_long_prompt_is_cut_at_its_end(dtype, d):
+def test_long_prompt_is_cut_at_its_end(dtype, d, kernels):
     """Whole waves of row tiles and a cut remainder: written and merged rows side by side."""
-    W = 2600 if dtype == BF else 700
+    W = 2600 if dtype == BF and kernels != "cuda_cores" else 700
     p = Problem(dtype=dtype, d=d, M=4, H=4, Hq=16, trajs=[(W + 300, W)]).upload()
     p.call()
     torch.cuda.synchronize()
