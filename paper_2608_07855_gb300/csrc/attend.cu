@@ -16,9 +16,10 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Items that share rows with others (split tokens), at most: bounds the
-// partial results.  Small row tiles are cheap to merge and come from calls
-// whose time is the reading of the cache, which wants many blocks.
+// Items that share rows with others (split tokens), at most, of all kernels of
+// a call that take up to 16 rows and of all others: bounds the partial
+// results.  Small row tiles are cheap to merge and come from calls whose time
+// is the reading of the cache, which wants many blocks.
 constexpr int64_t kMaxSplitSmall = 2048;  // up to 16 rows an item
 constexpr int64_t kMaxSplit = 768;
 
@@ -169,7 +170,7 @@ int64_t partial_rows(const commitkv_shape *s, int n, const commitkv_traj *tr, co
     most = std::max(most, rows_of(s, tr[t]));
   }
   if (prefix) most = all;
-  const int64_t split = std::max(kMaxSplitSmall * std::min<int64_t>(most, 16), kMaxSplit * std::min<int64_t>(most, 256));
+  const int64_t split = kMaxSplitSmall * std::min<int64_t>(most, 16) + kMaxSplit * std::min<int64_t>(most, 256);
   return split + (prefix ? 2 * all * s->kv_heads * s->layers : 0);
 }
 
@@ -392,8 +393,10 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
       rows_us += (double)slices * std::min<int64_t>(sg.S, most_seen(L, sg, 16)) * L.d *
                  (L.dtype == COMMITKV_BF16 ? 4 : 8) / kBytesPerUs;
   }
+  int64_t split_left[2] = {kMaxSplitSmall, kMaxSplit};
   for (int p = 0; p < kPaths; ++p) {
     const PathInfo pi = path_info(L, p);
+    int64_t &left = split_left[pi.rows > 16];
     Divide v;
     int ids[kMaxSeg];
     v.n = 0;
@@ -415,14 +418,14 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     if ((p == kTc || p == kTcF32) && v.n == 1 && rows_us > 0.0)
       slots = std::min(slots, std::max<int64_t>(
                                   1, (int64_t)(v.base[0] * v.tiles[0] / std::max(1.0, rows_us / pi.tile_us - 2 * pi.fixed))));
-    const Division dv =
-        divide(v, pi, slots, pi.rows <= 16 ? kMaxSplitSmall : kMaxSplit, slices, prefix != nullptr);
+    const Division dv = divide(v, pi, slots, left, slices, prefix != nullptr);
     int64_t items = 0;
     for (int i = 0; i < v.n; ++i) {
       Seg &sg = L.seg[ids[i]];
       const bool rest = dv.rest >= 0 && v.base[i] > 0 && v.tiles[i] > 0;
       sg.nchunk = (int32_t)(rest ? dv.chunks : std::max<int64_t>(1, cdiv(v.tiles[i], dv.len)));
       sg.nsplit = (int32_t)(rest ? dv.rest : sg.nchunk > 1 ? sg.nrt : 0);
+      left -= slices * sg.nsplit * sg.nchunk;
       if (prefix) sg.nsplit = sg.nrt;  // two caches: all results are partial
       sg.Rs = std::min(sg.R, sg.nsplit * pi.rows);
       items += slices * ((sg.nrt - sg.nsplit) + (int64_t)sg.nsplit * sg.nchunk);

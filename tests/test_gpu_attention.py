@@ -541,3 +541,34 @@ def test_prefix_beside_decoded_caches(d):
         g.replay()
         check()
         assert torch.equal(first, p.flat)
+
+
+def test_long_prompts_and_decoded_tokens_in_one_batch():
+    """Both kinds of rows are split over their tokens, each as far as it may be
+    alone: their partial results fit the workspace together."""
+    H, Hq, d, g = 8, 32, 64, torch.Generator().manual_seed(5)
+    shape = ck.make_shape(1, H, Hq, d, BF)
+
+    def trajectories(S, W, n):
+        k, v = ref.cache(1, H, S, d, BF, S)
+        dev, pos = (k.cuda(), v.cuda()), torch.arange(S, dtype=torch.int32, device="cuda")
+        for _ in range(n):
+            Q = torch.randn(1, Hq, W, d, generator=g).to(BF)
+            yield (k, v, np.arange(S)), Q, ck.TrajTensors(*dev, pos, Q.cuda(), pos[S - W:].clone())
+
+    every = [*trajectories(40000, 1500, 2), *trajectories(8192, 4, 40)]
+    trajs = [t for _, _, t in every]
+    out = [torch.full_like(t.q, float("nan")) for t in trajs]
+    lse = [torch.full(t.q.shape[:3], float("nan"), device="cuda") for t in trajs]
+    ws = ck.alloc_attention_workspace(shape, trajs)
+    ck.commitkv_window_attention(shape, trajs, out, lse, workspace=ws)
+    torch.cuda.synchronize()
+    assert ck.commitkv_workspace_status(ws) == ck.COMMITKV_OK
+    assert all(x.isfinite().all() for x in out + lse)
+    for i in (0, 1, 2, 20, 41):
+        part, Q, t = every[i]
+        W, S = Q.shape[2], part[0].shape[2]
+        rows = sorted({0, W // 2 + 1, W - 1})
+        o, l, to, tl = ref.attention([part], Q[:, :, rows], np.array(rows) + S - W, rounded_weights=True)
+        ref.check(out[i][:, :, rows], o, to, "out %d" % i)
+        ref.check(lse[i][:, :, rows], l, tl, "lse %d" % i)
