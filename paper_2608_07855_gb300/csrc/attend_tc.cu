@@ -54,7 +54,7 @@ struct Smem {
   uint64_t next_full, plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
       o_empty[2], pub_full, pub_empty, drain;
   uint32_t tmem;
-  int abort_flag;
+  int flags[kFlags];
 };
 
 __device__ __forceinline__ void tma4(void *dst, const CUtensorMap *m, int x, int tok, int h, int l, uint64_t *bar,
@@ -224,11 +224,11 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
   S &sm = *reinterpret_cast<S *>(smem_raw + ((0u - smem_addr(smem_raw)) & 1023u));
   const Launch &L = P.L;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-  volatile int *abort_flag = &sm.abort_flag;
+  volatile int *flags = sm.flags;
 
   pdl_start_next();
   if (threadIdx.x == 0) {
-    sm.abort_flag = 0;
+    sm.flags[kAbort] = sm.flags[kRedoing] = 0;
     for (int b = 0; b < 2; ++b) {
       mbar_init(&sm.plan_full[b], 1);
       mbar_init(&sm.plan_empty[b], 10);  // TMA, MMA, eight softmax warps
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       bool ok = true;
       auto load = [&](const CUtensorMap *m, int tok, const Item &it) {
         const int s = g % NST;
-        if (g >= NST && !wait(&sm.kv_empty[s], (g / NST - 1) & 1, abort_flag)) return false;
+        if (g >= NST && !wait(&sm.kv_empty[s], (g / NST - 1) & 1, flags)) return false;
         mbar_expect_tx(&sm.kv_full[s], S::kTile);
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) tma4(sm.kv[s] + x * kHalf, m, 64 * x, tok, it.kvh, it.l, &sm.kv_full[s], pol);
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         return true;
       };
       for (int n = 0; ok; ++n) {
-        if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+        if (!wait(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
         const Plan pl = sm.plan[n & 1];
         if (pl.rows == 0) break;
         mbar_arrive(&sm.plan_empty[n & 1]);
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           ok = load(&P.k[it.s], tok, it) && load(&P.v[it.s], tok, it);
         }
       }
-      if (*abort_flag)  // let the copies already issued land before the CTA leaves
+      if (flags[kAbort])  // let the copies already issued land before the CTA leaves
         for (uint32_t u = g > NST ? g - NST : 0; u < g; ++u) mbar_wait_drain(&sm.kv_full[u % NST], (u / NST) & 1, kWait);
     } else if (warp == 1) {
       // ------------------------------------------------------------ MMAs
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       // group: 2,330 against 2,050 us on a 4K prompt over 36K tokens.)
       uint32_t g = 0, np[2] = {0, 0}, uses[2] = {0, 0};  // earlier items: tiles, tiles of each group, items that filled O_b
       bool ok = true;
-      auto kv_wait = [&](uint32_t u) { return wait_warp(&sm.kv_full[u % NST], (u / NST) & 1, abort_flag); };
+      auto kv_wait = [&](uint32_t u) { return wait_warp(&sm.kv_full[u % NST], (u / NST) & 1, flags); };
       // descriptors of stage 0 and of Q: a stage, k-step or row tile further adds to the address field
       const uint64_t k0 = desc_kmajor(sm.kv[0], 0), v0 = desc_v(sm.kv[0], 0), q0 = desc_kmajor(sm.q[0], 0);
       constexpr uint64_t kStep = S::kTile >> 4;
@@ -333,16 +333,16 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       };
       // weights of group b's i-th tile of this item are there, and O_b may be written
       auto p_wait = [&](int b, int i) {
-        return (i > 0 || uses[b] == 0 || wait_warp(&sm.o_empty[b], (uses[b] - 1) & 1, abort_flag)) &&
-               wait_warp(&sm.p_full[b], (np[b] + i) & 1, abort_flag);
+        return (i > 0 || uses[b] == 0 || wait_warp(&sm.o_empty[b], (uses[b] - 1) & 1, flags)) &&
+               wait_warp(&sm.p_full[b], (np[b] + i) & 1, flags);
       };
       for (int n = 0; ok; ++n) {
-        if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+        if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
         const Plan pl = sm.plan[n & 1];
         if (pl.rows == 0) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
-        if (!wait_warp(&sm.q_full, n & 1, abort_flag)) break;
+        if (!wait_warp(&sm.q_full, n & 1, flags)) break;
         const int nt = pl.j1 - pl.j0;
         if (nt == 0 && lane == 0) mbar_arrive(&sm.q_empty);  // else behind the last Q K^T
         if (pl.rows > BM) {
@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         }
         g += nt;
       }
-      if (__any_sync(0xffffffffu, *abort_flag != 0)) {
+      if (__any_sync(0xffffffffu, flags[kAbort] != 0)) {
         if (elect_one()) {
           mma_commit(&sm.drain);  // every MMA issued by this thread has completed
           mbar_wait_drain(&sm.drain, 0, kWait);
@@ -431,9 +431,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       bool asked = false;
       for (int n = 0;; ++n) {
         const int buf = n & 1;
-        if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, abort_flag)) break;
+        if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, flags)) break;
         if (asked) {
-          if (!wait_warp(&sm.next_full, (n - 1) & 1, abort_flag)) break;
+          if (!wait_warp(&sm.next_full, (n - 1) & 1, flags)) break;
           asked = false;
           item = read_next(&sm.next);
           __syncwarp();
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
-        if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag)) break;
+        if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, flags)) break;
         if (n > 0 && P.has_q && sg.t >= 0) {
           // between two items nothing else hides this copy (by the warp's own
           // copies, as below: five prompts with an 86-token window 35 us, 32 so)
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       // left early: what is under way lands before the block's memory goes
       if (asked && lane == 0)
         for (int k = 0; k < 2; ++k) mbar_wait_drain(&sm.next_full, k, kWait / 4);
-      if (*abort_flag && q_last >= 0 && lane == 0) mbar_wait_drain(&sm.q_full, q_last & 1, kWait);
+      if (flags[kAbort] && q_last >= 0 && lane == 0) mbar_wait_drain(&sm.q_full, q_last & 1, kWait);
     }
   } else {
     // ------------------------------------------------------------ softmax
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     uint32_t ns = 0, uses = 0, npub = 0;  // score tiles, items that filled O_hb, joined items
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
       const Plan pl = sm.plan[n & 1];
       if (pl.rows == 0) break;
       const Tiles tl = pl.tl;
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       float m_used = -INFINITY, lsum = 0.0f;
       const int step = two ? 1 : 2, first = pl.j0 + (two ? 0 : hb);
       for (int j = first; j < pl.j1; j += step) {
-        if (!wait_warp(&sm.s_full[hb], ns & 1, abort_flag)) {
+        if (!wait_warp(&sm.s_full[hb], ns & 1, flags)) {
           ok = false;
           break;
         }
@@ -547,13 +547,13 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       if (!ok) break;
       // ---------------------------------------------------------- results
       const bool mine = first < pl.j1, other = !two && pl.j0 + 1 < pl.j1;  // O_hb / O_1 of a joined item was filled
-      if (mine && !wait_warp(&sm.o_full[hb], uses & 1, abort_flag)) break;
+      if (mine && !wait_warp(&sm.o_full[hb], uses & 1, flags)) break;
       if (mine) ++uses;
       tc_fence_after();
       float f0 = 1.0f, f1 = 0.0f, m = m_used;
       if (!two) {
         if (hb == 1) {
-          if (npub > 0 && !wait_warp(&sm.pub_empty, (npub - 1) & 1, abort_flag)) break;
+          if (npub > 0 && !wait_warp(&sm.pub_empty, (npub - 1) & 1, flags)) break;
           ++npub;
           sm.pub[row] = make_float2(m_used, lsum);
           tc_fence_before();
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           if (lane == 0) mbar_arrive(&sm.pub_full);
           continue;  // group 0 reads O_1
         }
-        if (!wait_warp(&sm.pub_full, npub & 1, abort_flag)) break;
+        if (!wait_warp(&sm.pub_full, npub & 1, flags)) break;
         ++npub;
         tc_fence_after();
         const float2 o1 = sm.pub[row];
@@ -637,6 +637,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (!two) mbar_arrive(&sm.pub_empty);
       }
       unsigned bad = __ballot_sync(0xffffffffu, valid && chk != 0.0f && isfinite(lsum));
+      const bool redo = bad != 0;
+      if (redo) redoing(flags, 1);
       while (bad) {  // a masked value that is not finite met a weight of zero
         const int b = __ffs(bad) - 1;
         bad &= bad - 1;
@@ -651,12 +653,13 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         __syncwarp();
         write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, lb);
       }
+      if (redo) redoing(flags, -1);
     }
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tm, 512);
-  if (threadIdx.x == 0 && sm.abort_flag) record_error(hdr, COMMITKV_ERR_TIMEOUT, 30);
+  if (threadIdx.x == 0 && sm.flags[kAbort]) record_error(hdr, COMMITKV_ERR_TIMEOUT, 30);
   pdl_wait();
 }
 

@@ -11,16 +11,37 @@ namespace at {
 using namespace ckv::sm103;
 
 constexpr int BM = 128;  // rows of a tile
-// Long enough for the rows that redo_row takes (32 rows of a million tokens: under a second).
 constexpr uint64_t kWait = 4000000000ull;
 constexpr float kLazy = 8.0f;
 
-// mbar_wait that parks the thread before it first reads the clock.
-__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+// A block's flags: set when a wait ran out, and how many of its warps are at
+// rows that redo_row takes.  Those go through the whole cache a row at a time
+// (bounded, but 4.9 s for 38,912 rows over 131,072 tokens that all need it,
+// bf16, 128 channels), so waits do not run out meanwhile.
+enum { kAbort, kRedoing, kFlags };
+
+// Waits for the phase with the given parity; parks the thread before it first
+// reads the clock.
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, volatile int *flags) {
 #pragma unroll 1
   for (int i = 0; i < 4; ++i)
     if (mbar_try_wait_sleep(bar, parity, 20000)) return true;
-  return mbar_wait(bar, parity, kWait, abort_flag);
+  uint64_t t0 = now_ns();
+#pragma unroll 1
+  while (!mbar_try_wait_sleep(bar, parity, 20000)) {
+    if (flags[kAbort]) return false;
+    if (flags[kRedoing]) t0 = now_ns();
+    else if (now_ns() - t0 > kWait) {
+      flags[kAbort] = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+// A warp enters (1) and leaves (-1) such rows.
+__device__ __forceinline__ void redoing(volatile int *flags, int change) {
+  if ((threadIdx.x & 31) == 0) atomicAdd_block(const_cast<int *>(flags) + kRedoing, change);
 }
 
 struct Plan {
@@ -67,8 +88,8 @@ __device__ __forceinline__ bool elect_one() {
   return e != 0;
 }
 
-__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
-  return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
+__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *flags) {
+  return __all_sync(0xffffffffu, wait(bar, parity, flags));
 }
 
 // Row r of an item: its query, and what it sees.  Behind the last row: zeros

@@ -48,7 +48,7 @@ struct Smem {
   uint64_t next_full, plan_full[2], plan_empty[2], q_full, q_empty, k_full, k_empty, v_full, v_empty, s_full[2], p_full[2],
       d_full[2], d_empty[2], drain;
   uint32_t tmem;
-  int abort_flag;
+  int flags[kFlags];
 };
 
 // Takes a term off two values: their bf16 roundings, the exact rests stay.
@@ -94,11 +94,11 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
   extern __shared__ uint8_t smem_raw[];
   S &sm = *reinterpret_cast<S *>(smem_raw + ((0u - smem_addr(smem_raw)) & 1023u));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-  volatile int *abort_flag = &sm.abort_flag;
+  volatile int *flags = sm.flags;
 
   pdl_start_next();
   if (threadIdx.x == 0) {
-    sm.abort_flag = 0;
+    sm.flags[kAbort] = sm.flags[kRedoing] = 0;
     for (int b = 0; b < 2; ++b) {
       mbar_init(&sm.plan_full[b], 1);
       mbar_init(&sm.plan_empty[b], 9);  // MMA, four softmax and four splitting warps
@@ -149,17 +149,17 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       uint32_t t = 0;  // tiles of earlier items
       bool ok = true;
       for (int n = 0; ok; ++n) {
-        if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+        if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
         const int nt = sm.plan[n & 1].j1 - sm.plan[n & 1].j0, rows = sm.plan[n & 1].rows;
         if (rows == 0) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_empty[n & 1]);
-        if (!wait_warp(&sm.q_full, n & 1, abort_flag)) break;
+        if (!wait_warp(&sm.q_full, n & 1, flags)) break;
         if (nt == 0 && lane == 0) mbar_arrive(&sm.q_empty);
         for (int j = 0; j <= nt && nt > 0; ++j) {
           if (j < nt) {
             const uint32_t T = t + j, b = T & 1;
-            if (!(ok = wait_warp(&sm.k_full, T & 1, abort_flag))) break;
+            if (!(ok = wait_warp(&sm.k_full, T & 1, flags))) break;
             tc_fence_after();
             if (elect_one()) {
               constexpr uint32_t idesc = idesc_bf16_f32(BM, BT, 0, 0);
@@ -179,9 +179,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
           }
           if (j > 0) {
             const uint32_t T = t + j - 1, b = T & 1, u = T >> 1;
-            ok = wait_warp(&sm.v_full, T & 1, abort_flag) &&
-                 (u == 0 || wait_warp(&sm.d_empty[b], (u - 1) & 1, abort_flag)) &&
-                 wait_warp(&sm.p_full[b], u & 1, abort_flag);
+            ok = wait_warp(&sm.v_full, T & 1, flags) &&
+                 (u == 0 || wait_warp(&sm.d_empty[b], (u - 1) & 1, flags)) &&
+                 wait_warp(&sm.p_full[b], u & 1, flags);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         }
         t += nt;
       }
-      if (__any_sync(0xffffffffu, *abort_flag != 0)) {
+      if (__any_sync(0xffffffffu, flags[kAbort] != 0)) {
         if (elect_one()) {
           mma_commit(&sm.drain);  // every MMA issued by this thread has completed
           mbar_wait_drain(&sm.drain, 0, kWait);
@@ -216,9 +216,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       bool asked = false;
       for (int n = 0;; ++n) {
         const int buf = n & 1;
-        if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, abort_flag)) break;
+        if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, flags)) break;
         if (asked) {
-          if (!wait_warp(&sm.next_full, (n - 1) & 1, abort_flag)) break;
+          if (!wait_warp(&sm.next_full, (n - 1) & 1, flags)) break;
           asked = false;
           item = read_next(&sm.next);
           __syncwarp();
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
     uint32_t t = 0;
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
       const Plan pl = sm.plan[n & 1];
       if (pl.rows == 0) break;
       const Span sp = sm.span[n & 1][row];
@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       for (int c = 0; c < D / 2; ++c) o[c] = make_float2(0.0f, 0.0f);
       auto take = [&](uint32_t T) {  // O += the P V of tile T
         const uint32_t b = T & 1;
-        if (!wait_warp(&sm.d_full[b], (T >> 1) & 1, abort_flag)) return false;
+        if (!wait_warp(&sm.d_full[b], (T >> 1) & 1, flags)) return false;
         tc_fence_after();
 #pragma unroll
         for (int c0 = 0; c0 < D; c0 += 32) {
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       };
       for (int j = 0; j < nt; ++j) {
         const uint32_t T = t + j, b = T & 1, col = tm + lanes + 96 * b;
-        if (!(ok = wait_warp(&sm.s_full[b], (T >> 1) & 1, abort_flag))) break;
+        if (!(ok = wait_warp(&sm.s_full[b], (T >> 1) & 1, flags))) break;
         tc_fence_after();
         const int t0 = tile_start(pl.tl, pl.j0 + j, BT), t1 = tile_end(pl.tl, pl.j0 + j, BT);
         const int a = t0 - sp.lo, end = min(sp.hi, t1) - sp.lo, se = min(sp.se, t1) - t0;
@@ -389,6 +389,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       // A value that is not finite: masked ones met a weight of zero, and an
       // infinite key's terms are NaN though its score may be -inf.
       unsigned bad = __ballot_sync(0xffffffffu, row < pl.rows && (chk != 0.0f || !isfinite(lsum)));
+      const bool redo = bad != 0;
+      if (redo) redoing(flags, 1);
       while (bad) {
         const int k = __ffs(bad) - 1;
         bad &= bad - 1;
@@ -405,6 +407,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         __syncwarp();
         write_row_warp<float, D>(L, sg, it, r - lane + k, ok_, mk, isfinite(lk) ? lk : l2);
       }
+      if (redo) redoing(flags, -1);
     }
   } else {
     // ------------------------------------------------------------ split
@@ -414,7 +417,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
     uint32_t t = 0;
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, abort_flag)) break;
+      if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
       const Plan pl = sm.plan[n & 1];
       if (pl.rows == 0) break;
       __syncwarp();
@@ -440,7 +443,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         }
       };
       fetch(0);
-      if (n > 0 && !(ok = wait_warp(&sm.q_empty, (n - 1) & 1, abort_flag))) break;
+      if (n > 0 && !(ok = wait_warp(&sm.q_empty, (n - 1) & 1, flags))) break;
       {
         // Q: a warp's 32 rows, D / 4 lanes to a row
         constexpr int RW = 32 / C4 > 0 ? 32 / C4 : 1;
@@ -472,7 +475,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         const int j = i == 0 ? 0 : is_v ? i / 2 - 1 : (i + 1) / 2;
         if (j < nt) {
           const uint32_t T = t + j;
-          ok = T == 0 || wait_warp(is_v ? &sm.v_empty : &sm.k_empty, (T - 1) & 1, abort_flag);
+          ok = T == 0 || wait_warp(is_v ? &sm.v_empty : &sm.k_empty, (T - 1) & 1, flags);
           if (!ok) break;
           const uint32_t tile = smem_addr(is_v ? sm.v[0] : sm.k[0]);
 #pragma unroll
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tm, 512);
-  if (threadIdx.x == 0 && sm.abort_flag) record_error(hdr, COMMITKV_ERR_TIMEOUT, 31);
+  if (threadIdx.x == 0 && sm.flags[kAbort]) record_error(hdr, COMMITKV_ERR_TIMEOUT, 31);
   pdl_wait();
 }
 

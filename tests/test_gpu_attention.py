@@ -572,3 +572,29 @@ def test_long_prompts_and_decoded_tokens_in_one_batch():
         o, l, to, tl = ref.attention([part], Q[:, :, rows], np.array(rows) + S - W, rounded_weights=True)
         ref.check(out[i][:, :, rows], o, to, "out %d" % i)
         ref.check(lse[i][:, :, rows], l, tl, "lse %d" % i)
+
+
+@pytest.mark.parametrize("dtype,W", [(BF, 1216), (F32, 608)], ids=["bf16", "f32"])
+def test_values_that_are_not_finite_in_a_long_cache(dtype, W, kernels):
+    """Every row of a prompt is done over by the definition, for longer than the
+    tile kernels' waits last."""
+    if kernels:
+        pytest.skip("the kernels of row tiles, which this call takes by itself")
+    H, Hq, d, S, g = 8, 32, 128, 131072, torch.Generator().manual_seed(9)
+    shape = ck.make_shape(1, H, Hq, d, dtype)
+    k, v = ref.cache(1, H, S, d, dtype, 4)
+    v[:, :, S - W:, 0] = float("nan")
+    Q, pos = torch.randn(1, Hq, W, d, generator=g).to(dtype), torch.arange(S, dtype=torch.int32)
+    trajs = [ck.TrajTensors(k.cuda(), v.cuda(), pos.cuda(), Q.cuda(), pos[S - W:].cuda())]
+    out, lse = [torch.empty_like(trajs[0].q)], [torch.empty(Q.shape[:3], device="cuda")]
+    ws = ck.alloc_attention_workspace(shape, trajs)
+    ck.commitkv_window_attention(shape, trajs, out, lse, workspace=ws)
+    torch.cuda.synchronize()
+    assert ck.commitkv_workspace_status(ws) == ck.COMMITKV_OK
+    assert out[0][..., 0].isnan().all() and out[0][..., 1:].isfinite().all() and lse[0].isfinite().all()
+    rows = [0, W - 1]
+    for h in (0, H - 1):
+        o, l, to, tl = ref.attention([(k[:, h:h + 1], v[:, h:h + 1], pos.numpy())], Q[:, 4 * h:4 * h + 4, rows],
+                                     np.array(rows) + S - W, rounded_weights=dtype == BF)
+        ref.check(out[0][:, 4 * h:4 * h + 4, rows], o, to, "out")
+        ref.check(lse[0][:, 4 * h:4 * h + 4, rows], l, tl, "lse")
