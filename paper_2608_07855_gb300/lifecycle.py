@@ -184,11 +184,13 @@ class Session:
         torch = _torch()
         s, S = self.shape, self.S
         tr = ck.TrajTensors(self.K[:, :, :S], self.V[:, :, :S], self.pos[:S], Q, qpos)
-        out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], device=self.dev)
+        out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=self.dev)
         need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
-        if self.attention_ws is None or self.attention_ws.numel() < need:
-            self.attention_ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
         ws = self.attention_ws
+        if torch.cuda.is_current_stream_capturing():  # a graph's own, which outlives the session's
+            ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+        elif ws is None or ws.numel() < need:
+            ws = self.attention_ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
         if prefix is None:
             ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
         else:

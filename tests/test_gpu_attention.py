@@ -598,3 +598,36 @@ def test_values_that_are_not_finite_in_a_long_cache(dtype, W, kernels):
                                      np.array(rows) + S - W, rounded_weights=dtype == BF)
         ref.check(out[0][:, 4 * h:4 * h + 4, rows], o, to, "out")
         ref.check(lse[0][:, 4 * h:4 * h + 4, rows], l, tl, "lse")
+
+
+def test_session_attention_in_graphs():
+    """Graphs of a session's attention share no workspace with one another or
+    with its later calls."""
+    from paper_2608_07855_gb300.lifecycle import Session
+
+    H, Hq, d, n = 2, 8, 64, 6000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF)  # noqa: E731
+    s = Session(ck.make_shape(1, H, Hq, d, BF), 32, 200, 0.5, n)
+    s.append(rand(1, H, n, d), rand(1, H, n, d), torch.arange(n, dtype=torch.int32, device="cuda"), [])
+    Q = [rand(1, Hq, 1, d), rand(1, Hq, 70, d)]
+    p = [torch.arange(n - q.shape[2], n, dtype=torch.int32, device="cuda") for q in Q]
+    s.attend(Q[0], p[0])  # the session's own workspace, too small for the other
+    graphs, outs = [], []
+    for q, at in zip(Q, p):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(s.attend(q, at))
+    for q in Q:
+        q.copy_(rand(*q.shape))
+    want = [s.attend(q, at) for q, at in zip(Q, p)]
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    again = [s.attend(q, at) for q, at in zip(Q, p)]
+    torch.cuda.synchronize()
+    for w, o, a in zip(want, outs, again):
+        assert all(torch.equal(x, y) and torch.equal(x, z) for x, y, z in zip(w, o, a))
