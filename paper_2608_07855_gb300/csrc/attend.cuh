@@ -220,7 +220,7 @@ struct Tiles {
 __device__ __forceinline__ Tiles make_tiles(int lo, int hi, int se, int tile) {
   Tiles t;
   if (hi <= lo) lo = 0, hi = se, se = 0;  // sinks alone
-  else if (se >= lo) lo = se = 0;         // one piece
+  else if (se >= lo) hi = max(hi, se), lo = se = 0;  // one piece
   t.lo = lo, t.hi = hi, t.se = se;
   t.nA = (se + tile - 1) / tile;
   t.n = t.nA + (hi - lo + tile - 1) / tile;

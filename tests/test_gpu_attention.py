@@ -631,3 +631,14 @@ def test_session_attention_in_graphs():
     torch.cuda.synchronize()
     for w, o, a in zip(want, outs, again):
         assert all(torch.equal(x, y) and torch.equal(x, z) for x, y, z in zip(w, o, a))
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("prefix", [0, 60])
+def test_queries_in_any_order(dtype, d, prefix):
+    """Early queries beside ones whose window is empty: the sinks go on behind
+    the end of what the early ones see."""
+    order = lambda pos, W: np.resize(pos[0] + np.array([2, 300, 140, -1, 5, 170, 89, 300, 0, 133]), W)  # noqa: E731
+    for window, sinks in ((1, 4), (3, 40), (50, 8), (1, 200)):
+        run(window, sinks, dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(90, 4), (90, 50), (150, 10)], qpos=order,
+            prefix=prefix)
