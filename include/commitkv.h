@@ -487,10 +487,10 @@ commitkv_status commitkv_compact_noalloc(const commitkv_shape *shape, int32_t n_
  * Which kernels run: where K, V, Q and the outputs are 16-byte aligned (pointers
  * and strides) the tensor cores, otherwise the CUDA cores.  Weights are fp32;
  * prompts of bf16 caches round them to bf16 for the product with the values
- * (2^-9 of each on average, as much as the output's own rounding), decoded
- * tokens to two bf16 terms.  fp32 operands are taken as sums of two tf32 or
- * three bf16 terms, which loses up to 2^-21 of a product.  The same call gives
- * the same bits every time.
+ * (up to 2^-8 of each, like the output's own rounding), decoded tokens to two
+ * bf16 terms.  fp32 operands are taken as sums of two tf32 terms (decoded
+ * tokens) or three bf16 terms (prompts), which loses up to 2^-21 or 2^-25 of
+ * each.  The same call gives the same bits every time.
  * -------------------------------------------------------------------- */
 commitkv_status commitkv_window_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
                                           const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,

@@ -1,5 +1,6 @@
-// Attention on the CUDA cores: fp32 caches, and bf16 ones that the tensor-core
-// kernels cannot read (unaligned pointers or strides).
+// Attention on the CUDA cores: caches, queries or outputs that the tensor-core
+// kernels cannot read or write (pointers or strides that are not 16-byte
+// aligned).
 //
 // One block of 256 threads per item; tiles of 64 tokens.  Thread (ty, tx) of a
 // 16 x 16 grid owns TM rows: their scores against four tokens (tx + 16 j) of a

@@ -633,6 +633,17 @@ def test_session_attention_in_graphs():
         assert all(torch.equal(x, y) and torch.equal(x, z) for x, y, z in zip(w, o, a))
 
 
+def test_windows_and_sinks_beyond_32_bits_are_refused():
+    p = Problem(dtype=BF, d=64, M=1, H=1, Hq=2, trajs=[(10, 1)]).upload()
+    for kw in (dict(window=1 << 32), dict(sinks=1 << 31)):
+        with pytest.raises(ValueError):
+            p.call(**kw)
+    p.guards()
+    assert (p.out[0] == SENT).all()
+    p.call(window=(1 << 31) - 1, sinks=(1 << 31) - 1)
+    p.check()
+
+
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 @pytest.mark.parametrize("prefix", [0, 60])
 def test_queries_in_any_order(dtype, d, prefix):
