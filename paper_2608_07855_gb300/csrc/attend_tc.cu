@@ -51,7 +51,7 @@ struct Smem {
   int3 first[8];  // what the rows of a softmax warp see of the first item
   float2 pub[BM];  // one row tile: group 1's (m, l)
   alignas(16) uint4 next;  // answer to the request for another item
-  uint64_t next_full, plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
+  uint64_t ask, next_full, plan_full[2], plan_empty[2], q_full, q_empty, kv_full[NST], kv_empty[NST], s_full[2], p_full[2], o_full[2],
       o_empty[2], pub_full, pub_empty, drain;
   uint32_t tmem;
   int flags[kFlags];
@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       mbar_init(&sm.o_full[b], 1);
       mbar_init(&sm.o_empty[b], 4);
     }
+    mbar_init(&sm.ask, 1);
     mbar_init(&sm.next_full, 1);
     mbar_init(&sm.q_full, 1);
     mbar_init(&sm.q_empty, 1);
@@ -293,7 +294,10 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (pl.rows == 0) break;
         mbar_arrive(&sm.plan_empty[n & 1]);
         const Item it = pl.it;
-        for (int j = pl.j0; j < pl.j1 && ok; ++j) {
+        const int j_ask = max(pl.j1 - kAsk, pl.j0);
+        for (int j = pl.j0; j < max(pl.j1, pl.j0 + 1) && ok; ++j) {
+          if (j == j_ask) mbar_arrive(&sm.ask);
+          if (j == pl.j1) break;  // no tiles
           const int tok = tile_start(pl.tl, j, BT);
           ok = load(&P.k[it.s], tok, it) && load(&P.v[it.s], tok, it);
         }
@@ -428,13 +432,16 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       // ------------------------------------------------------------ plans and Q rows
       int item = blockIdx.x;
       int q_last = -1;  // the last item whose Q TMA copied
-      bool asked = false;
       for (int n = 0;; ++n) {
         const int buf = n & 1;
         if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, flags)) break;
-        if (asked) {
-          if (!wait_warp(&sm.next_full, (n - 1) & 1, flags)) break;
-          asked = false;
+        if (n > 0) {
+          if (!wait_warp(&sm.ask, (n - 1) & 1, flags)) break;
+          if (lane == 0) ask_next(&sm.next, &sm.next_full);
+          if (!wait_warp(&sm.next_full, (n - 1) & 1, flags)) {
+            if (lane == 0) mbar_wait_drain(&sm.next_full, (n - 1) & 1, kWait);  // it lands before the block's memory goes
+            break;
+          }
           item = read_next(&sm.next);
           __syncwarp();
         }
@@ -445,8 +452,6 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
           }
           break;
         }
-        if (lane == 0) ask_next(&sm.next, &sm.next_full);
-        asked = true;
         const Item it = decode_item(L, item);
         const Seg &sg = L.seg[it.s];
         const int r0 = it.rt * L.rows_per_item, rows = min(L.rows_per_item, sg.R - r0);
@@ -495,8 +500,6 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (lane == 0) mbar_arrive(&sm.q_full);
       }
       // left early: what is under way lands before the block's memory goes
-      if (asked && lane == 0)
-        for (int k = 0; k < 2; ++k) mbar_wait_drain(&sm.next_full, k, kWait / 4);
       if (flags[kAbort] && q_last >= 0 && lane == 0) mbar_wait_drain(&sm.q_full, q_last & 1, kWait);
     }
   } else {

@@ -54,7 +54,15 @@ struct Plan {
 // One block is launched per item, and one that is done with its own takes the
 // next block's that has not started (PTX clusterlaunchcontrol), so items are
 // handed out as SMs get free while a block keeps its tensor memory, its
-// barriers and the pipeline across items.
+// barriers and the pipeline across items.  It asks kAsk tiles before its end:
+// long enough for the next item's plan, and not at the start, where the blocks
+// with the longest items would take the last ones too (20 prompts of up to 300
+// rows over up to 9,000 tokens: 301 us asking at the start, 274 so; 5 prompts
+// of 1,500: 229 and 207; a 4K prompt with a 4K window: 233, 234, and 240 with 3
+// tiles; short items lose most, 3 prompts of 2,452 without a window: 203, 206).
+// The warp that plans asks, told by the warp that copies (its asking itself: 2
+// us more on the windowed prompt).
+constexpr int kAsk = 6;
 __device__ __forceinline__ void ask_next(uint4 *answer, uint64_t *bar) {
   fence_proxy_async();  // the last answer has been read
   mbar_expect_tx(bar, 16);

@@ -45,7 +45,7 @@ struct Smem {
   float4 stage[4][RowsOut::kStage];
   int3 first[4];
   alignas(16) uint4 next;
-  uint64_t next_full, plan_full[2], plan_empty[2], q_full, q_empty, k_full, k_empty, v_full, v_empty, s_full[2], p_full[2],
+  uint64_t ask, next_full, plan_full[2], plan_empty[2], q_full, q_empty, k_full, k_empty, v_full, v_empty, s_full[2], p_full[2],
       d_full[2], d_empty[2], drain;
   uint32_t tmem;
   int flags[kFlags];
@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       mbar_init(&sm.d_full[b], 1);
       mbar_init(&sm.d_empty[b], 4);
     }
+    mbar_init(&sm.ask, 1);
     mbar_init(&sm.next_full, 1);
     mbar_init(&sm.q_full, 4);
     mbar_init(&sm.q_empty, 1);
@@ -213,13 +214,16 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
     } else if (warp == 3) {
       // ------------------------------------------------------------ plans
       int item = blockIdx.x;
-      bool asked = false;
       for (int n = 0;; ++n) {
         const int buf = n & 1;
         if (n >= 2 && !wait_warp(&sm.plan_empty[buf], ((n >> 1) - 1) & 1, flags)) break;
-        if (asked) {
-          if (!wait_warp(&sm.next_full, (n - 1) & 1, flags)) break;
-          asked = false;
+        if (n > 0) {
+          if (!wait_warp(&sm.ask, (n - 1) & 1, flags)) break;
+          if (lane == 0) ask_next(&sm.next, &sm.next_full);
+          if (!wait_warp(&sm.next_full, (n - 1) & 1, flags)) {
+            if (lane == 0) mbar_wait_drain(&sm.next_full, (n - 1) & 1, kWait);  // it lands before the block's memory goes
+            break;
+          }
           item = read_next(&sm.next);
           __syncwarp();
         }
@@ -230,8 +234,6 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
           }
           break;
         }
-        if (lane == 0) ask_next(&sm.next, &sm.next_full);
-        asked = true;
         const Item it = decode_item(L, item);
         const Seg &sg = L.seg[it.s];
         const int r0 = it.rt * BM, rows = min(BM, sg.R - r0);
@@ -254,8 +256,6 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
       }
-      if (asked && lane == 0)  // left early: the answer lands before the block's memory goes
-        for (int k = 0; k < 2; ++k) mbar_wait_drain(&sm.next_full, k, kWait / 4);
     }
   } else if (warp < 8) {
     // ------------------------------------------------------------ softmax
@@ -470,7 +470,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         if (lane == 0) mbar_arrive(&sm.q_full);
       }
 #pragma unroll 1
-      for (int i = 0; i <= 2 * nt && nt > 0; ++i) {
+      for (int i = 0; i <= 2 * nt; ++i) {
+        if (i == max(2 * (nt - kAsk), 0) && warp == 8 && lane == 0) mbar_arrive(&sm.ask);
+        if (nt == 0) break;
         const bool is_v = i > 0 && (i & 1) == 0;
         const int j = i == 0 ? 0 : is_v ? i / 2 - 1 : (i + 1) / 2;
         if (j < nt) {
