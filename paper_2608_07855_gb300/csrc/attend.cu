@@ -197,7 +197,7 @@ struct PathInfo {
   int resident;          // items at a time on an SM
   double fixed, tile_us;
 };
-struct Divide {
+struct Divide {  // segments in the order of their items
   int64_t base[kMaxSeg];   // slices x row tiles
   int64_t tiles[kMaxSeg];  // of a row tile, at most
   int64_t rows[kMaxSeg];   // of all slices
@@ -207,6 +207,49 @@ struct Division {
   int64_t len;  // every row tile in chunks of `len` tiles,
   int64_t rest, chunks;  // or, where rest >= 0, the last `rest` row tiles alone, in `chunks`
 };
+// When the last item ends, in tiles, where slots take items in their order as
+// they get free: slots that get free at the same time are kept together.  (The
+// work and half an item in its place: 8 prompts behind 32,768 tokens 788 us,
+// 703 so; 5 of up to 200 rows over 16,000 134 and 119; 40 agents with 40 rows
+// each behind 5,000 142 and 122.  Items of up to 16 rows share the memory's rate
+// instead, so their sum is what counts.)
+double last_end(const Divide &v, int64_t len, double fixed, int64_t slots) {
+  double at[kMaxSeg + 2];  // ascending; a segment leaves one kind of slots more at most
+  int64_t n[kMaxSeg + 2];
+  int k = 1;
+  at[0] = 0.0, n[0] = slots;
+  for (int s = 0; s < v.n; ++s) {
+    const int64_t c = std::max<int64_t>(1, cdiv(v.tiles[s], len));
+    const double item = (double)v.tiles[s] / c + fixed;
+    int64_t left = v.base[s] * c;
+    const int64_t rounds = left / slots - 1;  // of every slot
+    if (rounds > 0) {
+      left -= rounds * slots;
+      for (int i = 0; i < k; ++i) at[i] += rounds * item;
+    }
+    while (left > 0) {
+      const int64_t m = std::min(left, n[0]);
+      const double end = at[0] + item;
+      left -= m;
+      n[0] -= m;
+      if (n[0] == 0) {
+        --k;
+        for (int i = 0; i < k; ++i) at[i] = at[i + 1], n[i] = n[i + 1];
+      }
+      int i = k;  // behind all that end before
+      while (i > 0 && at[i - 1] > end) --i;
+      if (i > 0 && at[i - 1] == end) {
+        n[i - 1] += m;
+        continue;
+      }
+      for (int j = k; j > i; --j) at[j] = at[j - 1], n[j] = n[j - 1];
+      at[i] = end, n[i] = m;
+      ++k;
+    }
+  }
+  return at[k - 1];
+}
+
 Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most_items, int64_t slices, bool prefix) {
   int64_t longest = 1, kinds = 0, kind = 0;
   for (int s = 0; s < v.n; ++s) {
@@ -228,9 +271,10 @@ Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most
       work += (double)v.base[s] * (v.tiles[s] + c * pi.fixed);
     }
     if (split > most_items) break;
-    // whole waves where all items are alike, else the work and the tail that the last items leave
     const double one = len + pi.fixed;
-    double t = items <= slots ? one : kinds == 1 ? cdiv(items, slots) * one : work / slots + 0.5 * one;
+    double t = items <= slots ? one : kinds == 1 ? cdiv(items, slots) * one
+               : pi.rows > 16     ? last_end(v, len, pi.fixed, slots)
+                                  : work / slots + 0.5 * one;
     t = t * pi.tile_us + parts * kMergeRowUs + (split > 0 && !prefix ? kMergeUs : 0.0);
     if (t < best_t * 0.98) best_t = t, best.len = len;  // fewer chunks unless more are clearly better
   }
@@ -393,6 +437,9 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
       rows_us += (double)slices * std::min<int64_t>(sg.S, most_seen(L, sg, 16)) * L.d *
                  (L.dtype == COMMITKV_BF16 ? 4 : 8) / kBytesPerUs;
   }
+  for (int s = 0; s < L.n_seg; ++s) L.order[s] = (uint8_t)s;
+  std::sort(L.order, L.order + L.n_seg,
+            [&](int a, int b) { return L.seg[a].S != L.seg[b].S ? L.seg[a].S > L.seg[b].S : a < b; });
   int64_t split_left[2] = {kMaxSplitSmall, kMaxSplit};
   for (int p = 0; p < kPaths; ++p) {
     const PathInfo pi = path_info(L, p);
@@ -400,7 +447,8 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
     Divide v;
     int ids[kMaxSeg];
     v.n = 0;
-    for (int s = 0; s < L.n_seg; ++s) {
+    for (int k = 0; k < L.n_seg; ++k) {
+      const int s = L.order[k];
       Seg &sg = L.seg[s];
       if (path[s] != p) continue;
       sg.nrt = (int32_t)cdiv(sg.R, pi.rows);
@@ -443,9 +491,6 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   char *base = static_cast<char *>(workspace) + kAlign;
   L.po = reinterpret_cast<float *>(base);
   L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
-  for (int s = 0; s < L.n_seg; ++s) L.order[s] = (uint8_t)s;
-  std::sort(L.order, L.order + L.n_seg,
-            [&](int a, int b) { return L.seg[a].S != L.seg[b].S ? L.seg[a].S > L.seg[b].S : a < b; });
   cudaError_t e = cudaSuccess;
   bool launched = false;
   for (int p = 0; p < kPaths && e == cudaSuccess; ++p) {
