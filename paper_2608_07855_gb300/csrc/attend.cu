@@ -299,24 +299,27 @@ constexpr PathInfo kPath[kPaths] = {
 // For tests and diagnosis: COMMITKV_SCORING=simt takes the CUDA cores where a
 // call could have the tensor cores, COMMITKV_ATTENTION=tiles the kernels of row
 // tiles however few rows there are.
-bool env_starts(const char *name, char c) {
-  const char *e = getenv(name);
-  return e && e[0] == c;
+struct Forced {
+  bool cuda_cores, tiles;
+};
+Forced forced_paths() {
+  const char *s = getenv("COMMITKV_SCORING"), *a = getenv("COMMITKV_ATTENTION");
+  return {s && s[0] == 's', a && a[0] == 't'};
 }
 
 // Tensor cores where 16-byte copies can read the cache and the rows' queries
 // and outputs: up to 16 rows the kernel of 16-row items, others those of row
 // tiles (but see few_rows); TMA, which bf16 tiles take, also wants distinct
 // heads and layers.
-int path_of(const Launch &L, const Seg &sg) {
+int path_of(const Launch &L, const Seg &sg, const Forced &f) {
   const int cuda_cores = sg.R <= 16 ? kSimt16 : kSimt64;
-  if (env_starts("COMMITKV_SCORING", 's')) return cuda_cores;
+  if (f.cuda_cores) return cuda_cores;
   const int eb = L.dtype == COMMITKV_BF16 ? 2 : 4;
   uintptr_t bits = (uintptr_t)sg.k | (uintptr_t)sg.v | (uintptr_t)((sg.sl | sg.sh | sg.st) * eb);
   for (int t = sg.t < 0 ? 0 : sg.t; t < (sg.t < 0 ? L.n_traj : sg.t + 1); ++t)
     bits |= L.t[t].W ? (uintptr_t)L.t[t].q | (uintptr_t)L.t[t].out : 0;
   if (bits % 16) return cuda_cores;
-  if (sg.R <= 16 && !env_starts("COMMITKV_ATTENTION", 't')) return kRows;
+  if (sg.R <= 16 && !f.tiles) return kRows;
   if (eb == 4) return kTcF32;
   if (sg.S > 0 && (sg.sh == 0 || sg.sl == 0 || std::max(sg.sl, std::max(sg.sh, sg.st)) >= (1ll << 39))) return kRows;
   return kTc;
@@ -427,8 +430,9 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   int64_t parts = 0;
   bool merge = false;
   const int64_t slices = (int64_t)L.n_layers * L.H;
-  for (int s = 0; s < L.n_seg; ++s) path[s] = path_of(L, L.seg[s]);
-  if (!env_starts("COMMITKV_ATTENTION", 't') && few_rows(L, path, slices, sms))
+  const Forced forced = forced_paths();
+  for (int s = 0; s < L.n_seg; ++s) path[s] = path_of(L, L.seg[s], forced);
+  if (!forced.tiles && few_rows(L, path, slices, sms))
     for (int s = 0; s < L.n_seg; ++s) path[s] = path[s] == kTc || path[s] == kTcF32 ? kRows : path[s];
   double rows_us = 0.0;  // time of the decode kernel, which reads its caches at the memory's rate
   for (int s = 0; s < L.n_seg; ++s) {

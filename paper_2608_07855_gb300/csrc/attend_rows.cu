@@ -9,7 +9,7 @@
 // products from registers (the scores' fragments are the weights' operand as
 // they stand); a tcgen05 tile has 128 rows, and with its round trip through
 // tensor memory 4 rows over 64 caches of up to 8,192 tokens took 245 us against
-// 191 here (99 % of the copy rate).
+// 191 to 200 here (95 to 99 % of the copy rate).
 // bf16: the weights are split in two bf16 terms (2^-17 of each is lost): the
 // second product per tile is free, and the output is as exact as with fp32
 // weights.  fp32: every operand is split in two tf32 terms, three products
