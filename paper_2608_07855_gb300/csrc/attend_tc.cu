@@ -459,12 +459,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (n == 0) {
           if (lane < 8) u = sm.first[lane];
         } else {
-#pragma unroll 1
-          for (int i = lane; i < 2 * BM; i += 32) {
-            const int32_t *qpos = nullptr;
-            if (i < rows) row_query<__nv_bfloat16>(L, sg, it, r0 + i, D, qpos);
-            sm.span[buf][i] = row_sees(L, sg, qpos, u);
-          }
+          rows_see<__nv_bfloat16, D, 2 * BM>(L, sg, it, r0, rows, sm.span[buf], u);
         }
         u = join_warp(u);
         if (lane == 0) {

@@ -58,8 +58,8 @@ struct Plan {
 // long enough for the next item's plan, and not at the start, where the blocks
 // with the longest items would take the last ones too (20 prompts of up to 300
 // rows over up to 9,000 tokens: 301 us asking at the start, 274 so; 5 prompts
-// of 1,500: 229 and 207; a 4K prompt with a 4K window: 233, 234, and 240 with 3
-// tiles; short items lose most, 3 prompts of 2,452 without a window: 203, 206).
+// of 1,500: 229 and 207; short items lose most, 3 prompts of 2,452 without a
+// window: 203 and 206; 3 tiles or 9 are within 1 % of 6).
 // The warp that plans asks, told by the warp that copies (its asking itself: 2
 // us more on the windowed prompt).
 constexpr int kAsk = 6;
@@ -118,6 +118,27 @@ __device__ __forceinline__ Span row_sees(const Launch &L, const Seg &sg, const i
     u.z = max(u.z, sp.se);
   }
   return sp;
+}
+// What `rows` rows from r0 see, by a warp: a lane for each position, since the
+// rows of its g query heads see the same tokens (with gaps in the positions,
+// which cost searches, a lane a row took as long as nine tiles: three prompts of
+// up to 1,838 rows of 8 heads, a window of 1,030: 178.6 us, 162.2 so).  The rest of
+// the N rows has nothing to mask.
+template <typename T, int D, int N>
+__device__ __forceinline__ void rows_see(const Launch &L, const Seg &sg, const Item &it, int r0, int rows, Span *span,
+                                         int3 &u) {
+  const int lane = threadIdx.x & 31, p0 = r0 / L.g, end = (r0 + rows - 1) / L.g;
+#pragma unroll 1
+  for (int p = p0 + lane; p <= end; p += 32) {
+    const int a = max(r0, p * L.g), b = min(r0 + rows, (p + 1) * L.g);
+    const int32_t *qpos = nullptr;
+    row_query<T>(L, sg, it, a, D, qpos);
+    const Span sp = row_sees(L, sg, qpos, u);
+#pragma unroll 1
+    for (int r = a; r < b; ++r) span[r - r0] = sp;
+  }
+#pragma unroll 1
+  for (int i = rows + lane; i < N; i += 32) span[i] = {0, 0x7fffffff, 0};
 }
 // The union of what the rows of a warp see: (least lo, largest hi, largest se).
 __device__ __forceinline__ int3 join_warp(int3 u) {

@@ -241,12 +241,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         if (n == 0) {
           if (lane < 4) u = sm.first[lane];
         } else {
-#pragma unroll 1
-          for (int i = lane; i < BM; i += 32) {
-            const int32_t *qpos = nullptr;
-            row_query<float>(L, sg, it, r0 + i, D, qpos);
-            sm.span[buf][i] = row_sees(L, sg, qpos, u);
-          }
+          rows_see<float, D, BM>(L, sg, it, r0, rows, sm.span[buf], u);
         }
         u = join_warp(u);
         if (lane == 0) {
