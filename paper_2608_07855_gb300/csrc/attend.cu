@@ -294,7 +294,7 @@ Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most
 
 enum { kSimt16, kSimt64, kTc, kTcF32, kRows, kPaths };
 constexpr PathInfo kPath[kPaths] = {
-    {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {128, 64, 1, 3.0, 3.3}, {16, 64, 2, 2.0, 1.4}};
+    {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {128, 64, 1, 3.0, 2.7}, {16, 64, 2, 2.0, 1.4}};
 
 // For tests and diagnosis: COMMITKV_SCORING=simt takes the CUDA cores where a
 // call could have the tensor cores, COMMITKV_ATTENTION=tiles the kernels of row
@@ -349,9 +349,9 @@ PathInfo path_info(const Launch &L, int p) {
 // 16,000 26.0 and 23.4, 16 over 4,000 18.5 and 17.1, 100 over 500 21.2 and
 // 15.3, 8 agents behind 16,000 31.8 and 27.2; 5 over 16 caches to 16,000 127
 // and 161, 12 over 16 to 1,000 23 and 31, 32 over 32,768 44 and 120.  fp32, 16
-// on 4: 16 over 6,000 27 and 31, 32 over 2,000 24 and 25, 64 over 3,000 27 and
-// 56, 8 over 8 caches to 4,000 48 and 46, 16 agents behind 4,000 43 and 36; 4 on
-// 2: 40 over 1,000 19 and 15.
+// on 4: 16 over 6,000 25 and 32, 32 over 2,000 21 and 25, 64 over 3,000 26 and
+// 58, 8 over 8 caches to 4,000 42 and 47, 16 agents behind 4,000 25 and 30 (taken
+// for the other way); 4 on 2: 40 over 1,000 19 and 15.
 bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
   const bool bf16 = L.dtype == COMMITKV_BF16;
   const PathInfo few_pi = path_info(L, kRows), many_pi = path_info(L, bf16 ? kTc : kTcF32);

@@ -7,15 +7,18 @@
 // rounded, so P V of a tile is a sum by itself and the running O is kept in
 // fp32 registers.
 //
-// A CTA of 384 threads per SM takes items of up to 128 query rows over 64-token
-// tiles:
+// A CTA of 384 or 512 threads per SM takes items of up to 128 query rows over
+// 64-token tiles:
 //   warp 1      the MMAs: S = Q K^T of a tile, then P V of the one before
 //   warp 3      the plan of the next item
 //   warps 4-7   softmax, a thread per row: scores from TMEM, the weights' terms
 //               back over them, O += D (the tile's P V) in registers
-//   warps 8-11  the split: K, V and Q from memory to registers, their terms to
+//   warps 8-    the split: K, V and Q from memory to registers, their terms to
 //               shared memory in the MMA's layout; the next tile's K while the
-//               MMAs run this one's.  One piece of code for K and V: the roles'
+//               MMAs run this one's.  Eight warps for 128 channels, whose splits
+//               the MMAs waited for with four (six prompts of 300 rows over up to
+//               9,000 tokens: 628 and 512 us), four for 64, where the softmax is
+//               what they wait for (1,000 rows over 9,000: 403, with eight 407).  One piece of code for K and V: the roles'
 //               loops have to fit the instruction cache together (split apart,
 //               1,507 against 1,025 us for 4,000 rows of 16 heads, 8,000 tokens)
 // Shared memory holds one tile (Q, K and V of three terms: 192 KB), so a tile's
@@ -36,6 +39,7 @@ constexpr int NT = 3;   // terms
 
 template <int D>
 struct Smem {
+  static constexpr int SW = D == 128 ? 8 : 4;  // splitting warps
   static constexpr uint32_t kQ = BM * D * 2, kKV = BT * D * 2;
   alignas(1024) uint8_t q[NT][kQ];
   alignas(1024) uint8_t k[NT][kKV];
@@ -89,7 +93,7 @@ __device__ __forceinline__ int term_a(int c) { return c == 1 ? 2 : c == 2 || c =
 __device__ __forceinline__ int term_b(int c) { return c == 0 ? 2 : c == 2 || c == 3 ? 1 : 0; }
 
 template <int D>
-__global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ Launch L, WsHeader *hdr) {
+__global__ void __launch_bounds__((8 + Smem<D>::SW) * 32, 1) attend_tc_f32(const __grid_constant__ Launch L, WsHeader *hdr) {
   using S = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
   S &sm = *reinterpret_cast<S *>(smem_raw + ((0u - smem_addr(smem_raw)) & 1023u));
@@ -101,7 +105,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
     sm.flags[kAbort] = sm.flags[kRedoing] = 0;
     for (int b = 0; b < 2; ++b) {
       mbar_init(&sm.plan_full[b], 1);
-      mbar_init(&sm.plan_empty[b], 9);  // MMA, four softmax and four splitting warps
+      mbar_init(&sm.plan_empty[b], 5 + S::SW);  // MMA, four softmax and the splitting warps
       mbar_init(&sm.s_full[b], 1);
       mbar_init(&sm.p_full[b], 4);
       mbar_init(&sm.d_full[b], 1);
@@ -109,11 +113,11 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
     }
     mbar_init(&sm.ask, 1);
     mbar_init(&sm.next_full, 1);
-    mbar_init(&sm.q_full, 4);
+    mbar_init(&sm.q_full, S::SW);
     mbar_init(&sm.q_empty, 1);
-    mbar_init(&sm.k_full, 4);
+    mbar_init(&sm.k_full, S::SW);
     mbar_init(&sm.k_empty, 1);
-    mbar_init(&sm.v_full, 4);
+    mbar_init(&sm.v_full, S::SW);
     mbar_init(&sm.v_empty, 1);
     mbar_init(&sm.drain, 1);
     fence_mbar_init();
@@ -138,7 +142,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
   tc_fence_after();
   const uint32_t tm = sm.tmem;
 
-  // registers: 80 + 224 + 200 a thread of each group of four warps = 3 x 168
+  // registers a thread of each group of four warps: 80 + 224 + 200 = 3 x 168, or
+  // 80 + 224 + 2 x 104 = 4 x 128
   if (warp < 4) {
     regs_dec<80>();
     if (warp == 1) {
@@ -406,8 +411,9 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
     }
   } else {
     // ------------------------------------------------------------ split
-    regs_inc<200>();
-    constexpr int C4 = D / 4, NL = BT * C4 / 128;  // 16-byte pieces of a row, of a tile for each thread
+    if constexpr (S::SW == 8) regs_dec<104>();
+    else regs_inc<200>();
+    constexpr int C4 = D / 4, NL = BT * C4 / (32 * S::SW);  // 16-byte pieces of a row, of a tile for each thread
     const int tid = threadIdx.x - 256;
     uint32_t t = 0;
     bool ok = true;
@@ -432,7 +438,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
         const float *base = is_v ? vb : kb;
 #pragma unroll
         for (int k = 0; k < NL; ++k) {
-          const int e = k * 128 + tid, r = e / C4, c = e % C4;
+          const int e = k * 32 * S::SW + tid, r = e / C4, c = e % C4;
           x[k] = t0 + r < t1 ? *reinterpret_cast<const float4 *>(base + (int64_t)(t0 + r) * sg.st + 4 * c)
                              : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
@@ -440,16 +446,16 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
       fetch(0);
       if (n > 0 && !(ok = wait_warp(&sm.q_empty, (n - 1) & 1, flags))) break;
       {
-        // Q: a warp's 32 rows, D / 4 lanes to a row
-        constexpr int RW = 32 / C4 > 0 ? 32 / C4 : 1;
+        // Q: QR rows a warp, D / 4 lanes to a row
+        constexpr int RW = 32 / C4 > 0 ? 32 / C4 : 1, QR = BM / S::SW;
         const int32_t *qpos;
-        const int r32 = (warp - 8) * 32;
+        const int r32 = (warp - 8) * QR;
         const uint64_t src =
-            r32 + lane < pl.rows
+            lane < QR && r32 + lane < pl.rows
                 ? reinterpret_cast<uint64_t>(row_query<float>(L, sg, it, it.rt * BM + r32 + lane, D, qpos))
                 : 0;
 #pragma unroll 1
-        for (int k0 = 0; k0 < 32 / RW; k0 += 4) {
+        for (int k0 = 0; k0 < QR / RW; k0 += 4) {
           int r[4], c[4];
           float4 x[4];
 #pragma unroll
@@ -481,7 +487,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc_f32(const __grid_constant__ 
             float4 y[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int e = (k0 + k) * 128 + tid;
+              const int e = (k0 + k) * 32 * S::SW + tid;
               r[k] = e / C4, c[k] = e % C4, y[k] = x[k0 + k];
             }
             put_terms<BT>(tile, S::kKV, r, c, y);
@@ -508,7 +514,7 @@ cudaError_t launch(const Launch &L, WsHeader *hdr, cudaStream_t s, bool early) {
   static_assert(smem <= 232448, "shared memory");
   const cudaError_t e = cudaFuncSetAttribute(attend_tc_f32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_after(attend_tc_f32<D>, L.item_off[L.n_seg], 384, smem, s, early, L, hdr);
+  return launch_after(attend_tc_f32<D>, L.item_off[L.n_seg], (8 + Smem<D>::SW) * 32, smem, s, early, L, hdr);
 }
 
 }  // namespace
