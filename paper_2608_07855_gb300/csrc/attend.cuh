@@ -264,15 +264,18 @@ __device__ __forceinline__ float score_of(const T *q, const T *ki) {
 // A masked token's values have no part in it.  The tile kernels multiply masked
 // tokens by weights of zero, which is wrong where a masked value is infinite or
 // NaN, so they redo a row whose sums are not finite this way (its m and l never
-// see masked tokens).  32 tokens at a time, a lane each for the scores.
+// see masked tokens).  32 tokens at a time, a lane each for the scores.  Once the
+// row is NaN in every channel its values are not read any more; the sum of its
+// weights, where the caller wants it, is of all visible tokens all the same.
 template <typename T, int D>
 __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
-                                       Tiles tl, int tile, int j0, int j1, float m, float *o) {
+                                       Tiles tl, int tile, int j0, int j1, float m, float *o, bool want_sum) {
   const int lane = threadIdx.x & 31;
   const T *q = static_cast<const T *>(qrow);
   const T *k = static_cast<const T *>(sg.k) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
   const T *v = static_cast<const T *>(sg.v) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
   float lsum = 0.0f;
+  bool gone = false;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) o[c] = 0.0f;
   for (int j = j0; j < j1; ++j) {
@@ -282,6 +285,7 @@ __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, in
       const bool in = i < e && sees(sp, i);
       const float p = in ? exp2f(fmaf(score_of<T, D>(q, k + (int64_t)i * sg.st), L.scale_log2, -m)) : 0.0f;
       lsum += p;
+      if (gone) continue;
       const unsigned seen = __ballot_sync(0xffffffffu, in);
 #pragma unroll 8
       for (int u = 0; u < 32; ++u) {
@@ -294,7 +298,8 @@ __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, in
     bool done = true;  // NaN in every channel stays
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) done = done && isnan(o[c]);
-    if (__all_sync(0xffffffffu, done)) break;
+    gone = __all_sync(0xffffffffu, done);
+    if (gone && !want_sum) break;
   }
   return warp_sum(lsum);
 }

@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         const void *qb = row_query<__nv_bfloat16>(L, sg, it, r - lane + b, D, qpos);
         float o[D / 32];
         redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1, mb == -INFINITY ? 0.0f : mb,
-                                   o);
+                                   o, false);
         __syncwarp();
         write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, lb);
       }
