@@ -28,7 +28,9 @@ constexpr int64_t kMaxSplit = 768;
 // those of the prefix first.  NW warps to a row take kBatch parts each at a
 // time (no more registers than the call has parts, so that rows are in flight
 // together too), all loads of a batch in flight together: the call's time here is
-// latency (16 parts of 32 rows: 13 us a part after the other, 3.5 so).
+// latency (16 parts of 32 rows: 13 us a part after the other, 3.5 so).  A part
+// whose sum of weights is zero takes part like any other: it is zero, or NaN
+// where a token of score -inf has a value that is not finite.
 template <typename T, int D, int NW, int kBatch>
 __global__ void __launch_bounds__(128) combine(const __grid_constant__ Launch L) {
   constexpr int C = D / 32;  // channels of a lane: C lane ..
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(128) combine(const __grid_constant__ Launch L)
       const float wt = exp2f(ml[i].x - ref);
       lsum = fmaf(ml[i].y, wt, lsum);
 #pragma unroll
-      for (int c = 0; c < C; ++c) o[c] = ml[i].y != 0.0f ? fmaf(y[i][c], wt, o[c]) : o[c];
+      for (int c = 0; c < C; ++c) o[c] = fmaf(y[i][c], wt, o[c]);
     }
   }
   if constexpr (NW > 1) {
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(128) combine(const __grid_constant__ Launch L)
       const float wt = exp2f(sml[i].x - ref);
       lsum = fmaf(sml[i].y, wt, lsum);
 #pragma unroll
-      for (int c = 0; c < C; ++c) o[c] = sml[i].y != 0.0f ? fmaf(so[i][C * lane + c], wt, o[c]) : o[c];
+      for (int c = 0; c < C; ++c) o[c] = fmaf(so[i][C * lane + c], wt, o[c]);
     }
   }
   const int64_t row = row_index(L, t, l, kvh, r);
