@@ -259,6 +259,14 @@ __device__ __forceinline__ float score_of(const T *q, const T *ki) {
   return dot;
 }
 
+// The tile kernels take a weight as exp2 of the fused s scale - m, where m is the
+// rounded product for the largest s: up to half a step of m apart, the same
+// factor in all weights of the row.  Beyond |m| = 2^26 (half a step of 2) it
+// could pass the exponent's range, so such a row is done over with the product
+// rounded as m was.
+constexpr float kFar = 67108864.0f;
+__device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabsf(m) < INFINITY; }
+
 // sum of exp2(s - m) v and of exp2(s - m) over the visible tokens of tiles
 // [j0, j1) for one row, by the 32 lanes of a warp: o[k] is channel lane + 32 k.
 // A masked token's values have no part in it.  The tile kernels multiply masked
@@ -283,7 +291,7 @@ __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, in
     for (int i0 = a; i0 < e; i0 += 32) {
       const int i = i0 + lane;
       const bool in = i < e && sees(sp, i);
-      const float p = in ? exp2f(fmaf(score_of<T, D>(q, k + (int64_t)i * sg.st), L.scale_log2, -m)) : 0.0f;
+      const float p = in ? exp2f(__fmul_rn(score_of<T, D>(q, k + (int64_t)i * sg.st), L.scale_log2) - m) : 0.0f;
       lsum += p;
       if (gone) continue;
       const unsigned seen = __ballot_sync(0xffffffffu, in);
@@ -315,7 +323,7 @@ __device__ __noinline__ float redo_max(const Launch &L, const Seg &sg, int l, in
     const int e = tile_end(tl, j, tile);
     for (int i = tile_start(tl, j, tile) + (threadIdx.x & 31); i < e; i += 32) {
       if (!sees(sp, i)) continue;
-      const float s = score_of<T, D>(static_cast<const T *>(qrow), k + (int64_t)i * sg.st) * L.scale_log2;
+      const float s = __fmul_rn(score_of<T, D>(static_cast<const T *>(qrow), k + (int64_t)i * sg.st), L.scale_log2);
       bad = bad || isnan(s) || s == INFINITY;
       top = fmaxf(top, s);
     }

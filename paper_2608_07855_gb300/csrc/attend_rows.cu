@@ -355,22 +355,24 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
       for (int i = 0; i < NW; ++i) x[c] = fmaf(sm.o[i][r][lane + 32 * c], w[i], x[c]);
       fine = fine && isfinite(x[c]);
     }
-    if (!__all_sync(0xffffffffu, fine)) {
+    const bool far = is_far(mr);
+    if (far || !__all_sync(0xffffffffu, fine)) {
       const Span one = {__shfl_sync(0xffffffffu, mine.lo, r), __shfl_sync(0xffffffffu, mine.hi, r),
                         __shfl_sync(0xffffffffu, mine.se, r)};
       const void *qrow = reinterpret_cast<const void *>(__shfl_sync(0xffffffffu, qp, r));
+      // a visible infinite key, whose score may be -inf, is NaN in the split products of fp32
+      const bool anew = far || (F32 && !isfinite(lr));  // the maximum and the sum as well
       bool redo = isfinite(lr);
-      if constexpr (F32) {
-        // a visible infinite key, whose score may be -inf, is NaN in the split products
-        if (!redo) {
-          mr = redo_max<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1);
-          redo = !isnan(mr);
-        }
+      if (anew) {
+        const float top = redo_max<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1);
+        redo = !isnan(top);
+        if (redo) mr = top;
+        else lr = NAN;
       }
       if (redo) {
-        const float l2 = redo_row<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x,
-                                             F32 && !isfinite(lr));
-        if (F32 && !isfinite(lr)) lr = l2;
+        const float l2 =
+            redo_row<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x, anew);
+        if (anew) lr = l2;
       }
     }
     write_row_warp<T, D>(L, sg, it, r0 + r, x, mr, lr);

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Lau
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int tok = tx + 16 * t;
-        s[t] = tok < n && sees(sp[i], a + tok) ? (s2[i][t].x + s2[i][t].y) * L.scale_log2 : -INFINITY;
+        s[t] = tok < n && sees(sp[i], a + tok) ? __fmul_rn(s2[i][t].x + s2[i][t].y, L.scale_log2) : -INFINITY;
         mx = fmaxf(mx, s[t]);
       }
 #pragma unroll

@@ -634,22 +634,25 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (other) mbar_arrive(&sm.o_empty[1]);
         if (!two) mbar_arrive(&sm.pub_empty);
       }
-      unsigned bad = __ballot_sync(0xffffffffu, valid && chk != 0.0f && isfinite(lsum));
+      unsigned bad = __ballot_sync(0xffffffffu, valid && ((chk != 0.0f && isfinite(lsum)) || is_far(m)));
       const bool redo = bad != 0;
       if (redo) redoing(flags, 1);
-      while (bad) {  // a masked value that is not finite met a weight of zero
+      while (bad) {  // a masked value that is not finite met a weight of zero, or the scores are very large
         const int b = __ffs(bad) - 1;
         bad &= bad - 1;
         const Span one = {__shfl_sync(0xffffffffu, sp.lo, b), __shfl_sync(0xffffffffu, sp.hi, b),
                           __shfl_sync(0xffffffffu, sp.se, b)};
-        const float mb = __shfl_sync(0xffffffffu, m, b), lb = __shfl_sync(0xffffffffu, lsum, b);
+        float mb = __shfl_sync(0xffffffffu, m, b), lb = __shfl_sync(0xffffffffu, lsum, b);
         const int32_t *qpos;
         const void *qb = row_query<__nv_bfloat16>(L, sg, it, r - lane + b, D, qpos);
-        float o[D / 32];
-        redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1, mb == -INFINITY ? 0.0f : mb,
-                                   o, false);
+        const bool far = is_far(mb);
+        if (far) mb = redo_max<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1);
+        float o[D / 32] = {}, l2 = NAN;
+        if (!isnan(mb))  // else the row is NaN
+          l2 = redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1,
+                                          mb == -INFINITY ? 0.0f : mb, o, far);
         __syncwarp();
-        write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, lb);
+        write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, far ? l2 : lb);
       }
       if (redo) redoing(flags, -1);
     }

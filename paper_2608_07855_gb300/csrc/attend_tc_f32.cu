@@ -387,8 +387,9 @@ __global__ void __launch_bounds__((8 + Smem<D>::SW) * 32, 1) attend_tc_f32(const
       }
       const float chk = (ck[0] + ck[1]) + (ck[2] + ck[3]);
       // A value that is not finite: masked ones met a weight of zero, and an
-      // infinite key's terms are NaN though its score may be -inf.
-      unsigned bad = __ballot_sync(0xffffffffu, row < pl.rows && (chk != 0.0f || !isfinite(lsum)));
+      // infinite key's terms are NaN though its score may be -inf.  Or very
+      // large scores.
+      unsigned bad = __ballot_sync(0xffffffffu, row < pl.rows && (chk != 0.0f || !isfinite(lsum) || is_far(m)));
       const bool redo = bad != 0;
       if (redo) redoing(flags, 1);
       while (bad) {
@@ -399,13 +400,14 @@ __global__ void __launch_bounds__((8 + Smem<D>::SW) * 32, 1) attend_tc_f32(const
         float mk = __shfl_sync(0xffffffffu, m, k), lk = __shfl_sync(0xffffffffu, lsum, k);
         const int32_t *qpos;
         const float *qk = row_query<float>(L, sg, it, r - lane + k, D, qpos);
-        if (!isfinite(lk)) mk = redo_max<float, D>(L, sg, it.l, it.kvh, qk, one, pl.tl, BT, pl.j0, pl.j1);
-        if (isnan(mk)) continue;  // the row is NaN
-        float ok_[D / 32];
-        const float l2 = redo_row<float, D>(L, sg, it.l, it.kvh, qk, one, pl.tl, BT, pl.j0, pl.j1,
-                                            mk == -INFINITY ? 0.0f : mk, ok_, !isfinite(lk));
+        const bool anew = !isfinite(lk) || is_far(mk);  // the maximum and the sum as well
+        if (anew) mk = redo_max<float, D>(L, sg, it.l, it.kvh, qk, one, pl.tl, BT, pl.j0, pl.j1);
+        float ok_[D / 32] = {}, l2 = NAN;
+        if (!isnan(mk))  // else the row is NaN
+          l2 = redo_row<float, D>(L, sg, it.l, it.kvh, qk, one, pl.tl, BT, pl.j0, pl.j1, mk == -INFINITY ? 0.0f : mk, ok_,
+                                  anew);
         __syncwarp();
-        write_row_warp<float, D>(L, sg, it, r - lane + k, ok_, mk, isfinite(lk) ? lk : l2);
+        write_row_warp<float, D>(L, sg, it, r - lane + k, ok_, mk, anew ? l2 : lk);
       }
       if (redo) redoing(flags, -1);
     }

@@ -45,3 +45,46 @@ def test_values_of_nan_beside_scores_of_minus_infinity_alone(dtype, d, W):
 
     p = run(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(2500, W)], edit=edit)
     assert p.out[0][..., 5].isnan().all() and p.lse[0].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 40, 150])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("prefix", [0, 200])
+def test_scores_beyond_the_exponents_range(dtype, d, W, sign, prefix):
+    """Finite scores of 1e10 to 1e12, far apart: all weight is on the largest; a
+    NaN among them reaches the rows that see it.
+    Scores are products of two small integers and powers of two, so exact; a
+    weight of one times a value is off by the value's own terms and the
+    output's rounding; the reference times log 2 by two roundings, 2^-23."""
+    rng = np.random.RandomState(3)
+
+    def keys(k):
+        n = k.shape[2]
+        k.zero_()
+        k[..., 0] = torch.from_numpy(sign * 2.0 ** 16 * (1 + rng.randint(0, 200, n))).to(k.dtype)
+        # one largest score of every prefix of the text
+        k[:, :, 0, 0] = 2.0 ** 16 * (201 if sign > 0 else -0.25)
+
+    def edit(p):
+        for k, v, pos, q, qp in p.host:
+            keys(k)
+            q.zero_()
+            q[..., 0] = 2.0 ** 20
+        p.host[0][0][:, :, 899, 0] = float("nan")  # the last query's row
+        if prefix:
+            keys(p.pre[0])
+            for h in p.host:  # the prefix has the largest
+                h[0][..., 0] *= 2 if sign < 0 else 0.5
+
+    p = Problem(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(900, W), (300, W)], prefix=prefix,
+                edit=edit).upload()
+    p.call()
+    torch.cuda.synchronize()
+    eps = 2.0 ** -8 if dtype == BF else 2.0 ** -20
+    for i, (k, v, pos, q, qp) in enumerate(p.host):
+        parts = ([tuple(p.pre)] if prefix else []) + [(k, v, pos)]
+        o, l, _, _ = ref.attention(parts, q, qp)
+        ref.check(p.out[i], o, eps * np.abs(o) + 1e-30, "out %d" % i)
+        ref.check(p.lse[i], l, 2.0 ** -22 * np.abs(l), "lse %d" % i)
+    p.guards()
