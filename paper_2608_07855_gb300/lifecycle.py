@@ -7,7 +7,9 @@ library's entry points in the order of Algorithm 1:
   append       new tokens (decoded reasoning and tool calls, prefilled
                observations); tool-call and observation events are cut into
                pages from their first token, G tokens per page, the last page
-               taking the remainder (Section 3.1).
+               taking the remainder (Section 3.1).  A model that
+               computes its layers one after another appends the positions
+               first and writes each layer's K and V as it has them (fill).
   pre_commit   commit c_t: R- of every resident page over the pre-commit
                window (commitkv_page_effects); the non-retired pages form
                E_{c_t} and wait for their post-commit measurement.
@@ -28,7 +30,9 @@ library's entry points in the order of Algorithm 1:
                new tokens (a prompt chunk, or one decoded token) over the
                resident cache, whose positions have gaps after a checkpoint
                (commitkv_window_attention), or over a prefix that agents
-               share and the resident cache (commitkv_prefix_attention).
+               share and the resident cache (commitkv_prefix_attention); of
+               one layer, whose queries come from the layers below, or of all
+               (a probe window).
   post_commit  R+ over the post-commit window with the row stats;
                classification (Eq. 9-10, or an ablation variant of Section
                4.4); at most scan_cap candidates in order (the paper scans at
@@ -81,6 +85,8 @@ class Session:
         self.retired = set()  # D_c: accepted page ids still resident
         self.checkpoint_every = checkpoint_every  # decoded tokens between checkpoints (0: caller-driven only)
         self.decoded_since = 0  # decoded tokens appended since the last checkpoint
+        self.tail = (0, 0)      # resident tokens [a, b) of the latest append,
+        self.unfilled = set()   # and the layers that still lack their K and V
         self.ws = None
         self.attention_ws = None
 
@@ -105,6 +111,10 @@ class Session:
         if st != ck.COMMITKV_OK:
             raise RuntimeError(f"device status: {ck.status_string(st)}")
 
+    def _filled(self):
+        if self.unfilled:
+            raise ValueError(f"layers {sorted(self.unfilled)} lack K and V of the latest append")
+
     def page_ids(self):
         return [p[0] for p in self.pages]
 
@@ -115,6 +125,7 @@ class Session:
         of the latest pre-commit, the pages waiting for their post-commit
         measurement and D_c.  Tensors are copies on the session's device;
         torch.save writes the dict."""
+        self._filled()
         S = self.S
         return {
             "config": self._config(),
@@ -143,6 +154,7 @@ class Session:
         self.measured = list(st["measured"])
         self.retired = set(st["retired"])
         self.decoded_since = int(st.get("decoded_since", 0))
+        self.tail, self.unfilled = (S, S), set()
 
     def _config(self):
         s, th = self.shape, self.thresholds
@@ -158,14 +170,20 @@ class Session:
         positions [n] (device tensors); events = [(kind, first position,
         length)] of the tool calls and observations inside them; decoded =
         how many of the n the model decoded (reasoning, tool calls), for the
-        checkpoint cadence."""
+        checkpoint cadence.  With K and V None every layer's follow by fill."""
+        self._filled()
+        if (K is None) != (V is None):
+            raise ValueError("K and V together, or neither")
         self.decoded_since += int(decoded)
         n = int(pos.shape[0])
         if self.S + n > self.cap:
             raise ValueError("session capacity exceeded")
         S0, p0 = self.S, int(pos[0]) if n else 0
-        self.K[:, :, S0:S0 + n].copy_(K)
-        self.V[:, :, S0:S0 + n].copy_(V)
+        if K is not None:
+            self.K[:, :, S0:S0 + n].copy_(K)
+            self.V[:, :, S0:S0 + n].copy_(V)
+        self.tail = (S0, S0 + n)
+        self.unfilled = set(range(self.shape.layers)) if K is None and n else set()
         self.pos[S0:S0 + n].copy_(pos)
         self.S += n
         for kind, b, m in events:
@@ -175,15 +193,47 @@ class Session:
                 self.pages.append([self.next_id, S0 + (s - p0), min(self.G, b + m - s)])
                 self.next_id += 1
 
-    def attend(self, Q, qpos, window: int = 0, sinks: int = 0, prefix: ck.TrajTensors = None):
-        """Attention of the queries Q [M][Hq][W][d] at positions qpos [W]
-        (device tensors) over the resident cache, the new tokens appended
-        before: (out like Q, lse [M][Hq][W]).  window and sinks as in
-        commitkv_window_attention; prefix: a cache shared by agents, whose
-        positions come before this session's."""
+    def fill(self, layer: int, K, V):
+        """One layer's keys and values, [H][n][d] each, of the n tokens of the
+        latest append (which had none, or these are written over)."""
+        if not 0 <= layer < self.shape.layers:
+            raise ValueError(f"0 <= layer < {self.shape.layers}")
+        a, b = self.tail
+        want = (self.shape.kv_heads, b - a, self.shape.head_dim)
+        if tuple(K.shape) != want or tuple(V.shape) != want:
+            raise ValueError(f"K and V must be [H][n][d] = {want}")
+        self.K[layer, :, a:b].copy_(K)
+        self.V[layer, :, a:b].copy_(V)
+        self.unfilled.discard(layer)
+
+    def attend(self, Q, qpos, window: int = 0, sinks: int = 0, prefix: ck.TrajTensors = None, layer: int = None):
+        """Attention of the queries at positions qpos [W] (device tensors) over
+        the resident cache, the new tokens appended before: (out like Q, lse
+        without the channels).  With `layer`: that layer's, Q [Hq][W][d], as a
+        model calls it once it has filled the layer; without: all layers', Q
+        [M][Hq][W][d].  window and sinks as in commitkv_window_attention;
+        prefix: a cache of all layers shared by agents, whose positions come
+        before this session's."""
         torch = _torch()
         s, S = self.shape, self.S
-        tr = ck.TrajTensors(self.K[:, :, :S], self.V[:, :, :S], self.pos[:S], Q, qpos)
+        K, V = self.K, self.V
+        if layer is None:
+            self._filled()
+        else:
+            if not 0 <= layer < s.layers:
+                raise ValueError(f"0 <= layer < {s.layers}")
+            if layer in self.unfilled:
+                raise ValueError(f"layer {layer} lacks K and V of the latest append")
+            if Q.dim() != 3:
+                raise ValueError("a layer's Q is [Hq][W][d]")
+            one = slice(layer, layer + 1)
+            K, V, Q = K[one], V[one], Q[None]
+            if prefix is not None:
+                if prefix.k.shape[0] != s.layers:
+                    raise ValueError("a prefix has all layers")
+                prefix = ck.TrajTensors(prefix.k[one], prefix.v[one], prefix.pos)
+            s = ck.Shape(1, s.kv_heads, s.q_heads, s.head_dim, s.dtype, s.softmax_scale)
+        tr = ck.TrajTensors(K[:, :, :S], V[:, :, :S], self.pos[:S], Q, qpos)
         out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=self.dev)
         need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
         ws = self.attention_ws
@@ -195,13 +245,14 @@ class Session:
             ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
         else:
             ck.commitkv_prefix_attention(s, [tr], prefix, [out], [lse], window, sinks, workspace=ws)
-        return out, lse
+        return (out, lse) if layer is None else (out[0], lse[0])
 
     # ---------------------------------------------------------------- commit
     def pre_commit(self, Q, qpos):
         """R- (device float [P]) of every resident page over the pre-commit
         window Q [M][Hq][W][d], qpos [W]; the non-retired pages wait for their
         post-commit measurement."""
+        self._filled()
         torch = _torch()
         tr = self._traj(Q, qpos)
         ws = self._workspace(tr)
@@ -226,6 +277,7 @@ class Session:
         token's largest attention weight from the window Q [M][Hq][W][d],
         qpos [W] (commitkv_page_effects on the cache without pages for the
         window's row stats, then commitkv_token_scores)."""
+        self._filled()
         torch = _torch()
         s = self.shape
         S = self.S
@@ -249,6 +301,7 @@ class Session:
         """Compression checkpoint (Eq. 12-13, Eq. 4): fill = device float
         [S] per resident token.  Returns the retained resident indices I
         (device int32, ascending)."""
+        self._filled()
         torch = _torch()
         tr = self._traj()
         ws = self._workspace(tr)
@@ -277,6 +330,7 @@ class Session:
         self.pages, self.S = [[pid, a, b - a] for pid, (a, b) in zip(ids, spans) if b > a], n
         self.retired &= set(self.page_ids())
         self.decoded_since = 0
+        self.tail = (n, n)  # the latest append's tokens may have moved
         return idx[:n]
 
     def post_commit(self, Q, qpos):
@@ -284,6 +338,7 @@ class Session:
         returns dict(R_post (device [P]), cand, accepted (page ids in scan
         order / accepted ones), step_R (host list, one per scanned
         candidate))."""
+        self._filled()
         torch = _torch()
         tr = self._traj(Q, qpos)
         ws = self._workspace(tr)

@@ -1,0 +1,77 @@
+"""A session's own attention as a model uses it: layer by layer, on several
+streams, in graphs, with device errors reported."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_07855_gb300 import commitkv as ck  # noqa: E402
+from paper_2608_07855_gb300.lifecycle import Session  # noqa: E402
+
+import attention_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+BF = torch.bfloat16
+
+
+def i32(x):
+    return torch.from_numpy(np.ascontiguousarray(x, np.int32)).cuda()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("prefix", [0, 50])
+def test_model_of_several_layers(dtype, prefix):
+    """A small model runs through the session: a prompt, a checkpoint and decoded
+    tokens, where each layer's queries, keys and values are linear in what the
+    layer below put out.  Every layer's attention against 64 bits."""
+    M, H, Hq, d = 3, 2, 4, 64
+    g = torch.Generator(device="cuda").manual_seed(11)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    Wq, Wk, Wv = ([rand(Hq * d, h * d) / (Hq * d) ** 0.5 for _ in range(M)] for h in (Hq, H, H))
+    s = Session(ck.make_shape(M, H, Hq, d, dtype), 16, 96, 0.5, 400)
+    pre = None
+    if prefix:
+        pre = ck.TrajTensors(rand(M, H, prefix, d).to(dtype), rand(M, H, prefix, d).to(dtype), i32(np.arange(prefix)))
+    at = prefix
+    for n in (150, 1, 33, 1):
+        x = rand(n, Hq * d)  # the new tokens
+        pos = np.arange(at, at + n)
+        s.append(None, None, i32(pos), [("obs", at, n)], decoded=n == 1)
+        for layer in range(M):
+            heads = lambda w, h: (x @ w[layer]).view(n, h, d).transpose(0, 1).to(dtype).contiguous()  # noqa: E731, B023
+            s.fill(layer, heads(Wk, H), heads(Wv, H))
+            Q = heads(Wq, Hq)
+            o, lse = s.attend(Q, i32(pos), 120, 4, prefix=pre, layer=layer)
+            assert o.shape == Q.shape and lse.shape == Q.shape[:2]
+            parts = [] if pre is None else [(pre.k[layer:layer + 1].cpu(), pre.v[layer:layer + 1].cpu(), np.arange(prefix))]
+            parts.append((s.K[layer:layer + 1, :, :s.S].cpu(), s.V[layer:layer + 1, :, :s.S].cpu(), s.pos[:s.S].cpu().numpy()))
+            wo, wl, to, tl = ref.attention(parts, Q[None].cpu(), pos, 120, 4, rounded_weights=dtype == BF)
+            ref.check(o[None], wo, to, "layer %d" % layer)
+            ref.check(lse[None], wl, tl, "layer %d, lse" % layer)
+            x = x + o.transpose(0, 1).reshape(n, Hq * d).float()
+        at += n
+        if n == 150:
+            s.checkpoint(torch.rand(150, generator=g, device="cuda"))
+            assert s.S == 96
+            with pytest.raises(ValueError):  # the prompt's tokens have moved
+                s.fill(0, torch.zeros(H, 150, d, device="cuda"), torch.zeros(H, 150, d, device="cuda"))
+
+
+def test_layers_equal_one_call_over_all():
+    """Layer by layer and all layers at once agree where the queries are given."""
+    M, H, Hq, d, n = 3, 2, 8, 128, 300
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF)  # noqa: E731
+    s = Session(ck.make_shape(M, H, Hq, d, BF, 0.05), 16, 96, 0.5, 400)
+    s.append(rand(M, H, n, d), rand(M, H, n, d), i32(np.arange(n)), [])
+    for W in (1, 60):
+        Q, p = rand(M, Hq, W, d), i32(np.arange(n - W, n))
+        o, lse = s.attend(Q, p)
+        for layer in range(M):
+            a, b = s.attend(Q[layer], p, layer=layer)
+            parts = [(s.K[layer:layer + 1, :, :n].cpu(), s.V[layer:layer + 1, :, :n].cpu(), np.arange(n))]
+            wo, wl, to, tl = ref.attention(parts, Q[layer:layer + 1].cpu(), p.cpu().numpy(), scale=0.05, rounded_weights=True)
+            for out, l in ((a, b), (o[layer], lse[layer])):
+                ref.check(out[None], wo, to, "out")
+                ref.check(l[None], wl, tl, "lse")
