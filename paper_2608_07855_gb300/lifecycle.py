@@ -88,7 +88,9 @@ class Session:
         self.tail = (0, 0)      # resident tokens [a, b) of the latest append,
         self.unfilled = set()   # and the layers that still lack their K and V
         self.ws = None
-        self.attention_ws = None
+        self.attention_ws = None  # of eager attend calls
+        self.attended = False     # since the latest check
+        self.graph_ws = []        # of captured ones
 
     # ---------------------------------------------------------------- helpers
     def _traj(self, Q=None, qpos=None) -> ck.TrajTensors:
@@ -107,13 +109,29 @@ class Session:
         return self.ws
 
     def _check(self):
-        st = ck.commitkv_workspace_status(self.ws)
-        if st != ck.COMMITKV_OK:
-            raise RuntimeError(f"device status: {ck.status_string(st)}")
+        self._raise_status([self.ws])
+
+    def _raise_status(self, workspaces):
+        for st in [ck.commitkv_workspace_status(ws) for ws in workspaces]:
+            if st != ck.COMMITKV_OK:
+                raise RuntimeError(f"device status: {ck.status_string(st)}")
+
+    def check(self):
+        """Waits, and raises if the attention calls recorded a device error since
+        the latest check (attend by itself does not wait; the methods that
+        measure, compress or save check before they begin)."""
+        used = self.graph_ws + ([self.attention_ws] if self.attended else [])
+        self.attended = False
+        self._raise_status(used)
 
     def _filled(self):
         if self.unfilled:
             raise ValueError(f"layers {sorted(self.unfilled)} lack K and V of the latest append")
+
+    def _ready(self):
+        """Before the cache is measured, compressed or saved."""
+        self._filled()
+        self.check()
 
     def page_ids(self):
         return [p[0] for p in self.pages]
@@ -125,7 +143,7 @@ class Session:
         of the latest pre-commit, the pages waiting for their post-commit
         measurement and D_c.  Tensors are copies on the session's device;
         torch.save writes the dict."""
-        self._filled()
+        self._ready()
         S = self.S
         return {
             "config": self._config(),
@@ -213,7 +231,13 @@ class Session:
         model calls it once it has filled the layer; without: all layers', Q
         [M][Hq][W][d].  window and sinks as in commitkv_window_attention;
         prefix: a cache of all layers shared by agents, whose positions come
-        before this session's."""
+        before this session's.
+
+        Asynchronous: a device error (a wait that ran out; the outputs are then
+        unspecified) is raised by the next check, pre_commit, post_commit,
+        fill_scores, checkpoint or state_dict.  A captured call has a workspace of its own,
+        which the session keeps and reads there too: a replay clears it first,
+        so it tells of the latest replay."""
         torch = _torch()
         s, S = self.shape, self.S
         K, V = self.K, self.V
@@ -237,10 +261,16 @@ class Session:
         out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=self.dev)
         need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
         ws = self.attention_ws
-        if torch.cuda.is_current_stream_capturing():  # a graph's own, which outlives the session's
+        if torch.cuda.is_current_stream_capturing():
             ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
-        elif ws is None or ws.numel() < need:
-            ws = self.attention_ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+            self.graph_ws.append(ws)
+        else:
+            if ws is None or ws.numel() < need:
+                ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+                if self.attention_ws is not None:
+                    ws[:256].copy_(self.attention_ws[:256])  # the status so far
+                self.attention_ws = ws
+            self.attended = True
         if prefix is None:
             ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
         else:
@@ -252,7 +282,7 @@ class Session:
         """R- (device float [P]) of every resident page over the pre-commit
         window Q [M][Hq][W][d], qpos [W]; the non-retired pages wait for their
         post-commit measurement."""
-        self._filled()
+        self._ready()
         torch = _torch()
         tr = self._traj(Q, qpos)
         ws = self._workspace(tr)
@@ -277,7 +307,7 @@ class Session:
         token's largest attention weight from the window Q [M][Hq][W][d],
         qpos [W] (commitkv_page_effects on the cache without pages for the
         window's row stats, then commitkv_token_scores)."""
-        self._filled()
+        self._ready()
         torch = _torch()
         s = self.shape
         S = self.S
@@ -301,7 +331,7 @@ class Session:
         """Compression checkpoint (Eq. 12-13, Eq. 4): fill = device float
         [S] per resident token.  Returns the retained resident indices I
         (device int32, ascending)."""
-        self._filled()
+        self._ready()
         torch = _torch()
         tr = self._traj()
         ws = self._workspace(tr)
@@ -338,7 +368,7 @@ class Session:
         returns dict(R_post (device [P]), cand, accepted (page ids in scan
         order / accepted ones), step_R (host list, one per scanned
         candidate))."""
-        self._filled()
+        self._ready()
         torch = _torch()
         tr = self._traj(Q, qpos)
         ws = self._workspace(tr)

@@ -75,3 +75,54 @@ def test_layers_equal_one_call_over_all():
             for out, l in ((a, b), (o[layer], lse[layer])):
                 ref.check(out[None], wo, to, "out")
                 ref.check(l[None], wl, tl, "lse")
+
+
+@pytest.fixture
+def workspaces(monkeypatch):
+    """The attention workspaces that a session makes."""
+    made, alloc = [], ck.alloc_attention_workspace
+
+    def record(*a, **kw):
+        made.append(alloc(*a, **kw))
+        return made[-1]
+
+    monkeypatch.setattr(ck, "alloc_attention_workspace", record)
+    return made
+
+
+def small_session(n=400, H=2, d=64):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF)  # noqa: E731
+    s = Session(ck.make_shape(1, H, 4 * H, d, BF), 16, 96, 0.5, n)
+    s.append(rand(1, H, n, d), rand(1, H, n, d), i32(np.arange(n)), [("obs", 0, n)])
+    return s, rand
+
+
+@pytest.mark.parametrize("how", ["eager", "replaced", "captured"])
+@pytest.mark.parametrize("reader", ["check", "pre_commit", "post_commit", "fill_scores", "checkpoint", "state_dict"])
+def test_device_errors_of_attention_are_raised(how, reader, workspaces):
+    """A wait that ran out on an attention workspace (here the bounded barrier of
+    the test entry point) is raised by what the session does next, once."""
+    s, rand = small_session()
+    Q, p = rand(1, 8, 1, 64), i32([399])
+    if how == "captured":
+        s.attend(Q, p)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = s.attend(Q, p)  # noqa: F841
+        graph.replay()
+    else:
+        s.attend(Q, p)
+    ck.commitkv_test_barrier_timeout(workspaces[-1])
+    if how == "replaced":  # by a larger one
+        s.attend(rand(1, 8, 100, 64), i32(np.arange(300, 400)))
+        assert len(workspaces) == 2
+    call = {"check": s.check, "pre_commit": lambda: s.pre_commit(Q, p), "post_commit": lambda: s.post_commit(Q, p),
+            "fill_scores": lambda: s.fill_scores(Q, p), "state_dict": s.state_dict,
+            "checkpoint": lambda: s.checkpoint(torch.zeros(400, device="cuda"))}[reader]
+    with pytest.raises(RuntimeError, match="device status"):
+        call()
+    assert s.S == 400 and len(s.pages) == 25 and s.measured == []  # nothing was done
+    s.attend(Q, p)
+    s.check()
+    call()
