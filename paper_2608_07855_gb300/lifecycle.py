@@ -88,9 +88,9 @@ class Session:
         self.tail = (0, 0)      # resident tokens [a, b) of the latest append,
         self.unfilled = set()   # and the layers that still lack their K and V
         self.ws = None
-        self.attention_ws = None  # of eager attend calls
-        self.attended = False     # since the latest check
-        self.graph_ws = []        # of captured ones
+        self.attention_ws = {}  # of eager attend calls: by stream, since calls on two may overlap
+        self.attended = set()   # the streams since the latest check
+        self.graph_ws = []      # of captured ones
 
     # ---------------------------------------------------------------- helpers
     def _traj(self, Q=None, qpos=None) -> ck.TrajTensors:
@@ -109,19 +109,20 @@ class Session:
         return self.ws
 
     def _check(self):
-        self._raise_status([self.ws])
+        self._raise_status([(self.ws, None)])
 
     def _raise_status(self, workspaces):
-        for st in [ck.commitkv_workspace_status(ws) for ws in workspaces]:
+        for st in [ck.commitkv_workspace_status(ws, stream) for ws, stream in workspaces]:
             if st != ck.COMMITKV_OK:
                 raise RuntimeError(f"device status: {ck.status_string(st)}")
 
     def check(self):
-        """Waits, and raises if the attention calls recorded a device error since
-        the latest check (attend by itself does not wait; the methods that
-        measure, compress or save check before they begin)."""
-        used = self.graph_ws + ([self.attention_ws] if self.attended else [])
-        self.attended = False
+        """Waits for the attention calls of every stream, and raises if one
+        recorded a device error since the latest check (attend by itself does
+        not wait; the methods that measure, compress or save check before they
+        begin)."""
+        used = [(ws, None) for ws in self.graph_ws] + [(self.attention_ws[x], x) for x in sorted(self.attended)]
+        self.attended = set()
         self._raise_status(used)
 
     def _filled(self):
@@ -235,9 +236,10 @@ class Session:
 
         Asynchronous: a device error (a wait that ran out; the outputs are then
         unspecified) is raised by the next check, pre_commit, post_commit,
-        fill_scores, checkpoint or state_dict.  A captured call has a workspace of its own,
-        which the session keeps and reads there too: a replay clears it first,
-        so it tells of the latest replay."""
+        fill_scores, checkpoint or state_dict.  Calls on several streams may
+        overlap, each stream has a workspace.  A captured call has one of its
+        own, which the session keeps as long as it lives and reads there too: a
+        replay clears it first, so it tells of the latest replay."""
         torch = _torch()
         s, S = self.shape, self.S
         K, V = self.K, self.V
@@ -260,17 +262,17 @@ class Session:
         tr = ck.TrajTensors(K[:, :, :S], V[:, :, :S], self.pos[:S], Q, qpos)
         out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=self.dev)
         need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
-        ws = self.attention_ws
         if torch.cuda.is_current_stream_capturing():
             ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
             self.graph_ws.append(ws)
         else:
+            stream = torch.cuda.current_stream(self.K.device).cuda_stream
+            ws = old = self.attention_ws.get(stream)
             if ws is None or ws.numel() < need:
-                ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
-                if self.attention_ws is not None:
-                    ws[:256].copy_(self.attention_ws[:256])  # the status so far
-                self.attention_ws = ws
-            self.attended = True
+                ws = self.attention_ws[stream] = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+                if old is not None:
+                    ws[:256].copy_(old[:256])  # the status so far
+            self.attended.add(stream)
         if prefix is None:
             ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
         else:

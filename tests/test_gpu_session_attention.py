@@ -126,3 +126,32 @@ def test_device_errors_of_attention_are_raised(how, reader, workspaces):
     s.attend(Q, p)
     s.check()
     call()
+
+
+def test_streams_share_no_workspace(workspaces):
+    """Calls on two streams at once, prompts and single tokens that are split over
+    their tokens: a workspace for each stream, and the results of calls alone."""
+    s, rand = small_session(n=6000)
+    main = torch.cuda.current_stream()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    Q = [rand(1, 8, 1, 64), rand(1, 8, 70, 64)]
+    p = [i32(np.arange(6000 - q.shape[2], 6000)) for q in Q]
+    want = [s.attend(q, at) for q, at in zip(Q, p)]
+    torch.cuda.synchronize()
+    alone = len(workspaces)
+    for x in streams:
+        x.wait_stream(main)
+    got = [[], []]
+    for _ in range(20):
+        for i, x in enumerate(streams):
+            with torch.cuda.stream(x):
+                got[i].append(s.attend(Q[i], p[i]))
+    torch.cuda.synchronize()
+    made = workspaces[alone:]
+    assert len(made) == 2 and made[0].data_ptr() != made[1].data_ptr()
+    for w, outs in zip(want, got):
+        assert all(torch.equal(a, b) for o in outs for a, b in zip(o, w))
+    ck.commitkv_test_barrier_timeout(made[0], stream=streams[0])
+    with pytest.raises(RuntimeError, match="device status"):
+        s.check()
+    s.check()
