@@ -485,12 +485,21 @@ commitkv_status commitkv_compact_noalloc(const commitkv_shape *shape, int32_t n_
  *                trajectories or larger ones (S, W, n_traj), 256-byte aligned.
  * Outputs must not overlap inputs, the workspace or one another.
  * Which kernels run: where K, V, Q and the outputs are 16-byte aligned (pointers
- * and strides) the tensor cores, otherwise the CUDA cores.  Weights are fp32;
- * prompts of bf16 caches round them to bf16 for the product with the values
- * (up to 2^-8 of each, like the output's own rounding), decoded tokens to two
- * bf16 terms.  fp32 operands are taken as sums of two tf32 terms (decoded
- * tokens) or three bf16 terms (prompts), which loses up to 2^-21 or 2^-25 of
- * each.  The same call gives the same bits every time.
+ * and strides) the tensor cores, otherwise the CUDA cores.  Scores and sums of
+ * weights are fp32.  How a weight enters the product with the values goes by the
+ * rows that a KV head of a cache has: g W_t of a trajectory's own cache, and of
+ * a shared prefix those of all trajectories together.
+ *   bf16, up to 16 rows (decoded tokens): as two bf16 terms, 2^-17 of it is lost.
+ *   bf16, more rows (prompts; many agents' tokens behind a prefix): rounded to
+ *     bf16, by up to 2^-8 of it, like the output itself; where 16 rows at a time
+ *     take less time, as above.
+ *   fp32: every operand as two tf32 terms (up to 16 rows, or where they take
+ *     less time) or three bf16 terms (more), 2^-21 or 2^-25 of it is lost.
+ *   CUDA cores: as it is.
+ * So what a trajectory's output is rounded by depends on the other trajectories
+ * of the call.  The outputs of ordinary values are off in the 2-norm by 1.7e-3
+ * (bf16, up to 16 rows: their own rounding), 2.3e-3 (bf16, more rows) and below
+ * 1e-6 (fp32).  The same call gives the same bits every time.
  * -------------------------------------------------------------------- */
 commitkv_status commitkv_window_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
                                           const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,
