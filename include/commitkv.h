@@ -480,7 +480,11 @@ commitkv_status commitkv_compact_noalloc(const commitkv_shape *shape, int32_t n_
  *   lse_out      NULL, or host array [n_traj] of device float [M][Hq][W_t]
  *                (NULL entries allowed), natural logarithm.  With window = 0
  *                (m = lse, l = 1, o = out) are row statistics for
- *                commitkv_page_effects_from_stats.
+ *                commitkv_page_effects_from_stats: of fp32 caches as good as
+ *                its own; of bf16 caches out is rounded, and where that is off
+ *                by x |o_p| the effect of a page with attention mass A is off
+ *                by up to x (R + A / (1 - A)) more (x about 2e-3 on ordinary
+ *                values; stats_out of commitkv_page_effects is not rounded).
  *   workspace    at least commitkv_attention_workspace_size bytes for these
  *                trajectories or larger ones (S, W, n_traj), 256-byte aligned.
  * Outputs must not overlap inputs, the workspace or one another.
