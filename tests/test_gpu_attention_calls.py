@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 
 from paper_2608_07855_gb300 import commitkv as ck  # noqa: E402
 
-from test_gpu_attention import BF, SENT, Problem  # noqa: E402
+from test_gpu_attention import BF, F32, SENT, Problem, kernels  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +22,30 @@ def test_windows_and_sinks_that_32_bits_would_change(prefix, kw):
         p.call(**kw)
     torch.cuda.synchronize()
     assert (p.flat == SENT).all() and (p.flat_l == SENT).all()
+
+
+@pytest.mark.parametrize("dtype,d,H,g,many,prefix", [
+    (F32, 64, 4, 2, False, 0), (F32, 128, 4, 2, False, 0), (F32, 128, 4, 2, False, 900), (F32, 128, 2, 5, True, 0),
+    (BF, 128, 2, 5, False, 0), (BF, 64, 2, 5, False, 900), (BF, 128, 4, 4, True, 0), (BF, 128, 2, 5, True, 0)])
+def test_blocks_go_from_item_to_item(dtype, d, H, g, many, prefix, kernels):  # noqa: F811
+    """More work items than SMs, ragged ones and empty caches among them: of fp32
+    (whose widths differ in warps and barriers), and of bf16 where later items'
+    queries are not copied by TMA (heads that do not divide 128 rows, more than
+    32 trajectories)."""
+    if kernels == "cuda_cores":
+        pytest.skip("a block an item there")
+    trajs = [(300, 40), (0, 20), (420, 150), (700, 9), (64, 64), (333, 33)]
+    if many:
+        trajs = [((37 * i) % 400 if i % 9 else 0, 5 + (11 * i) % 40) for i in range(36)]
+    M = 24
+    p = Problem(dtype=dtype, d=d, M=M, H=H, Hq=g * H, prefix=prefix, gaps=0.8, trajs=trajs).upload()
+    for window, sinks in ((0, 0), (130, 3)):
+        p.flat.fill_(SENT)
+        p.flat_l.fill_(SENT)
+        p.call(window, sinks)
+        p.check(window, sinks, layers=[0, M - 1])
+        first = p.flat.clone(), p.flat_l.clone()
+        p.ws[256:].fill_(0xFF)
+        p.call(window, sinks)
+        torch.cuda.synchronize()
+        assert torch.equal(first[0], p.flat) and torch.equal(first[1], p.flat_l)
