@@ -327,8 +327,11 @@ int path_of(const Launch &L, const Seg &sg, const Forced &f) {
   return kTc;
 }
 
-// Tokens of a cache that a row tile needs, at most: with a window its rows see
-// `window` + `sinks` tokens each, their positions' span more.
+// Tokens of a cache that a row tile needs, estimated: with a window its rows see
+// `window` + `sinks` tokens each, their positions' span more.  No more than that
+// where a trajectory's queries are consecutive, or lie behind all of a shared
+// prefix (every window then ends at the prefix's end); queries in another order
+// may need up to all S, which the kernels find for themselves.
 int64_t most_seen(const Launch &L, const Seg &sg, int rows) {
   return L.window ? (int64_t)L.window + L.sinks + std::min(rows, sg.R) / L.g : sg.S;
 }
@@ -361,7 +364,7 @@ bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
   double few = 0.0, many = bf16 ? 15.0 : 18.0, tiles = 0.0, bytes = 0.0, start = bf16 ? 7.0 : 9.0;
   for (int s = 0; s < L.n_seg; ++s) {
     const Seg &sg = L.seg[s];
-    if (path[s] == kRows) start = 0.0;  // launched anyway
+    if (path[s] == kRows && sg.R > 0) start = 0.0;  // launched anyway
     if (path[s] != kTc && path[s] != kTcF32) continue;
     const int64_t seen = std::min<int64_t>(sg.S, most_seen(L, sg, many_pi.rows));
     few += few_us * slices * cdiv(sg.R, 16) * (cdiv(seen, few_pi.tile) + 1) / (2.0 * sms);
@@ -460,7 +463,8 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
       sg.nrt = (int32_t)cdiv(sg.R, pi.rows);
       v.base[v.n] = slices * sg.nrt;
       v.rows[v.n] = slices * sg.R;
-      v.tiles[v.n] = cdiv(std::min<int64_t>(sg.S, most_seen(L, sg, pi.rows)), pi.tile);
+      // a cache without queries has no items, however long
+      v.tiles[v.n] = sg.R > 0 ? cdiv(std::min<int64_t>(sg.S, most_seen(L, sg, pi.rows)), pi.tile) : 0;
       ids[v.n++] = s;
     }
     if (v.n == 0) continue;

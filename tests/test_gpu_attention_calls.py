@@ -49,3 +49,20 @@ def test_blocks_go_from_item_to_item(dtype, d, H, g, many, prefix, kernels):  # 
         p.call(window, sinks)
         torch.cuda.synchronize()
         assert torch.equal(first[0], p.flat) and torch.equal(first[1], p.flat_l)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,S,W", [(1, 2000, 1), (20, 2000, 100), (3, 900, 40)])
+def test_a_cache_without_queries_changes_nothing(dtype, n, S, W):
+    """The others' work is divided, and their results are, as without it."""
+    p = Problem(dtype=dtype, d=64, M=1, H=1, Hq=4, trajs=[(S + 10 * i, W) for i in range(n)]).upload()
+    p.call()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in p.out + p.lse]
+    long = 500000
+    K = torch.zeros(1, 1, long, 64, dtype=dtype, device="cuda")
+    rest = ck.TrajTensors(K, K, torch.arange(long, dtype=torch.int32, device="cuda"))
+    ck.commitkv_window_attention(p.shape, p.trajs + [rest], out=p.out + [None], lse_out=p.lse + [None], workspace=p.ws)
+    torch.cuda.synchronize()
+    p.guards()
+    assert all(torch.equal(a, b) for a, b in zip(want, p.out + p.lse))
