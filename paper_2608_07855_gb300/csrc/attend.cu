@@ -28,7 +28,7 @@ constexpr int64_t kMaxSplit = 768;
 // those of the prefix first.  NW warps to a row take kBatch parts each at a
 // time (no more registers than the call has parts, so that rows are in flight
 // together too), all loads of a batch in flight together: the call's time here is
-// latency (16 parts of 32 rows: 13 us a part after the other, 3.5 so).  A part
+// latency (3.5 us for 16 parts of 32 rows).  A part
 // whose sum of weights is zero takes part like any other: it is zero, or NaN
 // where a token of score -inf has a value that is not finite.
 template <typename T, int D, int NW, int kBatch>
@@ -190,7 +190,13 @@ int sm_count() {
 // How the row tiles of a path's segments are divided: estimated time in us of
 // `slots` concurrent items.  An item costs `fixed` tiles besides its own, a
 // call with partial results another kernel (kMergeUs) and their rows'
-// writing and reading back.  Measured: a three-prompt batch of 84 row tiles of
+// writing and reading back.  Estimates for this card at its clocks, which weigh
+// chunk lengths against one another.  To take tile_us and fixed again: event
+// times of calls of as many whole items as there are slots (152 slices of 256
+// rows, say) at two lengths; the slope is a tile, the rest is fixed, the launch
+// included.  Last so, for 128 channels: 256 rows of bf16 1.8 us, 128 of fp32 3.3,
+// 16 of bf16 1.4 and of fp32 1.9, on the CUDA cores 11.5 and 17; kPath's values
+// are of earlier calls.  Measured: a three-prompt batch of 84 row tiles of
 // 9 token tiles, 64 channels, 49 us in two chunks each, 28 whole; one token over
 // 4 caches of 4,096 tokens 15 us in chunks, 46 whole.
 constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3, kBytesPerUs = 6.5e6;
@@ -298,9 +304,10 @@ enum { kSimt16, kSimt64, kTc, kTcF32, kRows, kPaths };
 constexpr PathInfo kPath[kPaths] = {
     {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {128, 64, 1, 3.0, 2.7}, {16, 64, 2, 2.0, 1.4}};
 
-// For tests and diagnosis: COMMITKV_SCORING=simt takes the CUDA cores where a
-// call could have the tensor cores, COMMITKV_ATTENTION=tiles the kernels of row
-// tiles however few rows there are.
+// For tests and diagnosis, read in every call: COMMITKV_SCORING=simt takes the
+// CUDA cores where a call could have the tensor cores (attention as well as
+// scoring), COMMITKV_ATTENTION=tiles the kernels of row tiles however few rows
+// there are.
 struct Forced {
   bool cuda_cores, tiles;
 };
@@ -350,7 +357,8 @@ PathInfo path_info(const Launch &L, int p) {
 // Whether the segments of more than 16 rows go to the kernel of 16-row items as
 // well: it reads K and V again for every 16 rows, but has half the others'
 // start and end.  Estimates in us; measured there and here, bf16, 32 query on 8
-// KV heads of 128 channels: 8 queries over 1,000 tokens 17.4 and 11.4, over
+// KV heads of 128 channels (the constants here: fits to these calls, each run
+// both ways, with COMMITKV_ATTENTION=tiles and without): 8 queries over 1,000 tokens 17.4 and 11.4, over
 // 16,000 26.0 and 23.4, 16 over 4,000 18.5 and 17.1, 100 over 500 21.2 and
 // 15.3, 8 agents behind 16,000 31.8 and 27.2; 5 over 16 caches to 16,000 127
 // and 161, 12 over 16 to 1,000 23 and 31, 32 over 32,768 44 and 120.  fp32, 16

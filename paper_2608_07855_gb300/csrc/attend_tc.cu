@@ -307,8 +307,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
     } else if (warp == 1) {
       // ------------------------------------------------------------ MMAs
       // The whole warp keeps step and one elected lane issues: in code that a
-      // single lane runs, an MMA took 100 cycles to issue.  (A warp for each
-      // group: 2,330 against 2,050 us on a 4K prompt over 36K tokens.)
+      // single lane runs, an MMA took 100 cycles to issue.
       uint32_t g = 0, np[2] = {0, 0}, uses[2] = {0, 0};  // earlier items: tiles, tiles of each group, items that filled O_b
       bool ok = true;
       auto kv_wait = [&](uint32_t u) { return wait_warp(&sm.kv_full[u % NST], (u / NST) & 1, flags); };
@@ -470,8 +469,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         if (lane == 0) mbar_arrive(&sm.plan_full[buf]);
         if (n > 0 && !wait_warp(&sm.q_empty, (n - 1) & 1, flags)) break;
         if (n > 0 && P.has_q && sg.t >= 0) {
-          // between two items nothing else hides this copy (by the warp's own
-          // copies, as below: five prompts with an 86-token window 35 us, 32 so)
+          // between two items nothing else hides this copy: TMA, where it can
           if (lane == 0) {
             const int nq = rows > BM ? 2 : 1;
             mbar_expect_tx(&sm.q_full, nq * S::kTile);
@@ -588,9 +586,8 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
       float chk = 0.0f;
       if (warp_rows) {
         // 64 bytes of every row at a time through shared memory, so that four
-        // lanes store them side by side.  (Both groups and all SMs come here at
-        // the same time, with the tensor cores idle: with 16 channels a step and the
-        // rows' addresses exchanged in each a window of 4K took 246 us, 239 so.)
+        // lanes store them side by side, in few steps: both groups and all SMs
+        // come here at the same time, with the tensor cores idle.
         RowsOut rows_out(smem_addr(sm.stage[warp - 4]),
                          pdst ? reinterpret_cast<uint64_t>(pdst) : reinterpret_cast<uint64_t>(dst), lane);
 #pragma unroll 1

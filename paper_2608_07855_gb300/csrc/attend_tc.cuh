@@ -57,11 +57,8 @@ struct Plan {
 // barriers and the pipeline across items.  It asks kAsk tiles before its end:
 // long enough for the next item's plan, and not at the start, where the blocks
 // with the longest items would take the last ones too (20 prompts of up to 300
-// rows over up to 9,000 tokens: 301 us asking at the start, 274 so; 5 prompts
-// of 1,500: 229 and 207; short items lose most, 3 prompts of 2,452 without a
-// window: 203 and 206; 3 tiles or 9 are within 1 % of 6).
-// The warp that plans asks, told by the warp that copies (its asking itself: 2
-// us more on the windowed prompt).
+// rows over up to 9,000 tokens: 301 us asking at the start, 274 so; 3 tiles or 9
+// are within 1 % of 6).  The warp that plans asks, told by the warp that copies.
 constexpr int kAsk = 6;
 __device__ __forceinline__ void ask_next(uint4 *answer, uint64_t *bar) {
   fence_proxy_async();  // the last answer has been read
@@ -120,10 +117,8 @@ __device__ __forceinline__ Span row_sees(const Launch &L, const Seg &sg, const i
   return sp;
 }
 // What `rows` rows from r0 see, by a warp: a lane for each position, since the
-// rows of its g query heads see the same tokens (with gaps in the positions,
-// which cost searches, a lane a row took as long as nine tiles: three prompts of
-// up to 1,838 rows of 8 heads, a window of 1,030: 178.6 us, 162.2 so).  The rest of
-// the N rows has nothing to mask.
+// rows of its g query heads see the same tokens, and gaps in the positions cost
+// a search for each.  The rest of the N rows has nothing to mask.
 template <typename T, int D, int N>
 __device__ __forceinline__ void rows_see(const Launch &L, const Seg &sg, const Item &it, int r0, int rows, Span *span,
                                          int3 &u) {

@@ -3,7 +3,7 @@
 // Every fp32 operand is a sum of three bf16 terms, each the rounded rest of the
 // ones before (2^-25 of it is lost), and a product the six products of terms
 // whose places add up to at most two (the others are below 2^-24): six bf16
-// MMAs at 2,250 TFLOP/s against fp32's 80.  The MMA's sums are cut off, not
+// MMAs at 1,969 TFLOP/s (measured) against fp32's 80.  The MMA's sums are cut off, not
 // rounded, so P V of a tile is a sum by itself and the running O is kept in
 // fp32 registers.
 //
@@ -18,7 +18,9 @@
 //               MMAs run this one's.  Eight warps for 128 channels, whose splits
 //               the MMAs waited for with four (six prompts of 300 rows over up to
 //               9,000 tokens: 628 and 512 us), four for 64, where the softmax is
-//               what they wait for (1,000 rows over 9,000: 403, with eight 407).  One piece of code for K and V: the roles'
+//               what they wait for (1,000 rows over 9,000: 403, with eight 407).
+//               128 channels spill 80 bytes a thread and reload 200 (128 registers
+//               a thread at launch).  One piece of code for K and V: the roles'
 //               loops have to fit the instruction cache together (split apart,
 //               1,507 against 1,025 us for 4,000 rows of 16 heads, 8,000 tokens)
 // Shared memory holds one tile (Q, K and V of three terms: 192 KB), so a tile's
