@@ -501,7 +501,7 @@ def _attention(name, shape, trajs, prefix, out, lse_out, window, sinks, layer_ma
         raise ValueError("the outputs, the prefix and the shape are those of the batch")
     if (b._prefix is None) != (name == "commitkv_window_attention"):
         raise ValueError("commitkv_prefix_attention takes a prefix, commitkv_window_attention none")
-    if not all(-(1 << 31) <= x < 1 << 31 for x in (window, sinks)):
+    if not (-1 << 31 <= window < 1 << 31 and -1 << 31 <= sinks < 1 << 31):
         raise ValueError("window and sinks are 32-bit")
     torch = _torch()
     if workspace is None or workspace.get_device() != b.device or torch.cuda.current_device() != b.device:

@@ -89,7 +89,7 @@ class Session:
         self.unfilled = set()   # and the layers that still lack their K and V
         self.ws = None
         self.attention_ws = {}  # of eager attend calls: by stream, since calls on two may overlap
-        self.attended = set()   # the streams since the latest check
+        self.attended = {}      # by stream: the end of its latest one since the check
         self.graph_ws = []      # of captured ones
 
     # ---------------------------------------------------------------- helpers
@@ -109,20 +109,22 @@ class Session:
         return self.ws
 
     def _check(self):
-        self._raise_status([(self.ws, None)])
+        self._raise_status([self.ws])
 
     def _raise_status(self, workspaces):
-        for st in [ck.commitkv_workspace_status(ws, stream) for ws, stream in workspaces]:
+        for st in [ck.commitkv_workspace_status(ws) for ws in workspaces]:
             if st != ck.COMMITKV_OK:
                 raise RuntimeError(f"device status: {ck.status_string(st)}")
 
     def check(self):
-        """Waits for the attention calls of every stream, and raises if one
-        recorded a device error since the latest check (attend by itself does
-        not wait; the methods that measure, compress or save check before they
-        begin)."""
-        used = [(ws, None) for ws in self.graph_ws] + [(self.attention_ws[x], x) for x in sorted(self.attended)]
-        self.attended = set()
+        """Waits for the attention calls of every stream (and replays that the
+        current one is behind), and raises if one recorded a device error since
+        the latest check (attend by itself does not wait; the methods that
+        measure, compress or save check before they begin)."""
+        used = self.graph_ws + [self.attention_ws[x] for x in self.attended]
+        for end in self.attended.values():
+            end.wait()  # by the current stream, on which the status is read
+        self.attended = {}
         self._raise_status(used)
 
     def _filled(self):
@@ -262,6 +264,7 @@ class Session:
         tr = ck.TrajTensors(K[:, :, :S], V[:, :, :S], self.pos[:S], Q, qpos)
         out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=self.dev)
         need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
+        stream = None
         if torch.cuda.is_current_stream_capturing():
             ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
             self.graph_ws.append(ws)
@@ -272,11 +275,14 @@ class Session:
                 ws = self.attention_ws[stream] = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
                 if old is not None:
                     ws[:256].copy_(old[:256])  # the status so far
-            self.attended.add(stream)
         if prefix is None:
             ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
         else:
             ck.commitkv_prefix_attention(s, [tr], prefix, [out], [lse], window, sinks, workspace=ws)
+        if stream is not None:
+            if stream not in self.attended:
+                self.attended[stream] = torch.cuda.Event()
+            self.attended[stream].record()
         return (out, lse) if layer is None else (out[0], lse[0])
 
     # ---------------------------------------------------------------- commit

@@ -151,7 +151,9 @@ def test_streams_share_no_workspace(workspaces):
     assert len(made) == 2 and made[0].data_ptr() != made[1].data_ptr()
     for w, outs in zip(want, got):
         assert all(torch.equal(a, b) for o in outs for a, b in zip(o, w))
-    ck.commitkv_test_barrier_timeout(made[0], stream=streams[0])
+    with torch.cuda.stream(streams[0]):
+        ck.commitkv_test_barrier_timeout(made[0])  # a second, which the check waits for
+        s.attend(Q[0], p[0])
     with pytest.raises(RuntimeError, match="device status"):
         s.check()
     s.check()
