@@ -274,9 +274,11 @@ __device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabs
 // see masked tokens).  32 tokens at a time, a lane each for the scores.  Once the
 // row is NaN in every channel its values are not read any more; the sum of its
 // weights, where the caller wants it, is of all visible tokens all the same.
+// `fused`: the weights are as the caller's own sum has them (see is_far), not
+// relative to an m that is a rounded product.
 template <typename T, int D>
 __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
-                                       Tiles tl, int tile, int j0, int j1, float m, float *o, bool want_sum) {
+                                       Tiles tl, int tile, int j0, int j1, float m, float *o, bool want_sum, bool fused) {
   const int lane = threadIdx.x & 31;
   const T *q = static_cast<const T *>(qrow);
   const T *k = static_cast<const T *>(sg.k) + (int64_t)l * sg.sl + (int64_t)kvh * sg.sh;
@@ -290,7 +292,11 @@ __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, in
     for (int i0 = a; i0 < e; i0 += 32) {
       const int i = i0 + lane;
       const bool in = i < e && sees(sp, i);
-      const float p = in ? exp2f(__fmul_rn(score_of<T, D>(q, k + (int64_t)i * sg.st), L.scale_log2) - m) : 0.0f;
+      float p = 0.0f;
+      if (in) {
+        const float s = score_of<T, D>(q, k + (int64_t)i * sg.st);
+        p = exp2f(fused ? fmaf(s, L.scale_log2, -m) : __fmul_rn(s, L.scale_log2) - m);
+      }
       lsum += p;
       if (gone) continue;
       const unsigned seen = __ballot_sync(0xffffffffu, in);

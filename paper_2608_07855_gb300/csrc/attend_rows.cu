@@ -371,7 +371,8 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
       }
       if (redo) {
         const float l2 =
-            redo_row<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x, anew);
+            redo_row<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x, anew,
+                           !anew);
         if (anew) lr = l2;
       }
     }

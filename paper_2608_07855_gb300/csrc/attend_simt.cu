@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(NT, 2) attend_simt(const __grid_constant__ Lau
     const float mr = sml[2 * r], lr = sml[2 * r + 1];
     if (!__all_sync(0xffffffffu, fine) && isfinite(lr)) {
       const Span one = {sm.lo[r], sm.hi[r], sm.se[r]};
-      redo_row<T, D>(L, sg, it.l, it.kvh, sm.qrow[r], one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x, false);
+      redo_row<T, D>(L, sg, it.l, it.kvh, sm.qrow[r], one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x, false,
+                     false);
     }
     write_row_warp<T, D>(L, sg, it, r0 + r, x, mr, lr);
   }

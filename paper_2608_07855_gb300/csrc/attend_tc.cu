@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         float o[D / 32] = {}, l2 = NAN;
         if (!isnan(mb))  // else the row is NaN
           l2 = redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1,
-                                          mb == -INFINITY ? 0.0f : mb, o, far);
+                                          mb == -INFINITY ? 0.0f : mb, o, far, !far);
         __syncwarp();
         write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, far ? l2 : lb);
       }

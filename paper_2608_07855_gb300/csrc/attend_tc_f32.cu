@@ -407,7 +407,7 @@ __global__ void __launch_bounds__((8 + Smem<D>::SW) * 32, 1) attend_tc_f32(const
         float ok_[D / 32] = {}, l2 = NAN;
         if (!isnan(mk))  // else the row is NaN
           l2 = redo_row<float, D>(L, sg, it.l, it.kvh, qk, one, pl.tl, BT, pl.j0, pl.j1, mk == -INFINITY ? 0.0f : mk, ok_,
-                                  anew);
+                                  anew, !anew);
         __syncwarp();
         write_row_warp<float, D>(L, sg, it, r - lane + k, ok_, mk, anew ? l2 : lk);
       }

@@ -88,3 +88,34 @@ def test_scores_beyond_the_exponents_range(dtype, d, W, sign, prefix):
         ref.check(p.out[i], o, eps * np.abs(o) + 1e-30, "out %d" % i)
         ref.check(p.lse[i], l, 2.0 ** -22 * np.abs(l), "lse %d" % i)
     p.guards()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W", [1, 40, 150])
+@pytest.mark.parametrize("size", [2.0 ** 4, 2.0 ** 11, 2.0 ** 17])
+def test_values_of_nan_beside_large_scores(dtype, d, W, size):
+    """Rows that are done over for a value of NaN, seen in one channel or masked,
+    with scores of 1e4 to 1e8, many of them equal: their weights fit the sum that
+    they had before.  Scores are exact, and equal or far apart; beside the sums of
+    up to a thousand equal weights and of their values in fp32 there are the
+    roundings of weights and outputs."""
+    rng = np.random.RandomState(5)
+
+    def edit(p):
+        for k, v, pos, q, qp in p.host:
+            k.zero_()
+            k[..., 0] = torch.from_numpy(size * (100.0 + 27 * rng.randint(0, 2, k.shape[2]))).to(k.dtype)
+            q.zero_()
+            q[..., 0] = 32.0 * 3
+            v[:, :, -1 - W // 2, 5] = float("nan")
+
+    p = Problem(dtype=dtype, d=d, M=1, H=1, Hq=4, trajs=[(900, W), (333, W)], edit=edit).upload()
+    p.call(170)
+    torch.cuda.synchronize()
+    eps = 2.0 ** -7 if dtype == BF else 2.0 ** -17
+    for i, (k, v, pos, q, qp) in enumerate(p.host):
+        o, l, _, _ = ref.attention([(k, v, pos)], q, qp, 170)
+        spread = ref.attention([(k, v.abs(), pos)], q, qp, 170)[0]
+        ref.check(p.out[i], o, eps * spread, "out %d" % i)
+        ref.check(p.lse[i], l, 2.0 ** -22 * np.abs(l) + 2.0 ** -16, "lse %d" % i)
+    p.guards()
