@@ -260,7 +260,8 @@ __device__ __forceinline__ float score_of(const T *q, const T *ki) {
 
 // The tile kernels take a weight as exp2 of the fused s scale - m, where m is the
 // rounded product for the largest s: up to half a step of m apart, the same
-// factor in all weights of the row.  Beyond |m| = 2^26 (half a step of 2) it
+// factor in all weights of the row (the product is __fmul_rn, so that no
+// difference of two references is fused with it).  Beyond |m| = 2^26 (half a step of 2) it
 // could pass the exponent's range, so such a row is done over with the product
 // rounded as m was.
 constexpr float kFar = 67108864.0f;
@@ -274,8 +275,8 @@ __device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabs
 // see masked tokens).  32 tokens at a time, a lane each for the scores.  Once the
 // row is NaN in every channel its values are not read any more; the sum of its
 // weights, where the caller wants it, is of all visible tokens all the same.
-// `fused`: the weights are as the caller's own sum has them (see is_far), not
-// relative to an m that is a rounded product.
+// `fused`: the weights are as the caller's own and other parts' sums have them,
+// with the fused product (see is_far), not the one that m is.
 template <typename T, int D>
 __device__ __noinline__ float redo_row(const Launch &L, const Seg &sg, int l, int kvh, const void *qrow, Span sp,
                                        Tiles tl, int tile, int j0, int j1, float m, float *o, bool want_sum, bool fused) {

@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
           top = fmaxf(top, x);
         }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * L.scale_log2;
+      top = __fmul_rn(fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)), L.scale_log2);
       const bool raise = top > m[h] + kLazy;
       if (__any_sync(0xffffffffu, raise)) {
         const float f = raise ? (m[h] == -INFINITY ? 0.0f : exp2f(m[h] - top)) : 1.0f;
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(NW * 32, 2) attend_rows(const __grid_constant_
       if (redo) {
         const float l2 =
             redo_row<T, D>(L, sg, it.l, it.kvh, qrow, one, tl, TT, j0, j1, mr == -INFINITY ? 0.0f : mr, x, anew,
-                           !anew);
+                           !is_far(mr));
         if (anew) lr = l2;
       }
     }

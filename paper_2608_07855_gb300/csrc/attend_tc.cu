@@ -166,7 +166,7 @@ __device__ __forceinline__ void soft_full(uint32_t s_col, uint32_t o_col, float 
   for (int i = 0; i < BT; i += 8)
 #pragma unroll
     for (int k = 0; k < 4; ++k) mx[k] = fmax3(mx[k], x[i + 2 * k], x[i + 2 * k + 1]);
-  raise_max<D>(o_col, fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]) * scale, m, lsum);
+  raise_max<D>(o_col, __fmul_rn(fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]), scale), m, lsum);
   const float neg = m == -INFINITY ? 0.0f : -m;
   const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(neg, neg);
   float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
@@ -200,7 +200,7 @@ __device__ __forceinline__ void soft_masked(uint32_t s_col, uint32_t o_col, floa
     load(c);
     top = max32(x, top);
   }
-  raise_max<D>(o_col, top * scale, m, lsum);
+  raise_max<D>(o_col, __fmul_rn(top, scale), m, lsum);
   const float neg = m == -INFINITY ? 0.0f : -m;
   const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(neg, neg);
   float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(384, 1) attend_tc(const __grid_constant__ TcPa
         float o[D / 32] = {}, l2 = NAN;
         if (!isnan(mb))  // else the row is NaN
           l2 = redo_row<__nv_bfloat16, D>(L, sg, it.l, it.kvh, qb, one, pl.tl, BT, pl.j0, pl.j1,
-                                          mb == -INFINITY ? 0.0f : mb, o, far, !far);
+                                          mb == -INFINITY ? 0.0f : mb, o, far, !is_far(mb));
         __syncwarp();
         write_row_warp<__nv_bfloat16, D>(L, sg, it, r - lane + b, o, mb, far ? l2 : lb);
       }

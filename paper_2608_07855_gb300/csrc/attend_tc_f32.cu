@@ -318,7 +318,7 @@ __global__ void __launch_bounds__((8 + Smem<D>::SW) * 32, 1) attend_tc_f32(const
 #pragma unroll
           for (int i = 0; i < 32; i += 2) top = fmax3(top, x[i], x[i + 1]);
         }
-        top *= L.scale_log2;
+        top = __fmul_rn(top, L.scale_log2);
         const bool raise = top > m + kLazy;  // false while both are -inf
         const float f = raise && m != -INFINITY ? exp2f(m - top) : 1.0f;
         if (raise) m = top;
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__((8 + Smem<D>::SW) * 32, 1) attend_tc_f32(const
         float ok_[D / 32] = {}, l2 = NAN;
         if (!isnan(mk))  // else the row is NaN
           l2 = redo_row<float, D>(L, sg, it.l, it.kvh, qk, one, pl.tl, BT, pl.j0, pl.j1, mk == -INFINITY ? 0.0f : mk, ok_,
-                                  anew, !anew);
+                                  anew, !is_far(mk));
         __syncwarp();
         write_row_warp<float, D>(L, sg, it, r - lane + k, ok_, mk, anew ? l2 : lk);
       }

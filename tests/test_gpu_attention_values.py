@@ -119,3 +119,35 @@ def test_values_of_nan_beside_large_scores(dtype, d, W, size):
         ref.check(p.out[i], o, eps * spread, "out %d" % i)
         ref.check(p.lse[i], l, 2.0 ** -22 * np.abs(l) + 2.0 ** -16, "lse %d" % i)
     p.guards()
+
+
+@pytest.mark.parametrize("W", [1, 40])
+@pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 12, 2.0 ** 16])
+@pytest.mark.parametrize("where", ["own", "prefix"])
+def test_equal_scores_in_parts_that_are_done_over_and_others(W, size, where, kernels):  # noqa: F811
+    """Large equal scores in the prefix and in the cache, one of which has a key of
+    score -inf, so that its parts are done over: all weigh the same.  Scores are
+    127 size / 8, exact but for the rounding of scale / log 2, which is the same
+    for all, and of the CUDA cores' product."""
+    def keys(k, far):
+        k.zero_()
+        k[:, :, 7::50, 0] = 127.0 * size
+        if far:
+            k[:, :, 5::50, 1] = float("-inf")
+
+    def edit(p):
+        k, v, pos, q, qp = p.host[0]
+        q.zero_()
+        q[..., :2] = 1.0
+        keys(k, where == "own")
+        keys(p.pre[0], where == "prefix")
+
+    p = Problem(dtype=torch.float32, d=64, M=1, H=1, Hq=4, trajs=[(900, W)], prefix=700, edit=edit).upload()
+    p.call()
+    torch.cuda.synchronize()
+    k, v, pos, q, qp = p.host[0]
+    parts = [tuple(p.pre), (k, v, pos)]
+    o, l, _, _ = ref.attention(parts, q, qp)
+    spread = ref.attention([(a, b.abs(), c) for a, b, c in parts], q, qp)[0]
+    ref.check(p.out[0], o, 2.0 ** -17 * spread, "out")
+    ref.check(p.lse[0], l, 2.0 ** -22 * np.abs(l), "lse")
