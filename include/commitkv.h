@@ -536,6 +536,140 @@ commitkv_status commitkv_prefix_attention(const commitkv_shape *shape, int32_t n
 size_t commitkv_attention_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
                                          const commitkv_traj *prefix);
 
+/* ------------------------------------------------------------------------
+ * Packed caches: K and V held in 4 bits, 0.27 of the bytes of bf16.  A row of
+ * d channels (one token of one layer and KV head, of K or V) is
+ *     d / 2 bytes of codes  channel 2 j in the low, 2 j + 1 in the high four
+ *                           bits of byte j,
+ *     d / 32 scale bytes    one for each 32 channels,
+ * and stands for the values
+ *     (code - 8) sigma(b),   sigma(b) = 2^-6 times the fp16 number with the bits
+ *                            b << 7  for b < 0xf8 (0 to 960 in steps of 2^-3 of
+ *                            its binade, 2^-23 below 2^-20), NaN for b >= 0xf8.
+ * Code and sigma have four significant bits each, so every value is a bf16
+ * number: reading a row back is exact, and the entry points below compute with
+ * the values themselves, not with values rounded once more.
+ * -------------------------------------------------------------------- */
+
+/* One trajectory's packed cache; the rest as in commitkv_traj.
+ *   k, v        codes: the row of (layer l, KV head h, token i) of K starts at
+ *               k + l*stride_layer + h*stride_head + i*stride_tok (bytes).
+ *   k_scale, v_scale   scale bytes, the same with scale_layer, scale_head and
+ *               scale_tok.
+ * Any alignment and any strides (of at least a row for tokens, not negative);
+ * the fastest kernels want codes 16-byte aligned and scales d / 32 bytes aligned
+ * (pointers and strides).
+ */
+typedef struct {
+  uint8_t *k, *v;
+  int64_t stride_layer, stride_head, stride_tok;
+  uint8_t *k_scale, *v_scale;
+  int64_t scale_layer, scale_head, scale_tok;
+  int32_t *pos;
+  int32_t S;
+  const void *q;
+  const int32_t *q_pos;
+  int32_t W;
+  const int32_t *page_start;
+  const int32_t *page_len;
+  int32_t P;
+} commitkv_packed;
+
+/* Full-width rows, dtype of the shape, that stand at tokens first .. first +
+ * count - 1 of a packed cache.  Element (l, h, i, c) of K lives at
+ * k + l*stride_layer + h*stride_head + i*stride_tok + c, 0 <= i < count (strides
+ * in elements, any; the d channels are contiguous). */
+typedef struct {
+  void *k;
+  void *v;
+  int64_t stride_layer, stride_head, stride_tok;
+  int32_t first;
+  int32_t count;
+} commitkv_rows;
+
+/* ------------------------------------------------------------------------
+ * Writes rows into packed caches: K and V of new tokens as they are appended.
+ * Of each 32 channels x, with a = max |x|:
+ *     sigma = the number sigma(b), b < 0xf8, nearest to a / 7, of two as near the
+ *             one of even b (so 960 where a is above 6720);
+ *     code  = 8 + n, n the integer nearest to x / sigma, of two as near the even
+ *             one, at most 7 away from 0; 8 where sigma = 0.
+ * Both go by the exact quotients, so equal rows have equal codes wherever they
+ * are written.  A value is off by at most sigma / 2 while a is between 2^-18 and
+ * 6720 (7.5 sigma there at least reach a).  32 channels of which one is infinite
+ * or NaN get scale byte 0xff and codes 8: they read back as NaN.
+ *
+ *   caches       k, v, their scales and strides are used; first + count must not
+ *                exceed S.  Positions are the caller's to write.
+ *   rows         host array [n_traj]; count = 0: nothing is written.
+ *   layer_mask   as for commitkv_page_effects; other layers are left alone.
+ * Rows must not overlap the caches, or caches of a call one another.
+ * -------------------------------------------------------------------- */
+commitkv_status commitkv_packed_write(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *caches,
+                                      const commitkv_rows *rows, const uint8_t *layer_mask, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Reads rows of packed caches back, exactly, in the dtype of the shape: what
+ * the calls on full-width caches (page effects, joint test, token scores) take.
+ * Arguments as for commitkv_packed_write; rows of other layers are not written.
+ * -------------------------------------------------------------------- */
+commitkv_status commitkv_packed_read(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *caches,
+                                     const commitkv_rows *rows, const uint8_t *layer_mask, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * commitkv_window_attention over packed caches: the same sums, masks, outputs,
+ * errors and limits, over the values that the caches stand for.  A NaN scale of
+ * a visible token's values makes the 32 channels of the rows that see it NaN; of
+ * its keys, the whole rows.  What tokens hold that a query does not see does not
+ * reach its output.
+ *
+ *   workspace    at least commitkv_packed_workspace_size bytes for these
+ *                trajectories or larger ones (S, W, n_traj), 256-byte aligned.
+ * Which kernels run, by the rows g W_t of a trajectory:
+ *   up to 16, codes and scales aligned: tensor cores, on the codes as they are.  Scores
+ *     and sums are fp32; queries and weights enter the products as fp16 terms
+ *     relative to their row's largest: one (bf16: a query is kept whole, 2^-12 of
+ *     a weight is lost) or two (fp32: 2^-22 is lost).
+ *   more: the values are read back a layer at a time (at least) into the workspace, where
+ *     the kernels of commitkv_window_attention take them, with its precision.
+ *   other alignments: CUDA cores in fp32.
+ * The same call gives the same bits every time.
+ * -------------------------------------------------------------------- */
+commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs,
+                                          const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,
+                                          float *const *lse_out, void *workspace, size_t workspace_bytes,
+                                          cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * commitkv_compact and commitkv_compact_in_place for packed caches: the same
+ * selection, arguments and errors; codes, scale bytes and positions of the
+ * retained tokens move as they are.
+ *
+ *   dst          NULL: in place, as commitkv_compact_in_place (k, v, their
+ *                scales and pos of every cache with S > 0 must be there).  Or
+ *                host array [n_traj] of the caches that receive the retained
+ *                tokens as their first |I_j| ones: k, v, scales and strides are
+ *                used, S >= min(budget_B, S of the cache) is their room, pos may
+ *                be NULL (not written); rows behind |I_j| are left alone.  They
+ *                must not overlap the caches or one another.
+ *   workspace    at least commitkv_packed_workspace_size bytes.
+ * -------------------------------------------------------------------- */
+commitkv_status commitkv_packed_compact(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *cache,
+                                        const uint8_t *const *retired, const int32_t *const *pending,
+                                        const int32_t *n_pending, const float *const *pending_priority,
+                                        const float *const *fill_score, int32_t budget_B, int32_t pending_tokens_BN,
+                                        int32_t pending_cap_pages, int32_t *const *idx_out, int32_t *n_idx_out,
+                                        const commitkv_packed *dst, void *workspace, size_t workspace_bytes,
+                                        cudaStream_t stream);
+
+/* Size in bytes of the workspace of commitkv_packed_attention and
+ * commitkv_packed_compact for these trajectories, for fewer of them, smaller
+ * caches or fewer queries.  Where a trajectory has more than 16 rows g W_t (or
+ * codes or scales are not aligned as above: no difference) it has room for the
+ * values of one layer of all such trajectories.  Returns 0 for invalid
+ * arguments. */
+size_t commitkv_packed_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs);
+
 #ifdef __cplusplus
 }
 #endif

@@ -53,6 +53,22 @@ class Traj(ctypes.Structure):
                 ("P", ctypes.c_int32)]
 
 
+class Packed(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("stride_layer", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("scale_layer", ctypes.c_int64), ("scale_head", ctypes.c_int64), ("scale_tok", ctypes.c_int64),
+                ("pos", ctypes.c_void_p), ("S", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("q_pos", ctypes.c_void_p), ("W", ctypes.c_int32),
+                ("page_start", ctypes.c_void_p), ("page_len", ctypes.c_void_p), ("P", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride_layer", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64), ("first", ctypes.c_int32),
+                ("count", ctypes.c_int32)]
+
+
 class Thresholds(ctypes.Structure):
     _fields_ = [("tau_use", ctypes.c_float), ("tau_dead", ctypes.c_float),
                 ("rho_use", ctypes.c_float), ("rho_dead", ctypes.c_float)]
@@ -106,11 +122,19 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.commitkv_attention_workspace_size.restype = sz
     lib.commitkv_window_attention.argtypes = [P(Shape), i32, P(Traj), vp, i32, i32, vp, vp, vp, sz, vp]
     lib.commitkv_prefix_attention.argtypes = [P(Shape), i32, P(Traj), P(Traj), vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.commitkv_packed_workspace_size.argtypes = [P(Shape), i32, P(Packed)]
+    lib.commitkv_packed_workspace_size.restype = sz
+    lib.commitkv_packed_write.argtypes = [P(Shape), i32, P(Packed), P(Rows), vp, vp]
+    lib.commitkv_packed_read.argtypes = [P(Shape), i32, P(Packed), P(Rows), vp, vp]
+    lib.commitkv_packed_attention.argtypes = [P(Shape), i32, P(Packed), vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.commitkv_packed_compact.argtypes = [P(Shape), i32, P(Packed), vp, vp, vp, vp, vp, i32, i32, i32, vp, vp,
+                                            P(Packed), vp, sz, vp]
     for f in ("commitkv_workspace_init", "commitkv_workspace_status", "commitkv_page_effects",
               "commitkv_page_effects_from_stats", "commitkv_classify", "commitkv_classify_variant",
               "commitkv_joint_test", "commitkv_compact", "commitkv_compact_in_place", "commitkv_compact_noalloc",
               "commitkv_test_barrier_timeout", "commitkv_test_pruned_pages", "commitkv_token_scores",
-              "commitkv_window_attention", "commitkv_prefix_attention"):
+              "commitkv_window_attention", "commitkv_prefix_attention", "commitkv_packed_write", "commitkv_packed_read",
+              "commitkv_packed_attention", "commitkv_packed_compact"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -216,6 +240,54 @@ class TrajTensors:
                     0 if q is None else q.shape[2], start, length, 0 if ps is None else ps.numel())
 
 
+@dataclass
+class PackedTensors:
+    """One trajectory's packed cache: device tensors in 4 bits a value.
+
+    k, v: codes [M][H][S][d / 2] uint8 views (any strides with contiguous bytes
+    of a row), k_scale, v_scale: scale bytes [M][H][S][d / 32] uint8; the rest as
+    in TrajTensors (pos may be None where a call does not read positions)."""
+    k: object
+    v: object
+    k_scale: object
+    v_scale: object
+    pos: object = None
+    q: object = None
+    q_pos: object = None
+    page_start: object = None
+    page_len: object = None
+
+    def desc(self) -> Packed:
+        torch = _torch()
+        k, v, ks, vs, q, ps = self.k, self.v, self.k_scale, self.v_scale, self.q, self.page_start
+        ints = (self.pos, self.q_pos, ps, self.page_len)
+        _require_cuda(k, v, ks, vs, q, *ints)
+        shape, strides, gstrides = k.shape, k.stride(), ks.stride()
+        for x in (k, v, ks, vs):
+            if x.dtype != torch.uint8 or x.dim() != 4 or (x.numel() and x.stride(3) != 1):
+                raise ValueError("codes and scales must be 4-D uint8, the bytes of a row contiguous")
+        if v.shape != shape or vs.shape != ks.shape or ks.shape[:3] != shape[:3] or 16 * ks.shape[3] != shape[3] or \
+                (k.numel() and (v.stride() != strides or vs.stride() != gstrides)):
+            raise ValueError("codes must be [M][H][S][d / 2], scales [M][H][S][d / 32], of K and V alike")
+        n = shape[2]
+        if n == 0:  # strides mean nothing
+            strides, gstrides = (0, 0, shape[3]), (0, 0, ks.shape[3])
+        for x in ints:
+            if x is not None and (x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous()):
+                raise ValueError("positions and pages must be contiguous int32")
+        if self.pos is not None and self.pos.numel() != n:
+            raise ValueError("one position per cached token")
+        if (ps is None) != (self.page_len is None) or (ps is not None and ps.numel() != self.page_len.numel()):
+            raise ValueError("one length per page")
+        W = 0 if q is None else q.shape[2]
+        if q is not None and (q.dim() != 4 or not q.is_contiguous() or
+                              (W and (self.q_pos is None or self.q_pos.numel() != W))):
+            raise ValueError("q must be contiguous [M][Hq][W][d] with W positions")
+        pos, q_pos, start, length = map(_ptr, ints)
+        return Packed(_ptr(k), _ptr(v), strides[0], strides[1], strides[2], _ptr(ks), _ptr(vs), gstrides[0], gstrides[1],
+                      gstrides[2], pos, n, _ptr(q), q_pos, W, start, length, 0 if ps is None else ps.numel())
+
+
 def make_shape(M, H, Hq, d, dtype, softmax_scale=0.0) -> Shape:
     torch = _torch()
     code = {torch.float32: COMMITKV_F32, torch.bfloat16: COMMITKV_BF16}[dtype] \
@@ -227,7 +299,11 @@ def _descs(trajs: Sequence[TrajTensors]):
     n = len(trajs)
     if not 1 <= n <= MAX_TRAJ:
         raise ValueError("1 <= n_traj <= 64")
-    return (Traj * n)(*[t.desc() for t in trajs])
+    descs = [t.desc() for t in trajs]
+    kind = type(descs[0])
+    if any(type(d) is not kind for d in descs):
+        raise ValueError("packed caches or full-width ones, not both")
+    return (kind * n)(*descs)
 
 
 def _mask(layer_mask, M):
@@ -421,12 +497,20 @@ def commitkv_compact_noalloc(shape: Shape, cache, retired, pending, pending_prio
     _check(rc, "commitkv_compact_noalloc")
 
 
+def _packed_width(shape: Shape, t: PackedTensors):
+    M, H, d = shape.layers, shape.kv_heads, shape.head_dim
+    if tuple(t.k.shape[:2]) != (M, H) or 2 * t.k.shape[3] != d:
+        raise ValueError(f"codes must be [{M}][{H}][S][{d // 2}] of the shape")
+
+
 class AttentionBatch:
     """The arguments of an attention call, checked and marshalled once: the
     trajectories, their outputs and a shared prefix, for callers that issue
     many calls on the same buffers.  Caches that grow in place are passed as
     the whole buffers, and set_length says how many tokens they hold (the
-    workspace does not depend on it).  The batch keeps the tensors alive."""
+    workspace does not depend on it, but for packed caches, which it serves up
+    to the lengths it was made for).  The trajectories are TrajTensors, or all
+    PackedTensors (without a prefix).  The batch keeps the tensors alive."""
 
     def __init__(self, shape: Shape, trajs: Sequence[TrajTensors], out, lse_out=None, prefix: TrajTensors = None):
         torch = _torch()
@@ -439,8 +523,16 @@ class AttentionBatch:
         M, H, Hq, d = shape.layers, shape.kv_heads, shape.q_heads, shape.head_dim
         dt = torch.bfloat16 if shape.dtype == COMMITKV_BF16 else torch.float32
         devices = set()
+        self.packed = isinstance(trajs[0], PackedTensors)
+        if self.packed and prefix is not None:
+            raise ValueError("packed caches take no shared prefix")
         for i, t in enumerate(list(trajs) + ([prefix] if prefix is not None else [])):
-            if t.k.shape[0] != M or t.k.shape[1] != H or t.k.shape[3] != d or t.k.dtype != dt or t.v.dtype != dt:
+            if self.packed:
+                _packed_width(shape, t)
+                if t.pos is None or (t.q is not None and t.q.dtype != dt):
+                    raise ValueError(f"packed caches need positions, and q of {dt}")
+                devices |= {t.k_scale.device, t.v_scale.device}
+            elif t.k.shape[0] != M or t.k.shape[1] != H or t.k.shape[3] != d or t.k.dtype != dt or t.v.dtype != dt:
                 raise ValueError(f"K and V must be [{M}][{H}][S][{d}] of {dt}")
             if t.pos.shape != (t.k.shape[2],) or not t.pos.is_contiguous():
                 raise ValueError("pos must be contiguous, one position per cached token")
@@ -495,11 +587,15 @@ def alloc_attention_workspace(shape: Shape, trajs: Sequence[TrajTensors], prefix
 def _attention(name, shape, trajs, prefix, out, lse_out, window, sinks, layer_mask, workspace, stream):
     b = trajs
     if not isinstance(b, AttentionBatch):
+        if not 1 <= len(trajs) <= MAX_TRAJ:
+            raise ValueError("1 <= n_traj <= 64")
         b = AttentionBatch(shape, trajs, out, lse_out, prefix)
     elif out is not None or lse_out is not None or prefix is not None or \
             (b.shape is not shape and bytes(b.shape) != bytes(shape)):
         raise ValueError("the outputs, the prefix and the shape are those of the batch")
-    if (b._prefix is None) != (name == "commitkv_window_attention"):
+    if b.packed != (name == "commitkv_packed_attention"):
+        raise ValueError("packed caches and commitkv_packed_attention go together")
+    if (b._prefix is None) == (name == "commitkv_prefix_attention"):
         raise ValueError("commitkv_prefix_attention takes a prefix, commitkv_window_attention none")
     if not (-1 << 31 <= window < 1 << 31 and -1 << 31 <= sinks < 1 << 31):
         raise ValueError("window and sinks are 32-bit")
@@ -531,3 +627,161 @@ def commitkv_prefix_attention(shape: Shape, trajs, prefix=None, out=None, lse_ou
     own caches together; trajs may be an AttentionBatch with a prefix."""
     _attention("commitkv_prefix_attention", shape, trajs, prefix, out, lse_out, window, sinks, layer_mask, workspace,
                stream)
+
+
+# ----------------------------------------------------------------------------
+# packed caches
+
+
+def commitkv_packed_attention(shape: Shape, trajs, out=None, lse_out=None, window: int = 0, sinks: int = 0,
+                              layer_mask=None, workspace=None, stream=None):
+    """commitkv_window_attention over packed caches (PackedTensors); trajs may
+    be an AttentionBatch of them."""
+    _attention("commitkv_packed_attention", shape, trajs, None, out, lse_out, window, sinks, layer_mask, workspace,
+               stream)
+
+
+def alloc_packed_cache(shape: Shape, capacity: int, device="cuda") -> PackedTensors:
+    """An empty packed cache with room for `capacity` tokens."""
+    torch = _torch()
+    M, H, d = shape.layers, shape.kv_heads, shape.head_dim
+
+    def zeros(width):
+        return torch.zeros(M, H, capacity, width, dtype=torch.uint8, device=device)
+
+    return PackedTensors(zeros(d // 2), zeros(d // 2), zeros(d // 32), zeros(d // 32),
+                         torch.zeros(capacity, dtype=torch.int32, device=device))
+
+
+def commitkv_packed_workspace_size(shape: Shape, trajs: Sequence[PackedTensors]) -> int:
+    n = load_library().commitkv_packed_workspace_size(ctypes.byref(shape), len(trajs), _descs(trajs))
+    if n == 0:
+        raise CommitKVError(COMMITKV_ERR_INVALID_ARG, "commitkv_packed_workspace_size")
+    return int(n)
+
+
+def alloc_packed_workspace(shape: Shape, trajs: Sequence[PackedTensors], device=None):
+    """Allocate (with torch) and initialise a workspace for the attention and
+    the checkpoints of these packed caches."""
+    return _alloc(commitkv_packed_workspace_size(shape, trajs), device)
+
+
+def _on_current(*tensors):
+    devices = {x.device for x in tensors if x is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
+    device = next(iter(devices)).index
+    if _torch().cuda.current_device() != device:
+        raise ValueError("the tensors must be on the current GPU")
+    return device
+
+
+class PackedRows:
+    """The arguments of a write or a read, checked and marshalled once: packed
+    caches, the full-width rows k, v [M][H][n][d] of each (any strides with
+    contiguous d) and the token at which they begin.  Keeps the tensors alive."""
+
+    def __init__(self, shape: Shape, caches: Sequence[PackedTensors], k, v, first: Sequence[int]):
+        torch = _torch()
+        n = len(caches)
+        if not 1 <= n <= MAX_TRAJ or len(k) != n or len(v) != n or len(first) != n:
+            raise ValueError("1 <= n_traj <= 64, rows and a first token for each")
+        if not all(isinstance(c, PackedTensors) for c in caches):
+            raise ValueError("caches must be PackedTensors")
+        self.shape, self.tensors = shape, (caches, k, v)
+        self.descs = _descs(caches)
+        M, H, d = shape.layers, shape.kv_heads, shape.head_dim
+        dt = torch.bfloat16 if shape.dtype == COMMITKV_BF16 else torch.float32
+        self.rows = (Rows * n)()
+        for i, (c, x, y) in enumerate(zip(caches, k, v)):
+            _packed_width(shape, c)
+            if x.dim() != 4 or tuple(x.shape) != (M, H, x.shape[2], d) or y.shape != x.shape or x.dtype != dt or \
+                    y.dtype != dt or (x.numel() and (x.stride() != y.stride() or x.stride(3) != 1)):
+                raise ValueError(f"rows must be [{M}][{H}][n][{d}] of {dt} with contiguous channels, K and V alike")
+            sl, sh, st = x.stride()[:3]
+            self.rows[i] = Rows(_ptr(x), _ptr(y), sl, sh, st, 0, 0)
+        # once, and not in every call
+        self.device = _on_current(*[t for c in caches for t in (c.k, c.v, c.k_scale, c.v_scale)], *k, *v)
+        for i, f in enumerate(first):
+            self.set_rows(i, f)
+
+    def set_rows(self, i: int, first: int, count: int = None):
+        """Trajectory i's rows, or the first `count` of them, stand at tokens first .. of its cache."""
+        caches, k, _ = self.tensors
+        count = k[i].shape[2] if count is None else count
+        if not (0 <= count <= k[i].shape[2] and 0 <= first <= caches[i].k.shape[2] - count):
+            raise ValueError("rows outside the cache")
+        self.rows[i].first, self.rows[i].count = first, count
+
+
+def packed_rows(shape: Shape, caches: Sequence[PackedTensors], k, v, first) -> PackedRows:
+    return PackedRows(shape, caches, k, v, first)
+
+
+def _packed_copy(name, shape, caches, k, v, first, layer_mask, stream):
+    r = caches
+    if not isinstance(r, PackedRows):
+        r = PackedRows(shape, caches, k, v, first)
+    elif k is not None or v is not None or first is not None or \
+            (r.shape is not shape and bytes(r.shape) != bytes(shape)):
+        raise ValueError("the rows and the shape are those of the PackedRows")
+    if _torch().cuda.current_device() != r.device:
+        raise ValueError("the tensors must be on the current GPU")
+    _mbuf, mptr = _mask(layer_mask, shape.layers)
+    if stream is None:
+        stream = _current_stream(r.device)
+    rc = getattr(_lib or load_library(), name)(ctypes.byref(r.shape), len(r.rows), r.descs, r.rows, mptr, _stream(stream))
+    _check(rc, name)
+
+
+def commitkv_packed_write(shape: Shape, caches, k=None, v=None, first=None, layer_mask=None, stream=None):
+    """New tokens' rows into their places of packed caches; caches may be
+    PackedRows (then without k, v and first)."""
+    _packed_copy("commitkv_packed_write", shape, caches, k, v, first, layer_mask, stream)
+
+
+def commitkv_packed_read(shape: Shape, caches, k=None, v=None, first=None, layer_mask=None, stream=None):
+    """Rows of packed caches as full-width values, into k and v; caches may be
+    PackedRows (then without k, v and first)."""
+    _packed_copy("commitkv_packed_read", shape, caches, k, v, first, layer_mask, stream)
+
+
+def commitkv_packed_compact(shape: Shape, cache, retired, pending, pending_priority, fill_score, budget_B,
+                            pending_tokens_BN, pending_cap_pages, idx_out, n_idx_out, dst=None, workspace=None,
+                            stream=None):
+    """commitkv_compact for packed caches, into the caches `dst`; without them in
+    place, as commitkv_compact_in_place."""
+    torch = _torch()
+    n = len(cache)
+    d = _descs(cache)
+    for c in list(cache) + list(dst or ()):
+        if not isinstance(c, PackedTensors):
+            raise ValueError("caches must be PackedTensors")
+        _packed_width(shape, c)
+    if dst is not None and len(dst) != n:
+        raise ValueError("one destination per cache")
+    for xs, dt, what in ((retired, torch.uint8, "retired"), (pending, torch.int32, "pending"),
+                         (pending_priority, torch.float32, "pending_priority"), (fill_score, torch.float32, "fill_score"),
+                         (idx_out, torch.int32, "idx_out"), ([n_idx_out], torch.int32, "n_idx_out")):
+        for x in xs:
+            if x is not None and (x.dtype != dt or not x.is_contiguous()):
+                raise ValueError(f"{what} must be contiguous {dt}")
+    for i, c in enumerate(cache):
+        pages = 0 if c.page_start is None else c.page_start.numel()
+        some = pending[i] is not None and pending[i].numel() > 0
+        if fill_score[i].numel() < c.k.shape[2] or idx_out[i].numel() < budget_B or \
+                (pages and retired[i].numel() < pages) or (some and pending_priority[i].numel() < pages):
+            raise ValueError("scores for every token, marks and priorities for every page, budget_B indices")
+    if n_idx_out.numel() < n:
+        raise ValueError("n_idx_out has an entry per cache")
+    if workspace is None:
+        raise ValueError("a workspace is needed")
+    device = _on_current(workspace, n_idx_out, *[t for c in list(cache) + list(dst or ()) for t in (c.k, c.v, c.k_scale, c.v_scale)],
+                         *retired, *pending, *pending_priority, *fill_score, *idx_out)
+    npend = (ctypes.c_int32 * n)(*[0 if p is None else int(p.numel()) for p in pending])
+    rc = load_library().commitkv_packed_compact(
+        ctypes.byref(shape), n, d, _ptr_array(retired, n), _ptr_array(pending, n), ctypes.cast(npend, ctypes.c_void_p),
+        _ptr_array(pending_priority, n), _ptr_array(fill_score, n), int(budget_B), int(pending_tokens_BN),
+        int(pending_cap_pages), _ptr_array(idx_out, n), _ptr(n_idx_out), None if dst is None else _descs(dst),
+        _ptr(workspace), workspace.numel(), _stream(_current_stream(device) if stream is None else stream))
+    _check(rc, "commitkv_packed_compact")

@@ -12,17 +12,6 @@ namespace ckv {
 namespace at {
 namespace {
 
-constexpr size_t kAlign = 256;
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// Items that share rows with others (split tokens), at most, of all kernels of
-// a call that take up to 16 rows and of all others: bounds the partial
-// results.  Small row tiles are cheap to merge and come from calls whose time
-// is the reading of the cache, which wants many blocks.
-constexpr int64_t kMaxSplitSmall = 2048;  // up to 16 rows an item
-constexpr int64_t kMaxSplit = 768;
-
 // ------------------------------------------------------------------ merge
 // o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i over a row's partial results,
 // those of the prefix first.  NW warps to a row take kBatch parts each at a
@@ -144,10 +133,8 @@ cudaError_t launch_combine(const Launch &L, cudaStream_t s) {
   return L.d == 128 ? launch_combine_td<float, 128>(L, s) : launch_combine_td<float, 64>(L, s);
 }
 
-namespace {
-
 // ------------------------------------------------------------------ host
-int64_t rows_of(const commitkv_shape *s, const commitkv_traj &x) { return (int64_t)(s->q_heads / s->kv_heads) * x.W; }
+static int64_t rows_of(const commitkv_shape *s, const commitkv_traj &x) { return (int64_t)(s->q_heads / s->kv_heads) * x.W; }
 
 commitkv_status check_args(const commitkv_shape *s, int n, const commitkv_traj *tr, const commitkv_traj *prefix,
                            bool need_q) {
@@ -199,29 +186,14 @@ int sm_count() {
 // are of earlier calls.  Measured: a three-prompt batch of 84 row tiles of
 // 9 token tiles, 64 channels, 49 us in two chunks each, 28 whole; one token over
 // 4 caches of 4,096 tokens 15 us in chunks, 46 whole.
-constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3, kBytesPerUs = 6.5e6;
-struct PathInfo {
-  int rows, tile;        // of an item, tokens of a tile
-  int resident;          // items at a time on an SM
-  double fixed, tile_us;
-};
-struct Divide {  // segments in the order of their items
-  int64_t base[kMaxSeg];   // slices x row tiles
-  int64_t tiles[kMaxSeg];  // of a row tile, at most
-  int64_t rows[kMaxSeg];   // of all slices
-  int n;
-};
-struct Division {
-  int64_t len;  // every row tile in chunks of `len` tiles,
-  int64_t rest, chunks;  // or, where rest >= 0, the last `rest` row tiles alone, in `chunks`
-};
+static constexpr double kMergeUs = 3.5, kMergeRowUs = 0.25e-3, kBytesPerUs = 6.5e6;
 // When the last item ends, in tiles, where slots take items in their order as
 // they get free: slots that get free at the same time are kept together.  (The
 // work and half an item in its place: 8 prompts behind 32,768 tokens 788 us,
 // 703 so; 5 of up to 200 rows over 16,000 134 and 119; 40 agents with 40 rows
 // each behind 5,000 142 and 122.  Items of up to 16 rows share the memory's rate
 // instead, so their sum is what counts.)
-double last_end(const Divide &v, int64_t len, double fixed, int64_t slots) {
+static double last_end(const Divide &v, int64_t len, double fixed, int64_t slots) {
   double at[kMaxSeg + 2];  // ascending; a segment leaves one kind of slots more at most
   int64_t n[kMaxSeg + 2];
   int k = 1;
@@ -301,16 +273,13 @@ Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most
 }
 
 enum { kSimt16, kSimt64, kTc, kTcF32, kRows, kPaths };
-constexpr PathInfo kPath[kPaths] = {
+static constexpr PathInfo kPath[kPaths] = {
     {16, 64, 2, 1.0, 2.5}, {64, 64, 2, 1.0, 17.0}, {256, 128, 1, 2.0, 1.6}, {128, 64, 1, 3.0, 2.7}, {16, 64, 2, 2.0, 1.4}};
 
 // For tests and diagnosis, read in every call: COMMITKV_SCORING=simt takes the
 // CUDA cores where a call could have the tensor cores (attention as well as
 // scoring), COMMITKV_ATTENTION=tiles the kernels of row tiles however few rows
 // there are.
-struct Forced {
-  bool cuda_cores, tiles;
-};
 Forced forced_paths() {
   const char *s = getenv("COMMITKV_SCORING"), *a = getenv("COMMITKV_ATTENTION");
   return {s && s[0] == 's', a && a[0] == 't'};
@@ -320,7 +289,7 @@ Forced forced_paths() {
 // and outputs: up to 16 rows the kernel of 16-row items, others those of row
 // tiles (but see few_rows); TMA, which bf16 tiles take, also wants distinct
 // heads and layers.
-int path_of(const Launch &L, const Seg &sg, const Forced &f) {
+static int path_of(const Launch &L, const Seg &sg, const Forced &f) {
   const int cuda_cores = sg.R <= 16 ? kSimt16 : kSimt64;
   if (f.cuda_cores) return cuda_cores;
   const int eb = L.dtype == COMMITKV_BF16 ? 2 : 4;
@@ -344,7 +313,7 @@ int64_t most_seen(const Launch &L, const Seg &sg, int rows) {
 }
 
 // What of a path's costs goes by the type.
-PathInfo path_info(const Launch &L, int p) {
+static PathInfo path_info(const Launch &L, int p) {
   PathInfo pi = kPath[p];
   if (p == kRows) {
     pi.tile = rows_tile(L);
@@ -365,7 +334,7 @@ PathInfo path_info(const Launch &L, int p) {
 // on 4: 16 over 6,000 25 and 32, 32 over 2,000 21 and 25, 64 over 3,000 26 and
 // 58, 8 over 8 caches to 4,000 42 and 47, 16 agents behind 4,000 25 and 30 (taken
 // for the other way); 4 on 2: 40 over 1,000 19 and 15.
-bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
+static bool few_rows(const Launch &L, const int *path, int64_t slices, int sms) {
   const bool bf16 = L.dtype == COMMITKV_BF16;
   const PathInfo few_pi = path_info(L, kRows), many_pi = path_info(L, bf16 ? kTc : kTcF32);
   const double few_us = bf16 ? 1.25 : 2.3;
@@ -535,7 +504,6 @@ commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commit
   return COMMITKV_ERR_CUDA;
 }
 
-}  // namespace
 }  // namespace at
 }  // namespace ckv
 

@@ -372,5 +372,48 @@ __device__ __forceinline__ void write_row_warp(const Launch &L, const Seg &sg, c
   }
 }
 
+// ------------------------------------------------------------------ host (attend.cu)
+constexpr size_t kAlign = 256;
+inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Items that share rows with others (split tokens), at most, of all kernels of
+// a call that take up to 16 rows and of all others: bounds the partial
+// results.  Small row tiles are cheap to merge and come from calls whose time
+// is the reading of the cache, which wants many blocks.
+constexpr int64_t kMaxSplitSmall = 2048;  // up to 16 rows an item
+constexpr int64_t kMaxSplit = 768;
+
+struct PathInfo {
+  int rows, tile;        // of an item, tokens of a tile
+  int resident;          // items at a time on an SM
+  double fixed, tile_us;
+};
+struct Divide {  // segments in the order of their items
+  int64_t base[kMaxSeg];   // slices x row tiles
+  int64_t tiles[kMaxSeg];  // of a row tile, at most
+  int64_t rows[kMaxSeg];   // of all slices
+  int n;
+};
+struct Division {
+  int64_t len;  // every row tile in chunks of `len` tiles,
+  int64_t rest, chunks;  // or, where rest >= 0, the last `rest` row tiles alone, in `chunks`
+};
+Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most_items, int64_t slices, bool prefix);
+struct Forced {
+  bool cuda_cores, tiles;
+};
+Forced forced_paths();
+int sm_count();
+int64_t most_seen(const Launch &L, const Seg &sg, int rows);
+int64_t partial_rows(const commitkv_shape *s, int n, const commitkv_traj *tr, const commitkv_traj *prefix);
+size_t partial_bytes(const commitkv_shape *s, int64_t rows);
+commitkv_status check_args(const commitkv_shape *s, int n, const commitkv_traj *tr, const commitkv_traj *prefix,
+                           bool need_q);
+commitkv_status attend(const commitkv_shape *shape, int32_t n_traj, const commitkv_traj *trajs,
+                       const commitkv_traj *prefix, const uint8_t *layer_mask, int32_t window, int32_t sinks,
+                       void *const *out, float *const *lse_out, void *workspace, size_t workspace_bytes,
+                       cudaStream_t stream);
+
 }  // namespace at
 }  // namespace ckv

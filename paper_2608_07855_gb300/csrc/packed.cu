@@ -1,0 +1,568 @@
+// Packed caches: writing rows as codes and scales, reading them back, and the
+// gather of a checkpoint.
+//
+// All three move bytes: a thread has 8 channels of a row (write, read: 16 bytes
+// of bf16, 4 of codes, so that a warp's accesses are whole lines of consecutive
+// rows), or 32 channels (gather: 16 bytes of codes and their scale byte).
+#include <stdlib.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "packed.cuh"
+
+namespace ckv {
+namespace pk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;  // rows of a thread, loads in flight together
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Rows {
+  Cache c;
+  void *k, *v;
+  int64_t sl, sh, st;  // in elements
+  int32_t first, count;
+  int32_t heads_inner;  // rows are taken token by token
+  int32_t pad;
+};
+
+struct CopyLaunch {
+  Rows r[kMaxTraj];
+  int32_t off[kMaxTraj + 1];  // first block of a trajectory
+  int32_t n_traj, H, n_layers;
+  uint8_t layer_ids[kMaxLayers];
+};
+static_assert(sizeof(CopyLaunch) <= 32764, "kernel parameters");
+
+// The row of a thread: place p of a (trajectory, layer)'s H * count rows.
+struct Place {
+  int64_t code, scale, elem;
+};
+__device__ __forceinline__ Place place_of(const Rows &r, int l, int p, int H) {
+  int h, i;
+  if (r.heads_inner) i = p / H, h = p % H;
+  else h = p / r.count, i = p % r.count;
+  const int64_t tok = (int64_t)r.first + i;
+  return {l * r.c.sl + h * r.c.sh + tok * r.c.st, l * r.c.gl + h * r.c.gh + tok * r.c.gt,
+          l * r.sl + h * r.sh + i * r.st};
+}
+
+// Eight channels as fp32.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T *src, float (&x)[8]) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(src);
+    const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(y[i] << 16), x[2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
+  } else if constexpr (VEC) {
+    const float4 a = reinterpret_cast<const float4 *>(src)[0], b = reinterpret_cast<const float4 *>(src)[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_f32(src[i]);
+  }
+}
+
+// sigma's byte for a largest magnitude a (finite): the one nearest to a / 7, of
+// two the even.  An estimate rounded down, then one exact comparison: the middle
+// between two neighbours has five significant bits, seven times it eight.
+__device__ __forceinline__ unsigned scale_byte(float a) {
+  const unsigned b =
+      min(__half_as_ushort(__float2half_rz(__fmul_rn(__fmul_rn(a, 1.0f / 7.0f), 1.0f / kUnit))) >> 7, kNanScale - 1);
+  const float mid = __half2float(__ushort_as_half((unsigned short)((b << 7) | 64u))) * (7.0f * kUnit);
+  return b + (b < kNanScale - 1 && (a > mid || (a == mid && (b & 1))) ? 1u : 0u);
+}
+
+// The code of x for sigma > 0, inv near its inverse.  The product can only be on
+// the wrong side of a middle by rounding; the remainder is exact (a multiple of
+// x's last place, no larger than x) and says on which side x is, or that it is
+// a tie.
+__device__ __forceinline__ unsigned code_of(float x, float sigma, float inv) {
+  const float a = fabsf(x);
+  float n = fminf(rintf(a * inv), 8.0f);
+  const float r = fmaf(-n, sigma, a), t = 2.0f * fabsf(r);
+  if (t > sigma || (t == sigma && ((int)n & 1))) n += r > 0.0f ? 1.0f : -1.0f;
+  const int i = min((int)n, 7);
+  return 8 + (x < 0.0f ? -i : i);
+}
+
+// Four lanes have a group's 32 channels; returns the scale byte, and the eight
+// codes of the lane.
+__device__ __forceinline__ unsigned encode(const float (&x)[8], uint32_t &codes) {
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  codes = 0x88888888u;
+  if (top >= 0x7f800000u) return 0xff;  // infinite or NaN
+  const unsigned b = scale_byte(__uint_as_float(top));
+  if (b == 0) return 0;
+  const float sigma = sigma_of(b), inv = __frcp_rn(sigma);
+  codes = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) codes |= code_of(x[i], sigma, inv) << (4 * i);
+  return b;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t *dst, uint32_t codes) {
+  if (VEC) *reinterpret_cast<uint32_t *>(dst) = codes;
+  else
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = (uint8_t)(codes >> (8 * i));
+}
+
+// Write: bound by reading the rows (2.8 to 5.3 bytes a value with K and V's
+// codes); a lane's 16-byte loads of K and V of all its rows are issued first.
+template <typename T, int D, bool VEC>
+__global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ CopyLaunch L) {
+  constexpr int TR = D / 8, RB = kThreads / TR;  // threads of a row, rows of a step
+  int t = 0, e = L.n_traj;
+  while (e - t > 1) {
+    const int m = (t + e) >> 1;
+    if ((int)blockIdx.x >= L.off[m]) t = m;
+    else e = m;
+  }
+  const Rows &r = L.r[t];
+  const int rows = L.H * r.count, per = (rows + RB * kUnroll - 1) / (RB * kUnroll), b = blockIdx.x - L.off[t];
+  const int l = L.layer_ids[b / per], p0 = b % per * (RB * kUnroll) + threadIdx.x / TR, c = threadIdx.x % TR * 8;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    float x[kUnroll][8];
+    Place at[kUnroll];
+    const T *src = static_cast<const T *>(kv ? r.v : r.k);
+    uint8_t *codes = kv ? r.c.v : r.c.k, *scales = kv ? r.c.vs : r.c.ks;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int p = p0 + u * RB;
+      if (p < rows) {
+        at[u] = place_of(r, l, p, L.H);
+        load8<T, VEC>(src + at[u].elem + c, x[u]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[u][i] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      uint32_t w;
+      const unsigned s = encode(x[u], w);
+      if (p0 + u * RB < rows) {
+        store_codes<T, VEC>(codes + at[u].code + c / 2, w);
+        if (c % kGroup == 0) scales[at[u].scale + c / kGroup] = (uint8_t)s;
+      }
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pair_of(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pair_of<__nv_bfloat16>(float a, float b) {  // both are bf16 numbers: no rounding
+  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+
+// Read: bound by writing the rows.
+template <typename T, int D, bool VEC>
+__global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ CopyLaunch L) {
+  constexpr int TR = D / 8, RB = kThreads / TR;
+  int t = 0, e = L.n_traj;
+  while (e - t > 1) {
+    const int m = (t + e) >> 1;
+    if ((int)blockIdx.x >= L.off[m]) t = m;
+    else e = m;
+  }
+  const Rows &r = L.r[t];
+  const int rows = L.H * r.count, per = (rows + RB * kUnroll - 1) / (RB * kUnroll), b = blockIdx.x - L.off[t];
+  const int l = L.layer_ids[b / per], p0 = b % per * (RB * kUnroll) + threadIdx.x / TR, c = threadIdx.x % TR * 8;
+  uint32_t w[2][kUnroll];
+  unsigned s[2][kUnroll];
+  int64_t at[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int p = p0 + u * RB;
+    if (p >= rows) continue;
+    const Place pl = place_of(r, l, p, L.H);
+    at[u] = pl.elem + c;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint8_t *src = (kv ? r.c.v : r.c.k) + pl.code + c / 2;
+      if (VEC) {
+        w[kv][u] = *reinterpret_cast<const uint32_t *>(src);
+      } else {
+        w[kv][u] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[kv][u] |= (uint32_t)src[i] << (8 * i);
+      }
+      s[kv][u] = (kv ? r.c.vs : r.c.ks)[pl.scale + c / kGroup];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    if (p0 + u * RB >= rows) continue;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      T *dst = static_cast<T *>(kv ? r.v : r.k) + at[u];
+      const float sigma = sigma_of(s[kv][u]);
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = (float)((int)(w[kv][u] >> (4 * i) & 15u) - 8) * sigma;
+      if constexpr (VEC && sizeof(T) == 2) {
+        *reinterpret_cast<uint4 *>(dst) =
+            make_uint4(pair_of<T>(x[0], x[1]), pair_of<T>(x[2], x[3]), pair_of<T>(x[4], x[5]), pair_of<T>(x[6], x[7]));
+      } else if constexpr (VEC) {
+        reinterpret_cast<float4 *>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4 *>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dst[i] = at::from_f32<T>(x[i]);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ checkpoint
+struct GatherLaunch {
+  Cache src[kMaxTraj], dst[kMaxTraj];
+  const int32_t *idx[kMaxTraj];
+  const int32_t *pos[kMaxTraj];
+  int32_t *pos_out[kMaxTraj];
+  const int32_t *n_idx;
+  int32_t H, groups;  // groups of 32 channels in a row
+  int32_t B;
+};
+static_assert(sizeof(GatherLaunch) <= 32764, "kernel parameters");
+
+// 32 channels: codes and scale byte.
+struct Unit {
+  uint4 codes;
+  uint8_t scale;
+};
+template <bool VEC>
+__device__ __forceinline__ Unit load_unit(const uint8_t *codes, const uint8_t *scale) {
+  Unit x;
+  if (VEC) {
+    x.codes = *reinterpret_cast<const uint4 *>(codes);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = codes[4 * i] | codes[4 * i + 1] << 8 | codes[4 * i + 2] << 16 | (uint32_t)codes[4 * i + 3] << 24;
+    x.codes = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  x.scale = *scale;
+  return x;
+}
+template <bool VEC>
+__device__ __forceinline__ void store_unit(uint8_t *codes, uint8_t *scale, const Unit &x) {
+  if (VEC) {
+    *reinterpret_cast<uint4 *>(codes) = x.codes;
+  } else {
+    const uint32_t w[4] = {x.codes.x, x.codes.y, x.codes.z, x.codes.w};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) codes[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+  *scale = x.scale;
+}
+
+// Into other caches: blockIdx.y = 2 (l H + h) + (V), a thread kUnroll units.
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads) gather_kernel(const __grid_constant__ GatherLaunch L) {
+  const int t = blockIdx.z, kv = blockIdx.y & 1, l = (blockIdx.y >> 1) / L.H, h = (blockIdx.y >> 1) % L.H;
+  const Cache &s = L.src[t], &d = L.dst[t];
+  const int n = L.n_idx[t];
+  const int32_t *idx = L.idx[t];
+  const int64_t sc = l * s.sl + h * s.sh, sg = l * s.gl + h * s.gh, dc = l * d.sl + h * d.sh, dg = l * d.gl + h * d.gh;
+  const uint8_t *codes = (kv ? s.v : s.k) + sc, *scales = (kv ? s.vs : s.ks) + sg;
+  uint8_t *to = (kv ? d.v : d.k) + dc, *to_scales = (kv ? d.vs : d.ks) + dg;
+  Unit x[kUnroll];
+  int row[kUnroll], g[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t e = ((int64_t)blockIdx.x * kUnroll + u) * kThreads + threadIdx.x;
+    row[u] = (int)(e / L.groups), g[u] = (int)(e % L.groups);
+    if (row[u] >= n) continue;
+    const int i = idx[row[u]];
+    x[u] = load_unit<VEC>(codes + i * s.st + 16 * g[u], scales + i * s.gt + g[u]);
+    if (blockIdx.y == 0 && g[u] == 0 && L.pos_out[t]) L.pos_out[t][row[u]] = L.pos[t][i];
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u)
+    if (row[u] < n) store_unit<VEC>(to + row[u] * d.st + 16 * g[u], to_scales + row[u] * d.gt + g[u], x[u]);
+}
+
+// In place: a block per slice, chunk by chunk; a chunk's rows are all read
+// before any is written, and later chunks' sources lie behind all that was
+// written (I_j increases, I_j >= j).
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads) gather_in_place_kernel(const __grid_constant__ GatherLaunch L) {
+  const int t = blockIdx.z, kv = blockIdx.y & 1, l = (blockIdx.y >> 1) / L.H, h = (blockIdx.y >> 1) % L.H;
+  const Cache &s = L.src[t];
+  const int n = L.n_idx[t], rows = kThreads * kUnroll / L.groups;
+  const int32_t *idx = L.idx[t];
+  uint8_t *codes = (kv ? s.v : s.k) + l * s.sl + h * s.sh, *scales = (kv ? s.vs : s.ks) + l * s.gl + h * s.gh;
+  for (int j0 = 0; j0 < n; j0 += rows) {
+    Unit x[kUnroll];
+    int row[kUnroll];
+    bool move[kUnroll];
+    const int g = threadIdx.x % L.groups;  // the block's threads are a multiple of the groups
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      row[u] = j0 + (u * kThreads + (int)threadIdx.x) / L.groups;
+      move[u] = false;
+      if (row[u] >= n) continue;
+      const int i = idx[row[u]];
+      if ((move[u] = i != row[u])) x[u] = load_unit<VEC>(codes + i * s.st + 16 * g, scales + i * s.gt + g);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (move[u]) store_unit<VEC>(codes + row[u] * s.st + 16 * g, scales + row[u] * s.gt + g, x[u]);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) positions_in_place_kernel(const __grid_constant__ GatherLaunch L) {
+  const int t = blockIdx.x, n = L.n_idx[t];
+  const int32_t *idx = L.idx[t];
+  int32_t *pos = L.pos_out[t];
+  for (int j0 = 0; j0 < n; j0 += kThreads) {
+    const int j = j0 + threadIdx.x;
+    int v = 0;
+    if (j < n) v = pos[idx[j]];
+    __syncthreads();
+    if (j < n) pos[j] = v;
+  }
+}
+
+// ------------------------------------------------------------------ host
+// Rows are written through these strides: no two layers or heads in one place.
+bool distinct(const commitkv_shape *s, int64_t layer, int64_t head) {
+  return (s->layers == 1 || layer > 0) && (s->kv_heads == 1 || head > 0);
+}
+bool writable(const commitkv_shape *s, const commitkv_packed &x) {
+  return distinct(s, x.stride_layer, x.stride_head) && distinct(s, x.scale_layer, x.scale_head);
+}
+
+commitkv_status check_rows(const commitkv_shape *s, int n, const commitkv_packed *x, const commitkv_rows *r, bool write) {
+  commitkv_status st = check_shape(s);
+  if (st) return st;
+  if ((st = check_caches(s, n, x, false, false))) return st;
+  if (!r) return COMMITKV_ERR_INVALID_ARG;
+  for (int t = 0; t < n; ++t) {
+    if (r[t].first < 0 || r[t].count < 0 || r[t].first > x[t].S - r[t].count) return COMMITKV_ERR_INVALID_ARG;
+    if (r[t].count == 0) continue;
+    if (!r[t].k || !r[t].v) return COMMITKV_ERR_INVALID_ARG;
+    if (write ? !writable(s, x[t])
+              : (s->layers > 1 && r[t].stride_layer == 0) || (s->kv_heads > 1 && r[t].stride_head == 0) ||
+                    (r[t].count > 1 && r[t].stride_tok == 0))
+      return COMMITKV_ERR_INVALID_ARG;
+    if ((int64_t)r[t].count * s->kv_heads > (1 << 30)) return COMMITKV_ERR_UNSUPPORTED;
+  }
+  return COMMITKV_OK;
+}
+
+template <typename T, int D>
+void launch_copy(const CopyLaunch &L, bool write, bool vec, cudaStream_t s) {
+  const int blocks = L.off[L.n_traj];
+  if (write) {
+    if (vec) write_kernel<T, D, true><<<blocks, kThreads, 0, s>>>(L);
+    else write_kernel<T, D, false><<<blocks, kThreads, 0, s>>>(L);
+  } else {
+    if (vec) read_kernel<T, D, true><<<blocks, kThreads, 0, s>>>(L);
+    else read_kernel<T, D, false><<<blocks, kThreads, 0, s>>>(L);
+  }
+}
+
+// layers: the layer of each of n_layers; the cache's and the rows' strides both go by it.
+commitkv_status copy(const commitkv_shape *s, int n, const commitkv_packed *x, const commitkv_rows *r, const uint8_t *layers,
+                     int n_layers, bool write, cudaStream_t stream) {
+  static thread_local CopyLaunch L;
+  memset(&L, 0, sizeof L);
+  L.n_traj = n;
+  L.H = s->kv_heads;
+  L.n_layers = n_layers;
+  memcpy(L.layer_ids, layers, n_layers);
+  const int eb = s->dtype == COMMITKV_BF16 ? 2 : 4, per = kThreads / (s->head_dim / 8) * kUnroll;
+  uintptr_t wide_bits = 0, code_bits = 0;  // 16-byte rows, 4-byte codes
+  int64_t blocks = 0;
+  for (int t = 0; t < n; ++t) {
+    Rows &d = L.r[t];
+    d.c = to_dev(x[t]);
+    d.k = r[t].k, d.v = r[t].v;
+    d.sl = r[t].stride_layer, d.sh = r[t].stride_head, d.st = r[t].stride_tok;
+    d.first = r[t].first, d.count = r[t].count;
+    d.heads_inner = llabs(d.sh) < llabs(d.st);
+    L.off[t] = (int32_t)blocks;
+    blocks += (int64_t)n_layers * cdiv((int64_t)s->kv_heads * r[t].count, per);
+    if (blocks >= (1ll << 31)) return COMMITKV_ERR_UNSUPPORTED;
+    if (r[t].count == 0) continue;
+    wide_bits |= (uintptr_t)d.k | (uintptr_t)d.v | (uintptr_t)((d.sl | d.sh | d.st) * eb);
+    code_bits |= (uintptr_t)d.c.k | (uintptr_t)d.c.v | (uintptr_t)(d.c.sl | d.c.sh | d.c.st);
+  }
+  L.off[n] = (int32_t)blocks;
+  if (blocks == 0) return COMMITKV_OK;
+  const bool vec = wide_bits % 16 == 0 && code_bits % 4 == 0;
+  if (s->dtype == COMMITKV_BF16) {
+    if (s->head_dim == 128) launch_copy<__nv_bfloat16, 128>(L, write, vec, stream);
+    else launch_copy<__nv_bfloat16, 64>(L, write, vec, stream);
+  } else {
+    if (s->head_dim == 128) launch_copy<float, 128>(L, write, vec, stream);
+    else launch_copy<float, 64>(L, write, vec, stream);
+  }
+  ++launch_count();
+  return cudaGetLastError() == cudaSuccess ? COMMITKV_OK : COMMITKV_ERR_CUDA;
+}
+
+commitkv_status copy_rows(const commitkv_shape *s, int32_t n, const commitkv_packed *x, const commitkv_rows *r,
+                          const uint8_t *mask, bool write, cudaStream_t stream) {
+  const commitkv_status st = check_rows(s, n, x, r, write);
+  if (st) return st;
+  uint8_t ids[kMaxLayers];
+  int m = 0;
+  for (int l = 0; l < s->layers; ++l)
+    if (!mask || mask[l]) ids[m++] = (uint8_t)l;
+  return copy(s, n, x, r, ids, m, write, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_read(const commitkv_shape *s, int n, const commitkv_packed *c, const commitkv_rows *r,
+                        const uint8_t *layers, int n_layers, cudaStream_t stream) {
+  return copy(s, n, c, r, layers, n_layers, false, stream) == COMMITKV_OK ? cudaSuccess : cudaErrorUnknown;
+}
+
+commitkv_status check_caches(const commitkv_shape *s, int n, const commitkv_packed *x, bool positions, bool queries) {
+  if (n < 1 || n > kMaxTraj || !x) return COMMITKV_ERR_INVALID_ARG;
+  for (int t = 0; t < n; ++t) {
+    const commitkv_packed &c = x[t];
+    if (c.S < 0 || c.W < 0 || c.P < 0) return COMMITKV_ERR_INVALID_ARG;
+    if (c.S > 0 && (!c.k || !c.v || !c.k_scale || !c.v_scale || (positions && !c.pos))) return COMMITKV_ERR_INVALID_ARG;
+    if (queries && c.W > 0 && (!c.q || !c.q_pos)) return COMMITKV_ERR_INVALID_ARG;
+    if (c.stride_tok < s->head_dim / 2 || c.stride_head < 0 || c.stride_layer < 0 || c.scale_tok < s->head_dim / kGroup ||
+        c.scale_head < 0 || c.scale_layer < 0)
+      return COMMITKV_ERR_INVALID_ARG;
+    if ((int64_t)(s->q_heads / s->kv_heads) * c.W > (1 << 24)) return COMMITKV_ERR_INVALID_ARG;
+  }
+  return COMMITKV_OK;
+}
+
+}  // namespace pk
+}  // namespace ckv
+
+using namespace ckv;
+
+extern "C" {
+
+commitkv_status commitkv_packed_write(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *caches,
+                                      const commitkv_rows *rows, const uint8_t *layer_mask, cudaStream_t stream) {
+  return pk::copy_rows(shape, n_traj, caches, rows, layer_mask, true, stream);
+}
+
+commitkv_status commitkv_packed_read(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *caches,
+                                     const commitkv_rows *rows, const uint8_t *layer_mask, cudaStream_t stream) {
+  return pk::copy_rows(shape, n_traj, caches, rows, layer_mask, false, stream);
+}
+
+commitkv_status commitkv_packed_compact(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *cache,
+                                        const uint8_t *const *retired, const int32_t *const *pending,
+                                        const int32_t *n_pending, const float *const *pending_priority,
+                                        const float *const *fill_score, int32_t budget_B, int32_t pending_tokens_BN,
+                                        int32_t pending_cap_pages, int32_t *const *idx_out, int32_t *n_idx_out,
+                                        const commitkv_packed *dst, void *workspace, size_t workspace_bytes,
+                                        cudaStream_t stream) {
+  commitkv_status st = check_shape(shape);
+  if (st) return st;
+  if ((st = pk::check_caches(shape, n_traj, cache, true, false))) return st;
+  commitkv_traj tr[kMaxTraj] = {};  // what the selection reads of a trajectory
+  for (int t = 0; t < n_traj; ++t) {
+    const commitkv_packed &x = cache[t];
+    tr[t].k = x.k, tr[t].v = x.v;
+    tr[t].stride_tok = shape->head_dim;
+    tr[t].pos = x.pos;
+    tr[t].S = x.S;
+    tr[t].page_start = x.page_start, tr[t].page_len = x.page_len;
+    tr[t].P = x.P;
+  }
+  if ((st = check_compact_args(shape, n_traj, tr, retired, pending, n_pending, pending_priority, fill_score, budget_B,
+                               pending_tokens_BN, pending_cap_pages, idx_out, n_idx_out)))
+    return st;
+  if (dst && (st = pk::check_caches(shape, n_traj, dst, false, false))) return st;
+  for (int t = 0; t < n_traj; ++t) {
+    const commitkv_packed &to = dst ? dst[t] : cache[t];
+    const int32_t most = std::min(budget_B, cache[t].S);
+    if (most > 0 && (to.S < most || !pk::writable(shape, to))) return COMMITKV_ERR_INVALID_ARG;
+  }
+  if (!workspace || (uintptr_t)workspace % 256) return COMMITKV_ERR_WORKSPACE;
+  size_t need = 256;
+  for (int t = 0; t < n_traj; ++t) need += ((size_t)cache[t].S + 255) / 256 * 256;
+  if (workspace_bytes < need) return COMMITKV_ERR_WORKSPACE;
+
+  static thread_local CompactLaunch C;
+  static thread_local pk::GatherLaunch G;
+  memset(&C, 0, sizeof C);
+  memset(&G, 0, sizeof G);
+  C.n_traj = n_traj;
+  C.M = shape->layers;
+  C.H = shape->kv_heads;
+  C.d = shape->head_dim;
+  C.elem_bytes = 1;
+  uint8_t *cls = static_cast<uint8_t *>(workspace) + 256;
+  bool vec = true;
+  int32_t most = 0;
+  for (int t = 0; t < n_traj; ++t) {
+    const commitkv_packed &x = cache[t];
+    C.t[t].S = x.S, C.t[t].P = x.P, C.t[t].ps = x.page_start, C.t[t].pl = x.page_len, C.t[t].pos = x.pos;
+    C.retired[t] = retired[t];
+    C.n_pending[t] = n_pending[t];
+    C.pending[t] = n_pending[t] ? pending[t] : nullptr;
+    C.prio[t] = n_pending[t] ? pending_priority[t] : nullptr;
+    C.fill[t] = fill_score[t];
+    C.cls[t] = cls;
+    cls += ((size_t)x.S + 255) / 256 * 256;
+    C.idx[t] = idx_out[t];
+    G.src[t] = pk::to_dev(x);
+    G.dst[t] = dst ? pk::to_dev(dst[t]) : G.src[t];
+    G.idx[t] = idx_out[t];
+    G.pos[t] = x.pos;
+    G.pos_out[t] = dst ? dst[t].pos : x.pos;
+    most = std::max(most, std::min(budget_B, x.S));
+    for (const pk::Cache *c : {&G.src[t], &G.dst[t]})
+      if (x.S > 0)
+        vec = vec && ((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)(c->sl | c->sh | c->st)) % 16 == 0;
+  }
+  C.n_idx = n_idx_out;
+  C.B = budget_B;
+  C.B_N = pending_tokens_BN;
+  C.cap = pending_cap_pages;
+  G.n_idx = n_idx_out;
+  G.H = shape->kv_heads;
+  G.groups = shape->head_dim / pk::kGroup;
+  G.B = budget_B;
+  const int64_t slices = 2ll * shape->layers * shape->kv_heads;
+  if (slices > 65535) return COMMITKV_ERR_UNSUPPORTED;
+  cudaError_t e = launch_compact(C, static_cast<WsHeader *>(workspace), stream);  // no outputs: the selection alone
+  if (e == cudaSuccess && most > 0) {
+    if (dst) {
+      const dim3 grid((unsigned)pk::cdiv((int64_t)most * G.groups, pk::kThreads * pk::kUnroll), (unsigned)slices, n_traj);
+      if (vec) pk::gather_kernel<true><<<grid, pk::kThreads, 0, stream>>>(G);
+      else pk::gather_kernel<false><<<grid, pk::kThreads, 0, stream>>>(G);
+      ++launch_count();
+    } else {
+      const dim3 grid(1, (unsigned)slices, n_traj);
+      if (vec) pk::gather_in_place_kernel<true><<<grid, pk::kThreads, 0, stream>>>(G);
+      else pk::gather_in_place_kernel<false><<<grid, pk::kThreads, 0, stream>>>(G);
+      e = cudaGetLastError();
+      if (e == cudaSuccess) pk::positions_in_place_kernel<<<n_traj, pk::kThreads, 0, stream>>>(G);
+      launch_count() += 2;
+    }
+    if (e == cudaSuccess) e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? COMMITKV_OK : COMMITKV_ERR_CUDA;
+}
+
+}  // extern "C"

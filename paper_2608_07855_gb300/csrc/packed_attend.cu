@@ -1,0 +1,181 @@
+// Attention over packed caches: entry points and the division of their work.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "packed.cuh"
+
+namespace ckv {
+namespace pk {
+namespace {
+
+using at::kAlign;
+
+// The same trajectories as the full-width calls' checks and sizes see them.
+void as_trajs(const commitkv_shape *s, int n, const commitkv_packed *x, commitkv_traj *tr) {
+  memset(tr, 0, n * sizeof *tr);
+  for (int t = 0; t < n; ++t) {
+    tr[t].k = x[t].k, tr[t].v = x[t].v;
+    tr[t].stride_tok = s->head_dim;
+    tr[t].pos = x[t].pos;
+    tr[t].S = x[t].S;
+    tr[t].q = x[t].q, tr[t].q_pos = x[t].q_pos;
+    tr[t].W = x[t].W;
+  }
+}
+
+commitkv_status check_call(const commitkv_shape *s, int n, const commitkv_packed *x, commitkv_traj *tr, bool queries) {
+  commitkv_status st = check_shape(s);
+  if (st) return st;
+  if ((st = check_caches(s, n, x, true, queries))) return st;
+  as_trajs(s, n, x, tr);
+  return at::check_args(s, n, tr, nullptr, queries);
+}
+
+size_t compact_bytes(int n, const commitkv_packed *x) {
+  size_t b = 0;
+  for (int t = 0; t < n; ++t) b += at::align_up((size_t)x[t].S);
+  return b;
+}
+
+enum { kSimt16, kSimt64, kPaths };
+constexpr at::PathInfo kPath[kPaths] = {{16, 64, 2, 1.0, 11.5}, {64, 64, 2, 1.0, 17.0}};
+
+}  // namespace
+}  // namespace pk
+}  // namespace ckv
+
+using namespace ckv;
+
+extern "C" {
+
+size_t commitkv_packed_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs) {
+  commitkv_traj tr[kMaxTraj];
+  if (pk::check_call(shape, n_traj, trajs, tr, false) != COMMITKV_OK) return 0;
+  return at::kAlign + std::max(at::partial_bytes(shape, at::partial_rows(shape, n_traj, tr, nullptr)),
+                               pk::compact_bytes(n_traj, trajs));
+}
+
+commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs,
+                                          const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,
+                                          float *const *lse_out, void *workspace, size_t workspace_bytes,
+                                          cudaStream_t stream) {
+  using namespace at;
+  commitkv_traj tr[kMaxTraj];
+  commitkv_status st = pk::check_call(shape, n_traj, trajs, tr, true);
+  if (st) return st;
+  if (window < 0 || sinks < 0 || !out) return COMMITKV_ERR_INVALID_ARG;
+  for (int t = 0; t < n_traj; ++t)
+    if (trajs[t].W > 0 && !out[t]) return COMMITKV_ERR_INVALID_ARG;
+  if (!workspace || (uintptr_t)workspace % kAlign ||
+      workspace_bytes < kAlign + partial_bytes(shape, partial_rows(shape, n_traj, tr, nullptr)))
+    return COMMITKV_ERR_WORKSPACE;
+
+  static thread_local pk::Launch P;
+  memset(&P, 0, sizeof P);
+  Launch &L = P.L;
+  L.M = shape->layers;
+  L.H = shape->kv_heads;
+  L.Hq = shape->q_heads;
+  L.g = shape->q_heads / shape->kv_heads;
+  L.d = shape->head_dim;
+  L.dtype = shape->dtype;
+  const float scale = shape->softmax_scale > 0.0f ? shape->softmax_scale : 1.0f / sqrtf((float)shape->head_dim);
+  L.scale_log2 = scale * 1.4426950408889634f;
+  L.window = window;
+  L.sinks = sinks;
+  for (int l = 0; l < shape->layers; ++l)
+    if (!layer_mask || layer_mask[l]) L.layer_ids[L.n_layers++] = (uint8_t)l;
+  L.n_traj = L.n_seg = n_traj;
+  const int64_t slices = (int64_t)L.n_layers * L.H;
+  int64_t rows = 0;
+  int path[kMaxTraj];
+  for (int t = 0; t < n_traj; ++t) {
+    const commitkv_packed &x = trajs[t];
+    const pk::Cache c = pk::to_dev(x);
+    L.t[t] = {x.q, x.q_pos, out[t], lse_out ? lse_out[t] : nullptr, x.W, 0};
+    Seg &sg = L.seg[t];
+    sg.k = c.k, sg.v = c.v;
+    sg.sl = c.sl, sg.sh = c.sh, sg.st = c.st;
+    P.sc[t] = {c.ks, c.vs, c.gl, c.gh, c.gt};
+    sg.pos = x.pos;
+    sg.S = x.S;
+    sg.t = t;
+    sg.R = L.g * x.W;
+    rows += sg.R;
+    path[t] = sg.R <= 16 ? pk::kSimt16 : pk::kSimt64;
+  }
+  if (rows == 0 || L.n_layers == 0) return COMMITKV_OK;
+  const int sms = sm_count();
+  if (sms < 1) return COMMITKV_ERR_CUDA;
+  for (int s = 0; s < n_traj; ++s) L.order[s] = (uint8_t)s;
+  std::sort(L.order, L.order + n_traj,
+            [&](int a, int b) { return L.seg[a].S != L.seg[b].S ? L.seg[a].S > L.seg[b].S : a < b; });
+  int64_t split_left[2] = {kMaxSplitSmall, kMaxSplit};
+  for (int p = 0; p < pk::kPaths; ++p) {
+    const PathInfo &pi = pk::kPath[p];
+    int64_t &left = split_left[pi.rows > 16];
+    Divide v;
+    int ids[kMaxTraj];
+    v.n = 0;
+    for (int k = 0; k < n_traj; ++k) {
+      const int s = L.order[k];
+      Seg &sg = L.seg[s];
+      if (path[s] != p) continue;
+      sg.nrt = (int32_t)cdiv(sg.R, pi.rows);
+      v.base[v.n] = slices * sg.nrt;
+      v.rows[v.n] = slices * sg.R;
+      v.tiles[v.n] = sg.R > 0 ? cdiv(std::min<int64_t>(sg.S, most_seen(L, sg, pi.rows)), pi.tile) : 0;
+      ids[v.n++] = s;
+    }
+    if (v.n == 0) continue;
+    const Division dv = divide(v, pi, (int64_t)sms * pi.resident, left, slices, false);
+    int64_t items = 0;
+    for (int i = 0; i < v.n; ++i) {
+      Seg &sg = L.seg[ids[i]];
+      const bool rest = dv.rest >= 0 && v.base[i] > 0 && v.tiles[i] > 0;
+      sg.nchunk = (int32_t)(rest ? dv.chunks : std::max<int64_t>(1, cdiv(v.tiles[i], dv.len)));
+      sg.nsplit = (int32_t)(rest ? dv.rest : sg.nchunk > 1 ? sg.nrt : 0);
+      left -= slices * sg.nsplit * sg.nchunk;
+      sg.Rs = std::min(sg.R, sg.nsplit * pi.rows);
+      items += slices * ((sg.nrt - sg.nsplit) + (int64_t)sg.nsplit * sg.nchunk);
+      if (items > (1 << 30)) return COMMITKV_ERR_UNSUPPORTED;
+    }
+  }
+  int64_t parts = 0;
+  bool merge = false;
+  for (int s = 0; s < n_traj; ++s) {
+    Seg &sg = L.seg[s];
+    sg.part = parts;
+    parts += slices * sg.nchunk * sg.Rs;
+    L.out_off[s + 1] = L.out_off[s] + sg.Rs * L.H;
+    merge = merge || sg.Rs > 0;
+  }
+  if (kAlign + partial_bytes(shape, parts) > workspace_bytes) return COMMITKV_ERR_WORKSPACE;  // partial_rows bounds it
+  char *base = static_cast<char *>(workspace) + kAlign;
+  L.po = reinterpret_cast<float *>(base);
+  L.pml = reinterpret_cast<float2 *>(base + align_up((size_t)parts * L.d * 4));
+  cudaError_t e = cudaSuccess;
+  bool launched = false;
+  for (int p = 0; p < pk::kPaths && e == cudaSuccess; ++p) {
+    int32_t items = 0;
+    for (int k = 0; k < n_traj; ++k) {
+      const int s = L.order[k];
+      const Seg &sg = L.seg[s];
+      L.item_off[k] = items;
+      if (path[s] == p) items += (int32_t)(slices * (sg.nrt - sg.nsplit + sg.nsplit * sg.nchunk));
+    }
+    L.item_off[n_traj] = items;
+    if (items == 0) continue;
+    L.rows_per_item = pk::kPath[p].rows;
+    e = pk::launch_simt(P, stream, launched);
+    launched = true;
+  }
+  if (e == cudaSuccess && merge) e = launch_combine(L, stream);
+  if (e == cudaSuccess) return COMMITKV_OK;
+  cudaGetLastError();
+  return COMMITKV_ERR_CUDA;
+}
+
+}  // extern "C"
