@@ -51,6 +51,8 @@ static_assert(sizeof(Launch) <= 32764, "kernel parameters");
 
 // CUDA cores: any alignment.  Rows per item: 16 or 64.
 cudaError_t launch_simt(const Launch &P, cudaStream_t s, bool early);
+// Wide caches, queries 16-byte aligned; 8 rows per item, or 16 (bf16).
+cudaError_t launch_rows(const Launch &P, cudaStream_t s, bool early);
 
 // Fills the full-width rows from the codes: launch for `n` caches.
 cudaError_t launch_read(const commitkv_shape *s, int n, const commitkv_packed *c, const commitkv_rows *r,

@@ -39,8 +39,9 @@ size_t compact_bytes(int n, const commitkv_packed *x) {
   return b;
 }
 
-enum { kSimt16, kSimt64, kPaths };
-constexpr at::PathInfo kPath[kPaths] = {{16, 64, 2, 1.0, 11.5}, {64, 64, 2, 1.0, 17.0}};
+enum { kSimt16, kSimt64, kRows8, kRows16, kPaths };
+constexpr at::PathInfo kPath[kPaths] = {
+    {16, 64, 2, 1.0, 11.5}, {64, 64, 2, 1.0, 17.0}, {8, 128, 3, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}};
 
 }  // namespace
 }  // namespace pk
@@ -91,6 +92,7 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
   const int64_t slices = (int64_t)L.n_layers * L.H;
   int64_t rows = 0;
   int path[kMaxTraj];
+  const Forced forced = forced_paths();
   for (int t = 0; t < n_traj; ++t) {
     const commitkv_packed &x = trajs[t];
     const pk::Cache c = pk::to_dev(x);
@@ -104,7 +106,8 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     sg.t = t;
     sg.R = L.g * x.W;
     rows += sg.R;
-    path[t] = sg.R <= 16 ? pk::kSimt16 : pk::kSimt64;
+    const bool fast = !forced.cuda_cores && pk::wide(c, L.d) && (uintptr_t)x.q % 16 == 0;
+    path[t] = sg.R > 16 ? pk::kSimt64 : !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
   }
   if (rows == 0 || L.n_layers == 0) return COMMITKV_OK;
   const int sms = sm_count();
@@ -169,7 +172,7 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     L.item_off[n_traj] = items;
     if (items == 0) continue;
     L.rows_per_item = pk::kPath[p].rows;
-    e = pk::launch_simt(P, stream, launched);
+    e = p == pk::kRows8 || p == pk::kRows16 ? pk::launch_rows(P, stream, launched) : pk::launch_simt(P, stream, launched);
     launched = true;
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);

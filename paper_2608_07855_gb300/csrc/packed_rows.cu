@@ -1,0 +1,512 @@
+// Attention over packed caches with 8 or 16 query rows of a (layer, KV head)
+// slice to an item: decoded tokens (the g heads of one to a few positions).
+// Codes 16-byte aligned, scale rows whole.
+//
+// Such a call is bound by reading the codes once: 12 values a ns from memory,
+// some 40 a clock and SM, so that what a value costs in instructions decides
+// whether the memory is kept busy (three a lane and value would be all of them).
+// A warp works by itself on 32 tokens at a time, from a ring of its own in shared
+// memory (cp.async).  Products are warp-level MMAs of fp16 with the tokens and
+// channels as the 16 rows and the query rows as the 8 columns, S^T = K Q^T and
+// O^T = V^T P^T: one for 256 values, where the other way round (query rows as the
+// 16 rows) takes one for 128.
+//
+// Codes become fp16 operands in registers.  A word holds eight channels' codes;
+// (w << 4, w, w >> 4, w >> 8) & 0x00f000f0 | 0x54005400 are four pairs of the
+// fp16 numbers 64 + u, and one fma with (s, -72 s) makes (u - 8) s of each pair:
+// exact, since s has four significant bits, 72 s seven and the result eight.
+// s = sigma / 2, so that 72 s stays below 65504 for every sigma and the smallest
+// is the smallest fp16 number.  The channels of a pair are (i, i + 4) of a word:
+// Q is laid out the same way.  For V a pair is one channel of two tokens, from the
+// two tokens' words after two byte permutations.
+//
+// Queries enter as q 2^k, k of the row such that the largest is near 2^14: a bf16
+// number whole (what is below 2^-38 of the row's largest is cut), an fp32 number
+// as two fp16 terms (2^-22 is lost).  Weights are 2^11 times exp2(s - m), where
+// m is raised when it falls behind by 4, so at most 2^15, in one fp16 term for bf16
+// (2^-12 of a weight is lost: the output's own rounding is 2^-9) and two for fp32.
+#include <string.h>
+
+#include "packed.cuh"
+#include "sm103.cuh"
+
+namespace ckv {
+namespace pk {
+namespace {
+
+using at::Item;
+using at::Seg;
+using at::Span;
+using at::Tiles;
+using at::Traj;
+using sm103::fast_exp2;
+using sm103::smem_addr;
+
+constexpr int NW = 4;
+constexpr int WT = 32;  // tokens of a warp,
+constexpr int TT = NW * WT;  // of a tile
+constexpr float kLazy = 4.0f, kLift = 11.0f;
+
+template <int D, int QT>
+struct Smem {
+  static constexpr int kRow = D / 2;            // bytes of codes
+  static constexpr int kStage = 2 * WT * kRow;  // K and V
+  static constexpr int NST = D == 128 ? 4 : 6;
+  union {
+    alignas(128) uint8_t ring[NW][NST][kStage];
+    float o[NW][8 * QT][D + 4];
+  };
+  float2 ml[NW][8 * QT];
+  unsigned nan[NW][8 * QT];
+};
+
+// Where a row's bytes stand in its tile: rows that a fragment reads together lie
+// in different banks.
+template <int D>
+__device__ __forceinline__ uint32_t k_at(int t) {
+  return D == 128 ? t * 64 : (t * 32) ^ ((t >> 3 & 1) << 6);
+}
+template <int D>
+__device__ __forceinline__ uint32_t v_at(int t) {
+  return D == 128 ? (t * 64) ^ ((t >> 4 & 1) << 6) ^ ((t >> 3 & 1) << 5) : (t * 32) ^ ((t >> 3 & 3) << 5);
+}
+
+template <int N>
+__device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N]) {
+  if constexpr (N == 4)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a) : "memory");
+  else if constexpr (N == 2)
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a) : "memory");
+  else
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(a) : "memory");
+}
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
+__device__ __forceinline__ __half2 half2_of(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
+
+// A pair of scales and what the offset of their codes takes away again.
+struct Sc {
+  __half2 s, off;
+};
+// from the two bytes at bits 8 .. 15 and 24 .. 31 (the others are not read)
+__device__ __forceinline__ Sc scales_of(uint32_t x) {
+  Sc r;
+  r.s = __hmul2(half2_of(x >> 1 & 0x7f807f80u), __float2half2_rn(0.0078125f));
+  r.off = __hmul2(r.s, __float2half2_rn(-72.0f));
+  return r;
+}
+// pair P of a word's four
+template <int P>
+__device__ __forceinline__ uint32_t values_of(uint32_t w, const Sc &s) {
+  const uint32_t x = P == 0 ? w << 4 : P == 1 ? w : P == 2 ? w >> 4 : w >> 8;
+  return bits(__hfma2(half2_of((x & 0x00f000f0u) | 0x54005400u), s.s, s.off));
+}
+
+// x = hi + lo as fp16 terms.
+__device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t &lo) {
+  const __half2 h = __floats2half2_rn(x, y);
+  hi = bits(h);
+  lo = bits(__floats2half2_rn(x - __low2float(h), y - __high2float(h)));
+}
+
+// Bit g: byte g of a token's scale bytes is NaN.
+template <int D>
+__device__ __forceinline__ unsigned nan_groups(uint32_t w) {
+  unsigned m = 0;
+#pragma unroll
+  for (int g = 0; g < D / kGroup; ++g) m |= ((w >> (8 * g) & 0xffu) >= kNanScale ? 1u : 0u) << g;
+  return m;
+}
+
+template <typename T, int D, int QT>
+__global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(const __grid_constant__ Launch P) {
+  using S = Smem<D, QT>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int RI = 8 * QT, KW = D / 32, VW = D / 64, KS = D / 16, MT = D / 16, NST = S::NST;
+  extern __shared__ __align__(128) uint8_t raw[];
+  S &sm = *reinterpret_cast<S *>(raw);
+  const at::Launch &L = P.L;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, c = lane % 4;
+  at::pdl_start_next();
+  const Item it = at::decode_item(L, blockIdx.x);
+  const Seg &sg = L.seg[it.s];
+  const Scales &sc = P.sc[it.s];
+  const Traj &tj = L.t[it.s];
+
+  const int r0 = it.rt * RI, rows = min(RI, sg.R - r0);
+  // what the rows see: row r in lane r
+  Span mine = {0, 0x7fffffff, 0};
+  int lo = 0x7fffffff, hi = 0, se = 0;
+  if (lane < rows) {
+    mine = at::row_span(sg.pos, sg.S, tj.qpos[(r0 + lane) / L.g], L.window, L.sinks);
+    if (mine.lo < mine.hi) lo = mine.lo, hi = mine.hi;
+    se = mine.se;
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    se = max(se, __shfl_xor_sync(0xffffffffu, se, o));
+  }
+  lo = __shfl_sync(0xffffffffu, lo, 0), hi = __shfl_sync(0xffffffffu, hi, 0), se = __shfl_sync(0xffffffffu, se, 0);
+  const Tiles tl = at::make_tiles(lo, hi, se, TT);
+  const int j0 = at::chunk_tile(tl, it.c, it.n), j1 = at::chunk_tile(tl, it.c + 1, it.n);
+
+  const int64_t base = it.l * sg.sl + it.kvh * sg.sh, sbase = it.l * sc.gl + it.kvh * sc.gh;
+  const uint8_t *kb = static_cast<const uint8_t *>(sg.k) + base, *ksb = sc.k + sbase;
+  const int64_t dv = static_cast<const uint8_t *>(sg.v) - static_cast<const uint8_t *>(sg.k);
+  const uint8_t *vsb = sc.v + sbase;
+  const uint32_t ring = smem_addr(sm.ring[warp]);
+  // copies of tile j into its stage: tokens behind the tile's end as its last one's
+  auto load = [&](int j, int st) {
+    if (j < j1) {
+      const int a = at::tile_start(tl, j, TT) + WT * warp, e = at::tile_end(tl, j, TT);
+#pragma unroll
+      for (int i = 0; i < WT * KW / 32; ++i) {
+        const int x = i * 32 + lane, t = x / KW, ch = x % KW;
+        const uint8_t *src = kb + (int64_t)min(a + t, e - 1) * sg.st + 16 * ch;
+        const uint32_t dst = ring + st * S::kStage;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (k_at<D>(t) ^ (16 * ch))), "l"(src) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + WT * S::kRow + (v_at<D>(t) ^ (16 * ch))), "l"(src + dv)
+                     : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // a token's scale bytes, of K and V, in its lane; none: zeros
+  auto load_scales = [&](int j, uint32_t &k, uint32_t &v) {
+    k = v = 0;
+    if (j < j1) {
+      const int t = at::tile_start(tl, j, TT) + WT * warp + lane;
+      if (t < at::tile_end(tl, j, TT)) {
+        const int64_t at = (int64_t)t * sc.gt;
+        if constexpr (D == 128) {
+          k = __ldg(reinterpret_cast<const uint32_t *>(ksb + at));
+          v = __ldg(reinterpret_cast<const uint32_t *>(vsb + at));
+        } else {
+          k = __ldg(reinterpret_cast<const uint16_t *>(ksb + at));
+          v = __ldg(reinterpret_cast<const uint16_t *>(vsb + at));
+        }
+      }
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < NST - 1; ++s) load(j0 + s, s);
+  uint32_t ksc, vsc;
+  load_scales(j0, ksc, vsc);
+
+  // Q^T as the B operand: lane (r, c) holds query row r's channels of its K words
+  uint32_t q[QT][KS][2], ql[QT][F32 ? KS : 1][2];
+  float back[QT][2];  // 2^(1 - k) of the rows 2 c and 2 c + 1
+  Span sp[QT][2];
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const int row = r0 + 8 * n + r;
+    float f[KW][8], top = 0.0f;
+    if (8 * n + r < rows) {
+      const T *src = static_cast<const T *>(tj.q) + at::row_index(L, tj, it.l, it.kvh, row) * D + 8 * KW * c;
+#pragma unroll
+      for (int x = 0; x < KW; ++x) {
+        if constexpr (F32) {
+          const float4 a = reinterpret_cast<const float4 *>(src)[2 * x], b = reinterpret_cast<const float4 *>(src)[2 * x + 1];
+          f[x][0] = a.x, f[x][1] = a.y, f[x][2] = a.z, f[x][3] = a.w, f[x][4] = b.x, f[x][5] = b.y, f[x][6] = b.z, f[x][7] = b.w;
+        } else {
+          const uint4 w = reinterpret_cast<const uint4 *>(src)[x];
+          const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            f[x][2 * i] = __uint_as_float(y[i] << 16), f[x][2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = isfinite(f[x][i]) ? fmaxf(top, fabsf(f[x][i])) : top;
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < KW; ++x)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[x][i] = 0.0f;
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int k = top > 0.0f ? min(14 - ilogbf(top), 100) : 0;  // 100: smaller rows' scores are zero to fp32 anyway
+#pragma unroll
+    for (int x = 0; x < KW; ++x) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[x][i] = scalbnf(f[x][i], k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // pair i: k-step 2 x + i / 2, register i % 2
+        uint32_t h, l;
+        split2(f[x][i], f[x][i + 4], h, l);
+        q[n][2 * x + i / 2][i % 2] = h;
+        if constexpr (F32) ql[n][2 * x + i / 2][i % 2] = l;
+      }
+    }
+    const float b = scalbnf(1.0f, 1 - k);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      back[n][e] = __shfl_sync(0xffffffffu, b, 4 * (2 * c + e));
+      const int w = 8 * n + 2 * c + e;
+      sp[n][e] = {__shfl_sync(0xffffffffu, mine.lo, w), __shfl_sync(0xffffffffu, mine.hi, w),
+                  __shfl_sync(0xffffffffu, mine.se, w)};
+    }
+  }
+
+  float o[QT][MT][4];
+  float m[QT][2], lsum[QT][2];
+  unsigned gone[QT][2];  // groups of channels that are NaN
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][t][i] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, lsum[n][e] = 0.0f, gone[n][e] = 0;
+  }
+  // the lane's tokens of a tile: as rows of K's fragments tk + 4 i + 2 h (i: MMA,
+  // h: rows 0 .. 7 or 8 .. 15); as k of V's 8 c + 4 i + 2 h and the next one.  Row r
+  // of the scores is then k = r of the weights.
+  const int tk = 8 * (r >> 1) + (r & 1);
+  const uint32_t gk = D == 128 ? c : c >> 1, gv = D == 128 ? r >> 1 : r >> 2;  // the lane's groups
+  const uint32_t ksel = gk << 12 | gk << 4, vsel = (4 + gv) << 12 | gv << 4;
+  for (int j = j0, st = 0; j < j1; ++j) {
+    uint32_t kn, vn;
+    load_scales(j + 1, kn, vn);
+    asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
+    __syncwarp();  // every lane's copies of this stage are there, and its reads of the last one are done
+    load(j + NST - 1, st == 0 ? NST - 1 : st - 1);
+    const uint32_t ks = ring + st * S::kStage, vs = ks + WT * S::kRow;
+    st = st + 1 == NST ? 0 : st + 1;
+    const int a = at::tile_start(tl, j, TT) + WT * warp, e = at::tile_end(tl, j, TT);
+    if (a < e) {
+      float s[QT][2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int n = 0; n < QT; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[n][i][x] = 0.0f;
+        uint32_t w[2][KW];
+        Sc f[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = tk + 4 * i + 2 * h;
+          lds<KW>(ks + (k_at<D>(t) ^ (4 * KW * c)), w[h]);
+          f[h] = scales_of(__byte_perm(__shfl_sync(0xffffffffu, ksc, t), 0, ksel));
+        }
+#pragma unroll
+        for (int x = 0; x < KW; ++x) {
+          const uint32_t a0[4] = {values_of<0>(w[0][x], f[0]), values_of<0>(w[1][x], f[1]), values_of<1>(w[0][x], f[0]),
+                                  values_of<1>(w[1][x], f[1])};
+          const uint32_t a1[4] = {values_of<2>(w[0][x], f[0]), values_of<2>(w[1][x], f[1]), values_of<3>(w[0][x], f[0]),
+                                  values_of<3>(w[1][x], f[1])};
+#pragma unroll
+          for (int n = 0; n < QT; ++n) {
+            if constexpr (F32) {
+              mma(s[n][i], a0, ql[n][2 * x][0], ql[n][2 * x][1]);
+              mma(s[n][i], a1, ql[n][2 * x + 1][0], ql[n][2 * x + 1][1]);
+            }
+            mma(s[n][i], a0, q[n][2 * x][0], q[n][2 * x][1]);
+            mma(s[n][i], a1, q[n][2 * x + 1][0], q[n][2 * x + 1][1]);
+          }
+        }
+      }
+      const unsigned bad = nan_groups<D>(vsc);
+      if (__any_sync(0xffffffffu, bad)) {  // their values stand as zeros
+#pragma unroll
+        for (int g = 0; g < D / kGroup; ++g)
+          if (bad >> g & 1) vsc &= ~(0xffu << (8 * g));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned b = __shfl_sync(0xffffffffu, bad, tk + 2 * i);
+#pragma unroll
+          for (int n = 0; n < QT; ++n)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if (at::sees(sp[n][x], a + tk + 2 * i)) gone[n][x] |= b;
+        }
+      }
+      uint32_t p[QT][2][2], pl[QT][F32 ? 2 : 1][2];
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        float top[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const bool whole = a + WT <= e && sp[n][x].lo <= a && a + WT <= sp[n][x].hi;
+          top[x] = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float &y = s[n][i >> 1][2 * (i & 1) + x];
+            const int tok = a + tk + 2 * i;
+            y = __fmul_rn(y * back[n][x], L.scale_log2);
+            if (!whole) y = tok < e && at::sees(sp[n][x], tok) ? y : -INFINITY;
+            top[x] = fmaxf(top[x], y);
+          }
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[n][0] + kLazy || top[1] > m[n][1] + kLazy)) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], d));
+            if (top[x] > m[n][x] + kLazy) {
+              const float f = m[n][x] == -INFINITY ? 0.0f : exp2f(m[n][x] - top[x]);
+              lsum[n][x] *= f;
+#pragma unroll
+              for (int t = 0; t < MT; ++t) o[n][t][x] *= f, o[n][t][2 + x] *= f;
+              m[n][x] = top[x];
+            }
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float ref = m[n][x] == -INFINITY ? 0.0f : m[n][x];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float &y = s[n][i >> 1][2 * (i & 1) + x];
+            y = fast_exp2((y - ref) + kLift);
+            lsum[n][x] += y;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t hi2, lo2;
+            split2(s[n][i][2 * h], s[n][i][2 * h + 1], hi2, lo2);
+            p[n][i][h] = transposed(hi2);
+            if constexpr (F32) pl[n][i][h] = transposed(lo2);
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t w[4][VW];
+        Sc f[2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) lds<VW>(vs + (v_at<D>(8 * c + 4 * i + t) ^ (4 * VW * r)), w[t]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = 8 * c + 4 * i + 2 * h;
+          f[h] = scales_of(__byte_perm(__shfl_sync(0xffffffffu, vsc, t), __shfl_sync(0xffffffffu, vsc, t + 1), vsel));
+        }
+        // of each word the halves of two tokens side by side: y[h][word][half]
+        uint32_t y[2][VW][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int x = 0; x < VW; ++x) {
+            y[h][x][0] = __byte_perm(w[2 * h][x], w[2 * h + 1][x], 0x5410);
+            y[h][x][1] = __byte_perm(w[2 * h][x], w[2 * h + 1][x], 0x7632);
+          }
+        auto step = [&](int t, const uint32_t (&av)[4]) {
+#pragma unroll
+          for (int n = 0; n < QT; ++n) {
+            if constexpr (F32) mma(o[n][t], av, pl[n][i][0], pl[n][i][1]);
+            mma(o[n][t], av, p[n][i][0], p[n][i][1]);
+          }
+        };
+        // m-tile t: rows r and r + 8 are channels t of the lane's first and second
+        // word (128 channels), or t of the halves of its one word (64)
+#pragma unroll
+        for (int b = 0; b < MT / 4; ++b) {
+          auto part = [&](int h, int second) { return VW == 2 ? y[h][second % VW][b] : y[h][0][second]; };
+          const uint32_t a0[4] = {values_of<0>(part(0, 0), f[0]), values_of<0>(part(0, 1), f[0]),
+                                  values_of<0>(part(1, 0), f[1]), values_of<0>(part(1, 1), f[1])};
+          step(4 * b, a0);
+          const uint32_t a1[4] = {values_of<1>(part(0, 0), f[0]), values_of<1>(part(0, 1), f[0]),
+                                  values_of<1>(part(1, 0), f[1]), values_of<1>(part(1, 1), f[1])};
+          step(4 * b + 1, a1);
+          const uint32_t a2[4] = {values_of<2>(part(0, 0), f[0]), values_of<2>(part(0, 1), f[0]),
+                                  values_of<2>(part(1, 0), f[1]), values_of<2>(part(1, 1), f[1])};
+          step(4 * b + 2, a2);
+          const uint32_t a3[4] = {values_of<3>(part(0, 0), f[0]), values_of<3>(part(0, 1), f[0]),
+                                  values_of<3>(part(1, 0), f[1]), values_of<3>(part(1, 1), f[1])};
+          step(4 * b + 3, a3);
+        }
+      }
+    }
+    ksc = kn, vsc = vn;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+  for (int n = 0; n < QT; ++n)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        lsum[n][x] += __shfl_xor_sync(0xffffffffu, lsum[n][x], d);
+        gone[n][x] |= __shfl_xor_sync(0xffffffffu, gone[n][x], d);
+      }
+  __syncthreads();  // the rings are done with
+#pragma unroll
+  for (int n = 0; n < QT; ++n)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int w = 8 * n + 2 * c + x;
+      float *dst = &sm.o[warp][w][8 * VW * r];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        dst[t] = o[n][t][x] * 0.0009765625f;  // 2 / 2^11: values were halved, weights lifted
+        dst[MT + t] = o[n][t][2 + x] * 0.0009765625f;
+      }
+      if (r == 0) {
+        sm.ml[warp][w] = make_float2(m[n][x], lsum[n][x] * 0.00048828125f);
+        sm.nan[warp][w] = gone[n][x];
+      }
+    }
+  __syncthreads();
+  for (int w = warp; w < rows; w += NW) {
+    float mr = -INFINITY, lr = 0.0f, x[D / 32], f[NW];
+    unsigned nan = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) mr = fmaxf(mr, sm.ml[i][w].x), nan |= sm.nan[i][w];
+    const float ref = mr == -INFINITY ? 0.0f : mr;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      f[i] = exp2f(sm.ml[i][w].x - ref);
+      lr = fmaf(sm.ml[i][w].y, f[i], lr);
+    }
+#pragma unroll
+    for (int g = 0; g < D / 32; ++g) {  // channel lane + 32 g: group g
+      x[g] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) x[g] = fmaf(sm.o[i][w][lane + 32 * g], f[i], x[g]);
+      if (nan >> g & 1) x[g] = __int_as_float(0x7fffffff);
+    }
+    at::write_row_warp<T, D>(L, sg, it, r0 + w, x, mr, lr);
+  }
+  at::pdl_chain();
+}
+
+template <typename T, int D, int QT>
+cudaError_t launch(const Launch &P, cudaStream_t s, bool early) {
+  constexpr int smem = (int)sizeof(Smem<D, QT>);
+  const cudaError_t e =
+      cudaFuncSetAttribute(attend_packed_rows<T, D, QT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return at::launch_after(attend_packed_rows<T, D, QT>, P.L.item_off[P.L.n_seg], NW * 32, smem, s, early, P);
+}
+
+}  // namespace
+
+cudaError_t launch_rows(const Launch &P, cudaStream_t s, bool early) {
+  if (P.L.dtype == COMMITKV_F32) return P.L.d == 128 ? launch<float, 128, 1>(P, s, early) : launch<float, 64, 1>(P, s, early);
+  if (P.L.rows_per_item == 8)
+    return P.L.d == 128 ? launch<__nv_bfloat16, 128, 1>(P, s, early) : launch<__nv_bfloat16, 64, 1>(P, s, early);
+  return P.L.d == 128 ? launch<__nv_bfloat16, 128, 2>(P, s, early) : launch<__nv_bfloat16, 64, 2>(P, s, early);
+}
+
+}  // namespace pk
+}  // namespace ckv

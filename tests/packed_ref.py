@@ -50,7 +50,12 @@ def attention(k, v, pos, Q, qpos, window=0, sinks=0, scale=None, weights=0.0, qu
     lost; the rounding of scaled scores and of their maximum 2^-21 |s|.  2^x 2^-21,
     the reference and rescaling 2^-19 in all.  A weight enters the product with
     `weights` of it lost.  Sums of n weights in fp32: 2^-17 for the sizes here.
-    The output's own rounding: half a step."""
+    The output's own rounding: half a step.
+
+    fp16 terms end at 2^-24, so what they hold is off by 2^-25 at least.  A row's
+    weights stand as 2^11 and more for its largest: each may be off by 2^-36 of
+    that, which shows where the largest weights meet values of zero.  Its queries'
+    largest stands as 2^14 and more: an element may be off by 2^-39 of it."""
     M, Hq, W, d = Q.shape
     g = Hq // k.shape[1]
     scale = scale or d ** -0.5
@@ -75,8 +80,10 @@ def attention(k, v, pos, Q, qpos, window=0, sinks=0, scale=None, weights=0.0, qu
                     f = np.isfinite(sc)
                     top = (np.abs(kk[s][f]) @ np.abs(q[w])).max(initial=0) * scale
                     ds = ((d + 4) * 2.0 ** -23 + queries) * top + np.abs(sc[f]).max(initial=0) * 2.0 ** -21
+                    ds += 2.0 ** -39 * np.abs(q[w]).max() * np.abs(kk[s][f]).sum(1).max(initial=0) * scale
                     rel = 2 * (ds + 2.0 ** -19 + 2.0 ** -17) + weights
-                    to[l, h, w] = eps * np.abs(o[l, h, w]) + (1 + eps) * rel * (a @ np.abs(vv[s]))
+                    to[l, h, w] = eps * np.abs(o[l, h, w]) + \
+                        (1 + eps) * (rel * (a @ np.abs(vv[s])) + 2.0 ** -36 * a.max() * np.abs(vv[s]).sum(0))
                     tl[l, h, w] = ds + 2.0 ** -16 + 2.0 ** -22 * abs(lse[l, h, w])
     return o, lse, to, tl
 
