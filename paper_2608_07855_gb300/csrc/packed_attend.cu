@@ -41,7 +41,7 @@ size_t compact_bytes(int n, const commitkv_packed *x) {
 
 enum { kSimt16, kSimt64, kRows8, kRows16, kPaths };
 constexpr at::PathInfo kPath[kPaths] = {
-    {16, 64, 2, 1.0, 11.5}, {64, 64, 2, 1.0, 17.0}, {8, 128, 3, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}};
+    {16, 64, 2, 1.0, 11.5}, {64, 64, 2, 1.0, 17.0}, {8, 128, 4, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}};
 
 }  // namespace
 }  // namespace pk

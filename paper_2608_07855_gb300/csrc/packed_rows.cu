@@ -11,21 +11,26 @@
 // O^T = V^T P^T: one for 256 values, where the other way round (query rows as the
 // 16 rows) takes one for 128.
 //
-// Codes become fp16 operands in registers.  A word holds eight channels' codes;
-// (w << 4, w, w >> 4, w >> 8) & 0x00f000f0 | 0x54005400 are four pairs of the
-// fp16 numbers 64 + u, and one fma with (s, -72 s) makes (u - 8) s of each pair:
-// exact, since s has four significant bits, 72 s seven and the result eight.
-// s = sigma / 2, so that 72 s stays below 65504 for every sigma and the smallest
-// is the smallest fp16 number.  The channels of a pair are (i, i + 4) of a word:
-// Q is laid out the same way.  For V a pair is one channel of two tokens, from the
-// two tokens' words after two byte permutations.
+// Codes become fp16 operands in registers.  A word w holds eight channels' codes.
+// (w & 0x000f000f) | 0x3c003c00 is the pair of fp16 numbers 1 + u / 2^10 of the
+// channels 0 and 4, (w & 0x00f000f0) | 0x2c002c00 the pair (64 + u) / 2^10 of 1 and
+// 5, w >> 8 gives those of 2, 6 and 3, 7 (Q is laid out the same way); one fma with
+// (s, -c s), s the fp16 number of the scale byte, makes (u - 8) s / 2^10 of each:
+// exact, since s has four significant bits, 1032 / 2^10 s eleven and the result
+// eight, and nothing passes 65504; but a byte below 32 would want bits below 2^-24.
+// A warp that meets one (a vote a tile) takes (64 + u) / 2^7 for all, which holds every
+// scale and wants two more shifts a word.  For V a pair is one channel of two
+// tokens, from the two tokens' words after two byte permutations.
 //
 // Queries enter as q 2^k, k of the row such that the largest is near 2^14: a bf16
 // number whole (what is below 2^-38 of the row's largest is cut), an fp32 number
-// as two fp16 terms (2^-22 is lost).  Weights are 2^11 times exp2(s - m), where
-// m is raised when it falls behind by 4, so at most 2^15, in one fp16 term for bf16
-// (2^-12 of a weight is lost: the output's own rounding is 2^-9) and two for fp32.
+// as two fp16 terms (2^-22 is lost).  Weights are exp2(s - m) with m 11 below
+// the largest score so far, raised when a score is 4 above that: at most 2^15,
+// in one fp16 term for bf16 (2^-12 of a weight is lost: the output's own rounding is
+// 2^-9) and two for fp32; what is below 2^-36 of the row's largest is cut.
 #include <string.h>
+
+#include <type_traits>
 
 #include "packed.cuh"
 #include "sm103.cuh"
@@ -51,7 +56,7 @@ template <int D, int QT>
 struct Smem {
   static constexpr int kRow = D / 2;            // bytes of codes
   static constexpr int kStage = 2 * WT * kRow;  // K and V
-  static constexpr int NST = D == 128 ? 4 : 6;
+  static constexpr int NST = D == 128 ? 3 : 6;
   union {
     alignas(128) uint8_t ring[NW][NST][kStage];
     float o[NW][8 * QT][D + 4];
@@ -82,11 +87,17 @@ __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N]) {
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
       "%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// d = a b
+__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, "
+      "%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
@@ -97,22 +108,37 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 __device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
 __device__ __forceinline__ __half2 half2_of(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 
-// A pair of scales and what the offset of their codes takes away again.
+// A pair of scales, as the fp16 numbers of their bytes, and what the offsets of
+// the codes take away again.
+template <bool SMALL>
 struct Sc {
-  __half2 s, off;
+  __half2 s, low, high;
 };
-// from the two bytes at bits 8 .. 15 and 24 .. 31 (the others are not read)
-__device__ __forceinline__ Sc scales_of(uint32_t x) {
-  Sc r;
-  r.s = __hmul2(half2_of(x >> 1 & 0x7f807f80u), __float2half2_rn(0.0078125f));
-  r.off = __hmul2(r.s, __float2half2_rn(-72.0f));
+// from the two bytes at bits 7 .. 14 and 23 .. 30
+template <bool SMALL>
+__device__ __forceinline__ Sc<SMALL> scales_of(uint32_t x) {
+  Sc<SMALL> r;
+  r.s = half2_of(x);
+  if (SMALL) r.low = r.high = __hmul2(r.s, __float2half2_rn(-0.5625f));
+  else r.low = __hmul2(r.s, __float2half2_rn(-1.0078125f)), r.high = __hmul2(r.s, __float2half2_rn(-0.0703125f));
   return r;
 }
+// (x & mask) | number
+__device__ __forceinline__ __half2 number_of(uint32_t x, uint32_t mask, uint32_t number) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(mask), "r"(number));
+  return half2_of(y);
+}
 // pair P of a word's four
-template <int P>
-__device__ __forceinline__ uint32_t values_of(uint32_t w, const Sc &s) {
-  const uint32_t x = P == 0 ? w << 4 : P == 1 ? w : P == 2 ? w >> 4 : w >> 8;
-  return bits(__hfma2(half2_of((x & 0x00f000f0u) | 0x54005400u), s.s, s.off));
+template <int P, bool SMALL>
+__device__ __forceinline__ uint32_t values_of(uint32_t w, const Sc<SMALL> &s) {
+  if (SMALL) {
+    const uint32_t x = P == 0 ? w << 4 : P == 1 ? w : P == 2 ? w >> 4 : w >> 8;
+    return bits(__hfma2(number_of(x, 0x00f000f0u, 0x38003800u), s.s, s.low));
+  }
+  const uint32_t x = P < 2 ? w : w >> 8;
+  if (P % 2 == 0) return bits(__hfma2(number_of(x, 0x000f000fu, 0x3c003c00u), s.s, s.low));
+  return bits(__hfma2(number_of(x, 0x00f000f0u, 0x2c002c00u), s.s, s.high));
 }
 
 // x = hi + lo as fp16 terms.
@@ -132,7 +158,7 @@ __device__ __forceinline__ unsigned nan_groups(uint32_t w) {
 }
 
 template <typename T, int D, int QT>
-__global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(const __grid_constant__ Launch P) {
+__global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4) attend_packed_rows(const __grid_constant__ Launch P) {
   using S = Smem<D, QT>;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int RI = 8 * QT, KW = D / 32, VW = D / 64, KS = D / 16, MT = D / 16, NST = S::NST;
@@ -162,55 +188,81 @@ __global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(c
     se = max(se, __shfl_xor_sync(0xffffffffu, se, o));
   }
   lo = __shfl_sync(0xffffffffu, lo, 0), hi = __shfl_sync(0xffffffffu, hi, 0), se = __shfl_sync(0xffffffffu, se, 0);
+  // tokens that all rows see
+  int all_lo = lane < rows ? mine.lo : 0, all_hi = lane < rows ? mine.hi : 0x7fffffff;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    all_lo = max(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, o));
+    all_hi = min(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, o));
+  }
+  all_lo = __shfl_sync(0xffffffffu, all_lo, 0), all_hi = __shfl_sync(0xffffffffu, all_hi, 0);
   const Tiles tl = at::make_tiles(lo, hi, se, TT);
   const int j0 = at::chunk_tile(tl, it.c, it.n), j1 = at::chunk_tile(tl, it.c + 1, it.n);
 
   const int64_t base = it.l * sg.sl + it.kvh * sg.sh, sbase = it.l * sc.gl + it.kvh * sc.gh;
   const uint8_t *kb = static_cast<const uint8_t *>(sg.k) + base, *ksb = sc.k + sbase;
   const int64_t dv = static_cast<const uint8_t *>(sg.v) - static_cast<const uint8_t *>(sg.k);
-  const uint8_t *vsb = sc.v + sbase;
+  const int64_t dvs = sc.v - sc.k, step = 32 / KW * sg.st, tile_step = TT * sg.st, scale_step = TT * sc.gt;
   const uint32_t ring = smem_addr(sm.ring[warp]);
-  // copies of tile j into its stage: tokens behind the tile's end as its last one's
-  auto load = [&](int j, int st) {
-    if (j < j1) {
-      const int a = at::tile_start(tl, j, TT) + WT * warp, e = at::tile_end(tl, j, TT);
-#pragma unroll
-      for (int i = 0; i < WT * KW / 32; ++i) {
-        const int x = i * 32 + lane, t = x / KW, ch = x % KW;
-        const uint8_t *src = kb + (int64_t)min(a + t, e - 1) * sg.st + 16 * ch;
-        const uint32_t dst = ring + st * S::kStage;
+  // The chunk is one or two pieces of consecutive tokens (sinks, then the window);
+  // the warp's tokens of a piece's tiles begin at `at` and end with the piece.
+  struct Cursor {
+    int at, end;
+    const uint8_t *k, *s;  // the lane's rows of codes and scales there
+  };
+  auto cursor = [&](int j, int last) {  // tiles j .. last - 1 are of one piece
+    Cursor x;
+    x.at = at::tile_start(tl, j, TT) + WT * warp;
+    x.end = at::tile_end(tl, last - 1, TT);
+    x.k = kb + (int64_t)(x.at + lane / KW) * sg.st + 16 * (lane % KW);
+    x.s = ksb + (int64_t)(x.at + lane) * sc.gt;
+    return x;
+  };
+  // copies of the next tile into its stage: tokens behind the piece's end as its last one's
+  auto load = [&](Cursor &x, uint32_t dst) {
+    if (x.at < x.end) {
+      auto copy = [&](int i, const uint8_t *src) {
+        const int t = (i * 32 + lane) / KW, ch = lane % KW;
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (k_at<D>(t) ^ (16 * ch))), "l"(src) : "memory");
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + WT * S::kRow + (v_at<D>(t) ^ (16 * ch))), "l"(src + dv)
                      : "memory");
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  // a token's scale bytes, of K and V, in its lane; none: zeros
-  auto load_scales = [&](int j, uint32_t &k, uint32_t &v) {
-    k = v = 0;
-    if (j < j1) {
-      const int t = at::tile_start(tl, j, TT) + WT * warp + lane;
-      if (t < at::tile_end(tl, j, TT)) {
-        const int64_t at = (int64_t)t * sc.gt;
-        if constexpr (D == 128) {
-          k = __ldg(reinterpret_cast<const uint32_t *>(ksb + at));
-          v = __ldg(reinterpret_cast<const uint32_t *>(vsb + at));
-        } else {
-          k = __ldg(reinterpret_cast<const uint16_t *>(ksb + at));
-          v = __ldg(reinterpret_cast<const uint16_t *>(vsb + at));
+      };
+      if (x.at + WT <= x.end) {
+        const uint8_t *src = x.k;
+#pragma unroll
+        for (int i = 0; i < KW; ++i, src += step) copy(i, src);
+      } else {
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+          const int t = (i * 32 + lane) / KW;
+          copy(i, x.k + (int64_t)(min(x.at + t, x.end - 1) - x.at - lane / KW) * sg.st);
         }
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    x.at += TT, x.k += tile_step;
   };
+  // a token's scale bytes, of K and V, in its lane; none: zeros
+  auto load_scales = [&](Cursor &x, uint32_t &k, uint32_t &v) {
+    using W = typename std::conditional<D == 128, uint32_t, uint16_t>::type;
+    k = v = 0;
+    if (x.at + lane < x.end) {
+      k = __ldg(reinterpret_cast<const W *>(x.s));
+      v = __ldg(reinterpret_cast<const W *>(x.s + dvs));
+    }
+    x.at += TT, x.s += scale_step;
+  };
+  // the first piece's begin, before anything else is read
+  int j = j0, last = j0 < tl.nA ? min(tl.nA, j1) : j1;
+  Cursor in = j < last ? cursor(j, last) : Cursor{0, 0, kb, ksb}, sc_in = in;
 #pragma unroll
-  for (int s = 0; s < NST - 1; ++s) load(j0 + s, s);
+  for (int s = 0; s < NST - 1; ++s) load(in, ring + s * S::kStage);
   uint32_t ksc, vsc;
-  load_scales(j0, ksc, vsc);
+  load_scales(sc_in, ksc, vsc);
 
   // Q^T as the B operand: lane (r, c) holds query row r's channels of its K words
   uint32_t q[QT][KS][2], ql[QT][F32 ? KS : 1][2];
-  float back[QT][2];  // 2^(1 - k) of the rows 2 c and 2 c + 1
+  float back[QT][2];  // what makes scores of products, of the rows 2 c and 2 c + 1
   Span sp[QT][2];
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
@@ -241,11 +293,13 @@ __global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(c
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int k = top > 0.0f ? min(14 - ilogbf(top), 100) : 0;  // 100: smaller rows' scores are zero to fp32 anyway
+    // 100: smaller rows' scores are as good as zero
+    const int k = min(14 + 127 - (int)(__float_as_uint(top) >> 23), 100);
+    const float up = __uint_as_float((uint32_t)(127 + k) << 23);
 #pragma unroll
     for (int x = 0; x < KW; ++x) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[x][i] = scalbnf(f[x][i], k);
+      for (int i = 0; i < 8; ++i) f[x][i] *= up;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {  // pair i: k-step 2 x + i / 2, register i % 2
         uint32_t h, l;
@@ -254,7 +308,8 @@ __global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(c
         if constexpr (F32) ql[n][2 * x + i / 2][i % 2] = l;
       }
     }
-    const float b = scalbnf(1.0f, 1 - k);
+    // 16 / 2^k, and the softmax scale (which no score overflows by but that of a scale of 2^13 and more)
+    const float b = fminf(__uint_as_float((uint32_t)(131 - k) << 23) * L.scale_log2, 3.402823466e38f);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       back[n][e] = __shfl_sync(0xffffffffu, b, 4 * (2 * c + e));
@@ -265,7 +320,7 @@ __global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(c
   }
 
   float o[QT][MT][4];
-  float m[QT][2], lsum[QT][2];
+  float m[QT][2], over[QT][2], lsum[QT][2];  // the reference that weights are relative to, the score that raises it
   unsigned gone[QT][2];  // groups of channels that are NaN
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
@@ -274,170 +329,201 @@ __global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(c
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[n][t][i] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, lsum[n][e] = 0.0f, gone[n][e] = 0;
+    for (int e = 0; e < 2; ++e) m[n][e] = over[n][e] = -INFINITY, lsum[n][e] = 0.0f, gone[n][e] = 0;
   }
   // the lane's tokens of a tile: as rows of K's fragments tk + 4 i + 2 h (i: MMA,
   // h: rows 0 .. 7 or 8 .. 15); as k of V's 8 c + 4 i + 2 h and the next one.  Row r
   // of the scores is then k = r of the weights.
   const int tk = 8 * (r >> 1) + (r & 1);
   const uint32_t gk = D == 128 ? c : c >> 1, gv = D == 128 ? r >> 1 : r >> 2;  // the lane's groups
-  const uint32_t ksel = gk << 12 | gk << 4, vsel = (4 + gv) << 12 | gv << 4;
-  for (int j = j0, st = 0; j < j1; ++j) {
-    uint32_t kn, vn;
-    load_scales(j + 1, kn, vn);
-    asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
-    __syncwarp();  // every lane's copies of this stage are there, and its reads of the last one are done
-    load(j + NST - 1, st == 0 ? NST - 1 : st - 1);
-    const uint32_t ks = ring + st * S::kStage, vs = ks + WT * S::kRow;
-    st = st + 1 == NST ? 0 : st + 1;
-    const int a = at::tile_start(tl, j, TT) + WT * warp, e = at::tile_end(tl, j, TT);
-    if (a < e) {
-      float s[QT][2][4];
+  const uint32_t ksel = gk << 12 | gk << 4 | 0x0404, vsel = (4 + gv) << 12 | gv << 4;
+  auto tile = [&](auto is_small, int a, int e, uint32_t ks, uint32_t vs) {
+    constexpr bool SMALL = decltype(is_small)::value;
+    const bool whole = all_lo <= a && a + WT <= min(all_hi, e);
+    float s[QT][2][4];
+    uint32_t w[2][2][KW];
+    Sc<SMALL> f[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int t = tk + 4 * i + 2 * h;
+        lds<KW>(ks + (k_at<D>(t) ^ (4 * KW * c)), w[i][h]);
+        f[i][h] = scales_of<SMALL>(__byte_perm(__shfl_sync(0xffffffffu, ksc, t), 0, ksel) >> 1);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < KW; ++x)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        const uint32_t a0[4] = {values_of<0, SMALL>(w[i][0][x], f[i][0]), values_of<0, SMALL>(w[i][1][x], f[i][1]),
+                                values_of<1, SMALL>(w[i][0][x], f[i][0]), values_of<1, SMALL>(w[i][1][x], f[i][1])};
+        const uint32_t a1[4] = {values_of<2, SMALL>(w[i][0][x], f[i][0]), values_of<2, SMALL>(w[i][1][x], f[i][1]),
+                                values_of<3, SMALL>(w[i][0][x], f[i][0]), values_of<3, SMALL>(w[i][1][x], f[i][1])};
+#pragma unroll
+        for (int n = 0; n < QT; ++n) {
+          if constexpr (F32) {
+            if (x == 0) mma_first(s[n][i], a0, ql[n][0][0], ql[n][0][1]);
+            else mma(s[n][i], a0, ql[n][2 * x][0], ql[n][2 * x][1]);
+            mma(s[n][i], a1, ql[n][2 * x + 1][0], ql[n][2 * x + 1][1]);
+          }
+          if (x == 0 && !F32) mma_first(s[n][i], a0, q[n][0][0], q[n][0][1]);
+          else mma(s[n][i], a0, q[n][2 * x][0], q[n][2 * x][1]);
+          mma(s[n][i], a1, q[n][2 * x + 1][0], q[n][2 * x + 1][1]);
+        }
+      }
+    if constexpr (SMALL) {  // NaN scales of values stand as zeros
+      const unsigned bad = nan_groups<D>(vsc);
+#pragma unroll
+      for (int g = 0; g < D / kGroup; ++g)
+        if (bad >> g & 1) vsc &= ~(0xffu << (8 * g));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned b = __shfl_sync(0xffffffffu, bad, tk + 2 * i);
 #pragma unroll
         for (int n = 0; n < QT; ++n)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) s[n][i][x] = 0.0f;
-        uint32_t w[2][KW];
-        Sc f[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int t = tk + 4 * i + 2 * h;
-          lds<KW>(ks + (k_at<D>(t) ^ (4 * KW * c)), w[h]);
-          f[h] = scales_of(__byte_perm(__shfl_sync(0xffffffffu, ksc, t), 0, ksel));
-        }
-#pragma unroll
-        for (int x = 0; x < KW; ++x) {
-          const uint32_t a0[4] = {values_of<0>(w[0][x], f[0]), values_of<0>(w[1][x], f[1]), values_of<1>(w[0][x], f[0]),
-                                  values_of<1>(w[1][x], f[1])};
-          const uint32_t a1[4] = {values_of<2>(w[0][x], f[0]), values_of<2>(w[1][x], f[1]), values_of<3>(w[0][x], f[0]),
-                                  values_of<3>(w[1][x], f[1])};
-#pragma unroll
-          for (int n = 0; n < QT; ++n) {
-            if constexpr (F32) {
-              mma(s[n][i], a0, ql[n][2 * x][0], ql[n][2 * x][1]);
-              mma(s[n][i], a1, ql[n][2 * x + 1][0], ql[n][2 * x + 1][1]);
-            }
-            mma(s[n][i], a0, q[n][2 * x][0], q[n][2 * x][1]);
-            mma(s[n][i], a1, q[n][2 * x + 1][0], q[n][2 * x + 1][1]);
-          }
-        }
+          for (int x = 0; x < 2; ++x)
+            if (at::sees(sp[n][x], a + tk + 2 * i)) gone[n][x] |= b;
       }
-      const unsigned bad = nan_groups<D>(vsc);
-      if (__any_sync(0xffffffffu, bad)) {  // their values stand as zeros
+    }
+    uint32_t p[QT][2][2], pl[QT][F32 ? 2 : 1][2];
 #pragma unroll
-        for (int g = 0; g < D / kGroup; ++g)
-          if (bad >> g & 1) vsc &= ~(0xffu << (8 * g));
+    for (int n = 0; n < QT; ++n) {
+      float top[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const unsigned b = __shfl_sync(0xffffffffu, bad, tk + 2 * i);
-#pragma unroll
-          for (int n = 0; n < QT; ++n)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-              if (at::sees(sp[n][x], a + tk + 2 * i)) gone[n][x] |= b;
+          float &y = s[n][i >> 1][2 * (i & 1) + x];
+          y = __fmul_rn(SMALL ? y * 0.125f : y, back[n][x]);
         }
-      }
-      uint32_t p[QT][2][2], pl[QT][F32 ? 2 : 1][2];
+      if (!whole) {
 #pragma unroll
-      for (int n = 0; n < QT; ++n) {
-        float top[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const bool whole = a + WT <= e && sp[n][x].lo <= a && a + WT <= sp[n][x].hi;
-          top[x] = -INFINITY;
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float &y = s[n][i >> 1][2 * (i & 1) + x];
             const int tok = a + tk + 2 * i;
-            y = __fmul_rn(y * back[n][x], L.scale_log2);
-            if (!whole) y = tok < e && at::sees(sp[n][x], tok) ? y : -INFINITY;
-            top[x] = fmaxf(top[x], y);
+            y = tok < e && at::sees(sp[n][x], tok) ? y : -INFINITY;
           }
-        }
-        if (__any_sync(0xffffffffu, top[0] > m[n][0] + kLazy || top[1] > m[n][1] + kLazy)) {
+      }
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], d));
-            if (top[x] > m[n][x] + kLazy) {
-              const float f = m[n][x] == -INFINITY ? 0.0f : exp2f(m[n][x] - top[x]);
-              lsum[n][x] *= f;
-#pragma unroll
-              for (int t = 0; t < MT; ++t) o[n][t][x] *= f, o[n][t][2 + x] *= f;
-              m[n][x] = top[x];
-            }
-          }
-        }
+      for (int x = 0; x < 2; ++x)
+        top[x] = fmaxf(fmaxf(s[n][0][x], s[n][0][2 + x]), fmaxf(s[n][1][x], s[n][1][2 + x]));
+      if (__any_sync(0xffffffffu, top[0] > over[n][0] || top[1] > over[n][1])) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const float ref = m[n][x] == -INFINITY ? 0.0f : m[n][x];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float &y = s[n][i >> 1][2 * (i & 1) + x];
-            y = fast_exp2((y - ref) + kLift);
-            lsum[n][x] += y;
+          for (int d = 4; d < 32; d <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], d));
+          if (top[x] > over[n][x]) {
+            const float r2 = top[x] - kLift, f2 = m[n][x] == -INFINITY ? 0.0f : exp2f(m[n][x] - r2);
+            lsum[n][x] *= f2;
+#pragma unroll
+            for (int t = 0; t < MT; ++t) o[n][t][x] *= f2, o[n][t][2 + x] *= f2;
+            m[n][x] = r2;
+            over[n][x] = top[x] + kLazy;
           }
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t hi2, lo2;
-            split2(s[n][i][2 * h], s[n][i][2 * h + 1], hi2, lo2);
-            p[n][i][h] = transposed(hi2);
-            if constexpr (F32) pl[n][i][h] = transposed(lo2);
-          }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t w[4][VW];
-        Sc f[2];
+      for (int x = 0; x < 2; ++x) {
+        const float ref = m[n][x] == -INFINITY ? 0.0f : m[n][x];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) lds<VW>(vs + (v_at<D>(8 * c + 4 * i + t) ^ (4 * VW * r)), w[t]);
+        for (int i = 0; i < 4; ++i) {
+          float &y = s[n][i >> 1][2 * (i & 1) + x];
+          y = fast_exp2(y - ref);
+          lsum[n][x] += y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int t = 8 * c + 4 * i + 2 * h;
-          f[h] = scales_of(__byte_perm(__shfl_sync(0xffffffffu, vsc, t), __shfl_sync(0xffffffffu, vsc, t + 1), vsel));
+          uint32_t hi2, lo2;
+          constexpr float u = SMALL ? 0.125f : 1.0f;
+          split2(s[n][i][2 * h] * u, s[n][i][2 * h + 1] * u, hi2, lo2);
+          p[n][i][h] = transposed(hi2);
+          if constexpr (F32) pl[n][i][h] = transposed(lo2);
         }
-        // of each word the halves of two tokens side by side: y[h][word][half]
-        uint32_t y[2][VW][2];
+    }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < 2; ++i) {
+      uint32_t w[4][VW];
+      Sc<SMALL> f[2];
 #pragma unroll
-          for (int x = 0; x < VW; ++x) {
-            y[h][x][0] = __byte_perm(w[2 * h][x], w[2 * h + 1][x], 0x5410);
-            y[h][x][1] = __byte_perm(w[2 * h][x], w[2 * h + 1][x], 0x7632);
-          }
-        auto step = [&](int t, const uint32_t (&av)[4]) {
+      for (int t = 0; t < 4; ++t) lds<VW>(vs + (v_at<D>(8 * c + 4 * i + t) ^ (4 * VW * r)), w[t]);
 #pragma unroll
-          for (int n = 0; n < QT; ++n) {
-            if constexpr (F32) mma(o[n][t], av, pl[n][i][0], pl[n][i][1]);
-            mma(o[n][t], av, p[n][i][0], p[n][i][1]);
-          }
-        };
-        // m-tile t: rows r and r + 8 are channels t of the lane's first and second
-        // word (128 channels), or t of the halves of its one word (64)
+      for (int h = 0; h < 2; ++h) {
+        const int t = 8 * c + 4 * i + 2 * h;
+        f[h] = scales_of<SMALL>(
+            __byte_perm(__shfl_sync(0xffffffffu, vsc, t), __shfl_sync(0xffffffffu, vsc, t + 1), vsel) >> 1 & 0x7f807f80u);
+      }
+      // of each word the halves of two tokens side by side: y[h][word][half]
+      uint32_t y[2][VW][2];
 #pragma unroll
-        for (int b = 0; b < MT / 4; ++b) {
-          auto part = [&](int h, int second) { return VW == 2 ? y[h][second % VW][b] : y[h][0][second]; };
-          const uint32_t a0[4] = {values_of<0>(part(0, 0), f[0]), values_of<0>(part(0, 1), f[0]),
-                                  values_of<0>(part(1, 0), f[1]), values_of<0>(part(1, 1), f[1])};
-          step(4 * b, a0);
-          const uint32_t a1[4] = {values_of<1>(part(0, 0), f[0]), values_of<1>(part(0, 1), f[0]),
-                                  values_of<1>(part(1, 0), f[1]), values_of<1>(part(1, 1), f[1])};
-          step(4 * b + 1, a1);
-          const uint32_t a2[4] = {values_of<2>(part(0, 0), f[0]), values_of<2>(part(0, 1), f[0]),
-                                  values_of<2>(part(1, 0), f[1]), values_of<2>(part(1, 1), f[1])};
-          step(4 * b + 2, a2);
-          const uint32_t a3[4] = {values_of<3>(part(0, 0), f[0]), values_of<3>(part(0, 1), f[0]),
-                                  values_of<3>(part(1, 0), f[1]), values_of<3>(part(1, 1), f[1])};
-          step(4 * b + 3, a3);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int x = 0; x < VW; ++x) {
+          y[h][x][0] = __byte_perm(w[2 * h][x], w[2 * h + 1][x], 0x5410);
+          y[h][x][1] = __byte_perm(w[2 * h][x], w[2 * h + 1][x], 0x7632);
         }
+      auto step = [&](int t, const uint32_t (&av)[4]) {
+#pragma unroll
+        for (int n = 0; n < QT; ++n) {
+          if constexpr (F32) mma(o[n][t], av, pl[n][i][0], pl[n][i][1]);
+          mma(o[n][t], av, p[n][i][0], p[n][i][1]);
+        }
+      };
+      // m-tile t: rows r and r + 8 are channels t of the lane's first and second
+      // word (128 channels), or t of the halves of its one word (64)
+#pragma unroll
+      for (int b = 0; b < MT / 4; ++b) {
+        auto part = [&](int h, int second) { return VW == 2 ? y[h][second % VW][b] : y[h][0][second]; };
+        const uint32_t a0[4] = {values_of<0, SMALL>(part(0, 0), f[0]), values_of<0, SMALL>(part(0, 1), f[0]),
+                                values_of<0, SMALL>(part(1, 0), f[1]), values_of<0, SMALL>(part(1, 1), f[1])};
+        step(4 * b, a0);
+        const uint32_t a1[4] = {values_of<1, SMALL>(part(0, 0), f[0]), values_of<1, SMALL>(part(0, 1), f[0]),
+                                values_of<1, SMALL>(part(1, 0), f[1]), values_of<1, SMALL>(part(1, 1), f[1])};
+        step(4 * b + 1, a1);
+        const uint32_t a2[4] = {values_of<2, SMALL>(part(0, 0), f[0]), values_of<2, SMALL>(part(0, 1), f[0]),
+                                values_of<2, SMALL>(part(1, 0), f[1]), values_of<2, SMALL>(part(1, 1), f[1])};
+        step(4 * b + 2, a2);
+        const uint32_t a3[4] = {values_of<3, SMALL>(part(0, 0), f[0]), values_of<3, SMALL>(part(0, 1), f[0]),
+                                values_of<3, SMALL>(part(1, 0), f[1]), values_of<3, SMALL>(part(1, 1), f[1])};
+        step(4 * b + 3, a3);
       }
     }
-    ksc = kn, vsc = vn;
+  };
+  // a byte from 1 to 31
+  auto small = [](uint32_t x) { return (((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & ~(x | x << 1 | x << 2) & 0x80808080u; };
+  while (j < last) {
+    int a = at::tile_start(tl, j, TT) + WT * warp, st = 0;
+    const int e = at::tile_end(tl, last - 1, TT);
+    for (; j < last; ++j, a += TT) {
+      uint32_t kn, vn;
+      load_scales(sc_in, kn, vn);
+      asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
+      __syncwarp();  // every lane's copies of this stage are there, and its reads of the last one are done
+      load(in, ring + (st == 0 ? NST - 1 : st - 1) * S::kStage);
+      const uint32_t ks = ring + st * S::kStage, vs = ks + WT * S::kRow;
+      st = st + 1 == NST ? 0 : st + 1;
+      if (a < e) {
+        const uint32_t nan = vsc & ((vsc & 0x7f7f7f7fu) + 0x08080808u) & 0x80808080u;  // a byte from 0xf8 on
+        if (__any_sync(0xffffffffu, small(ksc) | small(vsc) | nan)) tile(std::true_type{}, a, e, ks, vs);
+        else tile(std::false_type{}, a, e, ks, vs);
+      }
+      ksc = kn, vsc = vn;
+    }
+    last = j1;
+    if (j < last) {  // the window behind the sinks
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      in = sc_in = cursor(j, last);
+#pragma unroll
+      for (int s = 0; s < NST - 1; ++s) load(in, ring + s * S::kStage);
+      load_scales(sc_in, ksc, vsc);
+    }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
@@ -458,11 +544,11 @@ __global__ void __launch_bounds__(NW * 32, QT == 1 ? 3 : 2) attend_packed_rows(c
       float *dst = &sm.o[warp][w][8 * VW * r];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        dst[t] = o[n][t][x] * 0.0009765625f;  // 2 / 2^11: values were halved, weights lifted
-        dst[MT + t] = o[n][t][2 + x] * 0.0009765625f;
+        dst[t] = o[n][t][x] * 16.0f;
+        dst[MT + t] = o[n][t][2 + x] * 16.0f;
       }
       if (r == 0) {
-        sm.ml[warp][w] = make_float2(m[n][x], lsum[n][x] * 0.00048828125f);
+        sm.ml[warp][w] = make_float2(m[n][x], lsum[n][x]);
         sm.nan[warp][w] = gone[n][x];
       }
     }
