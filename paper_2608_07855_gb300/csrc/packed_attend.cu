@@ -39,9 +39,69 @@ size_t compact_bytes(int n, const commitkv_packed *x) {
   return b;
 }
 
-enum { kSimt16, kSimt64, kRows8, kRows16, kPaths };
+// Many rows: the trajectories' values in full width, a layer of all of them, K
+// before V, each [H][S][d] dense.
+bool many(const commitkv_shape *s, const commitkv_packed &x) { return (int64_t)(s->q_heads / s->kv_heads) * x.W > 16; }
+size_t full_bytes(const commitkv_shape *s, const commitkv_packed &x) {  // K or V
+  return at::align_up((size_t)s->kv_heads * x.S * s->head_dim * (s->dtype == COMMITKV_BF16 ? 2 : 4));
+}
+size_t back_bytes(const commitkv_shape *s, int n, const commitkv_packed *x) {
+  size_t b = 0;
+  for (int t = 0; t < n; ++t)
+    if (many(s, x[t])) b += 2 * full_bytes(s, x[t]);
+  return b;
+}
+
+// Attention of the trajectories of more than 16 rows, layer by layer: the layer's
+// values into the workspace, behind what the full-width call takes of it, then
+// that call.
+commitkv_status attend_many(const commitkv_shape *s, int n, const commitkv_packed *x, const uint8_t *mask, int32_t window,
+                            int32_t sinks, void *const *out, float *const *lse_out, void *workspace, size_t attention,
+                            cudaStream_t stream) {
+  commitkv_packed c[kMaxTraj];
+  commitkv_rows rows[kMaxTraj];
+  commitkv_traj tr[kMaxTraj] = {};
+  int32_t ids[kMaxTraj];
+  int m = 0;
+  char *at = static_cast<char *>(workspace) + attention;
+  commitkv_shape one = *s;
+  one.layers = 1;
+  for (int t = 0; t < n; ++t) {
+    if (!many(s, x[t])) continue;
+    ids[m] = t;
+    c[m] = x[t];
+    rows[m] = {at, at + full_bytes(s, x[t]), 0, (int64_t)x[t].S * s->head_dim, s->head_dim, 0, x[t].S};
+    at += 2 * full_bytes(s, x[t]);
+    tr[m].k = rows[m].k, tr[m].v = rows[m].v;
+    tr[m].stride_layer = rows[m].stride_head * s->kv_heads;
+    tr[m].stride_head = rows[m].stride_head, tr[m].stride_tok = s->head_dim;
+    tr[m].pos = x[t].pos, tr[m].S = x[t].S;
+    tr[m].q_pos = x[t].q_pos, tr[m].W = x[t].W;
+    ++m;
+  }
+  for (int l = 0; l < s->layers && m > 0; ++l) {
+    if (mask && !mask[l]) continue;
+    void *o[kMaxTraj];
+    float *lse[kMaxTraj];
+    const uint8_t layer = (uint8_t)l;
+    for (int i = 0; i < m; ++i) {
+      const commitkv_packed &y = x[ids[i]];
+      const int64_t r = (int64_t)l * s->q_heads * y.W, eb = s->dtype == COMMITKV_BF16 ? 2 : 4;
+      tr[i].q = static_cast<const char *>(y.q) + r * s->head_dim * eb;
+      o[i] = static_cast<char *>(out[ids[i]]) + r * s->head_dim * eb;
+      lse[i] = lse_out && lse_out[ids[i]] ? lse_out[ids[i]] + r : nullptr;
+    }
+    if (launch_read(s, m, c, rows, &layer, 1, stream) != cudaSuccess) return COMMITKV_ERR_CUDA;
+    const commitkv_status st =
+        at::attend(&one, m, tr, nullptr, nullptr, window, sinks, o, lse, workspace, attention, stream);
+    if (st) return st;
+  }
+  return COMMITKV_OK;
+}
+
+enum { kSimt16, kRows8, kRows16, kPaths };
 constexpr at::PathInfo kPath[kPaths] = {
-    {16, 64, 2, 1.0, 11.5}, {64, 64, 2, 1.0, 17.0}, {8, 128, 4, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}};
+    {16, 64, 2, 1.0, 11.5}, {8, 128, 4, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}};
 
 }  // namespace
 }  // namespace pk
@@ -54,7 +114,8 @@ extern "C" {
 size_t commitkv_packed_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs) {
   commitkv_traj tr[kMaxTraj];
   if (pk::check_call(shape, n_traj, trajs, tr, false) != COMMITKV_OK) return 0;
-  return at::kAlign + std::max(at::partial_bytes(shape, at::partial_rows(shape, n_traj, tr, nullptr)),
+  return at::kAlign + std::max(at::partial_bytes(shape, at::partial_rows(shape, n_traj, tr, nullptr)) +
+                                   pk::back_bytes(shape, n_traj, trajs),
                                pk::compact_bytes(n_traj, trajs));
 }
 
@@ -69,8 +130,8 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
   if (window < 0 || sinks < 0 || !out) return COMMITKV_ERR_INVALID_ARG;
   for (int t = 0; t < n_traj; ++t)
     if (trajs[t].W > 0 && !out[t]) return COMMITKV_ERR_INVALID_ARG;
-  if (!workspace || (uintptr_t)workspace % kAlign ||
-      workspace_bytes < kAlign + partial_bytes(shape, partial_rows(shape, n_traj, tr, nullptr)))
+  const size_t attention = kAlign + partial_bytes(shape, partial_rows(shape, n_traj, tr, nullptr));
+  if (!workspace || (uintptr_t)workspace % kAlign || workspace_bytes < attention + pk::back_bytes(shape, n_traj, trajs))
     return COMMITKV_ERR_WORKSPACE;
 
   static thread_local pk::Launch P;
@@ -91,6 +152,7 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
   L.n_traj = L.n_seg = n_traj;
   const int64_t slices = (int64_t)L.n_layers * L.H;
   int64_t rows = 0;
+  bool big = false;
   int path[kMaxTraj];
   const Forced forced = forced_paths();
   for (int t = 0; t < n_traj; ++t) {
@@ -104,12 +166,13 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     sg.pos = x.pos;
     sg.S = x.S;
     sg.t = t;
-    sg.R = L.g * x.W;
+    sg.R = pk::many(shape, x) ? 0 : L.g * x.W;
     rows += sg.R;
+    big = big || pk::many(shape, x);
     const bool fast = !forced.cuda_cores && pk::wide(c, L.d) && (uintptr_t)x.q % 16 == 0;
-    path[t] = sg.R > 16 ? pk::kSimt64 : !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
+    path[t] = !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
   }
-  if (rows == 0 || L.n_layers == 0) return COMMITKV_OK;
+  if (L.n_layers == 0 || (rows == 0 && !big)) return COMMITKV_OK;
   const int sms = sm_count();
   if (sms < 1) return COMMITKV_ERR_CUDA;
   for (int s = 0; s < n_traj; ++s) L.order[s] = (uint8_t)s;
@@ -176,7 +239,9 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     launched = true;
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);
-  if (e == cudaSuccess) return COMMITKV_OK;
+  if (e == cudaSuccess)
+    return big ? pk::attend_many(shape, n_traj, trajs, layer_mask, window, sinks, out, lse_out, workspace, attention, stream)
+               : COMMITKV_OK;
   cudaGetLastError();
   return COMMITKV_ERR_CUDA;
 }

@@ -248,8 +248,7 @@ cudaError_t launch(const Launch &P, cudaStream_t s, bool early) {
 
 template <typename T>
 cudaError_t launch_t(const Launch &P, cudaStream_t s, bool early) {
-  if (P.L.rows_per_item == 16) return P.L.d == 128 ? launch<T, 128, 1>(P, s, early) : launch<T, 64, 1>(P, s, early);
-  return P.L.d == 128 ? launch<T, 128, 4>(P, s, early) : launch<T, 64, 4>(P, s, early);
+  return P.L.d == 128 ? launch<T, 128, 1>(P, s, early) : launch<T, 64, 1>(P, s, early);
 }
 
 }  // namespace
