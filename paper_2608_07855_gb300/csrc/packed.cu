@@ -4,7 +4,6 @@
 // All three move bytes: a thread has 8 channels of a row (write, read: 16 bytes
 // of bf16, 4 of codes, so that a warp's accesses are whole lines of consecutive
 // rows), or 32 channels (gather: 16 bytes of codes and their scale byte).
-#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -25,8 +24,7 @@ struct Rows {
   void *k, *v;
   int64_t sl, sh, st;  // in elements
   int32_t first, count;
-  int32_t heads_inner;  // rows are taken token by token
-  int32_t pad;
+  int32_t blocks;  // of a slice
 };
 
 struct CopyLaunch {
@@ -37,34 +35,76 @@ struct CopyLaunch {
 };
 static_assert(sizeof(CopyLaunch) <= 32764, "kernel parameters");
 
-// The row of a thread: place p of a (trajectory, layer)'s H * count rows.
+// A block's rows: tokens i0 .. of one (layer, KV head) of a trajectory, a head
+// after the other for the same tokens, so that rows that lie side by side in a
+// token-by-token layout are taken at the same time.  The thread's first row and
+// its channels' place in it; a step further is RB rows.
+template <int D>
 struct Place {
+  static constexpr int TR = D / 8, RB = kThreads / TR;  // threads of a row, rows of a step
+  const Rows &r;
+  int i, c;  // row, first channel
   int64_t code, scale, elem;
+  __device__ __forceinline__ Place(const CopyLaunch &L, const Rows &r_, int b) : r(r_) {
+    const int l = L.layer_ids[b / L.H / r.blocks], h = b % L.H, i0 = b / L.H % r.blocks * (RB * kUnroll);
+    i = i0 + (int)threadIdx.x / TR;
+    c = threadIdx.x % TR * 8;
+    const int64_t tok = (int64_t)r.first + i;
+    code = l * r.c.sl + h * r.c.sh + tok * r.c.st + c / 2;
+    scale = l * r.c.gl + h * r.c.gh + tok * r.c.gt + c / kGroup;
+    elem = l * r.sl + h * r.sh + i * r.st + c;
+  }
 };
-__device__ __forceinline__ Place place_of(const Rows &r, int l, int p, int H) {
-  int h, i;
-  if (r.heads_inner) i = p / H, h = p % H;
-  else h = p / r.count, i = p % r.count;
-  const int64_t tok = (int64_t)r.first + i;
-  return {l * r.c.sl + h * r.c.sh + tok * r.c.st, l * r.c.gl + h * r.c.gh + tok * r.c.gt,
-          l * r.sl + h * r.sh + i * r.st};
+__device__ __forceinline__ int traj_of_block(const CopyLaunch &L) {
+  int t = 0, e = L.n_traj;
+  while (e - t > 1) {
+    const int m = (t + e) >> 1;
+    if ((int)blockIdx.x >= L.off[m]) t = m;
+    else e = m;
+  }
+  return t;
 }
 
-// Eight channels as fp32.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T *src, float (&x)[8]) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    const uint4 w = *reinterpret_cast<const uint4 *>(src);
-    const uint32_t y[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(y[i] << 16), x[2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
-  } else if constexpr (VEC) {
-    const float4 a = reinterpret_cast<const float4 *>(src)[0], b = reinterpret_cast<const float4 *>(src)[1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f32(src[i]);
+// Eight channels of a row, as they are in memory.
+template <typename T>
+struct Eight {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ float get(int i) const {
+    if (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ Eight<T> load8(const T *src) {
+  Eight<T> x;
+#pragma unroll
+  for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+    if (VEC) {
+      const uint4 v = reinterpret_cast<const uint4 *>(src)[k];
+      x.w[4 * k] = v.x, x.w[4 * k + 1] = v.y, x.w[4 * k + 2] = v.z, x.w[4 * k + 3] = v.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (sizeof(T) == 4) x.w[4 * k + i] = reinterpret_cast<const uint32_t *>(src)[4 * k + i];
+        else
+          x.w[i] = reinterpret_cast<const uint16_t *>(src)[2 * i] |
+                   (uint32_t)reinterpret_cast<const uint16_t *>(src)[2 * i + 1] << 16;
+      }
+    }
+  }
+  return x;
+}
+// The largest magnitude, as an fp32 number's bits (from 0x7f800000 on: not finite).
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const Eight<T> &x) {
+  if (sizeof(T) == 4) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, x.w[i] & 0x7fffffffu);
+    return m;
+  }
+  uint32_t m = __vmaxu2(__vmaxu2(x.w[0] & 0x7fff7fffu, x.w[1] & 0x7fff7fffu), __vmaxu2(x.w[2] & 0x7fff7fffu, x.w[3] & 0x7fff7fffu));
+  return max(m << 16, m & 0xffff0000u);
 }
 
 // sigma's byte for a largest magnitude a (finite): the one nearest to a / 7, of
@@ -77,11 +117,11 @@ __device__ __forceinline__ unsigned scale_byte(float a) {
   return b + (b < kNanScale - 1 && (a > mid || (a == mid && (b & 1))) ? 1u : 0u);
 }
 
-// The code of x for sigma > 0, inv near its inverse.  The product can only be on
-// the wrong side of a middle by rounding; the remainder is exact (a multiple of
-// x's last place, no larger than x) and says on which side x is, or that it is
-// a tie.
-__device__ __forceinline__ unsigned code_of(float x, float sigma, float inv) {
+// The code of x for sigma > 0, inv near its inverse, whatever x.  The product can
+// only be on the wrong side of a middle by rounding; the remainder is exact (a
+// multiple of x's last place, no larger than x) and says on which side x is, or
+// that it is a tie.
+__device__ __noinline__ unsigned code_of(float x, float sigma, float inv) {
   const float a = fabsf(x);
   float n = fminf(rintf(a * inv), 8.0f);
   const float r = fmaf(-n, sigma, a), t = 2.0f * fabsf(r);
@@ -91,25 +131,51 @@ __device__ __forceinline__ unsigned code_of(float x, float sigma, float inv) {
 }
 
 // Four lanes have a group's 32 channels; returns the scale byte, and the eight
-// codes of the lane.
-__device__ __forceinline__ unsigned encode(const float (&x)[8], uint32_t &codes) {
-  unsigned top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+// codes of the lane.  x / sigma lies between x low and x high, the neighbours of
+// 1 / sigma; both products rounded to whole numbers (by adding 3 2^22, one rounding)
+// agree unless a middle lies between them, as it does for a tie.  A bf16 number
+// there is the middle itself (its distance to a middle is 0 or 2^-8 of it and more),
+// so the even one of the two is right; an fp32 number is looked at again.
+template <typename T>
+__device__ __forceinline__ unsigned encode(const Eight<T> &x, uint32_t &codes) {
+  unsigned top = top_of(x);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   codes = 0x88888888u;
   if (top >= 0x7f800000u) return 0xff;  // infinite or NaN
   const unsigned b = scale_byte(__uint_as_float(top));
   if (b == 0) return 0;
-  const float sigma = sigma_of(b), inv = __frcp_rn(sigma);
-  codes = 0;
+  const float sigma = sigma_of(b);
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sigma));
+  const float e = fmaf(-sigma, inv, 1.0f);  // 0: exact
+  const float low = e < 0.0f ? __uint_as_float(__float_as_uint(inv) - 1) : inv;
+  const float high = e > 0.0f ? __uint_as_float(__float_as_uint(inv) + 1) : inv;
+  bool again = b < 8 || b == kNanScale - 1;  // x may be more than 7.5 sigma
+  uint32_t w = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) codes |= code_of(x[i], sigma, inv) << (4 * i);
+  for (int i = 7; i >= 0; --i) {
+    // the bits of 3 2^22 + n: even as n is, and the digits of their sum need no masks
+    const int n = __float_as_int(fmaf(x.get(i), low, 12582912.0f)), d = __float_as_int(fmaf(x.get(i), high, 12582912.0f)) - n;
+    if (sizeof(T) == 4) again = again || d != 0;
+    w = w * 16 + (sizeof(T) == 4 ? n : n + (n & 1) * d);
+  }
+  w += 0x88888888u - 0x11111111u * 0x4b400000u;  // every digit is 8 + n
+  if (again) {
+    w = 0;
+#pragma unroll 1
+    for (int i = 7; i >= 0; --i) {
+      float y = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y = k == i ? x.get(k) : y;
+      w = w * 16 + code_of(y, sigma, inv);
+    }
+  }
+  codes = w;
   return b;
 }
 
-template <typename T, bool VEC>
+template <bool VEC>
 __device__ __forceinline__ void store_codes(uint8_t *dst, uint32_t codes) {
   if (VEC) *reinterpret_cast<uint32_t *>(dst) = codes;
   else
@@ -117,110 +183,102 @@ __device__ __forceinline__ void store_codes(uint8_t *dst, uint32_t codes) {
     for (int i = 0; i < 4; ++i) dst[i] = (uint8_t)(codes >> (8 * i));
 }
 
-// Write: bound by reading the rows (2.8 to 5.3 bytes a value with K and V's
-// codes); a lane's 16-byte loads of K and V of all its rows are issued first.
+// Write: bound by reading the rows (2.5 bytes a value of bf16 with its codes; 4.5 of
+// fp32); a lane's loads of its rows are issued first, K's then V's.
 template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ CopyLaunch L) {
-  constexpr int TR = D / 8, RB = kThreads / TR;  // threads of a row, rows of a step
-  int t = 0, e = L.n_traj;
-  while (e - t > 1) {
-    const int m = (t + e) >> 1;
-    if ((int)blockIdx.x >= L.off[m]) t = m;
-    else e = m;
-  }
+  const int t = traj_of_block(L);
   const Rows &r = L.r[t];
-  const int rows = L.H * r.count, per = (rows + RB * kUnroll - 1) / (RB * kUnroll), b = blockIdx.x - L.off[t];
-  const int l = L.layer_ids[b / per], p0 = b % per * (RB * kUnroll) + threadIdx.x / TR, c = threadIdx.x % TR * 8;
+  const Place<D> p(L, r, blockIdx.x - L.off[t]);
+  const int64_t row_step = p.RB * r.st;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
-    float x[kUnroll][8];
-    Place at[kUnroll];
-    const T *src = static_cast<const T *>(kv ? r.v : r.k);
-    uint8_t *codes = kv ? r.c.v : r.c.k, *scales = kv ? r.c.vs : r.c.ks;
+    Eight<T> x[kUnroll];
+    const T *src = static_cast<const T *>(kv ? r.v : r.k) + p.elem;
+    uint8_t *codes = (kv ? r.c.v : r.c.k) + p.code, *scales = (kv ? r.c.vs : r.c.ks) + p.scale;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int p = p0 + u * RB;
-      if (p < rows) {
-        at[u] = place_of(r, l, p, L.H);
-        load8<T, VEC>(src + at[u].elem + c, x[u]);
+    for (int u = 0; u < kUnroll; ++u, src += row_step) {
+      if (p.i + u * p.RB < r.count) {
+        x[u] = load8<T, VEC>(src);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[u][i] = 0.0f;
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) x[u].w[i] = 0;
       }
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kUnroll; ++u, codes += p.RB * r.c.st, scales += p.RB * r.c.gt) {
       uint32_t w;
       const unsigned s = encode(x[u], w);
-      if (p0 + u * RB < rows) {
-        store_codes<T, VEC>(codes + at[u].code + c / 2, w);
-        if (c % kGroup == 0) scales[at[u].scale + c / kGroup] = (uint8_t)s;
+      if (p.i + u * p.RB < r.count) {
+        store_codes<VEC>(codes, w);
+        if (p.c % kGroup == 0) *scales = (uint8_t)s;
       }
     }
   }
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t pair_of(float a, float b);
-template <>
-__device__ __forceinline__ uint32_t pair_of<__nv_bfloat16>(float a, float b) {  // both are bf16 numbers: no rounding
-  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+// The values of a word's eight codes: (w >> 4 i & 0x000f000f) | 0x43004300 are the bf16
+// numbers 128 + u of the channels i and i + 4, one fma with (s, -136 s) makes them
+// (u - 8) s: exact (136 s has eight significant bits).  Then side by side.
+__device__ __forceinline__ void values8(uint32_t w, unsigned b, uint32_t (&x)[4]) {
+  const __nv_bfloat162 s = __float2bfloat162_rn(sigma_of(b)), off = __hmul2(s, __float2bfloat162_rn(-136.0f));
+  uint32_t p[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));
+    const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&y), s, off);
+    p[i] = *reinterpret_cast<const uint32_t *>(&v);
+  }
+  x[0] = __byte_perm(p[0], p[1], 0x5410);
+  x[1] = __byte_perm(p[2], p[3], 0x5410);
+  x[2] = __byte_perm(p[0], p[1], 0x7632);
+  x[3] = __byte_perm(p[2], p[3], 0x7632);
 }
 
 // Read: bound by writing the rows.
 template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ CopyLaunch L) {
-  constexpr int TR = D / 8, RB = kThreads / TR;
-  int t = 0, e = L.n_traj;
-  while (e - t > 1) {
-    const int m = (t + e) >> 1;
-    if ((int)blockIdx.x >= L.off[m]) t = m;
-    else e = m;
-  }
+  const int t = traj_of_block(L);
   const Rows &r = L.r[t];
-  const int rows = L.H * r.count, per = (rows + RB * kUnroll - 1) / (RB * kUnroll), b = blockIdx.x - L.off[t];
-  const int l = L.layer_ids[b / per], p0 = b % per * (RB * kUnroll) + threadIdx.x / TR, c = threadIdx.x % TR * 8;
+  const Place<D> p(L, r, blockIdx.x - L.off[t]);
   uint32_t w[2][kUnroll];
-  unsigned s[2][kUnroll];
-  int64_t at[kUnroll];
+  uint8_t s[2][kUnroll];
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    const int p = p0 + u * RB;
-    if (p >= rows) continue;
-    const Place pl = place_of(r, l, p, L.H);
-    at[u] = pl.elem + c;
+  for (int kv = 0; kv < 2; ++kv) {
+    const uint8_t *codes = (kv ? r.c.v : r.c.k) + p.code, *scales = (kv ? r.c.vs : r.c.ks) + p.scale;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const uint8_t *src = (kv ? r.c.v : r.c.k) + pl.code + c / 2;
+    for (int u = 0; u < kUnroll; ++u, codes += p.RB * r.c.st, scales += p.RB * r.c.gt) {
+      if (p.i + u * p.RB >= r.count) continue;
+      s[kv][u] = *scales;
       if (VEC) {
-        w[kv][u] = *reinterpret_cast<const uint32_t *>(src);
+        w[kv][u] = *reinterpret_cast<const uint32_t *>(codes);
       } else {
         w[kv][u] = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[kv][u] |= (uint32_t)src[i] << (8 * i);
+        for (int i = 0; i < 4; ++i) w[kv][u] |= (uint32_t)codes[i] << (8 * i);
       }
-      s[kv][u] = (kv ? r.c.vs : r.c.ks)[pl.scale + c / kGroup];
     }
   }
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    if (p0 + u * RB >= rows) continue;
+  for (int kv = 0; kv < 2; ++kv) {
+    T *dst = static_cast<T *>(kv ? r.v : r.k) + p.elem;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      T *dst = static_cast<T *>(kv ? r.v : r.k) + at[u];
-      const float sigma = sigma_of(s[kv][u]);
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (float)((int)(w[kv][u] >> (4 * i) & 15u) - 8) * sigma;
+    for (int u = 0; u < kUnroll; ++u, dst += p.RB * r.st) {
+      if (p.i + u * p.RB >= r.count) continue;
+      uint32_t x[4];
+      values8(w[kv][u], s[kv][u], x);
       if constexpr (VEC && sizeof(T) == 2) {
-        *reinterpret_cast<uint4 *>(dst) =
-            make_uint4(pair_of<T>(x[0], x[1]), pair_of<T>(x[2], x[3]), pair_of<T>(x[4], x[5]), pair_of<T>(x[6], x[7]));
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
       } else if constexpr (VEC) {
-        reinterpret_cast<float4 *>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4 *>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          reinterpret_cast<uint4 *>(dst)[i] =
+              make_uint4(x[2 * i] << 16, x[2 * i] & 0xffff0000u, x[2 * i + 1] << 16, x[2 * i + 1] & 0xffff0000u);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dst[i] = at::from_f32<T>(x[i]);
+        for (int i = 0; i < 8; ++i)
+          dst[i] = at::from_f32<T>(__uint_as_float(i % 2 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16));
       }
     }
   }
@@ -361,7 +419,7 @@ commitkv_status check_rows(const commitkv_shape *s, int n, const commitkv_packed
               : (s->layers > 1 && r[t].stride_layer == 0) || (s->kv_heads > 1 && r[t].stride_head == 0) ||
                     (r[t].count > 1 && r[t].stride_tok == 0))
       return COMMITKV_ERR_INVALID_ARG;
-    if ((int64_t)r[t].count * s->kv_heads > (1 << 30)) return COMMITKV_ERR_UNSUPPORTED;
+    if (r[t].count > (1 << 30)) return COMMITKV_ERR_UNSUPPORTED;  // row numbers and a block's more are 32-bit
   }
   return COMMITKV_OK;
 }
@@ -387,7 +445,7 @@ commitkv_status copy(const commitkv_shape *s, int n, const commitkv_packed *x, c
   L.H = s->kv_heads;
   L.n_layers = n_layers;
   memcpy(L.layer_ids, layers, n_layers);
-  const int eb = s->dtype == COMMITKV_BF16 ? 2 : 4, per = kThreads / (s->head_dim / 8) * kUnroll;
+  const int eb = s->dtype == COMMITKV_BF16 ? 2 : 4, per = kThreads / (s->head_dim / 8) * kUnroll;  // rows of a block
   uintptr_t wide_bits = 0, code_bits = 0;  // 16-byte rows, 4-byte codes
   int64_t blocks = 0;
   for (int t = 0; t < n; ++t) {
@@ -396,9 +454,9 @@ commitkv_status copy(const commitkv_shape *s, int n, const commitkv_packed *x, c
     d.k = r[t].k, d.v = r[t].v;
     d.sl = r[t].stride_layer, d.sh = r[t].stride_head, d.st = r[t].stride_tok;
     d.first = r[t].first, d.count = r[t].count;
-    d.heads_inner = llabs(d.sh) < llabs(d.st);
+    d.blocks = (int32_t)cdiv(r[t].count, per);
     L.off[t] = (int32_t)blocks;
-    blocks += (int64_t)n_layers * cdiv((int64_t)s->kv_heads * r[t].count, per);
+    blocks += (int64_t)n_layers * s->kv_heads * d.blocks;
     if (blocks >= (1ll << 31)) return COMMITKV_ERR_UNSUPPORTED;
     if (r[t].count == 0) continue;
     wide_bits |= (uintptr_t)d.k | (uintptr_t)d.v | (uintptr_t)((d.sl | d.sh | d.st) * eb);
