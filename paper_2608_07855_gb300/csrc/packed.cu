@@ -1,9 +1,9 @@
 // Packed caches: writing rows as codes and scales, reading them back, and the
 // gather of a checkpoint.
 //
-// All three move bytes: a thread has 8 channels of a row (write, read: 16 bytes
-// of bf16, 4 of codes, so that a warp's accesses are whole lines of consecutive
-// rows), or 32 channels (gather: 16 bytes of codes and their scale byte).
+// All three move bytes.  A thread has 32 channels where codes move whole (write,
+// gather: 16 bytes of codes and their scale byte), and 8 where full-width rows are
+// written (read: 16 bytes of bf16), so that stores are whole lines.
 #include <string.h>
 
 #include <algorithm>
@@ -15,7 +15,8 @@ namespace pk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;  // rows of a thread, loads in flight together
+constexpr int kUnroll = 4;  // rows of a thread, loads in flight together,
+constexpr int kWriteUnroll = 1;  // and of one that writes codes
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -39,16 +40,16 @@ static_assert(sizeof(CopyLaunch) <= 32764, "kernel parameters");
 // after the other for the same tokens, so that rows that lie side by side in a
 // token-by-token layout are taken at the same time.  The thread's first row and
 // its channels' place in it; a step further is RB rows.
-template <int D>
+template <int D, int CH, int UN>
 struct Place {
-  static constexpr int TR = D / 8, RB = kThreads / TR;  // threads of a row, rows of a step
+  static constexpr int TR = D / CH, RB = kThreads / TR;  // threads of a row, rows of a step
   const Rows &r;
   int i, c;  // row, first channel
   int64_t code, scale, elem;
   __device__ __forceinline__ Place(const CopyLaunch &L, const Rows &r_, int b) : r(r_) {
-    const int l = L.layer_ids[b / L.H / r.blocks], h = b % L.H, i0 = b / L.H % r.blocks * (RB * kUnroll);
+    const int l = L.layer_ids[b / L.H / r.blocks], h = b % L.H, i0 = b / L.H % r.blocks * (RB * UN);
     i = i0 + (int)threadIdx.x / TR;
-    c = threadIdx.x % TR * 8;
+    c = threadIdx.x % TR * CH;
     const int64_t tok = (int64_t)r.first + i;
     code = l * r.c.sl + h * r.c.sh + tok * r.c.st + c / 2;
     scale = l * r.c.gl + h * r.c.gh + tok * r.c.gt + c / kGroup;
@@ -65,46 +66,47 @@ __device__ __forceinline__ int traj_of_block(const CopyLaunch &L) {
   return t;
 }
 
-// Eight channels of a row, as they are in memory.
+// 32 channels of a row, as they are in memory.
 template <typename T>
-struct Eight {
-  uint32_t w[2 * sizeof(T)];
+struct Group {
+  static constexpr int kWords = 8 * sizeof(T);
+  uint32_t w[kWords];
   __device__ __forceinline__ float get(int i) const {
     if (sizeof(T) == 4) return __uint_as_float(w[i]);
     return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
 };
 template <typename T, bool VEC>
-__device__ __forceinline__ Eight<T> load8(const T *src) {
-  Eight<T> x;
+__device__ __forceinline__ Group<T> load_group(const T *src) {
+  Group<T> x;
+  if (VEC) {
 #pragma unroll
-  for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-    if (VEC) {
+    for (int k = 0; k < x.kWords / 4; ++k) {
       const uint4 v = reinterpret_cast<const uint4 *>(src)[k];
       x.w[4 * k] = v.x, x.w[4 * k + 1] = v.y, x.w[4 * k + 2] = v.z, x.w[4 * k + 3] = v.w;
-    } else {
+    }
+  } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (sizeof(T) == 4) x.w[4 * k + i] = reinterpret_cast<const uint32_t *>(src)[4 * k + i];
-        else
-          x.w[i] = reinterpret_cast<const uint16_t *>(src)[2 * i] |
-                   (uint32_t)reinterpret_cast<const uint16_t *>(src)[2 * i + 1] << 16;
-      }
+    for (int i = 0; i < x.kWords; ++i) {
+      if (sizeof(T) == 4) x.w[i] = reinterpret_cast<const uint32_t *>(src)[i];
+      else
+        x.w[i] = reinterpret_cast<const uint16_t *>(src)[2 * i] |
+                 (uint32_t)reinterpret_cast<const uint16_t *>(src)[2 * i + 1] << 16;
     }
   }
   return x;
 }
 // The largest magnitude, as an fp32 number's bits (from 0x7f800000 on: not finite).
 template <typename T>
-__device__ __forceinline__ uint32_t top_of(const Eight<T> &x) {
-  if (sizeof(T) == 4) {
-    uint32_t m = 0;
+__device__ __forceinline__ uint32_t top_of(const Group<T> &x) {
+  constexpr uint32_t abs = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+  uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, x.w[i] & 0x7fffffffu);
-    return m;
+  for (int i = 0; i < x.kWords; i += 2) {
+    if (sizeof(T) == 4) m = max(max(m, x.w[i] & abs), x.w[i + 1] & abs);
+    else m = __vimax3_u16x2(m, x.w[i] & abs, x.w[i + 1] & abs);
   }
-  uint32_t m = __vmaxu2(__vmaxu2(x.w[0] & 0x7fff7fffu, x.w[1] & 0x7fff7fffu), __vmaxu2(x.w[2] & 0x7fff7fffu, x.w[3] & 0x7fff7fffu));
-  return max(m << 16, m & 0xffff0000u);
+  return sizeof(T) == 4 ? m : max(m << 16, m & 0xffff0000u);
 }
 
 // sigma's byte for a largest magnitude a (finite): the one nearest to a / 7, of
@@ -121,7 +123,7 @@ __device__ __forceinline__ unsigned scale_byte(float a) {
 // only be on the wrong side of a middle by rounding; the remainder is exact (a
 // multiple of x's last place, no larger than x) and says on which side x is, or
 // that it is a tie.
-__device__ __noinline__ unsigned code_of(float x, float sigma, float inv) {
+__device__ __forceinline__ unsigned code_of(float x, float sigma, float inv) {
   const float a = fabsf(x);
   float n = fminf(rintf(a * inv), 8.0f);
   const float r = fmaf(-n, sigma, a), t = 2.0f * fabsf(r);
@@ -130,89 +132,74 @@ __device__ __noinline__ unsigned code_of(float x, float sigma, float inv) {
   return 8 + (x < 0.0f ? -i : i);
 }
 
-// Four lanes have a group's 32 channels; returns the scale byte, and the eight
-// codes of the lane.  x / sigma lies between x low and x high, the neighbours of
-// 1 / sigma; both products rounded to whole numbers (by adding 3 2^22, one rounding)
-// agree unless a middle lies between them, as it does for a tie.  A bf16 number
-// there is the middle itself (its distance to a middle is 0 or 2^-8 of it and more),
-// so the even one of the two is right; an fp32 number is looked at again.
+// The scale byte of 32 channels, and their codes.  x / sigma lies between x low and
+// x high, the neighbours of 1 / sigma; both products rounded to whole numbers (by
+// adding 3 2^22, one rounding) agree unless a middle lies between them, as it does
+// for a tie.  A bf16 number there is the middle itself (its distance to a middle is
+// 0 or 2^-8 of it and more), so the even one of the two is right; an fp32 number
+// is looked at again.
 template <typename T>
-__device__ __forceinline__ unsigned encode(const Eight<T> &x, uint32_t &codes) {
-  unsigned top = top_of(x);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  codes = 0x88888888u;
-  if (top >= 0x7f800000u) return 0xff;  // infinite or NaN
-  const unsigned b = scale_byte(__uint_as_float(top));
-  if (b == 0) return 0;
-  const float sigma = sigma_of(b);
+__device__ __forceinline__ unsigned encode(const Group<T> &x, uint32_t (&codes)[4]) {
+  const unsigned top = top_of(x), b = top < 0x7f800000u ? scale_byte(__uint_as_float(top)) : 0;
+  if (b == 0) {
+    codes[0] = codes[1] = codes[2] = codes[3] = 0x88888888u;
+    return top < 0x7f800000u ? 0 : 0xff;  // infinite or NaN
+  }
+  const float sigma = __half2float(__ushort_as_half((unsigned short)(b << 7))) * kUnit;
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sigma));
   const float e = fmaf(-sigma, inv, 1.0f);  // 0: exact
   const float low = e < 0.0f ? __uint_as_float(__float_as_uint(inv) - 1) : inv;
   const float high = e > 0.0f ? __uint_as_float(__float_as_uint(inv) + 1) : inv;
   bool again = b < 8 || b == kNanScale - 1;  // x may be more than 7.5 sigma
-  uint32_t w = 0;
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    // the bits of 3 2^22 + n: even as n is, and the digits of their sum need no masks
-    const int n = __float_as_int(fmaf(x.get(i), low, 12582912.0f)), d = __float_as_int(fmaf(x.get(i), high, 12582912.0f)) - n;
-    if (sizeof(T) == 4) again = again || d != 0;
-    w = w * 16 + (sizeof(T) == 4 ? n : n + (n & 1) * d);
-  }
-  w += 0x88888888u - 0x11111111u * 0x4b400000u;  // every digit is 8 + n
-  if (again) {
-    w = 0;
-#pragma unroll 1
-    for (int i = 7; i >= 0; --i) {
-      float y = 0.0f;
+  for (int k = 0; k < 4; ++k) {
+    uint32_t w = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y = k == i ? x.get(k) : y;
-      w = w * 16 + code_of(y, sigma, inv);
+    for (int i = 8 * k + 7; i >= 8 * k; --i) {
+      // the bits of 3 2^22 + n: even as n is, and the digits of their sum need no masks
+      const int n = __float_as_int(fmaf(x.get(i), low, 12582912.0f)), d = __float_as_int(fmaf(x.get(i), high, 12582912.0f)) - n;
+      if (sizeof(T) == 4) again = again || d != 0;
+      w = w * 16 + (sizeof(T) == 4 ? n : n + (n & 1) * d);
     }
+    codes[k] = w + (0x88888888u - 0x11111111u * 0x4b400000u);  // every digit is 8 + n
   }
-  codes = w;
+  if (again) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) codes[k] = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) codes[i / 8] |= code_of(x.get(i), sigma, inv) << (4 * (i % 8));
+  }
   return b;
 }
 
 template <bool VEC>
-__device__ __forceinline__ void store_codes(uint8_t *dst, uint32_t codes) {
-  if (VEC) *reinterpret_cast<uint32_t *>(dst) = codes;
+__device__ __forceinline__ void store_codes(uint8_t *dst, const uint32_t (&codes)[4]) {
+  if (VEC) *reinterpret_cast<uint4 *>(dst) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
   else
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dst[i] = (uint8_t)(codes >> (8 * i));
+    for (int i = 0; i < 16; ++i) dst[i] = (uint8_t)(codes[i / 4] >> (8 * (i % 4)));
 }
 
 // Write: bound by reading the rows (2.5 bytes a value of bf16 with its codes; 4.5 of
 // fp32); a lane's loads of its rows are issued first, K's then V's.
 template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ CopyLaunch L) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) write_kernel(const __grid_constant__ CopyLaunch L) {
   const int t = traj_of_block(L);
   const Rows &r = L.r[t];
-  const Place<D> p(L, r, blockIdx.x - L.off[t]);
+  const Place<D, kGroup, kWriteUnroll> p(L, r, blockIdx.x - L.off[t]);
   const int64_t row_step = p.RB * r.st;
+#pragma unroll 1
+  for (int u = 0; u < kWriteUnroll; ++u) {
+    if (p.i + u * p.RB >= r.count) return;
+    Group<T> x[2];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    Eight<T> x[kUnroll];
-    const T *src = static_cast<const T *>(kv ? r.v : r.k) + p.elem;
-    uint8_t *codes = (kv ? r.c.v : r.c.k) + p.code, *scales = (kv ? r.c.vs : r.c.ks) + p.scale;
+    for (int kv = 0; kv < 2; ++kv) x[kv] = load_group<T, VEC>(static_cast<const T *>(kv ? r.v : r.k) + p.elem + u * row_step);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u, src += row_step) {
-      if (p.i + u * p.RB < r.count) {
-        x[u] = load8<T, VEC>(src);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2 * (int)sizeof(T); ++i) x[u].w[i] = 0;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u, codes += p.RB * r.c.st, scales += p.RB * r.c.gt) {
-      uint32_t w;
-      const unsigned s = encode(x[u], w);
-      if (p.i + u * p.RB < r.count) {
-        store_codes<VEC>(codes, w);
-        if (p.c % kGroup == 0) *scales = (uint8_t)s;
-      }
+    for (int kv = 0; kv < 2; ++kv) {
+      uint32_t w[4];
+      (kv ? r.c.vs : r.c.ks)[p.scale + u * (p.RB * r.c.gt)] = (uint8_t)encode(x[kv], w);
+      store_codes<VEC>((kv ? r.c.v : r.c.k) + p.code + u * (p.RB * r.c.st), w);
     }
   }
 }
@@ -241,7 +228,7 @@ template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ CopyLaunch L) {
   const int t = traj_of_block(L);
   const Rows &r = L.r[t];
-  const Place<D> p(L, r, blockIdx.x - L.off[t]);
+  const Place<D, 8, kUnroll> p(L, r, blockIdx.x - L.off[t]);
   uint32_t w[2][kUnroll];
   uint8_t s[2][kUnroll];
 #pragma unroll
@@ -445,8 +432,9 @@ commitkv_status copy(const commitkv_shape *s, int n, const commitkv_packed *x, c
   L.H = s->kv_heads;
   L.n_layers = n_layers;
   memcpy(L.layer_ids, layers, n_layers);
-  const int eb = s->dtype == COMMITKV_BF16 ? 2 : 4, per = kThreads / (s->head_dim / 8) * kUnroll;  // rows of a block
-  uintptr_t wide_bits = 0, code_bits = 0;  // 16-byte rows, 4-byte codes
+  const int eb = s->dtype == COMMITKV_BF16 ? 2 : 4, 
+            per = kThreads * (write ? kGroup * kWriteUnroll : 8 * kUnroll) / s->head_dim;  // rows of a block
+  uintptr_t wide_bits = 0, code_bits = 0;  // of the rows, of the codes
   int64_t blocks = 0;
   for (int t = 0; t < n; ++t) {
     Rows &d = L.r[t];
@@ -464,7 +452,7 @@ commitkv_status copy(const commitkv_shape *s, int n, const commitkv_packed *x, c
   }
   L.off[n] = (int32_t)blocks;
   if (blocks == 0) return COMMITKV_OK;
-  const bool vec = wide_bits % 16 == 0 && code_bits % 4 == 0;
+  const bool vec = wide_bits % 16 == 0 && code_bits % (write ? 16 : 4) == 0;
   if (s->dtype == COMMITKV_BF16) {
     if (s->head_dim == 128) launch_copy<__nv_bfloat16, 128>(L, write, vec, stream);
     else launch_copy<__nv_bfloat16, 64>(L, write, vec, stream);
