@@ -240,9 +240,22 @@ class TrajTensors:
                     0 if q is None else q.shape[2], start, length, 0 if ps is None else ps.numel())
 
 
-@dataclass
+def _one_gpu(*tensors) -> int:
+    devices = {x.get_device() for x in tensors if x is not None}
+    if len(devices) != 1 or min(devices) < 0:
+        raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
+    return devices.pop()
+
+
+def _on_current(device: int):
+    if _torch().cuda.current_device() != device:
+        raise ValueError("the tensors must be on the current GPU")
+
+
+@dataclass(frozen=True, eq=False)
 class PackedTensors:
-    """One trajectory's packed cache: device tensors in 4 bits a value.
+    """One trajectory's packed cache: device tensors in 4 bits a value.  Checked and
+    marshalled once, at the first call that takes it; its tensors are not exchanged.
 
     k, v: codes [M][H][S][d / 2] uint8 views (any strides with contiguous bytes
     of a row), k_scale, v_scale: scale bytes [M][H][S][d / 32] uint8; the rest as
@@ -258,6 +271,22 @@ class PackedTensors:
     page_len: object = None
 
     def desc(self) -> Packed:
+        d = self.__dict__.get("_desc")
+        if d is None:
+            d = self._marshal()
+            object.__setattr__(self, "_desc", d)
+        return d
+
+    def device(self) -> int:
+        """The GPU of all its tensors."""
+        d = self.__dict__.get("_device")
+        if d is None:
+            d = _one_gpu(self.k, self.v, self.k_scale, self.v_scale, self.pos, self.q, self.q_pos, self.page_start,
+                         self.page_len)
+            object.__setattr__(self, "_device", d)
+        return d
+
+    def _marshal(self) -> Packed:
         torch = _torch()
         k, v, ks, vs, q, ps = self.k, self.v, self.k_scale, self.v_scale, self.q, self.page_start
         ints = (self.pos, self.q_pos, ps, self.page_len)
@@ -666,16 +695,6 @@ def alloc_packed_workspace(shape: Shape, trajs: Sequence[PackedTensors], device=
     return _alloc(commitkv_packed_workspace_size(shape, trajs), device)
 
 
-def _on_current(*tensors):
-    devices = {x.device for x in tensors if x is not None}
-    if len(devices) != 1 or next(iter(devices)).type != "cuda":
-        raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
-    device = next(iter(devices)).index
-    if _torch().cuda.current_device() != device:
-        raise ValueError("the tensors must be on the current GPU")
-    return device
-
-
 class PackedRows:
     """The arguments of a write or a read, checked and marshalled once: packed
     caches, the full-width rows k, v [M][H][n][d] of each (any strides with
@@ -701,7 +720,8 @@ class PackedRows:
             sl, sh, st = x.stride()[:3]
             self.rows[i] = Rows(_ptr(x), _ptr(y), sl, sh, st, 0, 0)
         # once, and not in every call
-        self.device = _on_current(*[t for c in caches for t in (c.k, c.v, c.k_scale, c.v_scale)], *k, *v)
+        self.device = _one_gpu(*[t for c in caches for t in (c.k, c.v, c.k_scale, c.v_scale)], *k, *v)
+        _on_current(self.device)
         for i, f in enumerate(first):
             self.set_rows(i, f)
 
@@ -725,8 +745,7 @@ def _packed_copy(name, shape, caches, k, v, first, layer_mask, stream):
     elif k is not None or v is not None or first is not None or \
             (r.shape is not shape and bytes(r.shape) != bytes(shape)):
         raise ValueError("the rows and the shape are those of the PackedRows")
-    if _torch().cuda.current_device() != r.device:
-        raise ValueError("the tensors must be on the current GPU")
+    _on_current(r.device)
     _mbuf, mptr = _mask(layer_mask, shape.layers)
     if stream is None:
         stream = _current_stream(r.device)
@@ -753,35 +772,50 @@ def commitkv_packed_compact(shape: Shape, cache, retired, pending, pending_prior
     place, as commitkv_compact_in_place."""
     torch = _torch()
     n = len(cache)
-    d = _descs(cache)
-    for c in list(cache) + list(dst or ()):
+    every = list(cache) if dst is None else list(cache) + list(dst)
+    if dst is not None and len(dst) != n:
+        raise ValueError("one destination per cache")
+    for c in every:
         if not isinstance(c, PackedTensors):
             raise ValueError("caches must be PackedTensors")
         _packed_width(shape, c)
-    if dst is not None and len(dst) != n:
-        raise ValueError("one destination per cache")
-    for xs, dt, what in ((retired, torch.uint8, "retired"), (pending, torch.int32, "pending"),
-                         (pending_priority, torch.float32, "pending_priority"), (fill_score, torch.float32, "fill_score"),
-                         (idx_out, torch.int32, "idx_out"), ([n_idx_out], torch.int32, "n_idx_out")):
-        for x in xs:
-            if x is not None and (x.dtype != dt or not x.is_contiguous()):
-                raise ValueError(f"{what} must be contiguous {dt}")
-    for i, c in enumerate(cache):
-        pages = 0 if c.page_start is None else c.page_start.numel()
-        some = pending[i] is not None and pending[i].numel() > 0
-        if fill_score[i].numel() < c.k.shape[2] or idx_out[i].numel() < budget_B or \
-                (pages and retired[i].numel() < pages) or (some and pending_priority[i].numel() < pages):
-            raise ValueError("scores for every token, marks and priorities for every page, budget_B indices")
-    if n_idx_out.numel() < n:
-        raise ValueError("n_idx_out has an entry per cache")
     if workspace is None:
         raise ValueError("a workspace is needed")
-    device = _on_current(workspace, n_idx_out, *[t for c in list(cache) + list(dst or ()) for t in (c.k, c.v, c.k_scale, c.v_scale)],
-                         *retired, *pending, *pending_priority, *fill_score, *idx_out)
-    npend = (ctypes.c_int32 * n)(*[0 if p is None else int(p.numel()) for p in pending])
-    rc = load_library().commitkv_packed_compact(
-        ctypes.byref(shape), n, d, _ptr_array(retired, n), _ptr_array(pending, n), ctypes.cast(npend, ctypes.c_void_p),
-        _ptr_array(pending_priority, n), _ptr_array(fill_score, n), int(budget_B), int(pending_tokens_BN),
-        int(pending_cap_pages), _ptr_array(idx_out, n), _ptr(n_idx_out), None if dst is None else _descs(dst),
-        _ptr(workspace), workspace.numel(), _stream(_current_stream(device) if stream is None else stream))
+    d, to = _descs(cache), None if dst is None else _descs(dst)
+    devices = {c.device() for c in every}
+    devices.add(workspace.get_device())
+    pointers = []
+    for xs, dt, what in ((retired, torch.uint8, "retired"), (pending, torch.int32, "pending"),
+                         (pending_priority, torch.float32, "pending_priority"), (fill_score, torch.float32, "fill_score"),
+                         (idx_out, torch.int32, "idx_out"), ((n_idx_out,), torch.int32, "n_idx_out")):
+        got = []
+        if len(xs) != (1 if what == "n_idx_out" else n):
+            raise ValueError(f"{what}: one for each cache")
+        for x in xs:
+            if x is None:
+                got.append((0, None))
+                continue
+            if x.dtype != dt or not x.is_contiguous():
+                raise ValueError(f"{what} must be contiguous {dt}")
+            devices.add(x.get_device())
+            m = x.numel()
+            got.append((m, x.data_ptr() if m else None))
+        pointers.append(got)
+    for i in range(n):
+        S, P = d[i].S, d[i].P
+        marks, some, prio, fill, idx = (p[i] for p in pointers[:5])
+        if fill[0] < S or idx[0] < budget_B or marks[0] < P or (some[0] and prio[0] < P):
+            raise ValueError("scores for every token, marks and priorities for every page, budget_B indices")
+    if pointers[5][0][0] < n:
+        raise ValueError("n_idx_out has an entry per cache")
+    if len(devices) != 1 or min(devices) < 0:
+        raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
+    device = devices.pop()
+    _on_current(device)
+    arrays = [(ctypes.c_void_p * n)(*[q for _, q in p]) for p in pointers[:5]]
+    npend = (ctypes.c_int32 * n)(*[m for m, _ in pointers[1]])
+    rc = (_lib or load_library()).commitkv_packed_compact(
+        ctypes.byref(shape), n, d, arrays[0], arrays[1], ctypes.byref(npend), arrays[2], arrays[3], int(budget_B),
+        int(pending_tokens_BN), int(pending_cap_pages), arrays[4], pointers[5][0][1], to, workspace.data_ptr(),
+        workspace.numel(), _stream(_current_stream(device) if stream is None else stream))
     _check(rc, "commitkv_packed_compact")

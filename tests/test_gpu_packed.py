@@ -1,5 +1,7 @@
 """Packed caches against their definition in 64 bits: writing and reading rows,
 attention over them, checkpoints, and all of them together."""
+import dataclasses
+
 import numpy as np
 import pytest
 
@@ -528,7 +530,7 @@ def test_attention_refusals():
     t = p.trajs[0]
     for kw in (dict(q=t.q.float()), dict(pos=None), dict(k=t.k.repeat(1, 2, 1, 1), v=t.v.repeat(1, 2, 1, 1),
                                                           k_scale=t.k_scale.repeat(1, 2, 1, 1), v_scale=t.v_scale.repeat(1, 2, 1, 1))):
-        bad = ck.PackedTensors(**{**t.__dict__, **kw})
+        bad = dataclasses.replace(t, **kw)
         with pytest.raises(ValueError):
             ck.commitkv_packed_attention(p.shape, [bad], p.out, workspace=p.ws)
     torch.cuda.synchronize()
