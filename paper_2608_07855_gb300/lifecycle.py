@@ -39,6 +39,13 @@ library's entry points in the order of Algorithm 1:
                most 64 pages per commit); the greedy joint test (Eq. 11);
                D_c gains the accepted pages.
 
+With packed=True the resident cache is held in 4 bits (commitkv_packed_write as
+tokens are appended, 0.27 of the bytes of bf16): attend reads the codes
+(commitkv_packed_attention), a checkpoint moves them (commitkv_packed_compact),
+and a commit or fill_scores reads the values back into full width for its own
+duration (commitkv_packed_read).  Everything is computed from the values that the
+codes stand for.
+
 state_dict / load_state_dict carry the state between commits (the resident
 cache, the page table, R- of the latest pre-commit, the pages waiting for
 their post-commit measurement, D_c) for checkpoint and resume.
@@ -65,18 +72,21 @@ def _torch():
 class Session:
     def __init__(self, shape: ck.Shape, G: int, B: int, eta: float, capacity: int, scan_cap: int = 64,
                  protect_cap: int = 16, thresholds: ck.Thresholds = None, variant: int = 0,
-                 tau_joint: float = 0.05, checkpoint_every: int = 128, device="cuda"):
+                 tau_joint: float = 0.05, checkpoint_every: int = 128, device="cuda", packed: bool = False):
         torch = _torch()
         self.shape, self.G, self.B = shape, G, B
         self.B_N = int(math.floor(eta * B))
         self.cap, self.scan_cap, self.protect_cap = capacity, scan_cap, protect_cap
         self.thresholds, self.variant, self.tau_joint = thresholds, variant, tau_joint
         self.dev = device
-        dt = torch.bfloat16 if shape.dtype == ck.COMMITKV_BF16 else torch.float32
-        M, H, d = shape.layers, shape.kv_heads, shape.head_dim
-        self.K = torch.zeros(M, H, capacity, d, dtype=dt, device=device)
-        self.V = torch.zeros(M, H, capacity, d, dtype=dt, device=device)
-        self.pos = torch.zeros(capacity, dtype=torch.int32, device=device)
+        self.dt = torch.bfloat16 if shape.dtype == ck.COMMITKV_BF16 else torch.float32
+        self.packed = ck.alloc_packed_cache(shape, capacity, device) if packed else None
+        if packed:
+            self.K = self.V = None
+            self.pos = self.packed.pos
+        else:
+            self.K, self.V = (self._full(capacity).zero_() for _ in range(2))
+            self.pos = torch.zeros(capacity, dtype=torch.int32, device=device)
         self.S = 0
         self.pages = []       # [id, start, len] in resident order
         self.next_id = 0
@@ -93,10 +103,52 @@ class Session:
         self.graph_ws = []      # of captured ones
 
     # ---------------------------------------------------------------- helpers
-    def _traj(self, Q=None, qpos=None) -> ck.TrajTensors:
-        ps, pl = self._upload(np.array([[p[1] for p in self.pages], [p[2] for p in self.pages]], np.int32))
+    def _full(self, n):
+        """Room for K or V of n tokens of all layers."""
+        s = self.shape
+        return _torch().empty(s.layers, s.kv_heads, n, s.head_dim, dtype=self.dt, device=self.dev)
+
+    def _values(self):
+        """K and V of the resident tokens in full width: views, or what a packed
+        cache's codes stand for, for as long as the caller holds them."""
         S = self.S
-        return ck.TrajTensors(self.K[:, :, :S], self.V[:, :, :S], self.pos[:S], Q, qpos, ps, pl)
+        if self.packed is None:
+            return self.K[:, :, :S], self.V[:, :, :S]
+        K, V = self._full(S), self._full(S)
+        ck.commitkv_packed_read(self.shape, [self.packed], [K], [V], [0])
+        return K, V
+
+    def _codes(self, layer=None, **more) -> ck.PackedTensors:
+        """The resident tokens' codes, of one layer or all."""
+        c, S = self.packed, self.S
+        at = slice(None) if layer is None else slice(layer, layer + 1)
+        return ck.PackedTensors(c.k[at, :, :S], c.v[at, :, :S], c.k_scale[at, :, :S], c.v_scale[at, :, :S], self.pos[:S],
+                                **more)
+
+    def _put(self, K, V, first, layer=None):
+        """K and V of tokens first .. of one layer ([1][H][n][d]) or all ([M][H][n][d])."""
+        n = K.shape[2]
+        if self.packed is None:
+            at = slice(None) if layer is None else slice(layer, layer + 1)
+            self.K[at, :, first:first + n].copy_(K)
+            self.V[at, :, first:first + n].copy_(V)
+            return
+        K, V = (x.to(device=self.dev, dtype=self.dt) for x in (K, V))
+        if K.stride() != V.stride() or K.stride(3) != 1:
+            K, V = K.contiguous(), V.contiguous()
+        c, s = self.packed, self.shape
+        if layer is not None:
+            one = slice(layer, layer + 1)
+            c = ck.PackedTensors(c.k[one], c.v[one], c.k_scale[one], c.v_scale[one])
+            s = ck.Shape(1, s.kv_heads, s.q_heads, s.head_dim, s.dtype, s.softmax_scale)
+        ck.commitkv_packed_write(s, [c], [K], [V], [first])
+
+    def _pages(self):
+        return self._upload(np.array([[p[1] for p in self.pages], [p[2] for p in self.pages]], np.int32))
+
+    def _traj(self, Q=None, qpos=None) -> ck.TrajTensors:
+        ps, pl = self._pages()
+        return ck.TrajTensors(*self._values(), self.pos[:self.S], Q, qpos, ps, pl)
 
     def _upload(self, rows):
         """Rows of a host int32 array [n][P] as device tensors, in one copy."""
@@ -148,9 +200,12 @@ class Session:
         torch.save writes the dict."""
         self._ready()
         S = self.S
+        c = self.packed
+        cache = {"K": self.K, "V": self.V} if c is None else \
+            {"k": c.k, "v": c.v, "k_scale": c.k_scale, "v_scale": c.v_scale}
         return {
             "config": self._config(),
-            "K": self.K[:, :, :S].clone(), "V": self.V[:, :, :S].clone(), "pos": self.pos[:S].clone(),
+            **{n: x[:, :, :S].clone() for n, x in cache.items()}, "pos": self.pos[:S].clone(),
             "pages": [list(p) for p in self.pages], "next_id": self.next_id,
             "R_pre": dict(self.R_pre), "measured": list(self.measured), "retired": sorted(self.retired),
             "decoded_since": self.decoded_since,
@@ -160,13 +215,13 @@ class Session:
         """Resumes from state_dict() of a session with the same model shape,
         page size, budget and decision settings; the resident cache must fit
         this session's capacity."""
-        if st["config"] != self._config():
+        if {"packed": False, **st["config"]} != self._config():
             raise ValueError("state of a session with other settings")
         S = int(st["pos"].shape[0])
         if S > self.cap:
             raise ValueError("session capacity exceeded")
-        self.K[:, :, :S].copy_(st["K"])
-        self.V[:, :, :S].copy_(st["V"])
+        for n in ("K", "V") if self.packed is None else ("k", "v", "k_scale", "v_scale"):
+            getattr(self if self.packed is None else self.packed, n)[:, :, :S].copy_(st[n])
         self.pos[:S].copy_(st["pos"])
         self.S = S
         self.pages = [list(p) for p in st["pages"]]
@@ -182,7 +237,7 @@ class Session:
         return {"shape": (s.layers, s.kv_heads, s.q_heads, s.head_dim, s.dtype, float(s.softmax_scale)),
                 "G": self.G, "B": self.B, "B_N": self.B_N, "scan_cap": self.scan_cap,
                 "protect_cap": self.protect_cap, "variant": int(self.variant), "tau_joint": float(self.tau_joint),
-                "checkpoint_every": int(self.checkpoint_every),
+                "checkpoint_every": int(self.checkpoint_every), "packed": self.packed is not None,
                 "thresholds": None if th is None else (th.tau_use, th.tau_dead, th.rho_use, th.rho_dead)}
 
     # ---------------------------------------------------------------- cache
@@ -201,8 +256,7 @@ class Session:
             raise ValueError("session capacity exceeded")
         S0, p0 = self.S, int(pos[0]) if n else 0
         if K is not None:
-            self.K[:, :, S0:S0 + n].copy_(K)
-            self.V[:, :, S0:S0 + n].copy_(V)
+            self._put(K, V, S0)
         self.tail = (S0, S0 + n)
         self.unfilled = set(range(self.shape.layers)) if K is None and n else set()
         self.pos[S0:S0 + n].copy_(pos)
@@ -223,8 +277,7 @@ class Session:
         want = (self.shape.kv_heads, b - a, self.shape.head_dim)
         if tuple(K.shape) != want or tuple(V.shape) != want:
             raise ValueError(f"K and V must be [H][n][d] = {want}")
-        self.K[layer, :, a:b].copy_(K)
-        self.V[layer, :, a:b].copy_(V)
+        self._put(K[None], V[None], a, layer)
         self.unfilled.discard(layer)
 
     def attend(self, Q, qpos, window: int = 0, sinks: int = 0, prefix: ck.TrajTensors = None, layer: int = None):
@@ -234,7 +287,7 @@ class Session:
         model calls it once it has filled the layer; without: all layers', Q
         [M][Hq][W][d].  window and sinks as in commitkv_window_attention;
         prefix: a cache of all layers shared by agents, whose positions come
-        before this session's.
+        before this session's (not for a packed session).
 
         Asynchronous: a device error (a wait that ran out; the outputs are then
         unspecified) is raised by the next check, pre_commit, post_commit,
@@ -244,7 +297,9 @@ class Session:
         replay clears it first, so it tells of the latest replay."""
         torch = _torch()
         s, S = self.shape, self.S
-        K, V = self.K, self.V
+        if self.packed is not None and prefix is not None:
+            raise ValueError("a packed session takes no shared prefix")
+        one = slice(None)
         if layer is None:
             self._filled()
         else:
@@ -255,27 +310,35 @@ class Session:
             if Q.dim() != 3:
                 raise ValueError("a layer's Q is [Hq][W][d]")
             one = slice(layer, layer + 1)
-            K, V, Q = K[one], V[one], Q[None]
+            Q = Q[None]
             if prefix is not None:
                 if prefix.k.shape[0] != s.layers:
                     raise ValueError("a prefix has all layers")
                 prefix = ck.TrajTensors(prefix.k[one], prefix.v[one], prefix.pos)
             s = ck.Shape(1, s.kv_heads, s.q_heads, s.head_dim, s.dtype, s.softmax_scale)
-        tr = ck.TrajTensors(K[:, :, :S], V[:, :, :S], self.pos[:S], Q, qpos)
+        if self.packed is None:
+            tr = ck.TrajTensors(self.K[one, :, :S], self.V[one, :, :S], self.pos[:S], Q, qpos)
+            need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
+            alloc = lambda: ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)  # noqa: E731
+        else:
+            tr = self._codes(layer, q=Q, q_pos=qpos)
+            need = ck.commitkv_packed_workspace_size(s, [tr])
+            alloc = lambda: ck.alloc_packed_workspace(s, [tr], device=self.dev)  # noqa: E731
         out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=self.dev)
-        need = ck.commitkv_attention_workspace_size(s, [tr], prefix)
         stream = None
         if torch.cuda.is_current_stream_capturing():
-            ws = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+            ws = alloc()
             self.graph_ws.append(ws)
         else:
-            stream = torch.cuda.current_stream(self.K.device).cuda_stream
+            stream = torch.cuda.current_stream(self.pos.device).cuda_stream
             ws = old = self.attention_ws.get(stream)
             if ws is None or ws.numel() < need:
-                ws = self.attention_ws[stream] = ck.alloc_attention_workspace(s, [tr], prefix, device=self.dev)
+                ws = self.attention_ws[stream] = alloc()
                 if old is not None:
                     ws[:256].copy_(old[:256])  # the status so far
-        if prefix is None:
+        if self.packed is not None:
+            ck.commitkv_packed_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
+        elif prefix is None:
             ck.commitkv_window_attention(s, [tr], [out], [lse], window, sinks, workspace=ws)
         else:
             ck.commitkv_prefix_attention(s, [tr], prefix, [out], [lse], window, sinks, workspace=ws)
@@ -320,7 +383,7 @@ class Session:
         s = self.shape
         S = self.S
         none = torch.empty(0, dtype=torch.int32, device=self.dev)
-        tr = ck.TrajTensors(self.K[:, :, :S], self.V[:, :, :S], self.pos[:S], Q, qpos, none, none)
+        tr = ck.TrajTensors(*self._values(), self.pos[:S], Q, qpos, none, none)
         ws = self._workspace(tr)
         # both are written in full by the calls
         stats = torch.empty(s.layers, s.q_heads, Q.shape[2], s.head_dim + 4, device=self.dev)
@@ -341,8 +404,16 @@ class Session:
         (device int32, ascending)."""
         self._ready()
         torch = _torch()
-        tr = self._traj()
-        ws = self._workspace(tr)
+        if self.packed is None:
+            tr = self._traj()
+            ws = self._workspace(tr)
+        else:
+            ps, pl = self._pages()
+            tr = self._codes(page_start=ps, page_len=pl)
+            need = ck.commitkv_packed_workspace_size(self.shape, [tr])
+            if self.ws is None or self.ws.numel() < need:
+                self.ws = ck.alloc_packed_workspace(self.shape, [tr], device=self.dev)
+            ws = self.ws
         ids = self.page_ids()
         P, B = len(ids), self.B
         wait = set(self.measured)
@@ -356,8 +427,9 @@ class Session:
         pending, prio_p, retired = rows[0, :len(pend)], rows[1].view(torch.float32), rows[2].view(torch.uint8)
         out = torch.empty(max(B, 1) + 1, dtype=torch.int32, device=self.dev)
         idx, n_idx = out[1:], out[:1]
-        ck.commitkv_compact_in_place(self.shape, [tr], [retired], [pending], [prio_p], [fill[:self.S]], B,
-                                     self.B_N, self.protect_cap, [idx], n_idx, workspace=ws)
+        compact = ck.commitkv_compact_in_place if self.packed is None else ck.commitkv_packed_compact
+        compact(self.shape, [tr], [retired], [pending], [prio_p], [fill[:self.S]], B, self.B_N, self.protect_cap, [idx],
+                n_idx, workspace=ws)
         self._check()
         host = out.cpu().numpy()
         n = int(host[0])
