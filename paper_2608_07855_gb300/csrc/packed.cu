@@ -204,25 +204,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) write_kernel
   }
 }
 
-// The values of a word's eight codes: (w >> 4 i & 0x000f000f) | 0x43004300 are the bf16
-// numbers 128 + u of the channels i and i + 4, one fma with (s, -136 s) makes them
-// (u - 8) s: exact (136 s has eight significant bits).  Then side by side.
-__device__ __forceinline__ void values8(uint32_t w, unsigned b, uint32_t (&x)[4]) {
-  const __nv_bfloat162 s = __float2bfloat162_rn(sigma_of(b)), off = __hmul2(s, __float2bfloat162_rn(-136.0f));
-  uint32_t p[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t y;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));
-    const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&y), s, off);
-    p[i] = *reinterpret_cast<const uint32_t *>(&v);
-  }
-  x[0] = __byte_perm(p[0], p[1], 0x5410);
-  x[1] = __byte_perm(p[2], p[3], 0x5410);
-  x[2] = __byte_perm(p[0], p[1], 0x7632);
-  x[3] = __byte_perm(p[2], p[3], 0x7632);
-}
-
 // Read: bound by writing the rows.
 template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ CopyLaunch L) {

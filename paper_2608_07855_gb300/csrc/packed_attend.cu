@@ -42,6 +42,10 @@ size_t compact_bytes(int n, const commitkv_packed *x) {
 // Many rows: the trajectories' values in full width, a layer of all of them, K
 // before V, each [H][S][d] dense.
 bool many(const commitkv_shape *s, const commitkv_packed &x) { return (int64_t)(s->q_heads / s->kv_heads) * x.W > 16; }
+// Of these, those that the kernel of row tiles takes as they are.
+bool direct(const commitkv_shape *s, const commitkv_packed &x, const void *out, bool cuda_cores) {
+  return !cuda_cores && s->dtype == COMMITKV_BF16 && wide(to_dev(x), s->head_dim) && ((uintptr_t)x.q | (uintptr_t)out) % 16 == 0;
+}
 size_t full_bytes(const commitkv_shape *s, const commitkv_packed &x) {  // K or V
   return at::align_up((size_t)s->kv_heads * x.S * s->head_dim * (s->dtype == COMMITKV_BF16 ? 2 : 4));
 }
@@ -56,8 +60,8 @@ size_t back_bytes(const commitkv_shape *s, int n, const commitkv_packed *x) {
 // values into the workspace, behind what the full-width call takes of it, then
 // that call.
 commitkv_status attend_many(const commitkv_shape *s, int n, const commitkv_packed *x, const uint8_t *mask, int32_t window,
-                            int32_t sinks, void *const *out, float *const *lse_out, void *workspace, size_t attention,
-                            cudaStream_t stream) {
+                            int32_t sinks, void *const *out, float *const *lse_out, const bool *back, void *workspace,
+                            size_t attention, cudaStream_t stream) {
   commitkv_packed c[kMaxTraj];
   commitkv_rows rows[kMaxTraj];
   commitkv_traj tr[kMaxTraj] = {};
@@ -67,7 +71,7 @@ commitkv_status attend_many(const commitkv_shape *s, int n, const commitkv_packe
   commitkv_shape one = *s;
   one.layers = 1;
   for (int t = 0; t < n; ++t) {
-    if (!many(s, x[t])) continue;
+    if (!back[t]) continue;
     ids[m] = t;
     c[m] = x[t];
     rows[m] = {at, at + full_bytes(s, x[t]), 0, (int64_t)x[t].S * s->head_dim, s->head_dim, 0, x[t].S};
@@ -99,9 +103,9 @@ commitkv_status attend_many(const commitkv_shape *s, int n, const commitkv_packe
   return COMMITKV_OK;
 }
 
-enum { kSimt16, kRows8, kRows16, kPaths };
+enum { kSimt16, kRows8, kRows16, kTc, kPaths };
 constexpr at::PathInfo kPath[kPaths] = {
-    {16, 64, 2, 1.0, 11.5}, {8, 128, 4, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}};
+    {16, 64, 2, 1.0, 11.5}, {8, 128, 4, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}, {256, 128, 1, 2.0, 1.7}};
 
 }  // namespace
 }  // namespace pk
@@ -152,7 +156,7 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
   L.n_traj = L.n_seg = n_traj;
   const int64_t slices = (int64_t)L.n_layers * L.H;
   int64_t rows = 0;
-  bool big = false;
+  bool big = false, back[kMaxTraj];
   int path[kMaxTraj];
   const Forced forced = forced_paths();
   for (int t = 0; t < n_traj; ++t) {
@@ -166,11 +170,12 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     sg.pos = x.pos;
     sg.S = x.S;
     sg.t = t;
-    sg.R = pk::many(shape, x) ? 0 : L.g * x.W;
+    back[t] = pk::many(shape, x) && !pk::direct(shape, x, out[t], forced.cuda_cores);
+    sg.R = back[t] ? 0 : L.g * x.W;
     rows += sg.R;
-    big = big || pk::many(shape, x);
+    big = big || back[t];
     const bool fast = !forced.cuda_cores && pk::wide(c, L.d) && (uintptr_t)x.q % 16 == 0;
-    path[t] = !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
+    path[t] = sg.R > 16 ? pk::kTc : !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
   }
   if (L.n_layers == 0 || (rows == 0 && !big)) return COMMITKV_OK;
   const int sms = sm_count();
@@ -235,12 +240,14 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     L.item_off[n_traj] = items;
     if (items == 0) continue;
     L.rows_per_item = pk::kPath[p].rows;
-    e = p == pk::kRows8 || p == pk::kRows16 ? pk::launch_rows(P, stream, launched) : pk::launch_simt(P, stream, launched);
+    e = p == pk::kTc       ? pk::launch_tc(P, static_cast<WsHeader *>(workspace), stream, launched)
+        : p == pk::kSimt16 ? pk::launch_simt(P, stream, launched)
+                           : pk::launch_rows(P, stream, launched);
     launched = true;
   }
   if (e == cudaSuccess && merge) e = launch_combine(L, stream);
   if (e == cudaSuccess)
-    return big ? pk::attend_many(shape, n_traj, trajs, layer_mask, window, sinks, out, lse_out, workspace, attention, stream)
+    return big ? pk::attend_many(shape, n_traj, trajs, layer_mask, window, sinks, out, lse_out, back, workspace, attention, stream)
                : COMMITKV_OK;
   cudaGetLastError();
   return COMMITKV_ERR_CUDA;
