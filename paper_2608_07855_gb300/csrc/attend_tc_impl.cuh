@@ -234,8 +234,11 @@ __device__ __forceinline__ void soft_masked(uint32_t s_col, uint32_t o_col, floa
 // A warp of the four that write the values of a packed cache, K and V tile after
 // tile into the ring.  A lane has one token's 32 channels of a group, 16 bytes of
 // codes and a scale byte, D / 32 times a tile; eight lanes write eight rows' 16
-// bytes of one place, which lie in different banks.  A tile's codes are read while
-// the one before is written.
+// bytes of one place, which lie in different banks.  What is written is read a
+// tile of K and of V ahead: a warp alone on its scheduler's share has nothing else
+// to hide the loads' latency with (one tile of either ahead: 421 us for the probe
+// window of 12 layers over 36,896 tokens).  V's channels are left as the codes'
+// pairs (paired_place); the results are put in order on their way out.
 template <int D>
 __device__ __forceinline__ void write_values(const PackedParams &P, Smem<D> &sm, int pw, int lane) {
   constexpr int NST = Smem<D>::NST, UN = D / 32;
@@ -244,9 +247,8 @@ __device__ __forceinline__ void write_values(const PackedParams &P, Smem<D> &sm,
   const int grp = D == 128 ? lane >> 3 : (lane >> 3) & 1;
   const int row0 = 32 * pw + (lane & 7) + (D == 128 ? 0 : 8 * (lane >> 4));
   constexpr int kStep = D == 128 ? 8 : 16;  // rows between a lane's
-  uint32_t at[UN];  // where its rows begin in a tile, before the swizzle of the piece
-#pragma unroll
-  for (int i = 0; i < UN; ++i) at[i] = (grp >> 1) * kHalf + sw128_offset(row0 + kStep * i, (grp & 1) * 4);
+  // where its first row begins in a tile (a step further: 128 kStep bytes)
+  const uint32_t at = (grp >> 1) * kHalf + sw128_offset(row0, (grp & 1) * 4);
   uint32_t g = 0;  // tiles written
   for (int n = 0;; ++n) {
     if (!wait_warp(&sm.plan_full[n & 1], (n >> 1) & 1, flags)) break;
@@ -258,48 +260,46 @@ __device__ __forceinline__ void write_values(const PackedParams &P, Smem<D> &sm,
     const Seg &sg = L.seg[it.s];
     const pk::Scales &sc = P.sc[it.s];
     const int64_t base = it.l * sg.sl + it.kvh * sg.sh + 16 * grp, gbase = it.l * sc.gl + it.kvh * sc.gh + grp;
+    const uint8_t *kc = static_cast<const uint8_t *>(sg.k) + base, *ks = sc.k + gbase;
+    const int64_t dv = static_cast<const uint8_t *>(sg.v) - static_cast<const uint8_t *>(sg.k), dvs = sc.v - sc.k;
     const int j_ask = max(pl.j1 - kAsk, pl.j0);
     if (pl.j0 == pl.j1 && pw == 0 && lane == 0) mbar_arrive(&sm.ask);  // no tiles
-    uint4 w[UN];
-    unsigned s[UN];
-    auto read = [&](int j, bool v) {
-      const int a = tile_start(pl.tl, j, BT), e = tile_end(pl.tl, j, BT);
-      const uint8_t *codes = static_cast<const uint8_t *>(v ? sg.v : sg.k) + base, *scales = (v ? sc.v : sc.k) + gbase;
-#pragma unroll
-      for (int i = 0; i < UN; ++i) {
-        const int t = a + row0 + kStep * i;
-        const int64_t tok = min(t, e - 1);
-        w[i] = __ldg(reinterpret_cast<const uint4 *>(codes + tok * sg.st));
-        s[i] = t < e ? __ldg(scales + tok * sc.gt) : 0;
-      }
+    uint4 w[2][UN];
+    unsigned s[2][UN];
+    auto read = [&](int a, int e, int kv, int i) {
+      const int t = a + row0 + kStep * i;
+      const int64_t tok = min(t, e - 1);
+      w[kv][i] = __ldg(reinterpret_cast<const uint4 *>(kc + tok * sg.st + (kv ? dv : 0)));
+      s[kv][i] = t < e ? __ldg(ks + tok * sc.gt + (kv ? dvs : 0)) : 0;
     };
-    if (pl.j0 < pl.j1) read(pl.j0, false);
+    if (pl.j0 < pl.j1) {
+      const int a = tile_start(pl.tl, pl.j0, BT), e = tile_end(pl.tl, pl.j0, BT);
+#pragma unroll
+      for (int i = 0; i < UN; ++i) read(a, e, 0, i), read(a, e, 1, i);
+    }
     bool ok = true;
     for (int j = pl.j0; j < pl.j1 && ok; ++j) {
       if (j == j_ask && pw == 0 && lane == 0) mbar_arrive(&sm.ask);
+      const int jn = min(j + 1, pl.j1 - 1);  // the last tile is read once more, and not written
+      const int a = tile_start(pl.tl, jn, BT), e = tile_end(pl.tl, jn, BT);
 #pragma unroll
-      for (int kv = 0; kv < 2 && ok; ++kv) {
-        uint4 c[UN];
-        unsigned b[UN];
-#pragma unroll
-        for (int i = 0; i < UN; ++i) c[i] = w[i], b[i] = s[i];
-        if (kv == 0) read(j, true);
-        else if (j + 1 < pl.j1) read(j + 1, false);
+      for (int kv = 0; kv < 2; ++kv) {
         const int st = g % NST;
-        if (g >= NST && !wait_warp(&sm.kv_empty[st], (g / NST - 1) & 1, flags)) {
-          ok = false;
-          break;
-        }
-        const uint32_t dst = smem_addr(sm.kv[st]);
+        if (ok && g >= NST && !wait_warp(&sm.kv_empty[st], (g / NST - 1) & 1, flags)) ok = false;
+        if (!ok) break;
+        const uint32_t dst = smem_addr(sm.kv[st]) + at;
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
-          const uint32_t y[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+          const uint32_t y[4] = {w[kv][i].x, w[kv][i].y, w[kv][i].z, w[kv][i].w};
+          const pk::BfScale f = pk::bf_scale(s[kv][i]);
+          read(a, e, kv, i);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             uint32_t x[4];
-            pk::values8(y[k], b[i], x);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (at[i] ^ (k << 4))), "r"(x[0]), "r"(x[1]), "r"(x[2]),
-                         "r"(x[3])
+            if (kv) pk::values8_paired(y[k], f, x);
+            else pk::values8(y[k], f, x);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((dst ^ (k << 4)) + 128 * kStep * i), "r"(x[0]), "r"(x[1]),
+                         "r"(x[2]), "r"(x[3])
                          : "memory");
           }
         }
@@ -715,13 +715,14 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
           uint32_t w[32];
           if (it.split) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(y[i]);
+            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(y[PACKED ? pk::paired_place(i) : i]);
             rows_out.put(w);
             rows_out.put(w + 16);
           } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+              const int a = PACKED ? pk::paired_place(2 * i) : 2 * i, b = PACKED ? pk::paired_place(2 * i + 1) : 2 * i + 1;
+              const __nv_bfloat162 h = __floats2bfloat162_rn(y[a], y[b]);
               w[i] = *reinterpret_cast<const uint32_t *>(&h);
             }
             rows_out.put(w);

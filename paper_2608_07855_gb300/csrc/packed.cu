@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
     for (int u = 0; u < kUnroll; ++u, dst += p.RB * r.st) {
       if (p.i + u * p.RB >= r.count) continue;
       uint32_t x[4];
-      values8(w[kv][u], s[kv][u], x);
+      values8(w[kv][u], bf_scale(s[kv][u]), x);
       if constexpr (VEC && sizeof(T) == 2) {
         *reinterpret_cast<uint4 *>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
       } else if constexpr (VEC) {

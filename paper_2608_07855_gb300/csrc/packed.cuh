@@ -36,24 +36,43 @@ __device__ __forceinline__ float sigma_of(unsigned b) {
   return __half2float(__ushort_as_half((unsigned short)(b << 7))) * kUnit;
 }
 
-// The values of a word's eight codes: (w >> 4 i & 0x000f000f) | 0x43004300 are the bf16
-// numbers 128 + u of the channels i and i + 4, one fma with (s, -136 s) makes them
-// (u - 8) s: exact (136 s has eight significant bits).  Then side by side.
-__device__ __forceinline__ void values8(uint32_t w, unsigned b, uint32_t (&x)[4]) {
-  const __nv_bfloat162 s = __float2bfloat162_rn(sigma_of(b)), off = __hmul2(s, __float2bfloat162_rn(-136.0f));
-  uint32_t p[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t y;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));
-    const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&y), s, off);
-    p[i] = *reinterpret_cast<const uint32_t *>(&v);
-  }
-  x[0] = __byte_perm(p[0], p[1], 0x5410);
-  x[1] = __byte_perm(p[2], p[3], 0x5410);
-  x[2] = __byte_perm(p[0], p[1], 0x7632);
-  x[3] = __byte_perm(p[2], p[3], 0x7632);
+// Values as bf16 numbers: (x & 0x000f000f) | 0x43004300 are the numbers 128 + u of two
+// codes, one fma with (s, -136 s) makes them (u - 8) s: exact (136 s has eight
+// significant bits).
+struct BfScale {
+  __nv_bfloat162 s, off;
+};
+__device__ __forceinline__ BfScale bf_scale(unsigned b) {
+  // from 8 on the byte's exponent and mantissa are bf16's, 106 higher; below, steps of 2^-23
+  uint32_t x = b * 16 + (106u << 7);
+  if (b < 8) x = __float_as_uint((float)b * 1.1920928955078125e-7f) >> 16;
+  if (b >= kNanScale) x = 0x7fff;
+  x = __byte_perm(x, x, 0x1010);
+  BfScale r;
+  r.s = *reinterpret_cast<const __nv_bfloat162 *>(&x);
+  r.off = __hmul2(r.s, __float2bfloat162_rn(-136.0f));
+  return r;
 }
+__device__ __forceinline__ uint32_t bf_pair(uint32_t x, const BfScale &s) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(0x000f000fu), "r"(0x43004300u));
+  const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&y), s.s, s.off);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+// A word's eight values in their order.
+__device__ __forceinline__ void values8(uint32_t w, const BfScale &s, uint32_t (&x)[4]) {
+  const uint32_t h = w >> 4;
+  x[0] = bf_pair(__byte_perm(w, h, 0x4400), s);
+  x[1] = bf_pair(__byte_perm(w, h, 0x5511), s);
+  x[2] = bf_pair(__byte_perm(w, h, 0x6622), s);
+  x[3] = bf_pair(__byte_perm(w, h, 0x7733), s);
+}
+// The same in the order 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ void values8_paired(uint32_t w, const BfScale &s, uint32_t (&x)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = bf_pair(w >> (4 * i), s);
+}
+__device__ __forceinline__ constexpr int paired_place(int c) { return (c & ~7) + 2 * (c & 3) + (c >> 2 & 1); }
 
 // Score of a token against a query, both read by one thread.
 template <int D>
