@@ -18,7 +18,7 @@
 // are rounded to bf16 because the product with bf16 values takes one type: an
 // error of 2^-9 of each weight on average, that of the output's own rounding.
 // Sums of weights are fp32 and not rounded.
-// Packed caches have four more warps (12-15) in the place of warp 0: they read
+// Packed caches have eight more warps (12-19) in the place of warp 0: they read
 // codes and write the values, which are bf16 numbers, into the same stages.
 // TMEM: S/P of group b at column 128 b, O of group b at 256 + D b.
 #pragma once
@@ -196,6 +196,41 @@ __device__ __forceinline__ void soft_full(uint32_t s_col, uint32_t o_col, float 
   lsum += a.x + a.y;
 }
 
+// The same with half the registers: 64 scores at a time, the second half read twice
+// (its weights go where scores of the first half were).
+template <int D>
+__device__ __forceinline__ void soft_halves(uint32_t s_col, uint32_t o_col, float scale, float &m, float &lsum) {
+  float x[64], top = -INFINITY;
+#pragma unroll
+  for (int h = 1; h >= 0; --h) {
+    tmem_ld32f(s_col + 64 * h, x);
+    tmem_ld32f(s_col + 64 * h + 32, x + 32);
+    tmem_wait_ld();
+    top = max32(x + 32, max32(x, top));
+  }
+  raise_max<D>(o_col, __fmul_rn(top, scale), m, lsum);
+  const float neg = m == -INFINITY ? 0.0f : -m;
+  const float2 scale2 = make_float2(scale, scale), neg2 = make_float2(neg, neg);
+  float2 ps[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (h) {
+      tmem_ld32f(s_col + 64, x);
+      tmem_ld32f(s_col + 96, x + 32);
+      tmem_wait_ld();
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t p[16];
+      weigh32(x + 32 * c, scale2, neg2, ps, p);
+      tmem_st16(s_col + 32 * h + 16 * c, p);
+    }
+  }
+  tmem_wait_st();
+  const float2 a = fadd2(ps[0], ps[1]);
+  lsum += a.x + a.y;
+}
+
 // A tile that ends early or that some rows see in part: 32 columns at a time,
 // read twice.
 template <int D>
@@ -231,9 +266,16 @@ __device__ __forceinline__ void soft_masked(uint32_t s_col, uint32_t o_col, floa
   lsum += b.x + b.y;
 }
 
-// A warp of the four that write the values of a packed cache, K and V tile after
+// Where K and V of tile j of an item's nt stand among the item's 2 nt tiles in
+// the ring, for packed caches and items of one row tile: in the order in which the
+// MMAs take them, K0 K1 V0 K2 V1 .., so that a tile is written as soon as the one
+// four places before it is done with.
+__device__ __forceinline__ int k_place(int j) { return max(2 * j - 1, 0); }
+__device__ __forceinline__ int v_place(int j, int nt) { return min(2 * j + 2, 2 * nt - 1); }
+
+// A warp of the eight that write the values of a packed cache, K and V tile after
 // tile into the ring.  A lane has one token's 32 channels of a group, 16 bytes of
-// codes and a scale byte, D / 32 times a tile; eight lanes write eight rows' 16
+// codes and a scale byte, D / 64 times a tile; eight lanes write eight rows' 16
 // bytes of one place, which lie in different banks.  What is written is read a
 // tile of K and of V ahead: a warp alone on its scheduler's share has nothing else
 // to hide the loads' latency with (one tile of either ahead: 421 us for the probe
@@ -241,12 +283,12 @@ __device__ __forceinline__ void soft_masked(uint32_t s_col, uint32_t o_col, floa
 // pairs (paired_place); the results are put in order on their way out.
 template <int D>
 __device__ __forceinline__ void write_values(const PackedParams &P, Smem<D> &sm, int pw, int lane) {
-  constexpr int NST = Smem<D>::NST, UN = D / 32;
+  constexpr int NST = Smem<D>::NST, UN = D / 64;
   const Launch &L = P.L;
   volatile int *flags = sm.flags;
   const int grp = D == 128 ? lane >> 3 : (lane >> 3) & 1;
-  const int row0 = 32 * pw + (lane & 7) + (D == 128 ? 0 : 8 * (lane >> 4));
-  constexpr int kStep = D == 128 ? 8 : 16;  // rows between a lane's
+  const int row0 = 16 * pw + (lane & 7) + (D == 128 ? 0 : 8 * (lane >> 4));
+  constexpr int kStep = 8;  // rows between a lane's
   // where its first row begins in a tile (a step further: 128 kStep bytes)
   const uint32_t at = (grp >> 1) * kHalf + sw128_offset(row0, (grp & 1) * 4);
   uint32_t g = 0;  // tiles written
@@ -278,12 +320,15 @@ __device__ __forceinline__ void write_values(const PackedParams &P, Smem<D> &sm,
       for (int i = 0; i < UN; ++i) read(a, e, 0, i), read(a, e, 1, i);
     }
     bool ok = true;
-    for (int j = pl.j0; j < pl.j1 && ok; ++j) {
+    const int ahead = pl.rows > BM || pl.j0 == pl.j1 ? 0 : 1;  // K of this many tiles before V: k_place and v_place
+    for (int j = pl.j0 - ahead; j < pl.j1 && ok; ++j) {
       if (j == j_ask && pw == 0 && lane == 0) mbar_arrive(&sm.ask);
-      const int jn = min(j + 1, pl.j1 - 1);  // the last tile is read once more, and not written
-      const int a = tile_start(pl.tl, jn, BT), e = tile_end(pl.tl, jn, BT);
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
+        const int here = kv ? j : j + ahead;
+        if (here < pl.j0 || here >= pl.j1) continue;
+        const int jn = min(here + 1, pl.j1 - 1);  // the last tile is read once more, and not written
+        const int a = tile_start(pl.tl, jn, BT), e = tile_end(pl.tl, jn, BT);
         const int st = g % NST;
         if (ok && g >= NST && !wait_warp(&sm.kv_empty[st], (g / NST - 1) & 1, flags)) ok = false;
         if (!ok) break;
@@ -314,7 +359,7 @@ __device__ __forceinline__ void write_values(const PackedParams &P, Smem<D> &sm,
 }
 
 template <int D, typename Params>
-__global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(const __grid_constant__ Params P, WsHeader *hdr) {
+__global__ void __launch_bounds__(Params::kPacked ? 640 : 384, 1) attend_tc(const __grid_constant__ Params P, WsHeader *hdr) {
   using S = Smem<D>;
   constexpr int NST = S::NST;
   constexpr bool PACKED = Params::kPacked;
@@ -329,7 +374,7 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
     sm.flags[kAbort] = sm.flags[kRedoing] = 0;
     for (int b = 0; b < 2; ++b) {
       mbar_init(&sm.plan_full[b], 1);
-      mbar_init(&sm.plan_empty[b], PACKED ? 13 : 10);  // TMA or four warps that write values, MMA, eight softmax warps
+      mbar_init(&sm.plan_empty[b], PACKED ? 17 : 10);  // TMA or eight warps that write values, MMA, eight softmax warps
       mbar_init(&sm.s_full[b], 1);
       mbar_init(&sm.p_full[b], 4);
       mbar_init(&sm.o_full[b], 1);
@@ -340,7 +385,7 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
     mbar_init(&sm.q_full, 1);
     mbar_init(&sm.q_empty, 1);
     for (int s = 0; s < NST; ++s) {
-      mbar_init(&sm.kv_full[s], PACKED ? 4 : 1);
+      mbar_init(&sm.kv_full[s], PACKED ? 8 : 1);
       mbar_init(&sm.kv_empty[s], 1);
     }
     mbar_init(&sm.drain, 1);
@@ -370,12 +415,12 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
   const uint32_t tm = sm.tmem;
 
   // registers: 104 + 2 x 200 a thread of each group of four warps = 3 x 168
-  // (packed: 64 + 2 x 176 + 96 = 4 x 128)
+  // (packed: 48 + 2 x 128 + 2 x 88 = 5 x 96)
   if (PACKED && warp >= 12) {
-    regs_dec<96>();
+    regs_dec<88>();
     if constexpr (PACKED) write_values<D>(P, sm, warp - 12, lane);
   } else if (warp < 4) {
-    regs_dec<PACKED ? 64 : 104>();
+    regs_dec<PACKED ? 48 : 104>();
     if (!PACKED && warp == 0 && lane == 0) {
       // ------------------------------------------------------------ TMA
       if constexpr (!PACKED) {
@@ -495,7 +540,7 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
         } else {
           // one row tile, the groups take alternate token tiles
           for (int j = 0; j < nt + 2 && ok && nt > 0; ++j) {
-            const uint32_t uk = 2 * (g + j), uv = uk - 3;
+            const uint32_t uk = 2 * g + (PACKED ? k_place(j) : 2 * j), uv = 2 * g + (PACKED ? v_place(j - 2, nt) : 2 * j - 3);
             const int b = j & 1, i = (j - 2) >> 1;
             if (j >= 2) {
               ok = (uint32_t)(j - 2) >= (uint32_t)nt || (kv_wait(uv) && p_wait(b, i));
@@ -601,7 +646,7 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
     }
   } else {
     // ------------------------------------------------------------ softmax
-    regs_inc<PACKED ? 176 : 200>();
+    regs_inc<PACKED ? 128 : 200>();
     const int hb = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane;
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     const uint32_t s_col = tm + lanes + BT * hb, o_col = tm + lanes + 256 + D * hb;
@@ -637,7 +682,8 @@ __global__ void __launch_bounds__(Params::kPacked ? 512 : 384, 1) attend_tc(cons
         }
         const int t0 = tile_start(tl, j, BT), t1 = tile_end(tl, j, BT);
         if (__all_sync(0xffffffffu, sp.lo <= t0 && t0 + BT <= min(sp.hi, t1)))
-          soft_full<D>(s_col, o_col, L.scale_log2, m_used, lsum);
+          if constexpr (PACKED) soft_halves<D>(s_col, o_col, L.scale_log2, m_used, lsum);
+          else soft_full<D>(s_col, o_col, L.scale_log2, m_used, lsum);
         else
           soft_masked<D>(s_col, o_col, L.scale_log2, sp, t0, t1, m_used, lsum);
         tc_fence_before();

@@ -1,6 +1,6 @@
 // Attention over packed caches on the tensor cores (bf16, many rows): the
 // kernel's launch.  Codes are read and their values written to shared memory by
-// four warps of each block, for every row tile again.
+// eight warps of each block, for every row tile again.
 #include "attend_tc_impl.cuh"
 
 namespace ckv {
@@ -13,7 +13,7 @@ cudaError_t launch(const PackedParams &P, WsHeader *hdr, cudaStream_t s, bool ea
   const cudaError_t e =
       cudaFuncSetAttribute(attend_tc<D, PackedParams>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_after(attend_tc<D, PackedParams>, P.L.item_off[P.L.n_seg], 512, smem, s, early, P, hdr);
+  return launch_after(attend_tc<D, PackedParams>, P.L.item_off[P.L.n_seg], 640, smem, s, early, P, hdr);
 }
 
 }  // namespace
