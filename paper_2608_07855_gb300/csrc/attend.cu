@@ -279,10 +279,11 @@ static constexpr PathInfo kPath[kPaths] = {
 // For tests and diagnosis, read in every call: COMMITKV_SCORING=simt takes the
 // CUDA cores where a call could have the tensor cores (attention as well as
 // scoring), COMMITKV_ATTENTION=tiles the kernels of row tiles however few rows
-// there are.
+// there are (packed caches: from 17 rows), COMMITKV_ATTENTION=full the full-width
+// values of packed caches from 17 rows.
 Forced forced_paths() {
   const char *s = getenv("COMMITKV_SCORING"), *a = getenv("COMMITKV_ATTENTION");
-  return {s && s[0] == 's', a && a[0] == 't'};
+  return {s && s[0] == 's', a && a[0] == 't', a && a[0] == 'f'};
 }
 
 // Tensor cores where 16-byte copies can read the cache and the rows' queries

@@ -401,7 +401,7 @@ struct Division {
 };
 Division divide(const Divide &v, const PathInfo &pi, int64_t slots, int64_t most_items, int64_t slices, bool prefix);
 struct Forced {
-  bool cuda_cores, tiles;
+  bool cuda_cores, tiles, full;
 };
 Forced forced_paths();
 int sm_count();

@@ -42,10 +42,6 @@ size_t compact_bytes(int n, const commitkv_packed *x) {
 // Many rows: the trajectories' values in full width, a layer of all of them, K
 // before V, each [H][S][d] dense.
 bool many(const commitkv_shape *s, const commitkv_packed &x) { return (int64_t)(s->q_heads / s->kv_heads) * x.W > 16; }
-// Of these, those that the kernel of row tiles takes as they are.
-bool direct(const commitkv_shape *s, const commitkv_packed &x, const void *out, bool cuda_cores) {
-  return !cuda_cores && s->dtype == COMMITKV_BF16 && wide(to_dev(x), s->head_dim) && ((uintptr_t)x.q | (uintptr_t)out) % 16 == 0;
-}
 size_t full_bytes(const commitkv_shape *s, const commitkv_packed &x) {  // K or V
   return at::align_up((size_t)s->kv_heads * x.S * s->head_dim * (s->dtype == COMMITKV_BF16 ? 2 : 4));
 }
@@ -103,6 +99,46 @@ commitkv_status attend_many(const commitkv_shape *s, int n, const commitkv_packe
   return COMMITKV_OK;
 }
 
+// What trajectories of more than 16 rows take, of a call together: the kernel of
+// 8- or 16-row items, which reads the codes again for every one of them, the
+// kernel of row tiles on the codes, which writes their values to shared memory
+// again for every 256 rows, or the values read back once.  Estimated times in us,
+// fits to calls of these kinds (bf16, 8 KV heads of 128 channels, 4 query heads to one;
+// 8 queries over 4,000 tokens 14.7, 18.9 and 20.9, 16 over 16,000 31, 27 and 39, 64
+// over 16,000 93, 37 and 52, 256 over 16,000 307, 90 and 91, 1,024 over 16,000 1,101,
+// 278 and 233, 31 of 12 layers over 32,768 896, 279 and 803; fp32, 4 KV heads, 100
+// over 4,000 47 and, read back, 47, 300 over 4,000 93 and 85).
+enum Many { kManyRows, kManyTiles, kManyBack };
+Many many_path(const commitkv_shape *s, int n, const commitkv_packed *x, void *const *out, int n_layers, int window,
+               int sinks, const at::Forced &f, int sms) {
+  const bool bf16 = s->dtype == COMMITKV_BF16, wide128 = s->head_dim == 128;
+  const double slices = (double)n_layers * s->kv_heads, full = s->head_dim * (bf16 ? 2 : 4);
+  double rows = 10.0, tiles = 15.0, back = 22.0 + 4.0 * n_layers;
+  bool fast = !f.cuda_cores && !f.full, aligned = true;
+  for (int t = 0; t < n; ++t) {
+    if (!many(s, x[t])) continue;
+    const int64_t R = (int64_t)(s->q_heads / s->kv_heads) * x[t].W;
+    fast = fast && wide(to_dev(x[t]), s->head_dim) && (uintptr_t)x[t].q % 16 == 0;
+    aligned = aligned && (uintptr_t)out[t] % 16 == 0;
+    const int64_t seen = std::min<int64_t>(x[t].S, window ? (int64_t)window + sinks + x[t].W : x[t].S);
+    rows += 1e-6 * slices * seen *
+            (bf16 ? at::cdiv(R, 16) * (wide128 ? 38.0 : 27.0) : at::cdiv(R, 8) * (wide128 ? 34.0 : 21.0));
+    if (bf16) {
+      const double tile = slices * at::cdiv(R, 256) * at::cdiv(seen, 128) / sms;
+      tiles += tile * (R <= 128 ? (wide128 ? 1.6 : 1.2) : (wide128 ? 2.4 : 1.7));
+      back += tile * (wide128 ? 1.75 : 1.3);
+    } else {
+      back += slices * at::cdiv(R, 128) * at::cdiv(seen, 64) / sms * (wide128 ? 2.7 : 1.8);
+    }
+    back += slices * x[t].S * (s->head_dim * 1.0625 + 4 * full) / 6.5e6;
+  }
+  const bool can_tile = bf16 && aligned;
+  if (!fast) return kManyBack;
+  if (f.tiles) return can_tile ? kManyTiles : kManyBack;
+  if (rows <= back && (!can_tile || rows <= tiles)) return kManyRows;
+  return can_tile && tiles <= back ? kManyTiles : kManyBack;
+}
+
 enum { kSimt16, kRows8, kRows16, kTc, kPaths };
 constexpr at::PathInfo kPath[kPaths] = {
     {16, 64, 2, 1.0, 11.5}, {8, 128, 4, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}, {256, 128, 1, 2.0, 1.7}};
@@ -154,11 +190,16 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
   for (int l = 0; l < shape->layers; ++l)
     if (!layer_mask || layer_mask[l]) L.layer_ids[L.n_layers++] = (uint8_t)l;
   L.n_traj = L.n_seg = n_traj;
+  int64_t queries = 0;
+  for (int t = 0; t < n_traj; ++t) queries += trajs[t].W;
+  if (L.n_layers == 0 || queries == 0) return COMMITKV_OK;
   const int64_t slices = (int64_t)L.n_layers * L.H;
-  int64_t rows = 0;
   bool big = false, back[kMaxTraj];
   int path[kMaxTraj];
   const Forced forced = forced_paths();
+  const int sms = sm_count();
+  if (sms < 1) return COMMITKV_ERR_CUDA;
+  const pk::Many many = pk::many_path(shape, n_traj, trajs, out, L.n_layers, window, sinks, forced, sms);
   for (int t = 0; t < n_traj; ++t) {
     const commitkv_packed &x = trajs[t];
     const pk::Cache c = pk::to_dev(x);
@@ -170,16 +211,12 @@ commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n
     sg.pos = x.pos;
     sg.S = x.S;
     sg.t = t;
-    back[t] = pk::many(shape, x) && !pk::direct(shape, x, out[t], forced.cuda_cores);
+    back[t] = pk::many(shape, x) && many == pk::kManyBack;
     sg.R = back[t] ? 0 : L.g * x.W;
-    rows += sg.R;
     big = big || back[t];
     const bool fast = !forced.cuda_cores && pk::wide(c, L.d) && (uintptr_t)x.q % 16 == 0;
-    path[t] = sg.R > 16 ? pk::kTc : !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
+    path[t] = sg.R > 16 && many == pk::kManyTiles ? pk::kTc : !fast ? pk::kSimt16 : sg.R <= 8 || L.dtype == COMMITKV_F32 ? pk::kRows8 : pk::kRows16;
   }
-  if (L.n_layers == 0 || (rows == 0 && !big)) return COMMITKV_OK;
-  const int sms = sm_count();
-  if (sms < 1) return COMMITKV_ERR_CUDA;
   for (int s = 0; s < n_traj; ++s) L.order[s] = (uint8_t)s;
   std::sort(L.order, L.order + n_traj,
             [&](int a, int b) { return L.seg[a].S != L.seg[b].S ? L.seg[a].S > L.seg[b].S : a < b; });

@@ -221,10 +221,14 @@ def test_rows_beyond_32_bits():
 
 
 # ------------------------------------------------------------------------------------------------ attention
-@pytest.fixture(params=["", "cuda_cores"])
+@pytest.fixture(params=["", "tiles", "full", "cuda_cores"])
 def kernels(request, monkeypatch):
-    if request.param:
+    """On the kernels that the library picks; from 17 rows on, those of row tiles on the codes, and those of full-width
+    caches; the CUDA cores."""
+    if request.param == "cuda_cores":
         monkeypatch.setenv("COMMITKV_SCORING", "simt")
+    elif request.param:
+        monkeypatch.setenv("COMMITKV_ATTENTION", request.param)
     return request.param
 
 
