@@ -51,6 +51,9 @@ constexpr int NW = 4;
 constexpr int WT = 32;  // tokens of a warp,
 constexpr int TT = NW * WT;  // of a tile
 constexpr float kLazy = 4.0f, kLift = 11.0f;
+// Weights are exp2 of the fused s scale - m; the largest passes 2^15 by half a step
+// of its score then, 1/4 up to here, and not fp16's range.
+constexpr float kFar = 4194304.0f;
 
 template <int D, int QT>
 struct Smem {
@@ -61,19 +64,20 @@ struct Smem {
     alignas(128) uint8_t ring[NW][NST][kStage];
     float o[NW][8 * QT][D + 4];
   };
+  uint32_t sc[NW][2][2][WT];  // scale bytes of a tile's tokens, of K and V, of two tiles by turns
   float2 ml[NW][8 * QT];
   unsigned nan[NW][8 * QT];
 };
 
 // Where a row's bytes stand in its tile: rows that a fragment reads together lie
-// in different banks.
+// in different banks.  Row t at t kRow, with these bits turned over.
 template <int D>
-__device__ __forceinline__ uint32_t k_at(int t) {
-  return D == 128 ? t * 64 : (t * 32) ^ ((t >> 3 & 1) << 6);
+__device__ __forceinline__ uint32_t k_turn(int t) {
+  return D == 128 ? 0 : (t >> 3 & 1) << 6;
 }
 template <int D>
-__device__ __forceinline__ uint32_t v_at(int t) {
-  return D == 128 ? (t * 64) ^ ((t >> 4 & 1) << 6) ^ ((t >> 3 & 1) << 5) : (t * 32) ^ ((t >> 3 & 3) << 5);
+__device__ __forceinline__ uint32_t v_turn(int t) {
+  return D == 128 ? (t >> 4 & 1) << 6 | (t >> 3 & 1) << 5 : (t >> 3 & 3) << 5;
 }
 
 template <int N>
@@ -204,6 +208,9 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
   const int64_t dv = static_cast<const uint8_t *>(sg.v) - static_cast<const uint8_t *>(sg.k);
   const int64_t dvs = sc.v - sc.k, step = 32 / KW * sg.st, tile_step = TT * sg.st, scale_step = TT * sc.gt;
   const uint32_t ring = smem_addr(sm.ring[warp]);
+  // where the lane's copies go in a stage (16 bytes of row lane / KW, further ones 512 bytes on)
+  const uint32_t to_k = (lane / KW * S::kRow + 16 * (lane % KW)) ^ k_turn<D>(lane / KW);
+  const uint32_t to_v = WT * S::kRow + ((lane / KW * S::kRow + 16 * (lane % KW)) ^ v_turn<D>(lane / KW));
   // The chunk is one or two pieces of consecutive tokens (sinks, then the window);
   // the warp's tokens of a piece's tiles begin at `at` and end with the piece.
   struct Cursor {
@@ -222,9 +229,9 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
   auto load = [&](Cursor &x, uint32_t dst) {
     if (x.at < x.end) {
       auto copy = [&](int i, const uint8_t *src) {
-        const int t = (i * 32 + lane) / KW, ch = lane % KW;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (k_at<D>(t) ^ (16 * ch))), "l"(src) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + WT * S::kRow + (v_at<D>(t) ^ (16 * ch))), "l"(src + dv)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + to_k + 512 * i), "l"(src) : "memory");
+        // stages are 128-byte aligned: the turn of the row's bits above the lane's own
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(((dst + to_v) ^ v_turn<D>(32 / KW * i)) + 512 * i), "l"(src + dv)
                      : "memory");
       };
       if (x.at + WT <= x.end) {
@@ -309,7 +316,7 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
       }
     }
     // 16 / 2^k, and the softmax scale (which no score overflows by but that of a scale of 2^13 and more)
-    const float b = fminf(__uint_as_float((uint32_t)(131 - k) << 23) * L.scale_log2, 3.402823466e38f);
+    const float b = fmaxf(fminf(__uint_as_float((uint32_t)(131 - k) << 23) * L.scale_log2, 3.402823466e38f), 1.175494351e-38f);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       back[n][e] = __shfl_sync(0xffffffffu, b, 4 * (2 * c + e));
@@ -337,7 +344,16 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
   const int tk = 8 * (r >> 1) + (r & 1);
   const uint32_t gk = D == 128 ? c : c >> 1, gv = D == 128 ? r >> 1 : r >> 2;  // the lane's groups
   const uint32_t ksel = gk << 12 | gk << 4 | 0x0404, vsel = (4 + gv) << 12 | gv << 4;
-  auto tile = [&](auto is_small, int a, int e, uint32_t ks, uint32_t vs) {
+  // where the lane reads in a stage: K's rows tk + 2 h, and V's 8 c + t (i: 4 rows on, whose bits are turned alike)
+  uint32_t from_k[2], from_v[4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) from_k[h] = ((tk + 2 * h) * S::kRow + 4 * KW * c) ^ k_turn<D>(tk);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) from_v[t] = WT * S::kRow + (((8 * c + t) * S::kRow + 4 * VW * r) ^ v_turn<D>(8 * c));
+  const uint32_t scales = smem_addr(sm.sc[warp]);
+  bool far = false;  // a reference so large that products are rounded before they are compared with it
+  // a tile in stage `stage`, its scale bytes at `sc_at`; bad: groups of the lane's token whose values are NaN
+  auto tile = [&](auto is_small, int a, int e, uint32_t stage, uint32_t sc_at, unsigned bad) {
     constexpr bool SMALL = decltype(is_small)::value;
     const bool whole = all_lo <= a && a + WT <= min(all_hi, e);
     float s[QT][2][4];
@@ -347,9 +363,10 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int t = tk + 4 * i + 2 * h;
-        lds<KW>(ks + (k_at<D>(t) ^ (4 * KW * c)), w[i][h]);
-        f[i][h] = scales_of<SMALL>(__byte_perm(__shfl_sync(0xffffffffu, ksc, t), 0, ksel) >> 1);
+        lds<KW>(stage + from_k[h] + 4 * S::kRow * i, w[i][h]);
+        uint32_t b[1];
+        lds<1>(sc_at + 4 * tk + 16 * i + 8 * h, b);
+        f[i][h] = scales_of<SMALL>(__byte_perm(b[0], 0, ksel) >> 1);
       }
     }
 #pragma unroll
@@ -372,11 +389,7 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
           mma(s[n][i], a1, q[n][2 * x + 1][0], q[n][2 * x + 1][1]);
         }
       }
-    if constexpr (SMALL) {  // NaN scales of values stand as zeros
-      const unsigned bad = nan_groups<D>(vsc);
-#pragma unroll
-      for (int g = 0; g < D / kGroup; ++g)
-        if (bad >> g & 1) vsc &= ~(0xffu << (8 * g));
+    if constexpr (SMALL) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const unsigned b = __shfl_sync(0xffffffffu, bad, tk + 2 * i);
@@ -390,14 +403,6 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
     uint32_t p[QT][2][2], pl[QT][F32 ? 2 : 1][2];
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
-      float top[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float &y = s[n][i >> 1][2 * (i & 1) + x];
-          y = __fmul_rn(SMALL ? y * 0.125f : y, back[n][x]);
-        }
       if (!whole) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -408,9 +413,12 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
             y = tok < e && at::sees(sp[n][x], tok) ? y : -INFINITY;
           }
       }
+      float top[2], by[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-        top[x] = fmaxf(fmaxf(s[n][0][x], s[n][0][2 + x]), fmaxf(s[n][1][x], s[n][1][2 + x]));
+      for (int x = 0; x < 2; ++x) {
+        by[x] = SMALL ? back[n][x] * 0.125f : back[n][x];
+        top[x] = __fmul_rn(fmaxf(fmaxf(s[n][0][x], s[n][0][2 + x]), fmaxf(s[n][1][x], s[n][1][2 + x])), by[x]);
+      }
       if (__any_sync(0xffffffffu, top[0] > over[n][0] || top[1] > over[n][1])) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -425,6 +433,7 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
             over[n][x] = top[x] + kLazy;
           }
         }
+        far = far || __any_sync(0xffffffffu, fabsf(top[0]) > kFar || fabsf(top[1]) > kFar);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -432,7 +441,7 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float &y = s[n][i >> 1][2 * (i & 1) + x];
-          y = fast_exp2(y - ref);
+          y = fast_exp2(far ? __fmul_rn(y, by[x]) - ref : fmaf(y, by[x], -ref));
           lsum[n][x] += y;
         }
       }
@@ -449,16 +458,14 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      uint32_t w[4][VW];
+      uint32_t w[4][VW], b[4];
       Sc<SMALL> f[2];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) lds<VW>(vs + (v_at<D>(8 * c + 4 * i + t) ^ (4 * VW * r)), w[t]);
+      for (int t = 0; t < 4; ++t) lds<VW>(stage + from_v[t] + 4 * S::kRow * i, w[t]);
+      lds<4>(sc_at + 4 * WT + 32 * c + 16 * i, b);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int t = 8 * c + 4 * i + 2 * h;
-        f[h] = scales_of<SMALL>(
-            __byte_perm(__shfl_sync(0xffffffffu, vsc, t), __shfl_sync(0xffffffffu, vsc, t + 1), vsel) >> 1 & 0x7f807f80u);
-      }
+      for (int h = 0; h < 2; ++h)
+        f[h] = scales_of<SMALL>(__byte_perm(b[2 * h], b[2 * h + 1], vsel) >> 1 & 0x7f807f80u);
       // of each word the halves of two tokens side by side: y[h][word][half]
       uint32_t y[2][VW][2];
 #pragma unroll
@@ -478,20 +485,20 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
       // m-tile t: rows r and r + 8 are channels t of the lane's first and second
       // word (128 channels), or t of the halves of its one word (64)
 #pragma unroll
-      for (int b = 0; b < MT / 4; ++b) {
-        auto part = [&](int h, int second) { return VW == 2 ? y[h][second % VW][b] : y[h][0][second]; };
+      for (int u = 0; u < MT / 4; ++u) {
+        auto part = [&](int h, int second) { return VW == 2 ? y[h][second % VW][u] : y[h][0][second]; };
         const uint32_t a0[4] = {values_of<0, SMALL>(part(0, 0), f[0]), values_of<0, SMALL>(part(0, 1), f[0]),
                                 values_of<0, SMALL>(part(1, 0), f[1]), values_of<0, SMALL>(part(1, 1), f[1])};
-        step(4 * b, a0);
+        step(4 * u, a0);
         const uint32_t a1[4] = {values_of<1, SMALL>(part(0, 0), f[0]), values_of<1, SMALL>(part(0, 1), f[0]),
                                 values_of<1, SMALL>(part(1, 0), f[1]), values_of<1, SMALL>(part(1, 1), f[1])};
-        step(4 * b + 1, a1);
+        step(4 * u + 1, a1);
         const uint32_t a2[4] = {values_of<2, SMALL>(part(0, 0), f[0]), values_of<2, SMALL>(part(0, 1), f[0]),
                                 values_of<2, SMALL>(part(1, 0), f[1]), values_of<2, SMALL>(part(1, 1), f[1])};
-        step(4 * b + 2, a2);
+        step(4 * u + 2, a2);
         const uint32_t a3[4] = {values_of<3, SMALL>(part(0, 0), f[0]), values_of<3, SMALL>(part(0, 1), f[0]),
                                 values_of<3, SMALL>(part(1, 0), f[1]), values_of<3, SMALL>(part(1, 1), f[1])};
-        step(4 * b + 3, a3);
+        step(4 * u + 3, a3);
       }
     }
   };
@@ -503,15 +510,30 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4)
     for (; j < last; ++j, a += TT) {
       uint32_t kn, vn;
       load_scales(sc_in, kn, vn);
-      asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
-      __syncwarp();  // every lane's copies of this stage are there, and its reads of the last one are done
-      load(in, ring + (st == 0 ? NST - 1 : st - 1) * S::kStage);
-      const uint32_t ks = ring + st * S::kStage, vs = ks + WT * S::kRow;
-      st = st + 1 == NST ? 0 : st + 1;
+      unsigned bad = 0;
+      bool any_small = false;
+      const uint32_t sc_at = scales + (j & 1) * (8 * WT);
       if (a < e) {
         const uint32_t nan = vsc & ((vsc & 0x7f7f7f7fu) + 0x08080808u) & 0x80808080u;  // a byte from 0xf8 on
-        if (__any_sync(0xffffffffu, small(ksc) | small(vsc) | nan)) tile(std::true_type{}, a, e, ks, vs);
-        else tile(std::false_type{}, a, e, ks, vs);
+        any_small = __any_sync(0xffffffffu, small(ksc) | small(vsc) | nan);
+        if (any_small) {  // NaN scales of values stand as zeros
+          bad = nan_groups<D>(vsc);
+#pragma unroll
+          for (int g = 0; g < D / kGroup; ++g)
+            if (bad >> g & 1) vsc &= ~(0xffu << (8 * g));
+        }
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc_at + 4 * lane), "r"(ksc) : "memory");
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc_at + 4 * WT + 4 * lane), "r"(vsc) : "memory");
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
+      // every lane's copies of this stage and its scale bytes are there, and its reads of the last one are done
+      __syncwarp();
+      load(in, ring + (st == 0 ? NST - 1 : st - 1) * S::kStage);
+      const uint32_t stage = ring + st * S::kStage;
+      st = st + 1 == NST ? 0 : st + 1;
+      if (a < e) {
+        if (any_small) tile(std::true_type{}, a, e, stage, sc_at, bad);
+        else tile(std::false_type{}, a, e, stage, sc_at, 0u);
       }
       ksc = kn, vsc = vn;
     }
