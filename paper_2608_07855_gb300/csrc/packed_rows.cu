@@ -162,7 +162,7 @@ __device__ __forceinline__ unsigned nan_groups(uint32_t w) {
 }
 
 template <typename T, int D, int QT>
-__global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : sizeof(T) == 4 ? 3 : 4) attend_packed_rows(const __grid_constant__ Launch P) {
+__global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : 3) attend_packed_rows(const __grid_constant__ Launch P) {
   using S = Smem<D, QT>;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int RI = 8 * QT, KW = D / 32, VW = D / 64, KS = D / 16, MT = D / 16, NST = S::NST;
