@@ -141,7 +141,7 @@ Many many_path(const commitkv_shape *s, int n, const commitkv_packed *x, void *c
 
 enum { kSimt16, kRows8, kRows16, kTc, kPaths };
 constexpr at::PathInfo kPath[kPaths] = {
-    {16, 64, 2, 1.0, 11.5}, {8, 128, 3, 2.0, 1.2}, {16, 128, 2, 2.0, 1.4}, {256, 128, 1, 2.0, 1.7}};
+    {16, 64, 2, 1.0, 11.5}, {8, 128, 3, 2.0, 1.7}, {16, 128, 2, 2.0, 1.9}, {256, 128, 1, 2.0, 1.7}};
 
 }  // namespace
 }  // namespace pk
