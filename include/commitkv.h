@@ -595,15 +595,18 @@ typedef struct {
  *     code  = 8 + n, n the integer nearest to x / sigma, of two as near the even
  *             one, at most 7 away from 0; 8 where sigma = 0.
  * Both go by the exact quotients, so equal rows have equal codes wherever they
- * are written.  A value is off by at most sigma / 2 while a is between 2^-18 and
- * 6720 (7.5 sigma there at least reach a).  32 channels of which one is infinite
- * or NaN get scale byte 0xff and codes 8: they read back as NaN.
+ * are written.  A value is off by at most sigma / 2 while a is between 2^-17 and
+ * 7200 (a is at most 7.5 sigma there), larger values come out as 6720.  32 channels
+ * of which one is infinite or NaN get scale byte 0xff and codes 8: they read back as
+ * NaN.
  *
  *   caches       k, v, their scales and strides are used; first + count must not
  *                exceed S.  Positions are the caller's to write.
  *   rows         host array [n_traj]; count = 0: nothing is written.
  *   layer_mask   as for commitkv_page_effects; other layers are left alone.
- * Rows must not overlap the caches, or caches of a call one another.
+ * Rows must not overlap the caches, and the tokens that a call writes not one
+ * another; layers and heads of a cache lie apart (strides above 0, else
+ * COMMITKV_ERR_INVALID_ARG).
  * -------------------------------------------------------------------- */
 commitkv_status commitkv_packed_write(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *caches,
                                       const commitkv_rows *rows, const uint8_t *layer_mask, cudaStream_t stream);
@@ -611,7 +614,8 @@ commitkv_status commitkv_packed_write(const commitkv_shape *shape, int32_t n_tra
 /* ------------------------------------------------------------------------
  * Reads rows of packed caches back, exactly, in the dtype of the shape: what
  * the calls on full-width caches (page effects, joint test, token scores) take.
- * Arguments as for commitkv_packed_write; rows of other layers are not written.
+ * Arguments as for commitkv_packed_write, with the rows written (their elements lie
+ * apart, strides not 0) and the caches read; rows of other layers are not written.
  * -------------------------------------------------------------------- */
 commitkv_status commitkv_packed_read(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *caches,
                                      const commitkv_rows *rows, const uint8_t *layer_mask, cudaStream_t stream);
@@ -625,15 +629,20 @@ commitkv_status commitkv_packed_read(const commitkv_shape *shape, int32_t n_traj
  *
  *   workspace    at least commitkv_packed_workspace_size bytes for these
  *                trajectories or larger ones (S, W, n_traj), 256-byte aligned.
- * Which kernels run, by the rows g W_t of a trajectory:
- *   up to 16, codes and scales aligned: tensor cores, on the codes as they are.  Scores
- *     and sums are fp32; queries and weights enter the products as fp16 terms
- *     relative to their row's largest: one (bf16: a query is kept whole, 2^-12 of
- *     a weight is lost) or two (fp32: 2^-22 is lost).
- *   more: the values are read back a layer at a time (at least) into the workspace, where
- *     the kernels of commitkv_window_attention take them, with its precision.
- *   other alignments: CUDA cores in fp32.
- * The same call gives the same bits every time.
+ * Which kernels run, by the rows g W_t of a trajectory.  Scores and sums are fp32.
+ *   up to 16, and more where it takes less time (codes and scales aligned as above,
+ *     queries 16-byte aligned): tensor cores, 8 or 16 rows at a time.  Queries and
+ *     weights enter the products as fp16 terms relative to their row's largest: one
+ *     (bf16: a query is kept whole, 2^-12 of a weight is lost) or two (fp32: 2^-22 is
+ *     lost); below 2^-36 of a row's largest weight all of it is.
+ *   more rows: tensor cores, up to 256 rows at a time; weights rounded to bf16 as in
+ *     commitkv_window_attention.  Or, where that takes less time, for fp32 and for
+ *     other alignments, the values of a layer at a time are read back into the
+ *     workspace, where the kernels of commitkv_window_attention take them, with its
+ *     precision.
+ *   up to 16 rows of other alignments: CUDA cores in fp32.
+ * So what more than 16 rows are rounded by depends on the other trajectories of the
+ * call.  The same call gives the same bits every time.
  * -------------------------------------------------------------------- */
 commitkv_status commitkv_packed_attention(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs,
                                           const uint8_t *layer_mask, int32_t window, int32_t sinks, void *const *out,
@@ -664,10 +673,9 @@ commitkv_status commitkv_packed_compact(const commitkv_shape *shape, int32_t n_t
 
 /* Size in bytes of the workspace of commitkv_packed_attention and
  * commitkv_packed_compact for these trajectories, for fewer of them, smaller
- * caches or fewer queries.  Where a trajectory has more than 16 rows g W_t (or
- * codes or scales are not aligned as above: no difference) it has room for the
- * values of one layer of all such trajectories.  Returns 0 for invalid
- * arguments. */
+ * caches or fewer queries: it grows with S.  It has room for the full-width values
+ * of one layer of all trajectories with more than 16 rows g W_t, whichever kernels
+ * take them.  Returns 0 for invalid arguments (positions are wanted where S > 0). */
 size_t commitkv_packed_workspace_size(const commitkv_shape *shape, int32_t n_traj, const commitkv_packed *trajs);
 
 #ifdef __cplusplus
