@@ -169,7 +169,7 @@ struct Launch {
 };
 static_assert(sizeof(Launch) <= 32764, "kernel parameters");
 
-// CUDA cores: any alignment.  Rows per item: 16 or 64.
+// CUDA cores: any alignment; 16 rows per item.
 cudaError_t launch_simt(const Launch &P, cudaStream_t s, bool early);
 // Wide caches, queries 16-byte aligned; 8 rows per item, or 16 (bf16).
 cudaError_t launch_rows(const Launch &P, cudaStream_t s, bool early);

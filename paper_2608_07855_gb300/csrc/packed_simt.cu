@@ -2,8 +2,8 @@
 //
 // One block of 256 threads per item; tiles of 64 tokens, whose values are
 // written to shared memory as fp32 (exactly, from codes and scale).  Thread
-// (ty, tx) of a 16 x 16 grid owns TM rows: their scores against four tokens (tx
-// + 16 j) of a tile, then D / 16 channels of their sums, so a row's running max
+// (ty, tx) of a 16 x 16 grid has row ty: its scores against four tokens (tx
+// + 16 j) of a tile, then D / 16 channels of its sums, so a row's running max
 // and sum live in registers of the 16 lanes that share it.  Bound by fp32 FMAs
 // and the shared-memory reads that feed them; the kernel for what the others
 // cannot read.
@@ -29,10 +29,10 @@ using sm103::ffma2;
 
 constexpr int TT = 64;   // tokens per tile
 constexpr int NT = 256;  // threads
+constexpr int BM = 16;   // rows of an item
 
-template <int D, int TM>
+template <int D>
 struct Smem {
-  static constexpr int BM = 16 * TM;
   static constexpr int KP = D + 4;  // rows 16 bytes apart in the banks
   float q[BM][KP];
   union {  // the weights take the place of the keys
@@ -48,11 +48,11 @@ struct Smem {
   int u_lo, u_hi, u_se;
 };
 
-template <typename T, int D, int TM>
+template <typename T, int D>
 __global__ void __launch_bounds__(NT, 2) attend_packed_simt(const __grid_constant__ Launch P) {
-  constexpr int BM = 16 * TM, CH = D / 16, GR = D / kGroup;
+  constexpr int CH = D / 16, GR = D / kGroup;
   extern __shared__ __align__(16) uint8_t raw[];
-  Smem<D, TM> &sm = *reinterpret_cast<Smem<D, TM> *>(raw);
+  Smem<D> &sm = *reinterpret_cast<Smem<D> *>(raw);
   const at::Launch &L = P.L;
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
   at::pdl_start_next();
@@ -90,18 +90,11 @@ __global__ void __launch_bounds__(NT, 2) attend_packed_simt(const __grid_constan
   const int64_t base = it.l * sg.sl + it.kvh * sg.sh, sbase = it.l * sc.gl + it.kvh * sc.gh;
   const uint8_t *kb = static_cast<const uint8_t *>(sg.k) + base, *vb = static_cast<const uint8_t *>(sg.v) + base;
   const uint8_t *ksb = sc.k + sbase, *vsb = sc.v + sbase;
-  Span sp[TM];
-  float m[TM], lsum[TM];
-  float2 o[TM][CH / 2];
+  const Span sp = {sm.lo[ty], sm.hi[ty], sm.se[ty]};
+  float m = -INFINITY, lsum = 0.0f;
+  float2 o[CH / 2];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int r = ty * TM + i;
-    sp[i] = {sm.lo[r], sm.hi[r], sm.se[r]};
-    m[i] = -INFINITY;
-    lsum[i] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < CH / 2; ++c) o[i][c] = make_float2(0.0f, 0.0f);
-  }
+  for (int c = 0; c < CH / 2; ++c) o[c] = make_float2(0.0f, 0.0f);
   for (int j = j0; j < j1; ++j) {
     const int a = at::tile_start(tl, j, TT), n = at::tile_end(tl, j, TT) - a;
     __syncthreads();
@@ -141,91 +134,69 @@ __global__ void __launch_bounds__(NT, 2) attend_packed_simt(const __grid_constan
         if (i < n && sm.nan[i] && at::sees(s1, a + i)) atomicOr(&sm.row_nan[r], (unsigned)sm.nan[i]);
       }
     }
-    float2 s2[TM][4];
+    float2 s2[4];
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s2[i][c] = make_float2(0.0f, 0.0f);
+    for (int t = 0; t < 4; ++t) s2[t] = make_float2(0.0f, 0.0f);
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
-      float4 q4[TM], k4[4];
+      const float4 q4 = *reinterpret_cast<const float4 *>(&sm.q[ty][c]);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) q4[i] = *reinterpret_cast<const float4 *>(&sm.q[ty * TM + i][c]);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) k4[t] = *reinterpret_cast<const float4 *>(&sm.k[tx + 16 * t][c]);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          s2[i][t] = ffma2(make_float2(q4[i].x, q4[i].y), make_float2(k4[t].x, k4[t].y), s2[i][t]);
-          s2[i][t] = ffma2(make_float2(q4[i].z, q4[i].w), make_float2(k4[t].z, k4[t].w), s2[i][t]);
-        }
+      for (int t = 0; t < 4; ++t) {
+        const float4 k4 = *reinterpret_cast<const float4 *>(&sm.k[tx + 16 * t][c]);
+        s2[t] = ffma2(make_float2(q4.x, q4.y), make_float2(k4.x, k4.y), s2[t]);
+        s2[t] = ffma2(make_float2(q4.z, q4.w), make_float2(k4.z, k4.w), s2[t]);
+      }
     }
     __syncthreads();  // the keys have been read
+    float s[4], mx = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      float s[4], mx = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int tok = tx + 16 * t;
-        s[t] = tok < n && at::sees(sp[i], a + tok) ? __fmul_rn(s2[i][t].x + s2[i][t].y, L.scale_log2) : -INFINITY;
-        mx = fmaxf(mx, s[t]);
-      }
-#pragma unroll
-      for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-      const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.0f : mn;
-      const float f = exp2f(m[i] - ref);
-      float ps = 0.0f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float p = exp2f(s[t] - ref);
-        ps += p;
-        sm.p[ty * TM + i][tx + 16 * t] = p;
-      }
-#pragma unroll
-      for (int w = 8; w > 0; w >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, w);
-      lsum[i] = fmaf(lsum[i], f, ps);
-      m[i] = mn;
-#pragma unroll
-      for (int c = 0; c < CH / 2; ++c) o[i][c].x *= f, o[i][c].y *= f;
+    for (int t = 0; t < 4; ++t) {
+      const int tok = tx + 16 * t;
+      s[t] = tok < n && at::sees(sp, a + tok) ? __fmul_rn(s2[t].x + s2[t].y, L.scale_log2) : -INFINITY;
+      mx = fmaxf(mx, s[t]);
     }
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.0f : mn;
+    const float f = exp2f(m - ref);
+    float ps = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const float p = exp2f(s[t] - ref);
+      ps += p;
+      sm.p[ty][tx + 16 * t] = p;
+    }
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, w);
+    lsum = fmaf(lsum, f, ps);
+    m = mn;
+#pragma unroll
+    for (int c = 0; c < CH / 2; ++c) o[c].x *= f, o[c].y *= f;
     __syncwarp();  // a row's weights are written and read by the same half warp
 #pragma unroll 2
     for (int t = 0; t < TT; t += 4) {
-      float4 p4[TM];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) p4[i] = *reinterpret_cast<const float4 *>(&sm.p[ty * TM + i][t]);
+      const float4 p4 = *reinterpret_cast<const float4 *>(&sm.p[ty][t]);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        float2 v2[CH / 2];
+        const float p = u == 0 ? p4.x : u == 1 ? p4.y : u == 2 ? p4.z : p4.w;
 #pragma unroll
         for (int c = 0; c < CH / 4; ++c) {
           const float4 x = *reinterpret_cast<const float4 *>(&sm.v[t + u][64 * c + 4 * tx]);
-          v2[2 * c] = make_float2(x.x, x.y);
-          v2[2 * c + 1] = make_float2(x.z, x.w);
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const float p = u == 0 ? p4[i].x : u == 1 ? p4[i].y : u == 2 ? p4[i].z : p4[i].w;
-#pragma unroll
-          for (int c = 0; c < CH / 2; ++c) o[i][c] = ffma2(make_float2(p, p), v2[c], o[i][c]);
+          o[2 * c] = ffma2(make_float2(p, p), make_float2(x.x, x.y), o[2 * c]);
+          o[2 * c + 1] = ffma2(make_float2(p, p), make_float2(x.z, x.w), o[2 * c + 1]);
         }
       }
     }
   }
   // the rows' sums through shared memory, then a warp per row
   __syncthreads();
-  float(*so)[Smem<D, TM>::KP] = sm.q;
+  float(*so)[Smem<D>::KP] = sm.q;
   float *sml = &sm.p[0][0];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int r = ty * TM + i;
-#pragma unroll
-    for (int c = 0; c < CH / 4; ++c)
-      *reinterpret_cast<float4 *>(&so[r][64 * c + 4 * tx]) =
-          make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y);
-    if (tx == 0) sml[2 * r] = m[i], sml[2 * r + 1] = lsum[i];
-  }
+  for (int c = 0; c < CH / 4; ++c)
+    *reinterpret_cast<float4 *>(&so[ty][64 * c + 4 * tx]) =
+        make_float4(o[2 * c].x, o[2 * c].y, o[2 * c + 1].x, o[2 * c + 1].y);
+  if (tx == 0) sml[2 * ty] = m, sml[2 * ty + 1] = lsum;
   __syncthreads();
   for (int r = tid / 32; r < BM && r0 + r < sg.R; r += NT / 32) {
     float x[D / 32];
@@ -237,18 +208,18 @@ __global__ void __launch_bounds__(NT, 2) attend_packed_simt(const __grid_constan
   at::pdl_chain();
 }
 
-template <typename T, int D, int TM>
+template <typename T, int D>
 cudaError_t launch(const Launch &P, cudaStream_t s, bool early) {
-  const int smem = (int)sizeof(Smem<D, TM>);
+  const int smem = (int)sizeof(Smem<D>);
   const cudaError_t e =
-      cudaFuncSetAttribute(attend_packed_simt<T, D, TM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      cudaFuncSetAttribute(attend_packed_simt<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return at::launch_after(attend_packed_simt<T, D, TM>, P.L.item_off[P.L.n_seg], NT, smem, s, early, P);
+  return at::launch_after(attend_packed_simt<T, D>, P.L.item_off[P.L.n_seg], NT, smem, s, early, P);
 }
 
 template <typename T>
 cudaError_t launch_t(const Launch &P, cudaStream_t s, bool early) {
-  return P.L.d == 128 ? launch<T, 128, 1>(P, s, early) : launch<T, 64, 1>(P, s, early);
+  return P.L.d == 128 ? launch<T, 128>(P, s, early) : launch<T, 64>(P, s, early);
 }
 
 }  // namespace
