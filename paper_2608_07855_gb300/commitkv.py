@@ -527,9 +527,9 @@ def commitkv_compact_noalloc(shape: Shape, cache, retired, pending, pending_prio
 
 
 def _packed_width(shape: Shape, t: PackedTensors):
-    M, H, d = shape.layers, shape.kv_heads, shape.head_dim
-    if tuple(t.k.shape[:2]) != (M, H) or 2 * t.k.shape[3] != d:
-        raise ValueError(f"codes must be [{M}][{H}][S][{d // 2}] of the shape")
+    M, H, _, w = t.k.shape
+    if M != shape.layers or H != shape.kv_heads or 2 * w != shape.head_dim:
+        raise ValueError(f"codes must be [{shape.layers}][{shape.kv_heads}][S][{shape.head_dim // 2}] of the shape")
 
 
 class AttentionBatch:
@@ -772,50 +772,51 @@ def commitkv_packed_compact(shape: Shape, cache, retired, pending, pending_prior
     place, as commitkv_compact_in_place."""
     torch = _torch()
     n = len(cache)
-    every = list(cache) if dst is None else list(cache) + list(dst)
     if dst is not None and len(dst) != n:
         raise ValueError("one destination per cache")
-    for c in every:
+    if workspace is None:
+        raise ValueError("a workspace is needed")
+    for xs, what in ((retired, "retired"), (pending, "pending"), (pending_priority, "pending_priority"),
+                     (fill_score, "fill_score"), (idx_out, "idx_out")):
+        if len(xs) != n:
+            raise ValueError(f"{what}: one for each cache")
+    device = workspace.get_device()
+    for c in (cache if dst is None else [*cache, *dst]):
         if not isinstance(c, PackedTensors):
             raise ValueError("caches must be PackedTensors")
         _packed_width(shape, c)
-    if workspace is None:
-        raise ValueError("a workspace is needed")
-    d, to = _descs(cache), None if dst is None else _descs(dst)
-    devices = {c.device() for c in every}
-    devices.add(workspace.get_device())
-    pointers = []
-    for xs, dt, what in ((retired, torch.uint8, "retired"), (pending, torch.int32, "pending"),
-                         (pending_priority, torch.float32, "pending_priority"), (fill_score, torch.float32, "fill_score"),
-                         (idx_out, torch.int32, "idx_out"), ((n_idx_out,), torch.int32, "n_idx_out")):
-        got = []
-        if len(xs) != (1 if what == "n_idx_out" else n):
-            raise ValueError(f"{what}: one for each cache")
-        for x in xs:
-            if x is None:
-                got.append((0, None))
-                continue
-            if x.dtype != dt or not x.is_contiguous():
-                raise ValueError(f"{what} must be contiguous {dt}")
-            devices.add(x.get_device())
-            m = x.numel()
-            got.append((m, x.data_ptr() if m else None))
-        pointers.append(got)
-    for i in range(n):
-        S, P = d[i].S, d[i].P
-        marks, some, prio, fill, idx = (p[i] for p in pointers[:5])
-        if fill[0] < S or idx[0] < budget_B or marks[0] < P or (some[0] and prio[0] < P):
-            raise ValueError("scores for every token, marks and priorities for every page, budget_B indices")
-    if pointers[5][0][0] < n:
-        raise ValueError("n_idx_out has an entry per cache")
-    if len(devices) != 1 or min(devices) < 0:
-        raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
-    device = devices.pop()
+        if c.device() != device:
+            raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
+    descs, to = _descs(cache), None if dst is None else _descs(dst)
+
+    def pointer(x, dt, least, what):
+        m = 0 if x is None else x.numel()
+        if m < least:
+            raise ValueError("scores for every token, marks and priorities for every page, budget_B indices, a count per cache")
+        if x is None:
+            return None
+        if x.dtype is not dt or not x.is_contiguous():
+            raise ValueError(f"{what} must be contiguous {dt}")
+        if x.get_device() != device:
+            raise ValueError("CommitKV tensors must live on one GPU (no CPU fallback)")
+        return x.data_ptr() if m else None
+
+    u8, i32, f32 = torch.uint8, torch.int32, torch.float32
+    array = ctypes.c_void_p * n
+    marks, some, prio, fill, idx = array(), array(), array(), array(), array()
+    npend = (ctypes.c_int32 * n)()
+    for i, (c, x) in enumerate(zip(descs, pending)):
+        P, m = c.P, 0 if x is None else x.numel()
+        npend[i] = m
+        marks[i] = pointer(retired[i], u8, P, "retired")
+        some[i] = pointer(x, i32, 0, "pending")
+        prio[i] = pointer(pending_priority[i], f32, P if m else 0, "pending_priority")
+        fill[i] = pointer(fill_score[i], f32, c.S, "fill_score")
+        idx[i] = pointer(idx_out[i], i32, budget_B, "idx_out")
+    counts = pointer(n_idx_out, i32, n, "n_idx_out")
     _on_current(device)
-    arrays = [(ctypes.c_void_p * n)(*[q for _, q in p]) for p in pointers[:5]]
-    npend = (ctypes.c_int32 * n)(*[m for m, _ in pointers[1]])
     rc = (_lib or load_library()).commitkv_packed_compact(
-        ctypes.byref(shape), n, d, arrays[0], arrays[1], ctypes.byref(npend), arrays[2], arrays[3], int(budget_B),
-        int(pending_tokens_BN), int(pending_cap_pages), arrays[4], pointers[5][0][1], to, workspace.data_ptr(),
-        workspace.numel(), _stream(_current_stream(device) if stream is None else stream))
+        ctypes.byref(shape), n, descs, marks, some, ctypes.byref(npend), prio, fill, int(budget_B), int(pending_tokens_BN),
+        int(pending_cap_pages), idx, counts, to, workspace.data_ptr(), workspace.numel(),
+        _stream(_current_stream(device) if stream is None else stream))
     _check(rc, "commitkv_packed_compact")

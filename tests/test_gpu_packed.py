@@ -637,6 +637,31 @@ def test_checkpoint_device_errors(place):
 
 
 # ------------------------------------------------------------------------------------------------ together
+def test_checkpoint_refusals():
+    shape = ck.make_shape(2, 2, 4, 64, F32)
+    c = ck.alloc_packed_cache(shape, 100)
+    page = torch.tensor([0, 16], dtype=torch.int32, device="cuda")
+    t = dataclasses.replace(c, page_start=page, page_len=torch.full_like(page, 16))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    good = dict(cache=[t], retired=[torch.zeros(2, dtype=torch.uint8, device="cuda")], pending=[torch.ones(1, **i32)],
+                pending_priority=[torch.zeros(2, device="cuda")], fill_score=[torch.zeros(100, device="cuda")], budget_B=10,
+                pending_tokens_BN=0, pending_cap_pages=0, idx_out=[torch.empty(10, **i32)], n_idx_out=torch.empty(1, **i32),
+                workspace=ck.alloc_packed_workspace(shape, [t]))
+    ck.commitkv_packed_compact(shape, **good)
+    bad = [dict(workspace=None), dict(workspace=good["workspace"].cpu()), dict(dst=[]), dict(cache=[]), dict(retired=[]),
+           dict(pending=[]), dict(pending_priority=[]), dict(fill_score=[]), dict(idx_out=[]), dict(cache=[object()]),
+           dict(retired=[None]), dict(retired=[good["retired"][0][:1]]), dict(retired=[good["retired"][0].int()]),
+           dict(pending=[good["pending"][0].long()]), dict(pending_priority=[None]), dict(pending_priority=[good["fill_score"][0][:1]]),
+           dict(fill_score=[None]), dict(fill_score=[torch.zeros(99, device="cuda")]), dict(fill_score=[torch.zeros(200, device="cuda")[::2]]),
+           dict(idx_out=[torch.empty(9, **i32)]), dict(n_idx_out=torch.empty(0, **i32)), dict(n_idx_out=torch.empty(1)),
+           dict(fill_score=[torch.zeros(100)]), dict(dst=[ck.alloc_packed_cache(ck.make_shape(1, 2, 4, 64, F32), 100)])]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            ck.commitkv_packed_compact(shape, **{**good, **kw})
+    with pytest.raises(ck.CommitKVError):  # no room
+        ck.commitkv_packed_compact(shape, **good, dst=[ck.alloc_packed_cache(shape, 9)])
+
+
 @pytest.mark.parametrize("dtype", [F32, BF], ids=["f32", "bf16"])
 def test_write_attend_compact_attend(dtype, kernels):
     """A prompt written and attended to, a checkpoint in place, decoded tokens after it: against a cache of the values
