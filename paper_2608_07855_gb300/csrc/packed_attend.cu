@@ -139,6 +139,9 @@ Many many_path(const commitkv_shape *s, int n, const commitkv_packed *x, void *c
   return can_tile && tiles <= back ? kManyTiles : kManyBack;
 }
 
+// Times of items, by which work is divided: those of the CUDA cores and of the row
+// tiles from calls of one path (1,507 us and 306 for the cases at their kernels), of 8
+// and 16 rows a tile of a block with the SM's others at work.
 enum { kSimt16, kRows8, kRows16, kTc, kPaths };
 constexpr at::PathInfo kPath[kPaths] = {
     {16, 64, 2, 1.0, 11.5}, {8, 128, 3, 2.0, 1.7}, {16, 128, 2, 2.0, 1.9}, {256, 128, 1, 2.0, 1.7}};

@@ -28,6 +28,11 @@
 // the largest score so far, raised when a score is 4 above that: at most 2^15,
 // in one fp16 term for bf16 (2^-12 of a weight is lost: the output's own rounding is
 // 2^-9) and two for fp32; what is below 2^-36 of the row's largest is cut.
+//
+// bf16, 32 query on 8 KV heads of 128 channels: 131,071 tokens 39 us (3.7 TB/s with start
+// and merge, 8), 64 caches of up to 8,192 tokens 73 (3.9 TB/s).  665 instructions to a
+// warp's tile, 60 % of the issue slots: with scale bytes by shuffles and a multiply before
+// every weight 77.6, with four blocks an SM and 128 registers 75.5.
 #include <string.h>
 
 #include <type_traits>
