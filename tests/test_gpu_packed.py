@@ -1,6 +1,7 @@
 """Packed caches against their definition in 64 bits: writing and reading rows,
 attention over them, checkpoints, and all of them together."""
 import dataclasses
+import threading
 
 import numpy as np
 import pytest
@@ -700,3 +701,115 @@ def test_write_attend_compact_attend(dtype, kernels):
             kept = [torch.empty(M, H, B, d, dtype=dtype, device="cuda") for _ in range(2)]
             ck.commitkv_packed_read(shape, [cache], [kept[0]], [kept[1]], [0])
             assert all(torch.equal(x, y[:, :, idx.long()]) for x, y in zip(kept, (k, v)))
+
+
+def far_cache(n, d, seed):
+    """Tokens more than 2^31 bytes apart, codes and scale bytes, of one layer and head."""
+    far = (1 << 31) + 4096
+    base = torch.zeros((n - 1) * far + 256, dtype=torch.uint8, device="cuda")
+    c = Cache(1, 1, n, d, seed=seed)
+    c.dev = {}
+    for name, at in zip(NAMES, (0, 64, 128, 160)):
+        c.dev[name] = base[at:].as_strided((1, 1, n, c.host[name].shape[3]), (0, 0, far, 1))
+        c.dev[name].copy_(torch.from_numpy(c.host[name]))
+    return c
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+def test_attention_beyond_32_bits(dtype, d, kernels):
+    n = 5
+    c = far_cache(n, d, 3)
+    shape = ck.make_shape(1, 1, 4, d, dtype)
+    pos = np.arange(n)
+    for W in (1, 4, 40):
+        q, p = torch.randn(1, 4, W, d, device="cuda").to(dtype), [n] * W
+        tr = ck.PackedTensors(**c.dev, pos=i32(pos), q=q, q_pos=i32(p))
+        out, lse = torch.empty_like(q), torch.empty(1, 4, W, device="cuda")
+        ck.commitkv_packed_attention(shape, [tr], [out], [lse], workspace=ck.alloc_packed_workspace(shape, [tr]))
+        few = 4 * W <= 16
+        w, e = (2.0 ** -12 if few else 2.0 ** -8, 0.0) if dtype == BF else (2.0 ** -21, 2.0 ** -21)
+        o, l, to, tl = ref.attention(*c.values(), pos, q.cpu(), p, 0, 0, 0.0, w, e)
+        check(out, o, to)
+        check(lse, l, tl)
+
+
+@pytest.mark.parametrize("place", ["dst", "in place"])
+def test_checkpoint_beyond_32_bits(place):
+    n, B = 5, 3
+    c = far_cache(n, 64, 4)
+    shape = ck.make_shape(1, 1, 1, 64, BF)
+    none = torch.zeros(0, dtype=torch.uint8, device="cuda")
+    t = ck.PackedTensors(**c.dev, pos=i32(10 + np.arange(n)))
+    idx, m = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    to = far_cache(B, 64, 5) if place == "dst" else c
+    dst = [ck.PackedTensors(**to.dev, pos=i32(np.zeros(B)))] if place == "dst" else None
+    ck.commitkv_packed_compact(shape, [t], [none], [None], [None], [torch.tensor([1.0, 5, 2, 4, 3], device="cuda")], B, 0, 0,
+                               [idx], m, dst=dst, workspace=ck.alloc_packed_workspace(shape, [t]))
+    keep = idx.cpu().numpy()
+    assert int(m) == B and sorted(keep) == list(keep) and len(set(keep)) == B
+    now = to.now()
+    assert all(np.array_equal(now[name][:, :, :B], c.host[name][:, :, keep]) for name in NAMES)
+    assert np.array_equal((dst or [t])[0].pos[:B].cpu().numpy(), 10 + keep)
+
+
+def test_two_threads(kernels):
+    """Calls of two host threads at once, each with a stream and a workspace of its own."""
+    a = Problem(dtype=BF, d=128, M=2, H=2, Hq=8, gaps=0.7, trajs=[(900, 1), (2000, 4), (500, 40)]).upload()
+    b = Problem(dtype=F32, d=64, M=3, H=1, Hq=4, gaps=0.7, trajs=[(700, 60), (900, 2)], seed=3).upload()
+    want = []
+    for p in (a, b):
+        p.call(300, 4)
+        p.check(300, 4)
+        want.append((p.flat.clone(), p.flat_l.clone()))
+        p.flat.fill_(p.SENT), p.flat_l.fill_(p.SENT)
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(p, want):
+        try:
+            s = torch.cuda.Stream()
+            for _ in range(50):
+                p.call(300, 4, stream=s)
+            s.synchronize()
+            assert torch.equal(p.flat, want[0]) and torch.equal(p.flat_l, want[1])
+        except BaseException as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=x) for x in zip((a, b), want)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    assert not failed
+
+
+def test_captured_checkpoint():
+    """Append, checkpoint and read back as one graph, replayed over new rows and scores."""
+    M, H, S, d, B = 2, 2, 300, 64, 50
+    shape = ck.make_shape(M, H, H, d, BF)
+    t, dst = ck.alloc_packed_cache(shape, S), ck.alloc_packed_cache(shape, B)
+    t.pos.copy_(i32(np.arange(S)))
+    k, v = (torch.randn(M, H, S, d, device="cuda").to(BF) for _ in range(2))
+    got = [torch.zeros(M, H, B, d, dtype=BF, device="cuda") for _ in range(2)]
+    none = torch.zeros(0, dtype=torch.uint8, device="cuda")
+    fill = torch.rand(S, device="cuda")
+    idx, m = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = ck.alloc_packed_workspace(shape, [t])
+    write, read = ck.packed_rows(shape, [t], [k], [v], [0]), ck.packed_rows(shape, [dst], [got[0]], [got[1]], [0])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ck.commitkv_packed_write(shape, write)
+        ck.commitkv_packed_compact(shape, [t], [none], [None], [None], [fill], B, 0, 0, [idx], m, dst=[dst], workspace=ws)
+        ck.commitkv_packed_read(shape, read)
+    for seed in range(3):
+        r = torch.Generator(device="cuda").manual_seed(seed)
+        fill.copy_(torch.randperm(S, generator=r, device="cuda").float())
+        k.copy_(torch.randn(M, H, S, d, generator=r, device="cuda"))
+        v.copy_(torch.randn(M, H, S, d, generator=r, device="cuda"))
+        g.replay()
+        torch.cuda.synchronize()
+        keep = fill.topk(B).indices.sort().values
+        assert int(m) == B and torch.equal(idx, keep.int()) and torch.equal(dst.pos, keep.int())
+        for x, y in zip((k, v), got):
+            want = ref.values(*ref.pack(ref.numbers(x[:, :, keep].contiguous())))
+            assert np.array_equal(ref.numbers(y), want)
