@@ -317,7 +317,9 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : 3) attend_packed_rows(c
         uint32_t h, l;
         split2(f[x][i], f[x][i + 4], h, l);
         q[n][2 * x + i / 2][i % 2] = h;
-        if constexpr (F32) ql[n][2 * x + i / 2][i % 2] = l;
+        // an infinite number is its first term: with the rest, inf - inf, scores of -inf would be NaN
+        if constexpr (F32)
+          ql[n][2 * x + i / 2][i % 2] = (isinf(f[x][i]) ? 0u : l & 0xffffu) | (isinf(f[x][i + 4]) ? 0u : l & 0xffff0000u);
       }
     }
     // 16 / 2^k, and the softmax scale (which no score overflows by but that of a scale of 2^13 and more)
