@@ -125,18 +125,21 @@ class Session:
         return ck.PackedTensors(c.k[at, :, :S], c.v[at, :, :S], c.k_scale[at, :, :S], c.v_scale[at, :, :S], self.pos[:S],
                                 **more)
 
-    def _put(self, K, V, first, layer=None):
-        """K and V of tokens first .. of one layer ([1][H][n][d]) or all ([M][H][n][d])."""
-        n = K.shape[2]
+    def _put(self, K, V, first, n, layer=None):
+        """K and V of tokens first .. first + n - 1 of one layer ([1][H][n][d]) or all ([M][H][n][d])."""
+        s = self.shape
         if self.packed is None:
             at = slice(None) if layer is None else slice(layer, layer + 1)
             self.K[at, :, first:first + n].copy_(K)
             self.V[at, :, first:first + n].copy_(V)
             return
+        want = (s.layers if layer is None else 1, s.kv_heads, n, s.head_dim)
+        if tuple(K.shape) != want or tuple(V.shape) != want:
+            raise ValueError(f"K and V must be [M][H][n][d] = {want}")
         K, V = (x.to(device=self.dev, dtype=self.dt) for x in (K, V))
         if K.stride() != V.stride() or K.stride(3) != 1:
             K, V = K.contiguous(), V.contiguous()
-        c, s = self.packed, self.shape
+        c = self.packed
         if layer is not None:
             one = slice(layer, layer + 1)
             c = ck.PackedTensors(c.k[one], c.v[one], c.k_scale[one], c.v_scale[one])
@@ -256,7 +259,7 @@ class Session:
             raise ValueError("session capacity exceeded")
         S0, p0 = self.S, int(pos[0]) if n else 0
         if K is not None:
-            self._put(K, V, S0)
+            self._put(K, V, S0, n)
         self.tail = (S0, S0 + n)
         self.unfilled = set(range(self.shape.layers)) if K is None and n else set()
         self.pos[S0:S0 + n].copy_(pos)
@@ -277,7 +280,7 @@ class Session:
         want = (self.shape.kv_heads, b - a, self.shape.head_dim)
         if tuple(K.shape) != want or tuple(V.shape) != want:
             raise ValueError(f"K and V must be [H][n][d] = {want}")
-        self._put(K[None], V[None], a, layer)
+        self._put(K[None], V[None], a, b - a, layer)
         self.unfilled.discard(layer)
 
     def attend(self, Q, qpos, window: int = 0, sinks: int = 0, prefix: ck.TrajTensors = None, layer: int = None):
