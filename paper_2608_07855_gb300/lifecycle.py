@@ -253,8 +253,7 @@ class Session:
         self._filled()
         if (K is None) != (V is None):
             raise ValueError("K and V together, or neither")
-        self.decoded_since += int(decoded)
-        n = int(pos.shape[0])
+        n, decoded = int(pos.shape[0]), int(decoded)
         if self.S + n > self.cap:
             raise ValueError("session capacity exceeded")
         S0, p0 = self.S, int(pos[0]) if n else 0
@@ -264,6 +263,7 @@ class Session:
         self.unfilled = set(range(self.shape.layers)) if K is None and n else set()
         self.pos[S0:S0 + n].copy_(pos)
         self.S += n
+        self.decoded_since += decoded
         for kind, b, m in events:
             if kind not in ("call", "obs"):
                 continue

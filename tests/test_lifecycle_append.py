@@ -42,3 +42,17 @@ def test_as_many_rows_as_positions():
     s.append(rows(3), rows(3), positions(s, 3), [])
     s.append(rows(1), rows(1), positions(s, 1), [])
     assert s.S == 4 and s.K[0, 0, :5, 0].tolist() == [3, 3, 3, 1, 0]
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_a_refused_append_leaves_the_session_as_it_was(packed):
+    """What it decoded does not count towards the checkpoint cadence either: the caller appends it again."""
+    s = session(packed)
+    p = torch.arange(3, dtype=torch.int32)
+    for K, V, pos in ((rows(2), rows(2), p), (rows(3), rows(2), p), (rows(3), None, p),
+                      (rows(21), rows(21), torch.arange(21, dtype=torch.int32))):
+        with pytest.raises((ValueError, RuntimeError)):
+            s.append(K, V, pos, [("obs", 0, 3)], decoded=3)
+    assert (s.S, s.decoded_since, s.pages, s.tail, s.unfilled) == (0, 0, [], (0, 0), set())
+    s.append(None, None, p, [("obs", 0, 3)], decoded=3)
+    assert s.S == 3 and s.decoded_since == 3 and s.unfilled == {0, 1}
