@@ -247,6 +247,16 @@ def _one_gpu(*tensors) -> int:
     return devices.pop()
 
 
+def _strides(x):
+    """The strides of layers, heads and rows of x [M][H][n][w].  A dimension of one entry may have any
+    (torch keeps what a view leaves there, contiguous() too), so it gets that of rows side by side."""
+    M, H, n, w = x.shape
+    if 0 in (M, H, n):
+        return 0, 0, w
+    layer, head, row, _ = x.stride()
+    return layer if M > 1 else 0, head if H > 1 else 0, row if n > 1 else w
+
+
 def _on_current(device: int):
     if _torch().cuda.current_device() != device:
         raise ValueError("the tensors must be on the current GPU")
@@ -291,16 +301,14 @@ class PackedTensors:
         k, v, ks, vs, q, ps = self.k, self.v, self.k_scale, self.v_scale, self.q, self.page_start
         ints = (self.pos, self.q_pos, ps, self.page_len)
         _require_cuda(k, v, ks, vs, q, *ints)
-        shape, strides, gstrides = k.shape, k.stride(), ks.stride()
         for x in (k, v, ks, vs):
             if x.dtype != torch.uint8 or x.dim() != 4 or (x.numel() and x.stride(3) != 1):
                 raise ValueError("codes and scales must be 4-D uint8, the bytes of a row contiguous")
+        shape, strides, gstrides = k.shape, _strides(k), _strides(ks)
         if v.shape != shape or vs.shape != ks.shape or ks.shape[:3] != shape[:3] or 16 * ks.shape[3] != shape[3] or \
-                (k.numel() and (v.stride() != strides or vs.stride() != gstrides)):
+                _strides(v) != strides or _strides(vs) != gstrides:
             raise ValueError("codes must be [M][H][S][d / 2], scales [M][H][S][d / 32], of K and V alike")
         n = shape[2]
-        if n == 0:  # strides mean nothing
-            strides, gstrides = (0, 0, shape[3]), (0, 0, ks.shape[3])
         for x in ints:
             if x is not None and (x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous()):
                 raise ValueError("positions and pages must be contiguous int32")
@@ -715,10 +723,9 @@ class PackedRows:
         for i, (c, x, y) in enumerate(zip(caches, k, v)):
             _packed_width(shape, c)
             if x.dim() != 4 or tuple(x.shape) != (M, H, x.shape[2], d) or y.shape != x.shape or x.dtype != dt or \
-                    y.dtype != dt or (x.numel() and (x.stride() != y.stride() or x.stride(3) != 1)):
+                    y.dtype != dt or (x.numel() and (_strides(x) != _strides(y) or x.stride(3) != 1 or y.stride(3) != 1)):
                 raise ValueError(f"rows must be [{M}][{H}][n][{d}] of {dt} with contiguous channels, K and V alike")
-            sl, sh, st = x.stride()[:3]
-            self.rows[i] = Rows(_ptr(x), _ptr(y), sl, sh, st, 0, 0)
+            self.rows[i] = Rows(_ptr(x), _ptr(y), *_strides(x), 0, 0)
         # once, and not in every call
         self.device = _one_gpu(*[t for c in caches for t in (c.k, c.v, c.k_scale, c.v_scale)], *k, *v)
         _on_current(self.device)

@@ -137,7 +137,7 @@ class Session:
         if tuple(K.shape) != want or tuple(V.shape) != want:
             raise ValueError(f"K and V must be [M][H][n][d] = {want}")
         K, V = (x.to(device=self.dev, dtype=self.dt) for x in (K, V))
-        if K.stride() != V.stride() or K.stride(3) != 1:
+        if ck._strides(K) != ck._strides(V) or K.stride(3) != 1 or V.stride(3) != 1:
             K, V = K.contiguous(), V.contiguous()
         c = self.packed
         if layer is not None:

@@ -4,7 +4,12 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_packed import IDS, TYPES, Problem, kernels  # noqa: E402,F401
+from paper_2608_07855_gb300 import commitkv as ck  # noqa: E402
+from paper_2608_07855_gb300.lifecycle import Session  # noqa: E402
+
+import packed_ref as ref  # noqa: E402
+from attention_ref import check  # noqa: E402
+from test_gpu_packed import BF, IDS, TYPES, Problem, i32, kernels  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +42,74 @@ def test_infinite_queries_over_keys_of_one_sign(dtype, d, W, kernels):  # noqa: 
     assert np.isnan(out[3]).all() and np.isnan(lse[3]).all()
     assert np.isfinite(out[1, :W - 1]).all() and np.isfinite(lse[1, :W - 1]).all()
     p.guards()
+
+
+# ------------------------------------------------------------------------------------------------ single tokens
+def by_tokens(x):
+    return x.transpose(1, 2).contiguous().transpose(1, 2)
+
+
+def odd(x):
+    """x with strides of single entries that mean nothing."""
+    return x.as_strided(x.shape, [s if n > 1 else 7 for n, s in zip(x.shape, x.stride())])
+
+
+def rand(*shape, dtype):
+    return torch.randn(*shape, device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("M,H", [(3, 2), (1, 2), (3, 1), (1, 1)])
+def test_a_sessions_single_token_in_any_layout(dtype, d, M, H):
+    """K made anew by a rotary embedding, V a view of a projection, and the other way round; all layers and one by one."""
+    shape = ck.make_shape(M, H, 2 * H, d, dtype)
+    pos = i32([0])
+    for lay in ((odd, by_tokens), (by_tokens, odd), (lambda x: x, odd), (odd, lambda x: x),
+                (by_tokens, lambda x: torch.cat([x, x, x], 2)[:, :, 1:2])):
+        K, V = (f(rand(M, H, 1, d, dtype=dtype)) for f in lay)
+        s = Session(shape, 16, 40, 0.2, 50, packed=True)
+        s.append(K, V, pos, [], decoded=1)
+        s.append(None, None, pos + 1, [], decoded=1)
+        for layer in range(M):
+            s.fill(layer, K[layer], V[layer])
+        assert s.S == 2 and s.decoded_since == 2
+        for x, codes, scales in ((K, s.packed.k, s.packed.k_scale), (V, s.packed.v, s.packed.v_scale)):
+            want = ref.pack(ref.numbers(x))
+            for i in range(2):
+                assert np.array_equal(codes[:, :, i:i + 1].cpu().numpy(), want[0])
+                assert np.array_equal(scales[:, :, i:i + 1].cpu().numpy(), want[1])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("M,H,S", [(1, 2, 1), (2, 1, 1), (1, 1, 1), (1, 2, 5), (3, 1, 5)])
+def test_strides_of_single_entries_mean_nothing(dtype, d, M, H, S):
+    """Written, read, attended to and compacted, K and V alike but for such strides."""
+    shape = ck.make_shape(M, H, 4 * H, d, dtype)
+    c = ck.alloc_packed_cache(shape, S)
+    pos = i32(np.arange(S))
+    q, p = rand(M, 4 * H, 1, d, dtype=dtype), i32([S])
+    t = ck.PackedTensors(c.k, odd(c.v), odd(c.k_scale), c.v_scale, pos, q, p)
+    K, V = rand(M, H, S, d, dtype=dtype), odd(rand(M, H, S, d, dtype=dtype))
+    ck.commitkv_packed_write(shape, [t], [K], [V], [0])
+    values = []
+    for x, codes, scales in ((K, t.k, t.k_scale), (V, t.v, t.v_scale)):
+        want = ref.pack(ref.numbers(x))
+        assert np.array_equal(codes.cpu().numpy(), want[0]) and np.array_equal(scales.cpu().numpy(), want[1])
+        values.append(ref.values(*want))
+    back = odd(torch.zeros_like(K)), torch.zeros_like(K)
+    ck.commitkv_packed_read(shape, [t], [back[0]], [back[1]], [0])
+    assert all(np.array_equal(ref.numbers(x), w) for x, w in zip(back, values))
+    out, lse = torch.empty_like(q), torch.empty(M, 4 * H, 1, device="cuda")
+    ws = ck.alloc_packed_workspace(shape, [t])
+    ck.commitkv_packed_attention(shape, [t], [out], [lse], workspace=ws)
+    few = dict(weights=2.0 ** -11) if dtype is BF else dict(weights=2.0 ** -21, queries=2.0 ** -21)
+    o, l, to, tl = ref.attention(*values, np.arange(S), q, [S], **few)
+    check(out, o, to)
+    check(lse, l, tl)
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    to_ = ck.alloc_packed_cache(shape, S)
+    dst = ck.PackedTensors(odd(to_.k), to_.v, to_.k_scale, odd(to_.v_scale), to_.pos)
+    idx, n = i32(np.zeros(S)), i32([0])
+    ck.commitkv_packed_compact(shape, [t], [none], [None], [None], [torch.rand(S, device="cuda")], S, 0, 0, [idx], n, [dst],
+                               workspace=ws)
+    assert n.item() == S and all(torch.equal(getattr(dst, a), getattr(t, a)) for a in ("k", "v", "k_scale", "v_scale", "pos"))
