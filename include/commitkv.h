@@ -633,8 +633,10 @@ commitkv_status commitkv_packed_read(const commitkv_shape *shape, int32_t n_traj
  *   up to 16, and more where it takes less time (codes and scales aligned as above,
  *     queries 16-byte aligned): tensor cores, 8 or 16 rows at a time.  Queries and
  *     weights enter the products as fp16 terms relative to their row's largest: one
- *     (bf16: a query is kept whole, 2^-12 of a weight is lost) or two (fp32: 2^-22 is
- *     lost); below 2^-36 of a row's largest weight all of it is.
+ *     (bf16: a query is kept whole, a weight off by 2^-11 of it at most) or two (fp32:
+ *     either off by 2^-22 of it at most).  Small ones are off by more than that of
+ *     them: a weight by up to 2^-36 of its row's largest, a query's element by up to
+ *     2^-39 of its row's largest.
  *   more rows: tensor cores, up to 256 rows at a time; weights rounded to bf16 as in
  *     commitkv_window_attention.  Or, where that takes less time, for fp32 and for
  *     other alignments, the values of a layer at a time are read back into the

@@ -23,11 +23,11 @@
 // tokens, from the two tokens' words after two byte permutations.
 //
 // Queries enter as q 2^k, k of the row such that the largest is near 2^14: a bf16
-// number whole (what is below 2^-38 of the row's largest is cut), an fp32 number
-// as two fp16 terms (2^-22 is lost).  Weights are exp2(s - m) with m 11 below
-// the largest score so far, raised when a score is 4 above that: at most 2^15,
-// in one fp16 term for bf16 (2^-12 of a weight is lost: the output's own rounding is
-// 2^-9) and two for fp32; what is below 2^-36 of the row's largest is cut.
+// number whole, an fp32 number as two fp16 terms (off by 2^-22 of it at most), or by
+// 2^-39 of the row's largest where that is more.  Weights are exp2(s - m) with m 11
+// below the largest score so far, raised when a score is 4 above that: at most 2^15,
+// in one fp16 term for bf16 (off by 2^-11 of it at most, the output's own rounding by
+// 2^-8) and two for fp32 (2^-22), or by 2^-36 of the row's largest where that is more.
 //
 // bf16, 32 query on 8 KV heads of 128 channels: 131,071 tokens 39 us (3.7 TB/s with start
 // and merge, 8), 64 caches of up to 8,192 tokens 73 (3.9 TB/s).  665 instructions to a
@@ -457,12 +457,21 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : 3) attend_packed_rows(c
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t hi2, lo2;
-          constexpr float u = SMALL ? 0.125f : 1.0f;
-          split2(s[n][i][2 * h] * u, s[n][i][2 * h + 1] * u, hi2, lo2);
+          split2(s[n][i][2 * h], s[n][i][2 * h + 1], hi2, lo2);
           p[n][i][h] = transposed(hi2);
           if constexpr (F32) pl[n][i][h] = transposed(lo2);
         }
     }
+    // values of this tile are 8 times the others': the sums meanwhile too (weights of 1 / 8 would end at 2^-33)
+    auto times = [&](float f) {
+#pragma unroll
+      for (int n = 0; n < QT; ++n)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[n][t][x] *= f;
+    };
+    if (SMALL) times(8.0f);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       uint32_t w[4][VW], b[4];
@@ -508,6 +517,7 @@ __global__ void __launch_bounds__(NW * 32, QT == 2 ? 2 : 3) attend_packed_rows(c
         step(4 * u + 3, a3);
       }
     }
+    if (SMALL) times(0.125f);
   };
   // a byte from 1 to 31
   auto small = [](uint32_t x) { return (((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & ~(x | x << 1 | x << 2) & 0x80808080u; };

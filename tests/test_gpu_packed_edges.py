@@ -113,3 +113,35 @@ def test_strides_of_single_entries_mean_nothing(dtype, d, M, H, S):
     ck.commitkv_packed_compact(shape, [t], [none], [None], [None], [torch.rand(S, device="cuda")], S, 0, 0, [idx], n, [dst],
                                workspace=ws)
     assert n.item() == S and all(torch.equal(getattr(dst, a), getattr(t, a)) for a in ("k", "v", "k_scale", "v_scale", "pos"))
+
+
+# ------------------------------------------------------------------------------------------------ weights
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("W,S", [(1, 700), (1, 5000), (4, 700), (40, 700)])
+@pytest.mark.parametrize("scales", ["usual", "small", "nan"])
+def test_weights_far_below_the_largest(dtype, d, W, S, scales, kernels):  # noqa: F811
+    """One of 32 tokens, of values 0, has nearly all of the weight, the others 2^-31.5 or 2^-33.9 of it and positive
+    values: each weight is off by 2^-36 of the largest at most, whatever scales stand beside it (some below 32, or
+    some of values NaN)."""
+    def edit(p):
+        rng = np.random.RandomState(S + d)
+        for c, pos, Q, qp in p.host:
+            c.host["k_scale"][:] = c.host["v_scale"][:] = 168                        # sigma 1
+            c.host["k"][:] = 0x88
+            c.host["k"][..., 0] = 0x80 | rng.choice([1, 2], c.host["k"].shape[:3])  # channel 0: -7, -6
+            c.host["v"][:] = 0xff
+            c.host["k"][:, :, 5::32, 0], c.host["v"][:, :, 5::32] = 0x8f, 0x88      # 7; values 0
+            if scales == "small":
+                c.host["k_scale"][:, :, ::7, 1] = 9
+                c.host["v_scale"][:, :, 5::32] = 1
+            elif scales == "nan":
+                c.host["v_scale"][:, :, ::31, 0] = 0xff
+            Q[:] = 0
+            Q[..., 0] = 1.6796875                                                    # 2^-2.423 a step of the code
+
+    p = Problem(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(S, W)], edit=edit, scale=1.0).upload()
+    p.call(S - 30, 6)
+    p.check(S - 30, 6)
+    assert (p.out[0][..., 32:].float() > 1e-9).all()
+    if scales == "nan":
+        assert torch.isnan(p.out[0][..., :32]).all()
