@@ -30,7 +30,7 @@ struct Rows {
 struct CopyLaunch {
   Rows r[kMaxTraj];
   int32_t off[kMaxTraj + 1];  // first block of a trajectory
-  int32_t n_traj, H, n_layers;
+  int32_t n_traj, H;
   uint8_t layer_ids[kMaxLayers];
 };
 static_assert(sizeof(CopyLaunch) <= 32764, "kernel parameters");
@@ -417,7 +417,6 @@ commitkv_status copy(const commitkv_shape *s, int n, const commitkv_packed *x, c
   memset(&L, 0, sizeof L);
   L.n_traj = n;
   L.H = s->kv_heads;
-  L.n_layers = n_layers;
   memcpy(L.layer_ids, layers, n_layers);
   const int eb = s->dtype == COMMITKV_BF16 ? 2 : 4,
             per = kThreads * (write ? kGroup : 8 * kUnroll) / s->head_dim;  // rows of a block
