@@ -1,4 +1,6 @@
 """Packed caches where single rows, queries and weights are out of the ordinary."""
+import dataclasses
+
 import numpy as np
 import pytest
 
@@ -9,14 +11,21 @@ from paper_2608_07855_gb300.lifecycle import Session  # noqa: E402
 
 import packed_ref as ref  # noqa: E402
 from attention_ref import check  # noqa: E402
-from test_gpu_packed import BF, IDS, TYPES, Problem, i32, kernels  # noqa: E402,F401
+from test_gpu_packed import BF, IDS, NAMES, TYPES, Problem, i32, kernels, run  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 
 
+def rows_and_kernels(*Ws):
+    """W positions of 4 heads to one, on each set of kernels that takes them."""
+    return pytest.mark.parametrize("W,kernels", [(W, how) for W in Ws for how in
+                                                 (("", "cuda_cores") if W <= 4 else ("", "tiles", "full", "cuda_cores"))],
+                                   indirect=["kernels"])
+
+
 # ------------------------------------------------------------------------------------------------ queries
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
-@pytest.mark.parametrize("W", [1, 3, 8, 40])
+@rows_and_kernels(1, 3, 8, 40)
 def test_infinite_queries_over_keys_of_one_sign(dtype, d, W, kernels):  # noqa: F811
     """Scores of -inf alone: such a row is zero with a log-sum-exp of -inf.  The tokens of the other sign, which would
     make it NaN, lie behind its window."""
@@ -117,7 +126,8 @@ def test_strides_of_single_entries_mean_nothing(dtype, d, M, H, S):
 
 # ------------------------------------------------------------------------------------------------ weights
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
-@pytest.mark.parametrize("W,S", [(1, 700), (1, 5000), (4, 700), (40, 700)])
+@rows_and_kernels(1, 4, 40)
+@pytest.mark.parametrize("S", [700, 5000])
 @pytest.mark.parametrize("scales", ["usual", "small", "nan"])
 def test_weights_far_below_the_largest(dtype, d, W, S, scales, kernels):  # noqa: F811
     """One of 32 tokens, of values 0, has nearly all of the weight, the others 2^-31.5 or 2^-33.9 of it and positive
@@ -145,3 +155,53 @@ def test_weights_far_below_the_largest(dtype, d, W, S, scales, kernels):  # noqa
     assert (p.out[0][..., 32:].float() > 1e-9).all()
     if scales == "nan":
         assert torch.isnan(p.out[0][..., :32]).all()
+
+
+# ------------------------------------------------------------------------------------------------ calls
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@rows_and_kernels(1, 4, 40)
+@pytest.mark.parametrize("spread", [6.0, 40.0])
+def test_peaked_rows(dtype, d, W, spread, kernels):  # noqa: F811
+    """Scores far apart: the reference is raised often, the chunks of a row differ."""
+    run(dtype=dtype, d=d, M=1, H=2, Hq=8, trajs=[(1500, W), (200, W)], gaps=0.6, spread=spread)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@rows_and_kernels(1, 4, 40)
+@pytest.mark.parametrize("dims", ["heads", "layers", "both"])
+def test_caches_that_heads_or_layers_share(dtype, d, W, dims, kernels):  # noqa: F811
+    """Strides of 0, of expanded views."""
+    def cut(x):
+        return x[:1 if dims != "heads" else None, :1 if dims != "layers" else None]
+
+    def edit(p):
+        for c, pos, Q, qp in p.host:
+            for n in NAMES:
+                c.host[n][:] = cut(c.host[n])
+
+    p = Problem(dtype=dtype, d=d, M=2, H=2, Hq=8, trajs=[(300, W)], gaps=0.6, edit=edit).upload()
+    t = p.trajs[0]
+    p.trajs = [dataclasses.replace(t, **{n: cut(getattr(t, n)).expand_as(getattr(t, n)) for n in NAMES})]
+    p.call(200, 3)
+    p.check(200, 3)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@rows_and_kernels(1, 3, 40)
+@pytest.mark.parametrize("what", ["q", "out", "both"])
+def test_queries_and_outputs_at_odd_addresses(dtype, d, W, what, kernels):  # noqa: F811
+    """One trajectory's stand one element off, another's do not."""
+    p = Problem(dtype=dtype, d=d, M=2, H=1, Hq=4, trajs=[(500, W), (300, W)], gaps=0.6).upload()
+    t, n = p.trajs[0], p.trajs[0].q.numel()
+    ends = []
+    if what != "out":
+        q = torch.empty(n + 1, dtype=dtype, device="cuda")[1:].view(t.q.shape)
+        q.copy_(t.q)
+        p.trajs[0] = dataclasses.replace(t, q=q)
+    if what != "q":
+        x, y = torch.full((n + 2,), p.SENT, dtype=dtype, device="cuda"), torch.full((n // d + 2,), p.SENT, device="cuda")
+        p.out[0], p.lse[0] = x[1:-1].view(t.q.shape), y[1:-1].view(t.q.shape[:3])
+        ends = [x[0], x[-1], y[0], y[-1]]
+    p.call(250, 2)
+    p.check(250, 2)
+    assert all(e == p.SENT for e in ends)
