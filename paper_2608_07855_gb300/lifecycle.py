@@ -126,13 +126,15 @@ class Session:
                                 **more)
 
     def _put(self, K, V, first, n, layer=None):
-        """K and V of tokens first .. first + n - 1 of one layer ([1][H][n][d]) or all ([M][H][n][d])."""
+        """K and V of tokens first .. first + n - 1 of one layer ([H][n][d]) or all ([M][H][n][d])."""
         s = self.shape
         if self.packed is None:
-            at = slice(None) if layer is None else slice(layer, layer + 1)
+            at = slice(None) if layer is None else layer
             self.K[at, :, first:first + n].copy_(K)
             self.V[at, :, first:first + n].copy_(V)
             return
+        if layer is not None:
+            K, V = K[None], V[None]
         want = (s.layers if layer is None else 1, s.kv_heads, n, s.head_dim)
         if tuple(K.shape) != want or tuple(V.shape) != want:
             raise ValueError(f"K and V must be [M][H][n][d] = {want}")
@@ -280,7 +282,7 @@ class Session:
         want = (self.shape.kv_heads, b - a, self.shape.head_dim)
         if tuple(K.shape) != want or tuple(V.shape) != want:
             raise ValueError(f"K and V must be [H][n][d] = {want}")
-        self._put(K[None], V[None], a, b - a, layer)
+        self._put(K, V, a, b - a, layer)
         self.unfilled.discard(layer)
 
     def attend(self, Q, qpos, window: int = 0, sinks: int = 0, prefix: ck.TrajTensors = None, layer: int = None):
