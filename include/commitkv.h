@@ -637,6 +637,9 @@ commitkv_status commitkv_packed_read(const commitkv_shape *shape, int32_t n_traj
  *     either off by 2^-22 of it at most).  Small ones are off by more than that of
  *     them: a weight by up to 2^-36 of its row's largest, a query's element by up to
  *     2^-39 of its row's largest.
+ *     Sums of values (and of keys) below 2^-10 are as exact as those of numbers of
+ *     2^-10 are (2^-13 where a scale byte of the 32 tokens' is below 32), not more:
+ *     off by some 2^-33 (2^-36), 2e-6 of values of 2^-16, 2e-5 of 2^-22.
  *   more rows: tensor cores, up to 256 rows at a time; weights rounded to bf16 as in
  *     commitkv_window_attention.  Or, where that takes less time, for fp32 and for
  *     other alignments, the values of a layer at a time are read back into the

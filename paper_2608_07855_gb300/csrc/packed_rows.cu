@@ -28,6 +28,10 @@
 // below the largest score so far, raised when a score is 4 above that: at most 2^15,
 // in one fp16 term for bf16 (off by 2^-11 of it at most, the output's own rounding by
 // 2^-8) and two for fp32 (2^-22), or by 2^-36 of the row's largest where that is more.
+// The MMA takes an fp16 number below 2^-14, a value of 2^-10 here (2^-13 in tiles with
+// small scales), as one of that size when it lines its products up, so sums of such values
+// are as exact as sums of values of that size.  Measured, fp32, 3,000 tokens, in the
+// 2-norm: 7e-7 down to scales of 2^-14, 2.2e-6 at 2^-17, 1.6e-5 at 2^-23.
 //
 // bf16, 32 query on 8 KV heads of 128 channels: 131,071 tokens 39 us (3.7 TB/s with start
 // and merge, 8), 64 caches of up to 8,192 tokens 73 (3.9 TB/s).  665 instructions to a
