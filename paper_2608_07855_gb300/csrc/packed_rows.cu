@@ -2,9 +2,9 @@
 // slice to an item: decoded tokens (the g heads of one to a few positions).
 // Codes 16-byte aligned, scale rows whole.
 //
-// Such a call is bound by reading the codes once: 12 values a ns from memory,
-// some 40 a clock and SM, so that what a value costs in instructions decides
-// whether the memory is kept busy (three a lane and value would be all of them).
+// Such a call's floor is reading the codes once: 12 values a ns from memory,
+// some 40 a clock and SM, at which a value may cost three instructions a lane and
+// no more; it costs 2.6.
 // A warp works by itself on 32 tokens at a time, from a ring of its own in shared
 // memory (cp.async).  Products are warp-level MMAs of fp16 with the tokens and
 // channels as the 16 rows and the query rows as the 8 columns, S^T = K Q^T and
@@ -34,9 +34,12 @@
 // 2-norm: 7e-7 down to scales of 2^-14, 2.2e-6 at 2^-17, 1.6e-5 at 2^-23.
 //
 // bf16, 32 query on 8 KV heads of 128 channels: 131,071 tokens 39 us (3.7 TB/s with start
-// and merge, 8), 64 caches of up to 8,192 tokens 73 (3.9 TB/s).  665 instructions to a
-// warp's tile, 60 % of the issue slots: with scale bytes by shuffles and a multiply before
-// every weight 77.6, with four blocks an SM and 128 registers 75.5.
+// and merge, 8), 64 caches of up to 8,192 tokens 73 (3.9 TB/s).  Bound by latency: 665
+// instructions to a warp's tile, K products, softmax and V products one after the
+// other, in 11 warps an SM; 57 and 60 % of the issue slots, 52 and 51 % of the memory's
+// rate.  With scale bytes by shuffles and a multiply before every weight 77.6, with four
+// blocks an SM and 128 registers 75.5.  16 rows (248 registers, two blocks an SM) over
+// 131,071 tokens 51; 64 channels, 8 caches to 16,000 21.
 #include <string.h>
 
 #include <type_traits>

@@ -42,8 +42,9 @@ library's entry points in the order of Algorithm 1:
 With packed=True the resident cache is held in 4 bits (commitkv_packed_write as
 tokens are appended, 0.27 of the bytes of bf16): attend reads the codes
 (commitkv_packed_attention), a checkpoint moves them (commitkv_packed_compact),
-and a commit or fill_scores reads the values back into full width for its own
-duration (commitkv_packed_read).  Everything is computed from the values that the
+and a commit or fill_scores reads the values of all layers back into full width,
+which takes as much memory as a bf16 or fp32 cache for its own duration
+(commitkv_packed_read).  Everything is computed from the values that the
 codes stand for.
 
 state_dict / load_state_dict carry the state between commits (the resident
